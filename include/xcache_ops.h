@@ -147,6 +147,127 @@ xc_status xc_op_gate_static(int dtype, int n_cams, int tokens_per_cam, int d, co
                             const xc_gate_params *gate, uint8_t *flag, float *s_cos, float *d_max,
                             float *tau, void *stream);
 
+/* ---- branched rollouts over a paged key / value cache ----
+ *
+ * Several sequences (the branches of a rollout: candidate actions from one
+ * history) live in one pool of pages.  A page holds page_size consecutive
+ * tokens' keys and values of every head; a sequence is a row of page ids and
+ * a token count; sequences forked from one another share pages.  All of the
+ * state is on the device and every call is asynchronous, so a whole planning
+ * step (fork, extend, append, attend, free) needs no host synchronisation.
+ *
+ *   k, v   [n_layers][n_pages][page_size][n_kv_heads * head_dim], 16-byte aligned
+ *   ref    [n_pages] sequences that hold the page; 0 = free
+ *   table  [max_seqs][max_pages] page ids, token j of sequence s on page
+ *          table[s][j / page_size]; entries past the last page are -1
+ *   len    [max_seqs] tokens of each sequence
+ * An empty cache has ref = 0, table = -1, len = 0.  A partly filled last page
+ * belongs to one sequence (the calls below keep it so), so appending never
+ * writes to a shared page.  dtype XC_F32 / XC_BF16; head_dim 16, 32, 64 or
+ * 128; page_size a power of two from 16 to 1024; n_pages * page_size < 2^31.
+ * Calls on one cache must be ordered (one stream, or events).
+ *
+ * What the host cannot see is checked on the device: a call that finds a bad
+ * value sets a bit of the word xc_op_device_error() returns --
+ * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, which then
+ * change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
+ * whose token is then skipped. */
+typedef struct {
+    int dtype, n_layers, n_pages, page_size, n_kv_heads, head_dim, max_seqs, max_pages;
+    void *k, *v;
+    int *ref, *table, *len;
+} xc_kv_cache;
+
+enum {
+    XC_DEV_CACHE_FULL = 64,      /* not enough free pages, or a full table row */
+    XC_DEV_BAD_SEQUENCE = 128,   /* sequence id, length or page id out of range; a fork into
+                                    a sequence that is not empty; a sequence listed twice */
+    XC_DEV_BAD_POSITION = 256    /* rotation position or cache slot out of range */
+};
+
+/* Bytes of device workspace of xc_op_kv_fork / _extend / _compact on this
+ * cache (page lists and marks).  Contents on entry are ignored. */
+size_t xc_op_kv_workspace_bytes(const xc_kv_cache *cache);
+
+/* For i < n: sequence dst[i] (empty) becomes a copy of src[i] (device int
+ * arrays; a sequence may be forked to many).  Full pages are shared (ref + 1);
+ * the rows in use of a partly filled last page are copied, in every layer,
+ * into a fresh page: the lowest free page ids, in list order. */
+xc_status xc_op_kv_fork(const xc_kv_cache *cache, int n, const int *src, const int *dst, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* Appends n_new tokens to each of the n listed sequences: takes the pages they
+ * need (lowest free ids first, in list order, then token order), advances len
+ * and writes the cache slot of every new token, page * page_size + offset, to
+ * slots [n][n_new] (-1 everywhere when the call changes nothing). */
+xc_status xc_op_kv_extend(const xc_kv_cache *cache, int n, const int *seqs, int n_new, int *slots,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* Empties the n listed sequences: ref - 1 of their pages, table entries -1,
+ * len 0.  An empty sequence stays as it is. */
+xc_status xc_op_kv_free(const xc_kv_cache *cache, int n, const int *seqs, void *stream);
+
+/* Moves the pages in use to ids 0 .. n_live - 1: the k-th page in use with an
+ * id >= n_live goes to the k-th free id below n_live (both ascending), in
+ * every layer; ref and table follow.  *n_live (device) receives the count.
+ * The contents of pages that become free are left as they are. */
+xc_status xc_op_kv_compact(const xc_kv_cache *cache, int *n_live, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
+/* Rotation table: for each axis a of n_axes (1 to 4), positions 0 ..
+ * n_pos[a] - 1 and pairs 0 .. axis_pairs[a] - 1 (host arrays), (cos, sin) of
+ * position * theta^(-pair / axis_pairs[a]), as float pairs
+ * [n_pos[a]][axis_pairs[a]][2], axis after axis, computed in double. */
+xc_status xc_op_rope_table(int n_axes, const int *axis_pairs, const int *n_pos, double theta, float *table,
+                           void *stream);
+
+/* Head-wise RMS norm of queries and keys, position rotation and the write into
+ * the cache, in one pass.  For token t and head h, y = x / sqrt(mean(x^2) +
+ * eps) * gamma (gamma_q / gamma_k float [head_dim]), then pair p of y rotates
+ * by the table entry of the token's position on the pair's axis (axes own
+ * consecutive pairs, axis_pairs[a] each, head_dim / 2 in all): (a, b) -> (a cos -
+ * b sin, a sin + b cos), a pair being elements (2p, 2p + 1), or with
+ * half_split (p, p + head_dim / 2).  Queries go to q_out, keys and the
+ * unchanged values to row slots[t] of this layer's pages; slots[t] = -1 keeps
+ * no keys of the token.  Rounded once, at the store.
+ *   q, q_out  [n_tokens][n_heads * head_dim], rows q_stride / q_out_stride
+ *             elements apart; q_out may be q itself
+ *   k, v      [n_tokens][n_kv_heads * head_dim], rows k_stride / v_stride apart
+ *   pos       device int [n_tokens][n_axes], 0 <= pos < n_pos[axis]
+ *   slots     device int [n_tokens], distinct except for -1
+ * Rows are 16-byte aligned.  n_heads is a multiple of the cache's n_kv_heads. */
+xc_status xc_op_qk_norm_rope(const xc_kv_cache *cache, int layer, int n_tokens, int n_heads, const void *q,
+                             long q_stride, const void *k, long k_stride, const void *v, long v_stride,
+                             const float *gamma_q, const float *gamma_k, float eps, int n_axes,
+                             const int *axis_pairs, const int *n_pos, const int *pos, const float *table,
+                             int half_split, const int *slots, void *q_out, long q_out_stride, void *stream);
+
+/* Attention of a batch of branches over one layer of the cache.  Query row
+ * t = b * n_q + i (b < n_branches, i < n_q) belongs to sequence seqs[b]; head h
+ * reads key head h / (n_heads / n_kv_heads):
+ *   o[t] = sum_j p_j v_j, p = softmax over j < limit of scale * (q[t] . k_j),
+ * limit = len (causal = 0), or with causal = 1 len - n_q + i + 1: the queries
+ * are the sequence's last n_q tokens.  A row that sees no key gives 0.
+ *   shared_len  the first shared_len tokens (a multiple of page_size) of every
+ *               listed sequence are the same pages, as after a fork: they are
+ *               read once for all branches, from the row of seqs[0].  Which
+ *               keys a row sees does not depend on it.
+ *   scale       > 0, or 0 for 1 / sqrt(head_dim)
+ *   q, o        [n_branches * n_q][n_heads * head_dim], rows q_stride / o_stride
+ *               elements apart, 16-byte aligned
+ *   workspace   device, at least xc_op_branch_attention_workspace_bytes();
+ *               contents on entry are ignored; not shared by overlapping calls
+ * Cache rows that no sequence has reached (the rest of a last page) may hold
+ * anything.  A key that the causal limit hides from a row but that is part of
+ * the sequence must be finite, as must its value.  XC_BF16 needs head_dim 64
+ * or 128.  At most 128 query heads per key head. */
+size_t xc_op_branch_attention_workspace_bytes(const xc_kv_cache *cache, int n_branches, int n_q, int n_heads,
+                                              int shared_len);
+xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q,
+                                 int n_heads, const void *q, long q_stride, int shared_len, int causal,
+                                 float scale, void *o, long o_stride, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
 /* Reads and clears the process-wide device error word of operator calls
  * (synchronising).  0 = no error. */
 int xc_op_device_error(void);

@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libxcache.so")
-SOURCES = ["xc_api.cu", "k_gemm_tc.cu", "k_attn_tc.cu", "k_gate.cu", "k_elem.cu", "k_simt.cu"]
+SOURCES = ["xc_api.cu", "k_gemm_tc.cu", "k_attn_tc.cu", "k_gate.cu", "k_elem.cu", "k_simt.cu",
+           "xc_branch_api.cu", "k_branch_attn.cu", "k_kv_pages.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
          "--expt-relaxed-constexpr", "-I", os.path.join(HERE, "..", "include")]

@@ -17,6 +17,7 @@
 #include <string>
 #include <vector>
 
+#include "xc_branch.cuh"
 #include "xc_kernels.cuh"
 
 
@@ -1697,3 +1698,5 @@ xc_status xc_op_residual_reuse(int dtype, long n, const void *x, const void *rha
 }
 
 }  // extern "C"
+
+int *xc::op_error_word() { return op_err_word(); }

@@ -21,6 +21,7 @@ XC_DEC_FORCED, XC_DEC_COMPUTE, XC_DEC_SKIP = 0, 1, 2
 XC_EPI_BIAS, XC_EPI_GELU, XC_EPI_RESID_GATE, XC_EPI_RESID_CACHE = 0, 1, 2, 3
 XC_MAX_BLOCKS = 64
 XC_MAX_GROUPS = 4
+XC_DEV_CACHE_FULL, XC_DEV_BAD_SEQUENCE, XC_DEV_BAD_POSITION = 64, 128, 256
 STATUS_NAMES = {0: "XC_OK", 1: "XC_EINVAL", 2: "XC_ESTATE", 3: "XC_ENOMEM", 4: "XC_ECUDA",
                 5: "XC_ENUMERIC", 6: "XC_ETIMEOUT"}
 
@@ -79,6 +80,13 @@ class ProfileRec(ctypes.Structure):
                 ("ms", ctypes.c_float)]
 
 
+class KVCacheDesc(ctypes.Structure):
+    """xc_kv_cache: one pool of pages and the sequences in it."""
+    _fields_ = [(n, ctypes.c_int) for n in ("dtype", "n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim",
+                                            "max_seqs", "max_pages")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "ref", "table", "len")]
+
+
 KERNEL_KINDS = ("cond", "embed", "gate", "ln", "qkv", "attn", "oproj", "ffn1", "ffn2", "reuse", "head",
                 "xattn", "chain")
 
@@ -116,6 +124,16 @@ SIGNATURES = {
                         _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "xc_op_gate_static": (_I, [_I, _I, _I, _I, _P, _P, _I, _P, _P, _P, _P, _I, _I, _I,
                                ctypes.POINTER(GateParams), _P, _P, _P, _P, _P]),
+    "xc_op_kv_workspace_bytes": (ctypes.c_size_t, [_P]),
+    "xc_op_kv_fork": (_I, [_P, _I, _P, _P, _P, ctypes.c_size_t, _P]),
+    "xc_op_kv_extend": (_I, [_P, _I, _P, _I, _P, _P, ctypes.c_size_t, _P]),
+    "xc_op_kv_free": (_I, [_P, _I, _P, _P]),
+    "xc_op_kv_compact": (_I, [_P, _P, _P, ctypes.c_size_t, _P]),
+    "xc_op_rope_table": (_I, [_I, _P, _P, ctypes.c_double, _P, _P]),
+    "xc_op_qk_norm_rope": (_I, [_P, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _P, _F, _I, _P, _P, _P, _P, _I, _P, _P,
+                                _L, _P]),
+    "xc_op_branch_attention_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I, _I, _I]),
+    "xc_op_branch_attention": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _I, _I, _F, _P, _L, _P, ctypes.c_size_t, _P]),
 }
 
 
@@ -362,3 +380,157 @@ def op_gate(dtype, n_cams, tokens_per_cam, x, fp_rows, phi, phi_act, cell, actio
             step, ctypes.byref(gate) if gate is not None else None, _ptr(flag), _ptr(s_cos),
             _ptr(d_max), _ptr(tau), _ptr(workspace), workspace.numel() * workspace.element_size(),
             _stream(stream)))
+
+
+# --------------------------------- branched rollouts over a paged K/V cache
+class KVCache:
+    """Handle on a paged key / value cache (xc_kv_cache) over the caller's torch
+    CUDA tensors: k, v [n_layers, n_pages, page_size, n_kv_heads * head_dim]
+    (float32 or bfloat16), ref [n_pages], table [max_seqs, max_pages] and len
+    [max_seqs] int32, all contiguous.  Keeps the tensors, and one workspace per
+    stream that grows to the largest call.  ``empty`` allocates them."""
+
+    def __init__(self, dtype, n_kv_heads, head_dim, k, v, ref, table, length):
+        import torch
+        want = torch.float32 if dtype_code(dtype) == XC_F32 else torch.bfloat16
+        if k.dim() != 4 or k.shape != v.shape or k.shape[3] != n_kv_heads * head_dim or k.dtype != want or \
+                v.dtype != want:
+            raise ValueError("k, v: [n_layers, n_pages, page_size, n_kv_heads * head_dim] of the cache's dtype")
+        if table.dim() != 2 or ref.shape != k.shape[1:2] or length.shape != table.shape[:1]:
+            raise ValueError("ref [n_pages], table [max_seqs, max_pages], len [max_seqs]")
+        for t in (ref, table, length):
+            if t.dtype != torch.int32:
+                raise ValueError("ref, table and len are int32")
+        for t in (k, v, ref, table, length):
+            if not t.is_contiguous() or not t.is_cuda:
+                raise ValueError("cache tensors are contiguous CUDA tensors")
+        self.k, self.v, self.ref, self.table, self.len = k, v, ref, table, length
+        self.dtype, self.n_kv_heads, self.head_dim = dtype, n_kv_heads, head_dim
+        self.page_size = k.shape[2]
+        self.desc = KVCacheDesc(dtype_code(dtype), k.shape[0], k.shape[1], k.shape[2], n_kv_heads, head_dim,
+                                table.shape[0], table.shape[1], k.data_ptr(), v.data_ptr(), ref.data_ptr(),
+                                table.data_ptr(), length.data_ptr())
+        self.ptr = ctypes.addressof(self.desc)
+        self._ws = {}
+        self._attn_bytes = {}
+        self._page_bytes = LIB.xc_op_kv_workspace_bytes(self.ptr)
+
+    @classmethod
+    def empty(cls, dtype, n_layers, n_pages, page_size, n_kv_heads, head_dim, max_seqs, max_pages, device="cuda"):
+        import torch
+        dt = torch.float32 if dtype_code(dtype) == XC_F32 else torch.bfloat16
+        shape = (n_layers, n_pages, page_size, n_kv_heads * head_dim)
+        return cls(dtype, n_kv_heads, head_dim, torch.empty(shape, dtype=dt, device=device),
+                   torch.empty(shape, dtype=dt, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device),
+                   torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(max_seqs, dtype=torch.int32, device=device))
+
+    def workspace(self, nbytes: int, stream: int):
+        """Device workspace of at least nbytes for calls on this stream (cudaStream_t)."""
+        ws = self._ws.get(stream)
+        if ws is None or ws.numel() < nbytes:
+            import torch
+            ext = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+            with torch.cuda.stream(ext):       # freed memory is reused in this stream's order
+                ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.k.device)
+            self._ws[stream] = ws
+        return ws
+
+
+def _row_stride(t) -> int:
+    """Elements between the rows of a [rows, columns] tensor with unit column stride."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("rows must have unit column stride")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _int32(t, n):
+    import torch
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"expected a contiguous int32 tensor of {n} elements")
+    return t.data_ptr()
+
+
+def op_kv_fork(cache: KVCache, src, dst, stream=None):
+    """Sequence dst[i] becomes a copy of src[i] (int32 CUDA tensors)."""
+    st = _stream(stream)
+    n = src.numel()
+    ws = cache.workspace(cache._page_bytes, st)
+    check(LIB.xc_op_kv_fork(cache.ptr, n, _int32(src, n), _int32(dst, n), ws.data_ptr(), ws.numel(), st))
+
+
+def op_kv_extend(cache: KVCache, seqs, n_new: int, slots, stream=None):
+    """Appends n_new tokens to every listed sequence; slots [n, n_new] int32 receives their cache slots."""
+    st = _stream(stream)
+    n = seqs.numel()
+    ws = cache.workspace(cache._page_bytes, st)
+    check(LIB.xc_op_kv_extend(cache.ptr, n, _int32(seqs, n), n_new, _int32(slots, n * n_new), ws.data_ptr(),
+                              ws.numel(), st))
+
+
+def op_kv_free(cache: KVCache, seqs, stream=None):
+    n = seqs.numel()
+    check(LIB.xc_op_kv_free(cache.ptr, n, _int32(seqs, n), _stream(stream)))
+
+
+def op_kv_compact(cache: KVCache, n_live, stream=None):
+    """n_live: int32 CUDA tensor of one element, receives the pages in use."""
+    st = _stream(stream)
+    ws = cache.workspace(cache._page_bytes, st)
+    check(LIB.xc_op_kv_compact(cache.ptr, _int32(n_live, 1), ws.data_ptr(), ws.numel(), st))
+
+
+def op_rope_table(axis_pairs, n_pos, theta, out, stream=None):
+    """out: contiguous float32 CUDA tensor of 2 * sum(axis_pairs * n_pos) elements."""
+    n = len(axis_pairs)
+    if len(n_pos) != n or out.numel() != 2 * sum(a * b for a, b in zip(axis_pairs, n_pos)) or not out.is_contiguous():
+        raise ValueError("out: one (cos, sin) pair per position and pair of every axis")
+    check(LIB.xc_op_rope_table(n, (_I * n)(*axis_pairs), (_I * n)(*n_pos), float(theta), out.data_ptr(),
+                               _stream(stream)))
+
+
+def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_pairs, n_pos, table, slots, q_out,
+                    eps=1e-6, half_split=False, stream=None):
+    """q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] (row-strided views allowed), pos [T, axes]
+    and slots [T] int32, table from op_rope_table; axis_pairs, n_pos: host sequences."""
+    T, n = q.shape[0], len(axis_pairs)
+    hd = cache.head_dim
+    wide = cache.n_kv_heads * hd
+    if q.shape[1] % hd or q_out.shape != q.shape or k.shape != (T, wide) or v.shape != (T, wide) or \
+            not (q.dtype == k.dtype == v.dtype == q_out.dtype == cache.k.dtype):
+        raise ValueError("q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] of the cache's dtype")
+    if gamma_q.numel() != hd or gamma_k.numel() != hd or len(n_pos) != n or \
+            any(x.element_size() != 4 or not x.is_contiguous() for x in (gamma_q, gamma_k, table)) or \
+            table.numel() != 2 * sum(a * b for a, b in zip(axis_pairs, n_pos)):
+        raise ValueError("float32 gamma_q, gamma_k [head_dim]; table: one (cos, sin) pair per position and pair of every axis")
+    check(LIB.xc_op_qk_norm_rope(cache.ptr, layer, T, q.shape[1] // hd, q.data_ptr(), _row_stride(q), k.data_ptr(),
+                                 _row_stride(k), v.data_ptr(), _row_stride(v), gamma_q.data_ptr(),
+                                 gamma_k.data_ptr(), eps, n, (_I * n)(*axis_pairs), (_I * n)(*n_pos),
+                                 _int32(pos, T * n), table.data_ptr(), int(half_split), _int32(slots, T),
+                                 q_out.data_ptr(), _row_stride(q_out), _stream(stream)))
+
+
+def op_branch_attention_workspace_bytes(cache: KVCache, n_branches, n_q, n_heads, shared_len=0) -> int:
+    return LIB.xc_op_branch_attention_workspace_bytes(cache.ptr, n_branches, n_q, n_heads, shared_len)
+
+
+def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, causal=False, scale=0.0,
+                        workspace=None, stream=None):
+    """q, o [len(seqs) * n_q, n_heads * head_dim] (row-strided views allowed); seqs int32 CUDA tensor.
+    workspace: a device tensor of op_branch_attention_workspace_bytes, or None for the cache's own."""
+    B, hd = seqs.numel(), cache.head_dim
+    st = _stream(stream)
+    if q.shape[0] != B * n_q or q.shape[1] % hd or o.shape != q.shape or \
+            not (q.dtype == o.dtype == cache.k.dtype):
+        raise ValueError("q, o [len(seqs) * n_q, n_heads * head_dim] of the cache's dtype")
+    H = q.shape[1] // hd
+    if workspace is None:
+        key = (B, n_q, H, shared_len)
+        need = cache._attn_bytes.get(key)
+        if need is None:
+            need = cache._attn_bytes[key] = op_branch_attention_workspace_bytes(cache, B, n_q, H, shared_len)
+        workspace = cache.workspace(need, st)
+    check(LIB.xc_op_branch_attention(cache.ptr, layer, B, _int32(seqs, B), n_q, H, q.data_ptr(), _row_stride(q),
+                                     shared_len, int(causal), scale, o.data_ptr(), _row_stride(o),
+                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
