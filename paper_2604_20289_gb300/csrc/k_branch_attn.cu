@@ -21,6 +21,8 @@
 
 namespace xc {
 
+constexpr int LEN_CACHE = 128;   // branches whose table row and length are kept in shared memory
+
 struct BranchSched {
     int B, n_q, grp, Hk;
     int tt;                  // tokens of a row tile
@@ -28,97 +30,113 @@ struct BranchSched {
     int n_st, E;             // own row tiles per branch, of all branches
     int P;                   // keys of the prefix units: own keys begin there
     int causal, G;           // G: CTAs
+    int lead;                // what a unit costs beside its key tiles, in key tiles (see branch_plan)
     int max_seqs, max_pages, ps, n_pages;
     int pitch_p, pitch_o;    // rows of a partial slot
     long slots_p;            // prefix slots before the own ones
     const int *seqs, *len, *table;
-    float *ws_o;             // partial O rows, then (m, l) of each, then the scan
+    float *ws_o;             // partial O, then (m, l) of each row, then the scan
     float2 *ws_ml;
-    int *ws_off;             // [E + 1] own key tiles before each entry (same for every head)
+    int *ws_off;             // [E + 1] line length before each entry (same for every head)
+    int4 *ws_start;          // [G] per CTA: its first unit (head, entry), position in it, key tiles of it
 
     __host__ __device__ __forceinline__ int seq(int b) const {
         const int s = seqs[b];
         return s >= 0 && s < max_seqs ? s : -1;
     }
-    __host__ __device__ __forceinline__ int seq_len(int b) const {
+    __host__ __device__ __forceinline__ int load_len(int b) const {
         const int s = seq(b);
         const int l = s < 0 ? 0 : len[s];
         return l < 0 || l > max_pages * ps ? 0 : l;
     }
+    __host__ __device__ __forceinline__ int seq_len(int b, const int *cache) const {
+        return b < LEN_CACHE ? cache[b] : load_len(b);
+    }
+    __host__ __device__ __forceinline__ int table_row(int b, const int *cache) const {
+        return b < LEN_CACHE ? cache[LEN_CACHE + b] : seq(b);
+    }
+    // length on the line of a unit of n key tiles
+    __host__ __device__ __forceinline__ int line_len(int n) const { return n > 0 ? n + lead : 0; }
     // keys that query i of a branch of length l sees
     __host__ __device__ __forceinline__ int limit(int l, int i) const {
         const int x = causal ? l - n_q + i + 1 : l;
         return x > 0 ? x : 0;
     }
-    // keys past P that the entry's last row sees
-    __host__ __device__ __forceinline__ int own_keys(int e) const {
-        const int b = e / n_st, i = min((e - b * n_st + 1) * tt, n_q) - 1;
-        return max(limit(seq_len(b), i) - P, 0);
+    // keys past P that the last row of entry (branch b, row tile j) sees
+    __host__ __device__ __forceinline__ int own_keys(int b, int j, const int *cache) const {
+        return max(limit(seq_len(b, cache), min((j + 1) * tt, n_q) - 1) - P, 0);
     }
-    // CTA c runs the key tiles [begin(c), begin(c + 1)); with fewer tiles than
-    // CTAs the first T of them run one each
-    __host__ __device__ __forceinline__ long long begin(long long T, int c) const {
-        return T < G ? min((long long)c, T) : T * c / G;
+    __host__ __device__ __forceinline__ int own_keys(int e, const int *cache) const {
+        return own_keys(e / n_st, e % n_st, cache);
     }
-    __host__ __device__ __forceinline__ int owner(long long T, long long x) const {
-        return T < G ? (int)x : (int)(((x + 1) * G - 1) / T);
+};
+
+// The line of length T (< 2^31) over G CTAs: CTA c runs [begin(c),
+// begin(c + 1)), lengths that differ by one at most.  Key tile k of a unit
+// that begins at x sits at x + lead + k.
+struct BranchLine {
+    unsigned q, r;
+    __host__ __device__ __forceinline__ BranchLine(unsigned T, unsigned G) : q(T / G), r(T - q * G) {}
+    __host__ __device__ __forceinline__ unsigned begin(unsigned c) const { return q * c + (c < r ? c : r); }
+    __host__ __device__ __forceinline__ unsigned owner(unsigned x) const {   // the c with begin(c) <= x < begin(c + 1)
+        const unsigned longer = r * (q + 1);
+        return x < longer ? x / (q + 1) : r + (x - longer) / q;
     }
 };
 
 // One piece of a unit, as every role of a CTA walks them.
 struct BranchPiece {
     int h, t0, nt;           // key head, first token row, tokens
-    int row;                 // row of the page table, or -1
+    int b;                   // branch whose table row holds the keys
     int key0, keys;          // first key and keys of the unit
     int kt0, kt1, n_kt;      // key tiles of the piece and of the unit
     int idx;                 // unit of the head: prefix tiles, then entries
 };
 struct BranchStart {
-    long long T;
-    int h, idx, off, n;      // first unit, key tile in it, key tiles of this CTA
+    int h, idx, off, n;      // first unit, position in it, line length of this CTA
 };
 
 template <int KT>
 struct BranchWalk {
-    const BranchSched &s;
     int h, idx, off, left;
-    __host__ __device__ __forceinline__ BranchWalk(const BranchSched &sc, const BranchStart &st)
-        : s(sc), h(st.h), idx(st.idx), off(st.off), left(st.n) {}
-    __host__ __device__ __forceinline__ bool next(BranchPiece &p) {
+    int b, j;                // entry idx - n_pr (idx >= n_pr)
+    BranchWalk() = default;
+    __host__ __device__ __forceinline__ BranchWalk(const BranchSched &s, const BranchStart &st)
+        : h(st.h), idx(st.idx), off(st.off), left(st.n) {
+        const int e = max(idx - s.n_pr, 0);
+        b = e / s.n_st;
+        j = e - b * s.n_st;
+    }
+    __host__ __device__ __forceinline__ bool next(const BranchSched &s, const int *lens, BranchPiece &p) {
         while (left > 0) {
-            int keys;
-            if (idx < s.n_pr) {
-                keys = s.P;
-                p.n_kt = s.n_pt;
-            } else {
-                keys = s.own_keys(idx - s.n_pr);
-                p.n_kt = (keys + KT - 1) / KT;
-            }
-            if (off < p.n_kt) {
+            const bool own = idx >= s.n_pr;
+            const int keys = own ? s.own_keys(b, j, lens) : s.P;
+            const int n = own ? (keys + KT - 1) / KT : s.n_pt, len = s.line_len(n);
+            if (off < len) {
+                const int end = min(len, off + left);
+                p.n_kt = n;
                 p.h = h;
                 p.idx = idx;
                 p.keys = keys;
-                if (idx < s.n_pr) {
-                    p.t0 = idx * s.tt;
-                    p.nt = min(s.tt, s.B * s.n_q - p.t0);
-                    p.row = s.seq(0);
-                    p.key0 = 0;
-                } else {
-                    const int e = idx - s.n_pr, b = e / s.n_st, i0 = (e - b * s.n_st) * s.tt;
-                    p.t0 = b * s.n_q + i0;
-                    p.nt = min(s.tt, s.n_q - i0);
-                    p.row = s.seq(b);
-                    p.key0 = s.P;
-                }
-                p.kt0 = off;
-                p.kt1 = min(p.n_kt, off + left);
-                left -= p.kt1 - p.kt0;
-                off = p.kt1;
-                return true;
+                p.b = own ? b : 0;
+                p.t0 = own ? b * s.n_q + j * s.tt : idx * s.tt;
+                p.nt = min(s.tt, own ? s.n_q - j * s.tt : s.B * s.n_q - p.t0);
+                p.key0 = own ? s.P : 0;
+                p.kt0 = max(off - s.lead, 0);
+                p.kt1 = max(end - s.lead, 0);
+                left -= end - off;
+                off = end;
+                if (p.kt1 > p.kt0) return true;
+                continue;
             }
             off = 0;
+            if (own && ++j == s.n_st) {
+                j = 0;
+                ++b;
+            }
             if (++idx == s.n_pr + s.E) {
                 idx = 0;
+                b = 0;
                 ++h;
             }
         }
@@ -126,15 +144,23 @@ struct BranchWalk {
     }
 };
 
-// This CTA's share of the line.  Every thread calls it; sh holds 34 ints.
-// CTA 0 also leaves the entries' scan for the combine kernel.
+// This CTA's share of the line.  Every thread calls it; lens (2 LEN_CACHE ints)
+// receives the branches' lengths, then their table rows.  CTA 0 also leaves the entries' scan for
+// the combine kernel, and checks what the host could not see.
 template <int KT>
-__device__ BranchStart branch_start(const BranchSched &s, int *sh, BranchStart *out, int *err) {
+__device__ BranchStart branch_start(const BranchSched &s, int *lens, int *sh, BranchStart *out, int *err) {
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = nt >> 5;
+    const int c = blockIdx.x;
+    for (int b = tid; b < min(s.B, LEN_CACHE); b += nt) {
+        lens[b] = s.load_len(b);
+        lens[LEN_CACHE + b] = s.seq(b);
+    }
+    if (tid == 0) out->n = 0;
+    __syncthreads();
     const int per = (s.E + nt - 1) / nt;
     const int e0 = min(tid * per, s.E), e1 = min(e0 + per, s.E);
     int mine = 0;
-    for (int e = e0; e < e1; ++e) mine += (s.own_keys(e) + KT - 1) / KT;
+    for (int e = e0; e < e1; ++e) mine += s.line_len((s.own_keys(e, lens) + KT - 1) / KT);
     int x = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -142,7 +168,6 @@ __device__ BranchStart branch_start(const BranchSched &s, int *sh, BranchStart *
         if (lane >= d) x += y;
     }
     if (lane == 31) sh[warp] = x;
-    if (tid == 0) out->n = 0;
     __syncthreads();
     int before = 0, S = 0;
     for (int w = 0; w < nw; ++w) {
@@ -150,46 +175,61 @@ __device__ BranchStart branch_start(const BranchSched &s, int *sh, BranchStart *
         S += sh[w];
     }
     const int excl = before + x - mine;
-    const long long PP = (long long)s.n_pr * s.n_pt, Th = PP + S, T = Th * s.Hk;
-    const int c = blockIdx.x;
+    const unsigned PP = (unsigned)s.n_pr * s.line_len(s.n_pt), Th = PP + S, T = Th * s.Hk;
     if (c == 0) {
         int a = excl;
         for (int e = e0; e < e1; ++e) {
             s.ws_off[e] = a;
-            a += (s.own_keys(e) + KT - 1) / KT;
+            a += s.line_len((s.own_keys(e, lens) + KT - 1) / KT);
         }
         if (tid == 0) s.ws_off[s.E] = S;
-        for (int b = tid; b < s.B; b += nt) {          // what the host could not see
+        for (int b = tid; b < s.B; b += nt) {
             const int q = s.seqs[b];
             if (err && (q < 0 || q >= s.max_seqs || s.len[q] < 0 || s.len[q] > s.max_pages * s.ps || s.len[q] < s.P))
                 atomicOr(err, ERR_BAD_SEQ);
         }
     }
-    if (T > 0) {
-        const long long g0 = s.begin(T, c), g1 = s.begin(T, c + 1);
-        if (g1 > g0) {
-            const int h = (int)(g0 / Th);
-            const long long r = g0 - (long long)h * Th;
-            if (r < PP) {
-                if (tid == 0) *out = BranchStart{T, h, (int)(r / s.n_pt), (int)(r % s.n_pt), (int)(g1 - g0)};
-            } else if (r - PP >= excl && r - PP < excl + mine) {
-                int rest = (int)(r - PP) - excl, e = e0;
-                for (;; ++e) {
-                    const int n = (s.own_keys(e) + KT - 1) / KT;
-                    if (rest < n) break;
-                    rest -= n;
-                }
-                *out = BranchStart{T, h, s.n_pr + e, rest, (int)(g1 - g0)};
+    const BranchLine line(T, s.G);
+    const unsigned g0 = line.begin(c), g1 = line.begin(c + 1);
+    if (g1 > g0) {
+        const unsigned h = g0 / Th, r = g0 - h * Th;
+        if (r < PP) {
+            const int len = s.line_len(s.n_pt);
+            if (tid == 0) *out = BranchStart{(int)h, (int)r / len, (int)r % len, (int)(g1 - g0)};
+        } else if ((int)(r - PP) >= excl && (int)(r - PP) < excl + mine) {
+            int rest = (int)(r - PP) - excl, e = e0, n;
+            for (;; ++e) {
+                n = (s.own_keys(e, lens) + KT - 1) / KT;
+                if (rest < s.line_len(n)) break;
+                rest -= s.line_len(n);
             }
+            *out = BranchStart{(int)h, s.n_pr + e, rest, (int)(g1 - g0)};
+            s.ws_start[c] = make_int4(h, e, rest, n);
         }
     }
     __syncthreads();
     return *out;
 }
 
-// Partial slot of a piece: with prefix units, unit index + CTA (both only
-// grow along the line, so the sum names the piece); without, a CTA cuts at
-// most its first and its last unit.
+// Entries without a key to read: their rows are zero (with prefix units the
+// combine kernel writes every row).
+template <typename T>
+__device__ void branch_zero_rows(const BranchSched &s, const int *lens, T *o, long o_ld, int d) {
+    if (s.n_pr > 0) return;
+    for (int e = blockIdx.x; e < s.E; e += s.G) {
+        if (s.own_keys(e, lens) > 0) continue;
+        const int b = e / s.n_st, i0 = (e % s.n_st) * s.tt, nt = min(s.tt, s.n_q - i0);
+        const int vecs = d * (int)sizeof(T) / 16;
+        for (int x = threadIdx.x; x < nt * vecs; x += blockDim.x)
+            reinterpret_cast<uint4 *>(o + (size_t)(b * s.n_q + i0 + x / vecs) * o_ld)[x % vecs] = make_uint4(0, 0, 0, 0);
+    }
+}
+
+// Partial slot of a piece (its first row): with prefix units, unit index + CTA
+// (both only grow along the line, so the sum names the piece); without, a
+// CTA cuts at most its first and its last unit.  A slot holds its O by
+// 4-column chunks, [HD / 4][pitch rows][4]: threads that hold neighbouring
+// rows write neighbouring 16 bytes.
 __host__ __device__ __forceinline__ long branch_slot_row(const BranchSched &s, const BranchPiece &p, int c, bool first) {
     if (s.n_pr > 0)
         return p.idx < s.n_pr ? ((long)p.h * s.n_pr + p.idx + c) * s.pitch_p
@@ -207,7 +247,7 @@ struct BranchTile {
     static constexpr int STAGES = HD == 64 ? (QT == 2 ? 4 : 5) : (QT == 2 ? 2 : 3);
     static constexpr int OFF_K = QT * Q_BYTES, OFF_V = OFF_K + STAGES * KV_BYTES;
     static constexpr int OFF_BAR = OFF_V + STAGES * KV_BYTES;
-    static constexpr int SMEM_BYTES = OFF_BAR + 640 + 1024;
+    static constexpr int SMEM_BYTES = OFF_BAR + 384 + 1024;
     static constexpr bool SEP_P = HD == 64 || QT == 1;     // P has TMEM columns of its own
     static constexpr int ISSUERS = SEP_P ? QT : 1;
     static constexpr int S_COL(int i) { return 128 * i; }
@@ -216,6 +256,7 @@ struct BranchTile {
     static constexpr int TMEM_COLS = HD == 64 && QT == 1 ? 256 : 512;
     static constexpr int W_TMA = 4 * QT, W_MMA = W_TMA + 1, W_TAIL = W_MMA + ISSUERS;
     static constexpr int THREADS = 32 * (W_TAIL + 1);
+    static constexpr bool HALVES = SEP_P;              // P V in two halves of 64 keys
     static constexpr bool TURNS = HD == 64 && QT == 2;
     static constexpr float LAZY = 8.0f;                // rescale threshold (log2 units)
 };
@@ -237,6 +278,38 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *tm, ui
         : "memory");
 }
 
+// 4 x 4 transpose of 16-byte parts within each quad of lanes: lane i's u[j]
+// becomes lane j's u[i].
+__device__ __forceinline__ uint4 shfl_xor16(const uint4 &v, int d) {
+    return make_uint4(__shfl_xor_sync(0xffffffffu, v.x, d), __shfl_xor_sync(0xffffffffu, v.y, d),
+                      __shfl_xor_sync(0xffffffffu, v.z, d), __shfl_xor_sync(0xffffffffu, v.w, d));
+}
+__device__ __forceinline__ uint4 pick16(bool c, const uint4 &a, const uint4 &b) {
+    return make_uint4(c ? a.x : b.x, c ? a.y : b.y, c ? a.z : b.z, c ? a.w : b.w);
+}
+__device__ __forceinline__ void quad_transpose(uint4 (&u)[4], int lane) {
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+        const bool hi = lane & 1;
+        const uint4 got = shfl_xor16(pick16(hi, u[k], u[k + 1]), 1);
+        u[k] = pick16(hi, got, u[k]);
+        u[k + 1] = pick16(hi, u[k + 1], got);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const bool hi = lane & 2;
+        const uint4 got = shfl_xor16(pick16(hi, u[k], u[k + 2]), 2);
+        u[k] = pick16(hi, got, u[k]);
+        u[k + 2] = pick16(hi, u[k + 2], got);
+    }
+}
+
+struct BranchWarpWalk {
+    BranchWalk<128> w;
+    BranchPiece pc[2];       // piece p of the CTA in slot p & 1
+    int more;                // whether the piece walked to last exists
+};
+
 // Warps: 4 QT softmax (thread = row of a 128-row tile = TMEM lane), one that
 // loads (Q of a piece, then 128-key K and V tiles, page by page, by TMA), the
 // MMA issuers (one per row tile where P has its own TMEM columns, else one),
@@ -248,12 +321,10 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                        const __grid_constant__ CUtensorMap tmV, bf16 *o, const long o_ld, const float sl2,
                        const int tt1, const __grid_constant__ BranchSched sc, int *err) {
     using A = BranchTile<HD, QT>;
-    pdl_wait();
     extern __shared__ uint8_t smem_raw[];
-    __shared__ int sh_scan[32];
+    __shared__ int sh_len[2 * LEN_CACHE], sh_scan[32];
     __shared__ BranchStart sh_start;
-    const BranchStart start = branch_start<128>(sc, sh_scan, &sh_start, err);
-    if (start.n == 0) return;
+    __shared__ BranchWarpWalk sh_walk[4 * QT];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint8_t *sQ = smem, *sK = smem + A::OFF_K, *sV = smem + A::OFF_V;
     uint64_t *bar = reinterpret_cast<uint64_t *>(smem + A::OFF_BAR);
@@ -267,7 +338,8 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
     uint64_t *s_full = v_tail + A::STAGES;     // [QT] S_i computed
     uint64_t *s_cons = s_full + QT;            // [QT] S_i read (SEP_P)
     uint64_t *p_full = s_cons + QT;            // [QT] P_i written, O_i corrected
-    uint64_t *pv_done = p_full + QT;           // [QT] P_i V done (SEP_P: every tile; else last of a piece)
+    uint64_t *p_half = p_full + QT;            // [QT] first 64 keys of P_i written, O_i corrected
+    uint64_t *pv_done = p_half + QT;           // [QT] P_i V done (SEP_P: every tile; else last of a piece)
     uint64_t *o_free = pv_done + QT;           // [QT] O_i of piece p read out
     uint64_t *turn = o_free + QT;              // [2][4] exponential-phase hand-off (TURNS)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(turn + 8);
@@ -287,6 +359,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             mbar_init(&s_full[i], 1);
             mbar_init(&s_cons[i], 128);
             mbar_init(&p_full[i], 128);
+            mbar_init(&p_half[i], 128);
             mbar_init(&pv_done[i], 1);
             mbar_init(&o_free[i], 128);
         }
@@ -294,6 +367,10 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         mbar_fence_init();
     }
     if (warp == A::W_MMA) tmem_alloc(tmem_slot, A::TMEM_COLS);
+    // nothing above depends on the kernels before this one
+    pdl_wait();
+    const BranchStart start = branch_start<128>(sc, sh_len, sh_scan, &sh_start, err);
+    branch_zero_rows<bf16>(sc, sh_len, o, o_ld, sc.Hk * sc.grp * HD);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -301,14 +378,16 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
     BranchWalk<128> walk(sc, start);
     BranchPiece pc;
 
-    if (warp == A::W_TMA) {
+    if (start.n == 0) {
+        // a line shorter than the CTAs are many
+    } else if (warp == A::W_TMA) {
         // ------------------------------------------------------ TMA producer
         const int box = min(sc.ps, 128), log_ps = 31 - __clz(sc.ps);
         const int q_bytes = QT * A::NR * tt1 * sc.grp * 128;
         int p = 0, g = 0;
         uint32_t tails = 0, tail_ph = 0;       // stages whose last use was a tail, parity of their tail uses
         bool ok = true;
-        while (ok && walk.next(pc)) {
+        while (ok && walk.next(sc, sh_len, pc)) {
             if (p > 0) ok = mbar_wait(q_empty, (p - 1) & 1, err, ERR_WAIT_PRODUCER);
             if (!ok) break;
             if (lane == 0) {
@@ -319,11 +398,12 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                                     pc.t0 + i * tt1);
             }
             ++p;
-            const int *pages = sc.table + (size_t)max(pc.row, 0) * sc.max_pages;
+            const int row_id = sc.table_row(pc.b, sh_len);
+            const int *pages = sc.table + (size_t)max(row_id, 0) * sc.max_pages;
             // first pool row of this lane's page in key tile kt (lane < pages of a tile)
             auto page_row = [&](int kt) {
                 const int key = pc.key0 + kt * 128 + lane * box;
-                if (lane * box >= 128 || kt * 128 + lane * box >= pc.keys || pc.row < 0) return -1;
+                if (lane * box >= 128 || kt * 128 + lane * box >= pc.keys || row_id < 0) return -1;
                 const int id = pages[key >> log_ps];
                 if (id < 0 || id >= sc.n_pages) {
                     if (err) atomicOr(err, ERR_BAD_SEQ);
@@ -376,7 +456,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         uint32_t ph = 0;
         int g = 0;
         bool ok = true;
-        while (ok && walk.next(pc)) {
+        while (ok && walk.next(sc, sh_len, pc)) {
             const int kt = pc.kt1 - 1;
             g += pc.kt1 - pc.kt0;
             const int valid = pc.keys - kt * 128;
@@ -402,6 +482,8 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         const uint64_t dQ0 = sdesc_sw128(smem_u32(sQ), 16, 1024);
         const uint64_t dK0 = sdesc_sw128(smem_u32(sK), 16, 1024);
         const uint64_t dV0 = sdesc_sw128(smem_u32(sV), A::REGION, 1024);
+        // (issued for both tiles also where a unit has rows in the first only: a
+        // branch around the instructions cost 3 % on the large shapes)
         auto issue_s = [&](int i, int g) {             // S_i = Q_i K_g^T
             const uint64_t dq = dQ0 + (uint64_t)((i * A::Q_BYTES) >> 4);
             const uint64_t dk = dK0 + (uint64_t)(((g % A::STAGES) * A::KV_BYTES) >> 4);
@@ -412,12 +494,14 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             }
             tc_commit_warp(&s_full[i]);
         };
-        auto issue_pv = [&](int i, int g, bool fresh) {   // O_i (+)= P_i V_g, P_i in TMEM
+        auto issue_pv = [&](int i, int g, bool fresh, int half) {   // O_i (+)= P_i V_g over 64 keys, P_i in TMEM
             const uint64_t dv = dV0 + (uint64_t)(((g % A::STAGES) * A::KV_BYTES) >> 4);
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
+            for (int k = 0; k < 4; ++k) {
+                const int ks = 4 * half + k;
                 tc_mma_tmem_a_warp(tmem + A::O_COL(i), tmem + A::P_COL(i) + 8 * ks, dv + ((ks * 16 * 128) >> 4), idesc_o,
                                    (!fresh || ks > 0) ? 1u : 0u);
+            }
         };
         auto wait = [&](uint64_t *b, int parity) -> bool {
             const bool r = mbar_wait(b, parity & 1, err, ERR_WAIT_MMA);
@@ -433,7 +517,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         Tile ts{-1, -1, false, true}, tv{-1, -1, false, true};
         auto step = [&](BranchWalk<128> &w, BranchPiece &c, Tile &t) -> bool {
             if (t.last) {
-                if (!w.next(c)) return false;
+                if (!w.next(sc, sh_len, c)) return false;
                 ++t.p;
                 t.first = true;
             } else {
@@ -448,16 +532,31 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             if (t.first && !wait(q_full, t.p)) return false;
             return wait(&k_full[t.g % A::STAGES], t.g / A::STAGES);
         };
-        auto pv_ready = [&](int i, const Tile &t) -> bool {
+        // P_i V of a tile; in two halves, the first while the softmax is still
+        // at the exponentials of the second
+        auto do_pv = [&](int i, const Tile &t) -> bool {
             if (t.first && t.p > 0 && !wait(&o_free[i], t.p - 1)) return false;
-            return wait(&p_full[i], t.g) && wait(&v_full[t.g % A::STAGES], t.g / A::STAGES);
+            if (A::HALVES) {
+                if (!wait(&v_full[t.g % A::STAGES], t.g / A::STAGES) || !wait(&p_half[i], t.g)) return false;
+                tc_fence_after();
+                issue_pv(i, t.g, t.first, 0);
+                if (!wait(&p_full[i], t.g)) return false;
+                tc_fence_after();
+                issue_pv(i, t.g, t.first, 1);
+            } else {
+                if (!wait(&p_full[i], t.g) || !wait(&v_full[t.g % A::STAGES], t.g / A::STAGES)) return false;
+                tc_fence_after();
+                issue_pv(i, t.g, t.first, 0);
+                issue_pv(i, t.g, t.first, 1);
+            }
+            return true;
         };
         if constexpr (A::SEP_P) {
             // S_i of the next tile as soon as the softmax has read S_i, then
             // P_i V once P_i is ready
             const int i = warp - A::W_MMA;
             bool more = step(walk_s, ps, ts);
-            bool ok = s_ready(ts);
+            bool ok = more && s_ready(ts);
             if (ok) {
                 tc_fence_after();
                 issue_s(i, 0);
@@ -473,9 +572,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                     tc_commit_warp(&k_empty[ts.g % A::STAGES]);
                     if (ts.last) tc_commit_warp(q_empty);
                 }
-                if (!pv_ready(i, tv)) break;
-                tc_fence_after();
-                issue_pv(i, tv.g, tv.first);
+                if (!do_pv(i, tv)) break;
                 tc_commit_warp(&pv_done[i]);
                 tc_commit_warp(&v_empty[tv.g % A::STAGES]);
             }
@@ -483,7 +580,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             // P_i overwrites S_i: P0 V, next S0, P1 V, next S1 -- the order in
             // which the warpgroups finish
             bool more = step(walk_s, ps, ts);
-            bool ok = s_ready(ts);
+            bool ok = more && s_ready(ts);
             if (ok) {
                 tc_fence_after();
                 issue_s(0, 0);
@@ -493,18 +590,14 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             }
             while (ok && step(walk, pv, tv)) {
                 more = more && step(walk_s, ps, ts);
-                if (!pv_ready(0, tv)) break;
-                tc_fence_after();
-                issue_pv(0, tv.g, tv.first);
+                if (!do_pv(0, tv)) break;
                 if (tv.last) tc_commit_warp(&pv_done[0]);
                 if (more) {
                     if (!s_ready(ts)) break;
                     tc_fence_after();
                     issue_s(0, ts.g);
                 }
-                if (!pv_ready(1, tv)) break;
-                tc_fence_after();
-                issue_pv(1, tv.g, tv.first);
+                if (!do_pv(1, tv)) break;
                 tc_commit_warp(&v_empty[tv.g % A::STAGES]);
                 if (tv.last) tc_commit_warp(&pv_done[1]);
                 if (more) {
@@ -523,54 +616,48 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
         const uint32_t tS = lanes + A::S_COL(wg), tP = lanes + A::P_COL(wg), tO = lanes + A::O_COL(wg);
         // One key tile: S_i -> running max m, P_i = 2^(S_i sl2 - m) into TMEM,
-        // running sum l.  cols: keys of this tile the row sees.  false: a wait
-        // ran out.
-        auto tile = [&](int g, int cols, bool fresh, bool live, float &m, float &l) -> bool {
+        // running sum l.  cols: keys of this tile the row sees; masked: some
+        // row of the warp does not see all 128.  false: a wait ran out.
+        auto tile = [&](int g, int cols, bool masked, bool fresh, float &m, float &l) -> bool {
             bool ok = mbar_wait(&s_full[wg], g & 1, err, ERR_WAIT_SOFTMAX);
+            __syncwarp();
             if (!__all_sync(0xffffffffu, ok)) return false;
             tc_fence_after();
             float s[128];
-            float alpha = 1.0f;
-            bool grow = false;
-            if (live) {
-                tmem_ld128_sync(tS, s);
-                if constexpr (A::SEP_P) {
-                    tc_fence_before();
-                    mbar_arrive(&s_cons[wg]);
-                }
-                if (__any_sync(0xffffffffu, cols < 128)) {
-#pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (c >= cols) s[c] = -INFINITY;
-                }
-                float mx[16];
-#pragma unroll
-                for (int k = 0; k < 16; ++k) mx[k] = s[k];
-#pragma unroll
-                for (int c = 16; c < 112; c += 32) {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) mx[k] = max3(mx[k], s[c + k], s[c + 16 + k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 16; ++k) mx[k] = fmaxf(mx[k], s[112 + k]);
-#pragma unroll
-                for (int k = 0; k < 5; ++k) mx[k] = max3(mx[k], mx[k + 5], mx[k + 10]);
-                const float m_new = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[15]), mx[0]) * sl2;
-                // a row that sees no key of a piece's first tile sees none of
-                // the piece: m stays -inf, every weight 0
-                if (fresh) m = m_new;
-                grow = !fresh && m_new > m + A::LAZY;
-                if (grow) {
-                    alpha = exp2_mufu(m - m_new);
-                    m = m_new;
-                }
-            } else if constexpr (A::SEP_P) {
+            tmem_ld128_sync(tS, s);
+            if constexpr (A::SEP_P) {
+                tc_fence_before();
                 mbar_arrive(&s_cons[wg]);
             }
+            if (masked) {
+#pragma unroll
+                for (int c = 0; c < 128; ++c)
+                    if (c >= cols) s[c] = -INFINITY;
+            }
+            float mx[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) mx[k] = s[k];
+#pragma unroll
+            for (int c = 16; c < 112; c += 32) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) mx[k] = max3(mx[k], s[c + k], s[c + 16 + k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) mx[k] = fmaxf(mx[k], s[112 + k]);
+#pragma unroll
+            for (int k = 0; k < 5; ++k) mx[k] = max3(mx[k], mx[k + 5], mx[k + 10]);
+            const float m_new = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[15]), mx[0]) * sl2;
+            // a row that sees no key of a piece's first tile sees none of the
+            // piece: m stays -inf, every weight 0
+            if (fresh) m = m_new;
+            const bool grow = !fresh && m_new > m + A::LAZY;
+            const float alpha = grow ? exp2_mufu(m - m_new) : 1.0f;
+            if (grow) m = m_new;
             if constexpr (A::SEP_P) {
                 // P_i free and O_i stable once P V of the previous tile is done
                 if (g >= 1) {
                     ok = mbar_wait(&pv_done[wg], (g - 1) & 1, err, ERR_WAIT_SOFTMAX);
+                    __syncwarp();
                     if (!__all_sync(0xffffffffu, ok)) return false;
                     tc_fence_after();
                 }
@@ -590,92 +677,163 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                 // MUFU-bound exponentials
                 if (wg == 1 || g > 0) {
                     ok = mbar_wait(&turn[4 * wg + q], (wg == 1 ? g : g - 1) & 1, err, ERR_WAIT_SOFTMAX);
+                    __syncwarp();
                     if (!__all_sync(0xffffffffu, ok)) return false;
                 }
             }
-            if (live) {
-                const float nm = m == -INFINITY ? 0.0f : -m;
-                const float2 sc2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm);
-                float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
+            const float nm = m == -INFINITY ? 0.0f : -m;
+            const float2 sc2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm);
+            float2 rs0 = make_float2(0.f, 0.f), rs1 = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int qt = 0; qt < 4; ++qt) {
-                    uint32_t w[16];
+            for (int qt = 0; qt < 4; ++qt) {
+                uint32_t w[16];
 #pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        const int c = 32 * qt + 2 * k;
-                        const float2 a = __ffma2_rn(make_float2(s[c], s[c + 1]), sc2, nm2);
-                        const float2 b = __ffma2_rn(make_float2(s[c + 2], s[c + 3]), sc2, nm2);
-                        const float2 pa = make_float2(exp2_mufu(a.x), exp2_mufu(a.y));
-                        const float2 pb = make_float2(exp2_mufu(b.x), exp2_mufu(b.y));
-                        rs0 = __fadd2_rn(rs0, pa);
-                        rs1 = __fadd2_rn(rs1, pb);
-                        const __nv_bfloat162 h0 = __floats2bfloat162_rn(pa.x, pa.y);
-                        const __nv_bfloat162 h1 = __floats2bfloat162_rn(pb.x, pb.y);
-                        w[k] = *reinterpret_cast<const uint32_t *>(&h0);
-                        w[k + 1] = *reinterpret_cast<const uint32_t *>(&h1);
-                    }
-                    tmem_st16u_sync(tP + 16 * qt, w);
+                for (int k = 0; k < 16; k += 2) {
+                    const int c = 32 * qt + 2 * k;
+                    const float2 a = __ffma2_rn(make_float2(s[c], s[c + 1]), sc2, nm2);
+                    const float2 b = __ffma2_rn(make_float2(s[c + 2], s[c + 3]), sc2, nm2);
+                    const float2 pa = make_float2(exp2_mufu(a.x), exp2_mufu(a.y));
+                    const float2 pb = make_float2(exp2_mufu(b.x), exp2_mufu(b.y));
+                    rs0 = __fadd2_rn(rs0, pa);
+                    rs1 = __fadd2_rn(rs1, pb);
+                    const __nv_bfloat162 h0 = __floats2bfloat162_rn(pa.x, pa.y);
+                    const __nv_bfloat162 h1 = __floats2bfloat162_rn(pb.x, pb.y);
+                    w[k] = *reinterpret_cast<const uint32_t *>(&h0);
+                    w[k + 1] = *reinterpret_cast<const uint32_t *>(&h1);
                 }
-                const float2 rs = __fadd2_rn(rs0, rs1);
-                l = l * alpha + (rs.x + rs.y);
+                tmem_st16u_sync(tP + 16 * qt, w);
+                if (A::HALVES && qt == 1) {
+                    tc_fence_before();
+                    mbar_arrive(&p_half[wg]);
+                }
             }
+            const float2 rs = __fadd2_rn(rs0, rs1);
+            l = l * alpha + (rs.x + rs.y);
             tc_fence_before();
             mbar_arrive(&p_full[wg]);
-            if constexpr (A::TURNS) {
-                __syncwarp();
+            __syncwarp();
+            if constexpr (A::TURNS)
                 if (lane == 0) mbar_arrive(&turn[4 * (wg ^ 1) + q]);
-            }
             return true;
         };
+        // The same steps of a warp none of whose rows exist: barriers only.
+        auto idle_tile = [&](int g) -> bool {
+            bool ok = mbar_wait(&s_full[wg], g & 1, err, ERR_WAIT_SOFTMAX);
+            if constexpr (A::SEP_P) {
+                mbar_arrive(&s_cons[wg]);
+                if (g >= 1) ok = ok && mbar_wait(&pv_done[wg], (g - 1) & 1, err, ERR_WAIT_SOFTMAX);
+            }
+            if constexpr (A::TURNS)
+                if (wg == 1 || g > 0)
+                    ok = ok && mbar_wait(&turn[4 * wg + q], (wg == 1 ? g : g - 1) & 1, err, ERR_WAIT_SOFTMAX);
+            ok = __all_sync(0xffffffffu, ok);
+            if constexpr (A::HALVES) mbar_arrive(&p_half[wg]);
+            mbar_arrive(&p_full[wg]);
+            if constexpr (A::TURNS)
+                if (lane == 0) mbar_arrive(&turn[4 * (wg ^ 1) + q]);
+            return ok;
+        };
+        // The walk of a softmax warp lives in shared memory, so that its piece
+        // takes no registers during the key tiles.
+        BranchWarpWalk &ww = sh_walk[warp];
+        auto advance = [&](int slot) {
+            __syncwarp();
+            if (lane == 0) {
+                BranchWalk<128> w = ww.w;
+                BranchPiece c;
+                ww.more = w.next(sc, sh_len, c);
+                ww.w = w;
+                ww.pc[slot] = c;
+            }
+            __syncwarp();
+        };
+        if (lane == 0) ww.w = walk;
+        advance(0);
         int g = 0, p = 0;
         bool ok = true;
-        while (ok && walk.next(pc)) {
-            const bool row_ok = in_tile && tl_ < pc.nt;
+        while (ok && ww.more) {
+            const BranchPiece &cur = ww.pc[p & 1];
+            const bool row_ok = in_tile && tl_ < cur.nt;
             const bool live = __any_sync(0xffffffffu, row_ok) != 0;
-            const int t = pc.t0 + tl_;
             int see = 1 << 30;                             // keys of the unit this row sees
             if (row_ok) {
-                const int b = t / sc.n_q;
-                see = min(sc.limit(sc.seq_len(b), t - b * sc.n_q) - pc.key0, pc.keys);
+                const int t = cur.t0 + tl_, b = cur.idx < sc.n_pr ? t / sc.n_q : cur.b;
+                see = min(sc.limit(sc.seq_len(b, sh_len), t - b * sc.n_q) - cur.key0, cur.keys);
             }
             float m = -INFINITY, l = 0.0f;
-            for (int kt = pc.kt0; kt < pc.kt1; ++kt, ++g) {
-                ok = tile(g, see - kt * 128, kt == pc.kt0, live, m, l);
-                if (!ok) break;
+            const int kt0 = cur.kt0, kt1 = cur.kt1;
+            if (live) {
+                const int least = __reduce_min_sync(0xffffffffu, see);
+                for (int kt = kt0; kt < kt1; ++kt, ++g) {
+                    ok = tile(g, see - kt * 128, least < (kt + 1) * 128, kt == kt0, m, l);
+                    if (!ok) break;
+                }
+            } else {
+                for (int kt = kt0; ok && kt < kt1; ++kt, ++g) ok = idle_tile(g);
             }
             if (!ok) break;
+            advance((p + 1) & 1);                          // while the last P V runs
             ok = mbar_wait(&pv_done[wg], (A::SEP_P ? g - 1 : p) & 1, err, ERR_WAIT_SOFTMAX);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
-            if (live) {
-                if (sc.n_pr == 0 && pc.kt1 - pc.kt0 == pc.n_kt) {
-                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                    bf16 *dst = o + (size_t)t * o_ld + (pc.h * sc.grp + gq) * HD;
-#pragma unroll 1
-                    for (int c = 0; c < HD / 16; ++c) {
-                        float x[16];
-                        tmem_ld16_sync(tO + 16 * c, x);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] *= inv;
-                        if (row_ok) store16<bf16>(dst + 16 * c, x);
-                    }
-                } else {
-                    const long row = branch_slot_row(sc, pc, blockIdx.x, p == 0) + tl_ * sc.grp + gq;
-#pragma unroll 1
-                    for (int c = 0; c < HD / 16; ++c) {
-                        float x[16];
-                        tmem_ld16_sync(tO + 16 * c, x);
-                        if (row_ok) store16<float>(sc.ws_o + row * HD + 16 * c, x);
-                    }
-                    if (row_ok) sc.ws_ml[row] = make_float2(m, l);
-                }
+            if (!live) {
+                tc_fence_before();
+                mbar_arrive(&o_free[wg]);
+                ++p;
+                continue;
+            }
+            float x[HD];
+            if constexpr (HD == 128) {
+                tmem_ld128_sync(tO, x);
+            } else {
+                tmem_ld32_sync(tO, *reinterpret_cast<float(*)[32]>(x));
+                tmem_ld32_sync(tO + 32, *reinterpret_cast<float(*)[32]>(x + 32));
             }
             tc_fence_before();
-            mbar_arrive(&o_free[wg]);
+            mbar_arrive(&o_free[wg]);                      // the next piece may write O_i
+            const BranchPiece c = cur;
+            if (sc.n_pr == 0 && c.kt1 - c.kt0 == c.n_kt) {
+                // Whole unit: 32 columns (64 bytes) of a row at a time.  Each
+                // quad of lanes exchanges its four rows' 16-byte parts, so
+                // that a store covers 64 consecutive bytes of 8 rows.
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                const long long mine = row_ok ? (long long)(c.t0 + tl_) * o_ld + (c.h * sc.grp + gq) * HD : -1;
+                long long at[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) at[j] = __shfl_sync(0xffffffffu, mine, (lane & ~3) + j);
+#pragma unroll
+                for (int cb = 0; cb < HD / 32; ++cb) {
+                    uint4 u[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int at_c = 32 * cb + 8 * i + 2 * j;
+                            const __nv_bfloat162 y = __floats2bfloat162_rn(x[at_c] * inv, x[at_c + 1] * inv);
+                            w[j] = *reinterpret_cast<const uint32_t *>(&y);
+                        }
+                        u[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    quad_transpose(u, lane);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (at[j] >= 0) *reinterpret_cast<uint4 *>(o + at[j] + 32 * cb + 8 * (lane & 3)) = u[j];
+                }
+            } else if (row_ok) {
+                const long row0 = branch_slot_row(sc, c, blockIdx.x, p == 0);
+                const int rr = tl_ * sc.grp + gq, pitch = c.idx < sc.n_pr ? sc.pitch_p : sc.pitch_o;
+                float4 *dst = reinterpret_cast<float4 *>(sc.ws_o + row0 * HD) + rr;
+#pragma unroll
+                for (int i = 0; i < HD / 4; ++i)
+                    dst[(size_t)i * pitch] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                sc.ws_ml[row0 + rr] = make_float2(m, l);
+            }
             ++p;
         }
     }
+    pdl_release();
     tc_fence_before();
     __syncthreads();
     if (warp == A::W_MMA) {
@@ -700,9 +858,10 @@ __global__ void __launch_bounds__(256)
     using A = BranchTileF32<HD>;
     pdl_wait();
     extern __shared__ __align__(16) float sm[];
-    __shared__ int sh_scan[32];
+    __shared__ int sh_len[2 * LEN_CACHE], sh_scan[32];
     __shared__ BranchStart sh_start;
-    const BranchStart start = branch_start<64>(sc, sh_scan, &sh_start, err);
+    const BranchStart start = branch_start<64>(sc, sh_len, sh_scan, &sh_start, err);
+    branch_zero_rows<float>(sc, sh_len, o, o_ld, sc.Hk * sc.grp * HD);
     float *sQ = sm, *sK = sQ + 64 * A::LD, *sV = sK + 64 * A::LD, *sP = sV + 64 * A::LD;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int log_ps = 31 - __clz(sc.ps);
@@ -712,8 +871,8 @@ __global__ void __launch_bounds__(256)
     BranchWalk<64> walk(sc, start);
     BranchPiece pc;
     int np = 0;
-    while (walk.next(pc)) {
-        const int rows = pc.nt * sc.grp;
+    while (walk.next(sc, sh_len, pc)) {
+        const int rows = pc.nt * sc.grp, row_id = sc.table_row(pc.b, sh_len);
         __syncthreads();
         for (int x = tid; x < 64 * V4; x += 256) {
             const int r = x / V4, c = x % V4;
@@ -731,7 +890,7 @@ __global__ void __launch_bounds__(256)
             see[i] = 0;
             if (r < rows) {
                 const int t = pc.t0 + r / sc.grp, b = t / sc.n_q;
-                see[i] = min(sc.limit(sc.seq_len(b), t - b * sc.n_q) - pc.key0, pc.keys);
+                see[i] = min(sc.limit(sc.seq_len(b, sh_len), t - b * sc.n_q) - pc.key0, pc.keys);
             }
             m[i] = -INFINITY;
             l[i] = 0.0f;
@@ -743,9 +902,9 @@ __global__ void __launch_bounds__(256)
             for (int x = tid; x < 64 * V4; x += 256) {
                 const int r = x / V4, c = x % V4, key = kt * 64 + r;
                 float4 fk = make_float4(0, 0, 0, 0), fv = fk;
-                if (key < pc.keys && pc.row >= 0) {
+                if (key < pc.keys && row_id >= 0) {
                     const int at = pc.key0 + key;
-                    const int id = sc.table[(size_t)pc.row * sc.max_pages + (at >> log_ps)];
+                    const int id = sc.table[(size_t)row_id * sc.max_pages + (at >> log_ps)];
                     if (id >= 0 && id < sc.n_pages) {
                         const size_t off = ((size_t)id * sc.ps + (at & (sc.ps - 1))) * ld + pc.h * HD + 4 * c;
                         fk = *reinterpret_cast<const float4 *>(k + off);
@@ -830,6 +989,7 @@ __global__ void __launch_bounds__(256)
         }
         const bool whole = sc.n_pr == 0 && pc.kt1 - pc.kt0 == pc.n_kt;
         const long row0 = whole ? 0 : branch_slot_row(sc, pc, blockIdx.x, np == 0);
+        const int pitch = pc.idx < sc.n_pr ? sc.pitch_p : sc.pitch_o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = 4 * ty + i;
@@ -841,7 +1001,10 @@ __global__ void __launch_bounds__(256)
                 for (int j = 0; j < NC; ++j) dst[tx + 16 * j] = acc[i][j] * inv;
             } else {
 #pragma unroll
-                for (int j = 0; j < NC; ++j) sc.ws_o[(row0 + r) * HD + tx + 16 * j] = acc[i][j];
+                for (int j = 0; j < NC; ++j) {
+                    const int col = tx + 16 * j;
+                    sc.ws_o[row0 * HD + ((size_t)(col >> 2) * pitch + r) * 4 + (col & 3)] = acc[i][j];
+                }
                 if (tx == 0) sc.ws_ml[row0 + r] = make_float2(m[i], l[i]);
             }
         }
@@ -850,96 +1013,139 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---------------------------------------------------------------- combine
-// grid.x = (key head, own entry), grid.y = 8 rows of it, one warp each.  Adds
-// the pieces of the row's prefix unit and of its own unit in CTA order; rows
-// already written are left, rows without keys get zeros.
-template <typename T, int HD>
+// Adds the pieces of a row's prefix unit and of its own unit in CTA order.
+// PREFIX: grid.x is (key head, own entry), and every row is merged.  Else
+// grid.x is the CTA boundaries, of which the first one inside a unit merges
+// it (units that one CTA ran whole are written already).  grid.y: NI RB rows
+// of the unit.  A thread owns four columns of every RB-th row, neighbouring
+// threads neighbouring rows.  Latency bound, so nothing passes between
+// threads and the loads of NI rows x KB pieces are in flight together: one
+// row and 8 pieces where many pieces meet few rows (PREFIX), 4 rows and 2
+// pieces where few pieces meet many rows.
+template <typename T, int HD, bool PREFIX>
 __global__ void __launch_bounds__(256)
     branch_combine_kernel(T *o, const long o_ld, const __grid_constant__ BranchSched s) {
     pdl_wait();
-    constexpr int W = HD >= 32 ? HD / 32 : 1;              // columns of a lane
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.x / s.E, e = blockIdx.x - h * s.E;
+    constexpr int RB = 256 / (HD / 4), NI = PREFIX ? 1 : 4, KB = PREFIX ? 8 : 2;
+    const unsigned PP = PREFIX ? (unsigned)s.n_pr * s.line_len(s.n_pt) : 0;
+    int h, e, off, len;                                    // own unit: position in its head's line, line length
+    if (PREFIX) {
+        h = blockIdx.x / s.E;
+        e = blockIdx.x - h * s.E;
+        off = s.ws_off[e];
+        len = s.ws_off[e + 1] - off;
+    } else {
+        const int4 st = s.ws_start[blockIdx.x + 1];
+        h = st.x;
+        e = st.y;
+        off = st.z;
+        len = s.line_len(st.w);
+    }
+    const unsigned Th = PP + s.ws_off[s.E], Tl = Th * s.Hk;
+    const BranchLine line(Tl, s.G);
+    unsigned so;                                           // the own unit's start on the line
+    int no = 0, co = 0;                                    // its pieces, their first CTA
+    if (PREFIX) {
+        so = h * Th + PP + off;
+        if (len > 0) {
+            co = line.owner(so + s.lead);
+            no = line.owner(so + len - 1) - co + 1;
+        }
+    } else {
+        const unsigned c = blockIdx.x + 1, x = line.begin(c);
+        if (x >= Tl || off <= s.lead) return;          // no key tile of the unit lies before CTA c
+        so = x - off;
+        co = c - 1;
+        if (line.begin(co) > so + s.lead) return;      // an earlier boundary merges the unit
+        no = line.owner(so + len - 1) - co + 1;
+    }
     const int b = e / s.n_st, i0 = (e - b * s.n_st) * s.tt;
-    const int r = blockIdx.y * 8 + warp;
-    if (r >= min(s.tt, s.n_q - i0) * s.grp) return;
-    const long long Th = (long long)s.n_pr * s.n_pt + s.ws_off[s.E], Tl = Th * s.Hk;
-    const int n_own = s.ws_off[e + 1] - s.ws_off[e];
-    const int t = b * s.n_q + i0 + r / s.grp;
-    int np = 0, no = 0, cp = 0, co = 0;                    // pieces and first CTA of both units
-    long long so = 0;
-    long row_p = 0;
-    if (s.n_pr > 0) {
-        const int pi = t / s.tt;
-        const long long s0 = h * Th + (long long)pi * s.n_pt;
-        cp = s.owner(Tl, s0);
-        np = s.owner(Tl, s0 + s.n_pt - 1) - cp + 1;
-        row_p = ((long)h * s.n_pr + pi) * s.pitch_p + (t - pi * s.tt) * s.grp + r % s.grp;
+    const int rows = min(s.tt, s.n_q - i0) * s.grp;
+    const int ch = threadIdx.x / RB, r0 = blockIdx.y * (NI * RB) + threadIdx.x % RB;
+    if (r0 >= rows) return;
+    int np = 0;
+    const float4 *px = nullptr;                            // first prefix piece: this row's float4, (m, l)
+    const float2 *pml = nullptr;
+    if (PREFIX) {
+        const int t = b * s.n_q + i0 + r0 / s.grp, pi = t / s.tt, in = (t - pi * s.tt) * s.grp + r0 % s.grp;
+        const unsigned s0 = h * Th + (unsigned)pi * s.line_len(s.n_pt) + s.lead;
+        const int cp = line.owner(s0);
+        np = line.owner(s0 + s.n_pt - 1) - cp + 1;
+        const long slot = ((long)h * s.n_pr + pi + cp) * s.pitch_p;
+        px = reinterpret_cast<const float4 *>(s.ws_o + slot * HD) + (size_t)ch * s.pitch_p + in;
+        pml = s.ws_ml + slot + in;
     }
-    if (n_own > 0) {
-        so = h * Th + (long long)s.n_pr * s.n_pt + s.ws_off[e];
-        co = s.owner(Tl, so);
-        no = s.owner(Tl, so + n_own - 1) - co + 1;
-        if (s.n_pr == 0 && no == 1) return;                // written by the CTA that ran it whole
-    }
-    auto row_of = [&](int k) -> long {                     // partial row of the k-th piece
-        if (k < np) return row_p + (long)(cp + k) * s.pitch_p;
-        const int c = co + k - np;
-        if (s.n_pr > 0) return s.slots_p * s.pitch_p + ((long)h * s.E + e + c) * s.pitch_o + r;
-        return (2l * c + (s.begin(Tl, c) >= so ? 0 : 1)) * s.pitch_o + r;
-    };
+    const long own0 = s.slots_p * s.pitch_p + ((long)h * s.E + e + co) * s.pitch_o;
     const int n = np + no;
-    float mm = -INFINITY;
-    for (int k = lane; k < n; k += 32) mm = fmaxf(mm, s.ws_ml[row_of(k)].x);
+    float m[NI], den[NI];
+    float4 acc[NI];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-    float den = 0.0f, acc[W];
+    for (int i = 0; i < NI; ++i) {
+        m[i] = -INFINITY;
+        den[i] = 0.0f;
+        acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int k0 = 0; k0 < n; k0 += KB) {
+        float4 x[NI][KB];
+        float2 ml[NI][KB];
 #pragma unroll
-    for (int j = 0; j < W; ++j) acc[j] = 0.0f;
-    for (int k0 = 0; k0 < n; k0 += 32) {
-        float w = 0.0f;
-        long row = 0;
-        if (k0 + lane < n) {
-            row = row_of(k0 + lane);
-            const float2 ml = s.ws_ml[row];
-            w = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - mm);
-            den += w * ml.y;
-        }
-        const int m = min(32, n - k0);
-#pragma unroll 4
-        for (int k = 0; k < m; ++k) {
-            const float wk = __shfl_sync(0xffffffffu, w, k);
-            const long rk = __shfl_sync(0xffffffffu, row, k);
-            if (wk == 0.0f || lane * W >= HD) continue;    // a piece without keys for this row
-            const float *src = s.ws_o + rk * HD + lane * W;
-            float x[W];
-            if constexpr (W == 4) {
-                const float4 f = *reinterpret_cast<const float4 *>(src);
-                x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
-            } else if constexpr (W == 2) {
-                const float2 f = *reinterpret_cast<const float2 *>(src);
-                x[0] = f.x; x[1] = f.y;
-            } else {
-                x[0] = src[0];
+        for (int k = 0; k < KB; ++k) {
+            const int kk = min(k0 + k, n - 1);             // a piece that exists: its loads are always sound
+            const bool pre = PREFIX && kk < np;
+            long slot = 0;                                 // the own slot's first row
+            if (!pre) slot = PREFIX ? own0 + (long)(kk - np) * s.pitch_o : (2l * (co + kk) + (line.begin(co + kk) >= so ? 0 : 1)) * s.pitch_o;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int r = min(r0 + i * RB, rows - 1);
+                x[i][k] = pre ? px[(size_t)kk * s.pitch_p * (HD / 4)]
+                              : reinterpret_cast<const float4 *>(s.ws_o + slot * HD)[(size_t)ch * s.pitch_o + r];
+                ml[i][k] = pre ? pml[(size_t)kk * s.pitch_p] : s.ws_ml[slot + r];
+                if (k0 + k >= n) ml[i][k] = make_float2(-INFINITY, 0.0f);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < W; ++j) acc[j] = fmaf(wk, x[j], acc[j]);
+        for (int i = 0; i < NI; ++i) {
+            float top = m[i];
+#pragma unroll
+            for (int k = 0; k < KB; ++k) top = fmaxf(top, ml[i][k].x);
+            const float use = top == -INFINITY ? 0.0f : top;
+            const float a = exp2f(m[i] - use);
+            m[i] = top;
+            den[i] *= a;
+            acc[i] = make_float4(acc[i].x * a, acc[i].y * a, acc[i].z * a, acc[i].w * a);
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                if (ml[i][k].x == -INFINITY) continue;     // no key of this piece for the row
+                const float w = exp2f(ml[i][k].x - use);
+                den[i] = fmaf(w, ml[i][k].y, den[i]);
+                acc[i].x = fmaf(w, x[i][k].x, acc[i].x);
+                acc[i].y = fmaf(w, x[i][k].y, acc[i].y);
+                acc[i].z = fmaf(w, x[i][k].z, acc[i].z);
+                acc[i].w = fmaf(w, x[i][k].w, acc[i].w);
+            }
         }
     }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) den += __shfl_xor_sync(0xffffffffu, den, d);
-    const float inv = den > 0.0f ? 1.0f / den : 0.0f;
-    T *dst = o + (size_t)t * o_ld + (h * s.grp + r % s.grp) * HD + lane * W;
-    if (lane * W < HD) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) dst[j] = from_f<T>(acc[j] * inv);
+    for (int i = 0; i < NI; ++i) {
+        const int r = r0 + i * RB;
+        if (r >= rows) break;
+        const float inv = den[i] > 0.0f ? 1.0f / den[i] : 0.0f;
+        const int tr = r / s.grp;
+        T *dst = o + (size_t)(b * s.n_q + i0 + tr) * o_ld + (h * s.grp + r - tr * s.grp) * HD + 4 * ch;
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4 *>(dst) = make_float4(acc[i].x * inv, acc[i].y * inv, acc[i].z * inv, acc[i].w * inv);
+        } else {
+            const __nv_bfloat162 y0 = __floats2bfloat162_rn(acc[i].x * inv, acc[i].y * inv);
+            const __nv_bfloat162 y1 = __floats2bfloat162_rn(acc[i].z * inv, acc[i].w * inv);
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&y0), *reinterpret_cast<const uint32_t *>(&y1));
+        }
     }
 }
 
 // ------------------------------------------------------------------- host
 struct BranchPlan {
     BranchSched s;
-    int qt, tt1, chunks;
+    int qt, tt1;
     size_t rows, bytes;       // partial rows, workspace bytes
 };
 static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
@@ -973,20 +1179,24 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
         s.n_pr = (int)packed;
         s.n_pt = (shared + KT - 1) / KT;
     }
+    // A unit's query load, pipeline ramp and output take about as long as one
+    // key tile where its rows are few, two where they fill the tile (measured:
+    // 1 against 2 with prefix units 64.9 / 67.1 us for 32 single tokens over
+    // 38880 keys, without them 74.6 / 70.2 us for 6 prompts of 1031 tokens).
+    s.lead = s.n_pr > 0 ? 1 : 2;
     s.pitch_p = (int)(tokens < s.tt ? tokens : s.tt) * s.grp;
     s.pitch_o = (n_q < s.tt ? n_q : s.tt) * s.grp;
     s.slots_p = s.n_pr > 0 ? (long)s.Hk * s.n_pr + s.G : 0;
     const size_t slots_o = s.n_pr > 0 ? (size_t)s.Hk * s.E + s.G : 2 * (size_t)s.G;
     p.rows = (size_t)s.slots_p * s.pitch_p + slots_o * s.pitch_o;
-    p.chunks = (s.pitch_o + 7) / 8;
-    p.bytes = p.rows * (c.head_dim * sizeof(float) + sizeof(float2)) + ((size_t)s.E + 1) * sizeof(int);
+    p.bytes = s.G * sizeof(int4) + p.rows * (c.head_dim * sizeof(float) + sizeof(float2)) + ((size_t)s.E + 1) * sizeof(int);
     return p;
 }
 bool branch_attn_fits(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     const BranchPlan p = branch_plan(c, B, n_q, H, shared);
     const long long kt = c.dtype == XC_F32 ? 64 : 128;
-    const long long own = (long long)p.s.E * (((long long)c.max_pages * c.page_size + kt - 1) / kt);
-    return (long long)B * ((n_q + p.s.tt - 1) / p.s.tt) < (1ll << 30) && p.s.Hk * ((long long)p.s.n_pr * p.s.n_pt + own) < (1ll << 31);
+    const long long own = (long long)p.s.E * (((long long)c.max_pages * c.page_size + kt - 1) / kt + p.s.lead);
+    return (long long)B * ((n_q + p.s.tt - 1) / p.s.tt) < (1ll << 30) && p.s.Hk * ((long long)p.s.n_pr * (p.s.n_pt + p.s.lead) + own) < (1ll << 31);
 }
 size_t branch_attn_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     return branch_plan(c, B, n_q, H, shared).bytes;
@@ -1027,15 +1237,22 @@ static cudaError_t launch_f32(const BranchAttnArgs &a, const BranchPlan &p, floa
 }
 template <typename T, int HD>
 static cudaError_t launch_combine(const BranchAttnArgs &a, const BranchPlan &p, cudaStream_t st) {
-    return launch_pdl(branch_combine_kernel<T, HD>, dim3((unsigned)(p.s.Hk * p.s.E), p.chunks), dim3(256), 0, st,
-                      reinterpret_cast<T *>(a.o), a.o_ld, p.s);
+    constexpr int RB = 256 / (HD / 4);
+    T *o = reinterpret_cast<T *>(a.o);
+    if (p.s.n_pr > 0)
+        return launch_pdl(branch_combine_kernel<T, HD, true>, dim3((unsigned)(p.s.Hk * p.s.E), (p.s.pitch_o + RB - 1) / RB),
+                          dim3(256), 0, st, o, a.o_ld, p.s);
+    if (p.s.G == 1) return cudaSuccess;
+    return launch_pdl(branch_combine_kernel<T, HD, false>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + 4 * RB - 1) / (4 * RB)),
+                      dim3(256), 0, st, o, a.o_ld, p.s);
 }
 
 cudaError_t branch_attn(const xc_kv_cache &c, const BranchAttnArgs &a, void *ws, int *err, cudaStream_t st) {
     BranchPlan p = branch_plan(c, a.B, a.n_q, a.H, a.shared);
     p.s.seqs = a.seqs;
     p.s.causal = a.causal;
-    p.s.ws_o = reinterpret_cast<float *>(ws);
+    p.s.ws_start = reinterpret_cast<int4 *>(ws);
+    p.s.ws_o = reinterpret_cast<float *>(p.s.ws_start + p.s.G);
     p.s.ws_ml = reinterpret_cast<float2 *>(p.s.ws_o + p.rows * c.head_dim);
     p.s.ws_off = reinterpret_cast<int *>(p.s.ws_ml + p.rows);
     const float sl2 = a.scale * 1.4426950408889634f;

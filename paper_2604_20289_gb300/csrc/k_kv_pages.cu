@@ -433,118 +433,139 @@ template <typename T> __device__ __forceinline__ uint4 pack(const float (&x)[16 
 }
 
 // y = rot(x / sqrt(mean x^2 + eps) * gamma) per head; q -> q_out, k and v ->
-// the token's cache row.  A lane holds 16 bytes of a head, LPH = head bytes /
-// 16 lanes a head (the mean and the halves' partners by shuffles), a CTA the
-// same token's heads, so each thread's rotation pairs and gains are loaded
-// once and stay in registers over its heads.  HBM bound: every input and
-// output byte once.
-template <typename T, int HD, bool HALF, int U>
-__global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeArgs a) {
+// the token's cache row.  A warp takes one token and SEG passes over its
+// query, its key or its value heads; a lane holds 16 bytes of a head, LPH =
+// head bytes / 16 lanes a head (the sum of squares and the halves' partners
+// by shuffles).  Gain and rotation are folded once per warp,
+//   y_a = r (x_a (g_a c) - x_b (g_b s)),  y_b = r (x_a (g_a s) + x_b (g_b c)),
+// r the reciprocal root, so a lane's factors stay in registers over the
+// passes.  HBM bound, every input and output byte once; the SEG input loads
+// are issued before anything waits for the token's position and slot.
+template <typename T, int HD, bool HALF, int SEG>
+__global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeArgs a, const int seg_q, const int seg_k) {
     pdl_wait();
     pdl_release();
-    constexpr int VPT = 16 / sizeof(T), LPH = HD / VPT, HP = 256 / LPH;
-    constexpr int NP = HALF ? VPT : VPT / 2;               // rotation pairs of a lane
-    const int t = blockIdx.x, li = threadIdx.x % LPH, sub = threadIdx.x / LPH;
-    const int heads = a.H + 2 * a.Hk, h0 = blockIdx.y * (HP * U) + sub;
+    constexpr int VPT = 16 / sizeof(T), LPH = HD / VPT, HPW = 32 / LPH;
+    const int lane = threadIdx.x & 31, li = lane % LPH;
+    const int n_seg = seg_q + 2 * seg_k, item = blockIdx.x * 8 + (threadIdx.x >> 5), t = item / n_seg;
+    if (t >= a.T) return;
+    int seg = item - t * n_seg;
+    const int kind = seg < seg_q ? 0 : seg < seg_q + seg_k ? 1 : 2;       // queries, keys, values
+    seg -= kind == 0 ? 0 : kind == 1 ? seg_q : seg_q + seg_k;
+    const int heads = kind == 0 ? a.H : a.Hk, hw = seg * (SEG * HPW), h0 = hw + lane / LPH;
+    const T *src = (kind == 0   ? reinterpret_cast<const T *>(a.q) + (size_t)t * a.q_ld
+                    : kind == 1 ? reinterpret_cast<const T *>(a.k) + (size_t)t * a.k_ld
+                                : reinterpret_cast<const T *>(a.v) + (size_t)t * a.v_ld) + h0 * HD + li * VPT;
+    uint4 in[SEG];
+#pragma unroll
+    for (int u = 0; u < SEG; ++u) {
+        in[u] = make_uint4(0, 0, 0, 0);
+        if (h0 + u * HPW < heads) in[u] = *reinterpret_cast<const uint4 *>(src + u * (HPW * HD));
+    }
     const long slot = a.slots[t];
     bool ok = slot >= -1 && slot < a.n_rows;
-    int pos[ROPE_AXES];
-    long base[ROPE_AXES];                                  // table entry of (position, pair 0) of each axis
-    long at = 0;
-    int first = 0;
+    int base[ROPE_AXES];                                   // table entry of (position, pair 0) of each axis
+    int at = 0, first = 0;
 #pragma unroll
     for (int x = 0; x < ROPE_AXES; ++x) {
-        pos[x] = x < a.ax.n ? a.pos[(size_t)t * a.ax.n + x] : 0;
-        if (x < a.ax.n && (pos[x] < 0 || pos[x] >= a.ax.n_pos[x])) ok = false;
-        base[x] = at + (long)pos[x] * a.ax.pairs[x] - first;
+        base[x] = 0;
         if (x < a.ax.n) {
-            at += (long)a.ax.n_pos[x] * a.ax.pairs[x];
+            const int pos = a.pos[(size_t)t * a.ax.n + x];
+            if (pos < 0 || pos >= a.ax.n_pos[x]) ok = false;
+            base[x] = at + pos * a.ax.pairs[x] - first;
+            at += a.ax.n_pos[x] * a.ax.pairs[x];
             first += a.ax.pairs[x];
         }
     }
     if (!ok) {
-        if (threadIdx.x == 0 && blockIdx.y == 0 && a.err) atomicOr(a.err, ERR_BAD_POS);
+        if (lane == 0 && item == t * n_seg && a.err) atomicOr(a.err, ERR_BAD_POS);
         return;
     }
-    float2 cs[NP];
+    if (kind != 0 && slot < 0) return;                     // a token that keeps no keys
+    T *dst = (kind == 0 ? reinterpret_cast<T *>(a.q_out) + (size_t)t * a.o_ld
+                        : reinterpret_cast<T *>(kind == 1 ? a.k_pool : a.v_pool) + (size_t)slot * a.Hk * HD) + h0 * HD + li * VPT;
+    if (kind == 2) {
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-        const int p = HALF ? (li * VPT + j) % (HD / 2) : li * NP + j;
-        long b = base[0];
-        int end = a.ax.pairs[0];
+        for (int u = 0; u < SEG; ++u)
+            if (h0 + u * HPW < heads) *reinterpret_cast<uint4 *>(dst + u * (HPW * HD)) = in[u];
+        return;
+    }
+    // factors of the lane's element j and of its partner
+    const float *gamma = kind == 0 ? a.gamma_q : a.gamma_k;
+    const int mate = HALF ? (li * VPT + HD / 2) % HD : li * VPT;
+    float g[VPT], gm[VPT], fx[VPT], fo[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; j += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(gamma + li * VPT + j), y = *reinterpret_cast<const float4 *>(gamma + mate + j);
+        g[j] = x.x; g[j + 1] = x.y; g[j + 2] = x.z; g[j + 3] = x.w;
+        gm[j] = y.x; gm[j + 1] = y.y; gm[j + 2] = y.z; gm[j + 3] = y.w;
+    }
+#pragma unroll
+    for (int j = 0; j < VPT; j += HALF ? 1 : 2) {
+        const int p = HALF ? (li * VPT + j) % (HD / 2) : (li * VPT + j) / 2;
+        int b = base[0], end = a.ax.pairs[0];
 #pragma unroll
         for (int x = 1; x < ROPE_AXES; ++x)
             if (x < a.ax.n && p >= end) {
                 b = base[x];
                 end += a.ax.pairs[x];
             }
-        cs[j] = a.table[b + p];
-    }
-    float gq[VPT], gk[VPT];
-#pragma unroll
-    for (int j = 0; j < VPT; j += 4) {
-        const float4 x = *reinterpret_cast<const float4 *>(a.gamma_q + li * VPT + j);
-        const float4 y = *reinterpret_cast<const float4 *>(a.gamma_k + li * VPT + j);
-        gq[j] = x.x; gq[j + 1] = x.y; gq[j + 2] = x.z; gq[j + 3] = x.w;
-        gk[j] = y.x; gk[j + 1] = y.y; gk[j + 2] = y.z; gk[j + 3] = y.w;
-    }
-    uint4 in[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int h = h0 + u * HP;
-        in[u] = make_uint4(0, 0, 0, 0);
-        if (h < heads) {
-            const T *src = h < a.H          ? reinterpret_cast<const T *>(a.q) + (size_t)t * a.q_ld + h * HD
-                           : h < a.H + a.Hk ? reinterpret_cast<const T *>(a.k) + (size_t)t * a.k_ld + (h - a.H) * HD
-                                            : reinterpret_cast<const T *>(a.v) + (size_t)t * a.v_ld + (h - a.H - a.Hk) * HD;
-            in[u] = *reinterpret_cast<const uint4 *>(src + li * VPT);
+        const float2 cs = a.table[b + p];
+        if constexpr (HALF) {
+            fx[j] = g[j] * cs.x;
+            fo[j] = gm[j] * (li < LPH / 2 ? -cs.y : cs.y);
+        } else {
+            fx[j] = g[j] * cs.x;
+            fo[j] = -g[j + 1] * cs.y;
+            fx[j + 1] = g[j + 1] * cs.x;
+            fo[j + 1] = g[j] * cs.y;
         }
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int h = h0 + u * HP;
-        const bool is_q = h < a.H;
-        float x[VPT], y[VPT];
+    for (int u = 0; u < SEG; ++u) {
+        if (hw + u * HPW >= heads) break;                  // the whole warp is past the last head
+        float x[VPT], o[VPT], y[VPT];
         unpack<T>(in[u], x);
         float ss = 0.0f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) ss = fmaf(x[j], x[j], ss);
 #pragma unroll
         for (int d = LPH / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        const float inv = 1.0f / sqrtf(ss * (1.0f / HD) + a.eps);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) x[j] = x[j] * inv * (is_q ? gq[j] : gk[j]);
+        const float r = rsqrtf(ss * (1.0f / HD) + a.eps);
         if constexpr (HALF) {
-#pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                const float o = __shfl_xor_sync(0xffffffffu, x[j], LPH / 2);
-                y[j] = li < LPH / 2 ? x[j] * cs[j].x - o * cs[j].y : o * cs[j].y + x[j] * cs[j].x;
-            }
+            uint4 other;
+            other.x = __shfl_xor_sync(0xffffffffu, in[u].x, LPH / 2);
+            other.y = __shfl_xor_sync(0xffffffffu, in[u].y, LPH / 2);
+            other.z = __shfl_xor_sync(0xffffffffu, in[u].z, LPH / 2);
+            other.w = __shfl_xor_sync(0xffffffffu, in[u].w, LPH / 2);
+            unpack<T>(other, o);
         } else {
 #pragma unroll
-            for (int j = 0; j < VPT / 2; ++j) {
-                y[2 * j] = x[2 * j] * cs[j].x - x[2 * j + 1] * cs[j].y;
-                y[2 * j + 1] = x[2 * j] * cs[j].y + x[2 * j + 1] * cs[j].x;
-            }
+            for (int j = 0; j < VPT; ++j) o[j] = x[j ^ 1];
         }
-        if (h >= heads) continue;
-        if (is_q) {
-            *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.q_out) + (size_t)t * a.o_ld + h * HD + li * VPT) = pack<T>(y);
-        } else if (slot >= 0) {
-            const bool is_k = h < a.H + a.Hk;
-            T *dst = reinterpret_cast<T *>(is_k ? a.k_pool : a.v_pool) + (size_t)slot * a.Hk * HD +
-                     (h - a.H - (is_k ? 0 : a.Hk)) * HD + li * VPT;
-            *reinterpret_cast<uint4 *>(dst) = is_k ? pack<T>(y) : in[u];
-        }
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) y[j] = r * fmaf(o[j], fo[j], x[j] * fx[j]);
+        if (h0 + u * HPW < heads) *reinterpret_cast<uint4 *>(dst + u * (HPW * HD)) = pack<T>(y);
     }
 }
 
+template <typename T, int HD, int SEG>
+static cudaError_t launch_norm_rope(bool half, const NormRopeArgs &a, cudaStream_t st) {
+    constexpr int PER = SEG * (32 / (HD * (int)sizeof(T) / 16));          // heads of a warp
+    const int seg_q = (a.H + PER - 1) / PER, seg_k = (a.Hk + PER - 1) / PER;
+    const dim3 grid((unsigned)(((long long)a.T * (seg_q + 2 * seg_k) + 7) / 8));
+    return half ? launch_pdl(qk_norm_rope_kernel<T, HD, true, SEG>, grid, dim3(256), 0, st, a, seg_q, seg_k)
+                : launch_pdl(qk_norm_rope_kernel<T, HD, false, SEG>, grid, dim3(256), 0, st, a, seg_q, seg_k);
+}
+// Passes a warp: 4 where that many still fill the SMs with 16 warps each (12960
+// tokens of 3 x 40 heads x 128, bf16, 796 MB: 116 us at 4 passes, 6.9 TB/s;
+// 131 at 8, 145 at 2, 237 at 1; 4099 tokens of 40 + 2 x 8 heads x 64: 15.8 /
+// 19.1 / 16.5 / 26.9 us), one for few tokens, whose latency is the passes'
+// (8 tokens of 3 x 40 heads x 128: 2.5 us).
 template <typename T, int HD>
 static cudaError_t launch_norm_rope(bool half, const NormRopeArgs &a, cudaStream_t st) {
-    constexpr int HP = 256 / (HD * (int)sizeof(T) / 16), U = 4;
-    const dim3 grid(a.T, (a.H + 2 * a.Hk + HP * U - 1) / (HP * U));
-    return half ? launch_pdl(qk_norm_rope_kernel<T, HD, true, U>, grid, dim3(256), 0, st, a)
-                : launch_pdl(qk_norm_rope_kernel<T, HD, false, U>, grid, dim3(256), 0, st, a);
+    const long long passes = (long long)a.T * ((a.H + 2ll * a.Hk) * HD * (int)sizeof(T) / 512 + 1);
+    return passes / 4 >= 16ll * device_sms() ? launch_norm_rope<T, HD, 4>(half, a, st) : launch_norm_rope<T, HD, 1>(half, a, st);
 }
 template <typename T> static cudaError_t norm_rope_hd(int hd, bool half, const NormRopeArgs &a, cudaStream_t st) {
     switch (hd) {

@@ -160,6 +160,8 @@ xc_status xc_op_qk_norm_rope(const xc_kv_cache *cache, int layer, int n_tokens, 
     if (layer < 0 || layer >= c.n_layers || n_tokens < 0) return fail(XC_EINVAL, "%s: layer or token count", who);
     if (n_heads < 1 || n_heads % c.n_kv_heads != 0 || n_heads > 65536)
         return fail(XC_EINVAL, "%s: n_heads must be a multiple of the cache's n_kv_heads", who);
+    if ((long long)n_tokens * (n_heads + 2 * c.n_kv_heads) >= (1ll << 31))
+        return fail(XC_EINVAL, "%s: too many token rows", who);
     if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(XC_EINVAL, "%s: eps", who);
     NormRopeArgs a{};
     long sum = 0;

@@ -173,7 +173,7 @@ def _ptr(t) -> int | None:
 def _stream(stream) -> int | None:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -412,7 +412,7 @@ class KVCache:
                                 table.data_ptr(), length.data_ptr())
         self.ptr = ctypes.addressof(self.desc)
         self._ws = {}
-        self._attn_bytes = {}
+        self._attn_bytes, self._axes = {}, {}
         self._page_bytes = LIB.xc_op_kv_workspace_bytes(self.ptr)
 
     @classmethod
@@ -494,19 +494,26 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
                     eps=1e-6, half_split=False, stream=None):
     """q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] (row-strided views allowed), pos [T, axes]
     and slots [T] int32, table from op_rope_table; axis_pairs, n_pos: host sequences."""
-    T, n = q.shape[0], len(axis_pairs)
+    T = q.shape[0]
     hd = cache.head_dim
     wide = cache.n_kv_heads * hd
+    key = (len(axis_pairs), *axis_pairs, *n_pos)
+    axes = cache._axes.get(key)
+    if axes is None:
+        if len(n_pos) != len(axis_pairs):
+            raise ValueError("one n_pos per axis")
+        axes = cache._axes[key] = (len(axis_pairs), (_I * len(axis_pairs))(*axis_pairs), (_I * len(n_pos))(*n_pos),
+                                   2 * sum(a * b for a, b in zip(axis_pairs, n_pos)))
+    n, c_pairs, c_pos, entries = axes
     if q.shape[1] % hd or q_out.shape != q.shape or k.shape != (T, wide) or v.shape != (T, wide) or \
             not (q.dtype == k.dtype == v.dtype == q_out.dtype == cache.k.dtype):
         raise ValueError("q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] of the cache's dtype")
-    if gamma_q.numel() != hd or gamma_k.numel() != hd or len(n_pos) != n or \
-            any(x.element_size() != 4 or not x.is_contiguous() for x in (gamma_q, gamma_k, table)) or \
-            table.numel() != 2 * sum(a * b for a, b in zip(axis_pairs, n_pos)):
+    if gamma_q.numel() != hd or gamma_k.numel() != hd or table.numel() != entries or \
+            any(x.element_size() != 4 or not x.is_contiguous() for x in (gamma_q, gamma_k, table)):
         raise ValueError("float32 gamma_q, gamma_k [head_dim]; table: one (cos, sin) pair per position and pair of every axis")
     check(LIB.xc_op_qk_norm_rope(cache.ptr, layer, T, q.shape[1] // hd, q.data_ptr(), _row_stride(q), k.data_ptr(),
                                  _row_stride(k), v.data_ptr(), _row_stride(v), gamma_q.data_ptr(),
-                                 gamma_k.data_ptr(), eps, n, (_I * n)(*axis_pairs), (_I * n)(*n_pos),
+                                 gamma_k.data_ptr(), eps, n, c_pairs, c_pos,
                                  _int32(pos, T * n), table.data_ptr(), int(half_split), _int32(slots, T),
                                  q_out.data_ptr(), _row_stride(q_out), _stream(stream)))
 
