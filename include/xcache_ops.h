@@ -186,17 +186,17 @@ enum {
 };
 
 /* Bytes of device workspace of xc_op_kv_fork / _extend / _compact on this
- * cache (page lists and marks).  Contents on entry are ignored. */
+ * cache (page lists).  Contents on entry are ignored. */
 size_t xc_op_kv_workspace_bytes(const xc_kv_cache *cache);
 
-/* For i < n: sequence dst[i] (empty) becomes a copy of src[i] (device int
- * arrays; a sequence may be forked to many).  Full pages are shared (ref + 1);
+/* For i < n (n <= 1024): sequence dst[i] (empty) becomes a copy of src[i]
+ * (device int arrays; a sequence may be forked to many).  Full pages are shared (ref + 1);
  * the rows in use of a partly filled last page are copied, in every layer,
  * into a fresh page: the lowest free page ids, in list order. */
 xc_status xc_op_kv_fork(const xc_kv_cache *cache, int n, const int *src, const int *dst, void *workspace,
                         size_t workspace_bytes, void *stream);
 
-/* Appends n_new tokens to each of the n listed sequences: takes the pages they
+/* Appends n_new tokens to each of the n <= 1024 listed sequences: takes the pages they
  * need (lowest free ids first, in list order, then token order), advances len
  * and writes the cache slot of every new token, page * page_size + offset, to
  * slots [n][n_new] (-1 everywhere when the call changes nothing). */

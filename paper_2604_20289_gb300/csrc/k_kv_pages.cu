@@ -5,39 +5,35 @@
 // CTA plans a call over it, in the order the interface promises, and a second
 // kernel over the whole GPU moves the pages it listed.  A plan validates its
 // whole input before it writes anything.
+#include <algorithm>
+
 #include "xc_branch.cuh"
 
 namespace xc {
 
 // Workspace (ints): copy list (source page, destination page, rows) with its
-// length, free page ids, marks per sequence, new id per page.
+// length, free page ids, new id per page.
 struct KvPlan {
     int *n_copy, *n_live;
-    int *src, *dst, *rows;      // [cap]
+    int *src, *dst, *rows;      // [n_pages]
     int *free_ids;              // [n_pages]
-    int *mark;                  // [max_seqs]
     int *map;                   // [n_pages]
 };
-static size_t kv_cap(const xc_kv_cache &c) { return c.n_pages > c.max_seqs ? c.n_pages : c.max_seqs; }
-size_t kv_workspace_bytes(const xc_kv_cache &c) {
-    return (4 + 3 * kv_cap(c) + 2 * (size_t)c.n_pages + c.max_seqs) * sizeof(int);
-}
+size_t kv_workspace_bytes(const xc_kv_cache &c) { return (4 + 5 * (size_t)c.n_pages) * sizeof(int); }
 static KvPlan kv_plan(const xc_kv_cache &c, void *ws) {
-    const size_t cap = kv_cap(c);
     int *p = reinterpret_cast<int *>(ws);
     KvPlan k;
     k.n_copy = p;
     k.n_live = p + 1;
     k.src = p + 4;
-    k.dst = k.src + cap;
-    k.rows = k.dst + cap;
-    k.free_ids = k.rows + cap;
-    k.mark = k.free_ids + c.n_pages;
-    k.map = k.mark + c.max_seqs;
+    k.dst = k.src + c.n_pages;
+    k.rows = k.dst + c.n_pages;
+    k.free_ids = k.rows + c.n_pages;
+    k.map = k.free_ids + c.n_pages;
     return k;
 }
 
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = KV_LIST_MAX;   // a thread for every listed sequence
 
 // Exclusive scan over the CTA; `total` receives the sum.  Every thread calls it.
 __device__ __forceinline__ int block_scan(int v, int *sh, int &total) {
@@ -98,86 +94,91 @@ static KvState kv_state(const xc_kv_cache &c) {
     return KvState{c.n_pages, c.page_size, c.max_seqs, c.max_pages, c.ref, c.table, c.len};
 }
 
+// Latency bound (one CTA, a few dependent loads), so each thread keeps its pair
+// in registers and the free pages are listed while the lengths are on their
+// way; 4 pairs: 10.1 -> 5 us against a version that re-read them per step.
 __global__ void __launch_bounds__(PLAN_THREADS)
     kv_fork_plan_kernel(const KvState c, const int n, const int *src, const int *dst, const KvPlan pl, int *err) {
     pdl_wait();
     pdl_release();
-    __shared__ int sh[32], bad;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) {
-        bad = 0;
-        *pl.n_copy = 0;
+    __shared__ int sh[32], sh_src[PLAN_THREADS], sh_dst[PLAN_THREADS], sh_pages[PLAN_THREADS],
+        sh_times[PLAN_THREADS];
+    const int tid = threadIdx.x;
+    const bool mine = tid < n;
+    const int s = mine ? src[tid] : 0, d = mine ? dst[tid] : 0;
+    bool bad = s < 0 || s >= c.max_seqs || d < 0 || d >= c.max_seqs;
+    const int l = mine && !bad ? c.len[s] : 0, ld = mine && !bad ? c.len[d] : 0;
+    sh_src[tid] = s;
+    sh_dst[tid] = d;
+    const int found = list_pages(c.ref, 0, c.n_pages, false, n, pl.free_ids, sh);
+    if (tid == 0) *pl.n_copy = 0;
+    bad = bad || ld != 0 || l < 0 || (long long)l > (long long)c.max_pages * c.ps;
+    int times = 0;                                     // pairs that share this pair's source, at its first one
+    if (mine)
+        for (int j = 0; j < n; ++j) {                  // a destination listed twice, or a source that is one
+            if ((j < tid && sh_dst[j] == d) || sh_dst[j] == s) bad = true;
+            if (sh_src[j] == s) times = j < tid ? -n : times + 1;
+        }
+    sh_times[tid] = max(times, 0);
+    sh_pages[tid] = mine && !bad ? (l + c.ps - 1) / c.ps : 0;
+    const int full = l / c.ps, part = l - full * c.ps;
+    bool any = __syncthreads_or(mine && bad);
+    int last = -1;                                     // the page that is copied
+    // 2^lg threads walk a pair's table row; the first KEEP ids of each stay in registers
+    constexpr int KEEP = 8;
+    const int lg = 31 - __clz(PLAN_THREADS / n), pair = tid >> lg, per = 1 << lg, j0 = tid & (per - 1);
+    const int *row = c.table + (size_t)(pair < n ? sh_src[pair] : 0) * c.max_pages;
+    int ids[KEEP];
+    if (!any) {
+        const int np = pair < n ? sh_pages[pair] : 0;
+        bool wrong = false;
+        if (mine && part != 0) last = c.table[(size_t)s * c.max_pages + full];
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) ids[i] = j0 + i * per < np ? row[j0 + i * per] : 0;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) wrong = wrong || ids[i] < 0 || ids[i] >= c.n_pages;
+        for (int j = j0 + KEEP * per; j < np; j += per) wrong = wrong || row[j] < 0 || row[j] >= c.n_pages;
+        any = __syncthreads_or(wrong);
     }
-    __syncthreads();
-    for (int i = tid; i < n; i += PLAN_THREADS) {
-        const int s = src[i], d = dst[i];
-        if (s < 0 || s >= c.max_seqs || d < 0 || d >= c.max_seqs) {
-            bad = 1;
-        } else {
-            pl.mark[s] = 0;
-            pl.mark[d] = 0;
-        }
-    }
-    __syncthreads();
-    if (!bad)
-        for (int i = tid; i < n; i += PLAN_THREADS) {
-            const int l = c.len[src[i]];
-            if (atomicAdd(&pl.mark[dst[i]], 1) > 0 || c.len[dst[i]] != 0 || l < 0 ||
-                (long long)l > (long long)c.max_pages * c.ps)
-                bad = 1;
-        }
-    __syncthreads();
-    if (!bad)
-        for (int i = warp; i < n; i += PLAN_THREADS / 32) {   // no source is a destination; its pages exist
-            const int s = src[i], np = (c.len[s] + c.ps - 1) / c.ps;
-            if (pl.mark[s] != 0) bad = 1;
-            for (int j = lane; j < np; j += 32) {
-                const int p = c.table[(size_t)s * c.max_pages + j];
-                if (p < 0 || p >= c.n_pages) bad = 1;
-            }
-        }
-    __syncthreads();
-    if (bad) {
+    if (any) {
         if (tid == 0 && err) atomicOr(err, ERR_BAD_SEQ);
         return;
     }
-    int need = 0;
-    for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
-        const int i = i0 + tid;
-        int total;
-        block_scan(i < n && c.len[src[i]] % c.ps != 0 ? 1 : 0, sh, total);
-        need += total;
-    }
-    if (list_pages(c.ref, 0, c.n_pages, false, need, pl.free_ids, sh) < need) {
+    int need;
+    const int at = block_scan(mine && part != 0 ? 1 : 0, sh, need);
+    if (found < need) {
         if (tid == 0 && err) atomicOr(err, ERR_CACHE_FULL);
         return;
     }
-    int base = 0;
-    for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
-        const int i = i0 + tid;
-        const int l = i < n ? c.len[src[i]] : 0;
-        const int part = l % c.ps, full = l / c.ps;
-        int total;
-        const int at = base + block_scan(part != 0 ? 1 : 0, sh, total);
+    if (mine) {
         if (part != 0) {
             const int fresh = pl.free_ids[at];
             c.ref[fresh] = 1;
-            c.table[(size_t)dst[i] * c.max_pages + full] = fresh;
-            pl.src[at] = c.table[(size_t)src[i] * c.max_pages + full];
+            c.table[(size_t)d * c.max_pages + full] = fresh;
+            pl.src[at] = last;
             pl.dst[at] = fresh;
             pl.rows[at] = part;
         }
-        if (i < n) c.len[dst[i]] = l;
-        base += total;
+        c.len[d] = l;
     }
     if (tid == 0) *pl.n_copy = need;
-    for (int i = warp; i < n; i += PLAN_THREADS / 32) {
-        const int s = src[i], d = dst[i], full = c.len[s] / c.ps;
-        for (int j = lane; j < full; j += 32) {
-            const int p = c.table[(size_t)s * c.max_pages + j];
-            c.table[(size_t)d * c.max_pages + j] = p;
-            atomicAdd(&c.ref[p], 1);
+    sh_pages[tid] = mine ? full : 0;
+    __syncthreads();
+    if (pair >= n) return;
+    int *to = c.table + (size_t)sh_dst[pair] * c.max_pages;
+    const int nf = sh_pages[pair], add = sh_times[pair];   // a page's count goes up once for all children of a source
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int j = j0 + i * per;
+        if (j < nf) {
+            to[j] = ids[i];
+            if (add > 0) atomicAdd(&c.ref[ids[i]], add);
         }
+    }
+    for (int j = j0 + KEEP * per; j < nf; j += per) {
+        const int p = row[j];
+        to[j] = p;
+        if (add > 0) atomicAdd(&c.ref[p], add);
     }
 }
 
@@ -186,76 +187,57 @@ __global__ void __launch_bounds__(PLAN_THREADS)
                      int *err) {
     pdl_wait();
     pdl_release();
-    __shared__ int sh[32], bad;
+    __shared__ int sh[32], sh_seq[PLAN_THREADS], sh_len[PLAN_THREADS], sh_at[PLAN_THREADS], sh_k[PLAN_THREADS], why;
     __shared__ unsigned long long want;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long n_slots = (long long)n * n_new;
+    const bool mine = tid < n;
+    const int s = mine ? seqs[tid] : 0;
+    int bad = s < 0 || s >= c.max_seqs ? ERR_BAD_SEQ : 0;
+    const int l = mine && !bad ? c.len[s] : 0;
+    sh_seq[tid] = s;
     if (tid == 0) {
-        bad = 0;
+        why = 0;
         want = 0;
     }
-    __syncthreads();
-    for (int i = tid; i < n; i += PLAN_THREADS) {
-        const int s = seqs[i];
-        if (s < 0 || s >= c.max_seqs) bad = ERR_BAD_SEQ;
-        else pl.mark[s] = 0;
-    }
-    __syncthreads();
-    if (!bad)
-        for (int i = tid; i < n; i += PLAN_THREADS) {
-            const int s = seqs[i], l = c.len[s];
-            if (atomicAdd(&pl.mark[s], 1) > 0 || l < 0) {
-                atomicOr(&bad, ERR_BAD_SEQ);
-            } else if ((long long)l + n_new > (long long)c.max_pages * c.ps) {
-                atomicOr(&bad, ERR_CACHE_FULL);
-            } else if (l % c.ps != 0) {          // the last page is written: it must be this sequence's own
-                const int p = c.table[(size_t)s * c.max_pages + l / c.ps];
-                if (p < 0 || p >= c.n_pages || c.ref[p] != 1) atomicOr(&bad, ERR_BAD_SEQ);
-            }
+    const long long most = (long long)n * ((n_new + c.ps - 1) / c.ps);    // pages that n_new tokens may need
+    const int found = list_pages(c.ref, 0, c.n_pages, false, (int)min(most, (long long)c.n_pages), pl.free_ids, sh);
+    if (mine && !bad) {
+        for (int j = 0; j < tid; ++j)
+            if (sh_seq[j] == s) bad = ERR_BAD_SEQ;
+        if (l < 0) bad = ERR_BAD_SEQ;
+        else if ((long long)l + n_new > (long long)c.max_pages * c.ps) bad |= ERR_CACHE_FULL;
+        if (!bad && l % c.ps != 0) {                   // the last page is written: it must be this sequence's own
+            const int p = c.table[(size_t)s * c.max_pages + l / c.ps];
+            if (p < 0 || p >= c.n_pages || c.ref[p] != 1) bad = ERR_BAD_SEQ;
         }
-    __syncthreads();
-    int need = 0;
-    if (!bad) {
-        for (int i = tid; i < n; i += PLAN_THREADS) {
-            const int l = c.len[seqs[i]];
-            atomicAdd(&want, (unsigned long long)((l + n_new + c.ps - 1) / c.ps - (l + c.ps - 1) / c.ps));
-        }
-        __syncthreads();
-        if (want <= (unsigned long long)c.n_pages) need = (int)want;
-        else if (tid == 0) bad = ERR_CACHE_FULL;
-        __syncthreads();
     }
-    if (!bad && list_pages(c.ref, 0, c.n_pages, false, need, pl.free_ids, sh) < need) {
-        __syncthreads();
-        if (tid == 0) bad = ERR_CACHE_FULL;
-    }
+    const int have = (l + c.ps - 1) / c.ps, k = mine && !bad ? (l + n_new + c.ps - 1) / c.ps - have : 0;
+    if (mine && bad) atomicOr(&why, bad);
+    if (k > 0) atomicAdd(&want, (unsigned long long)k);
     __syncthreads();
-    if (bad) {
+    const int fault = why != 0 ? why : want > (unsigned long long)found ? ERR_CACHE_FULL : 0;
+    if (fault != 0) {
         for (long long e = tid; e < n_slots; e += PLAN_THREADS) slots[e] = -1;
-        if (tid == 0 && err) atomicOr(err, bad);
+        if (tid == 0 && err) atomicOr(err, fault);
         return;
     }
-    int base = 0;
-    for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
-        const int i = i0 + tid;
-        const int s = i < n ? seqs[i] : 0, l = i < n ? c.len[s] : 0;
-        const int have = (l + c.ps - 1) / c.ps;
-        const int k = i < n ? (l + n_new + c.ps - 1) / c.ps - have : 0;
-        int total;
-        const int at = base + block_scan(k, sh, total);
-        for (int j = 0; j < k; ++j) {
-            const int p = pl.free_ids[at + j];
+    int total;
+    sh_at[tid] = block_scan(k, sh, total);
+    sh_k[tid] = k;
+    sh_len[tid] = l;
+    if (mine) c.len[s] = l + n_new;
+    __syncthreads();
+    for (int i = warp; i < n; i += PLAN_THREADS / 32)
+        for (int j = lane; j < sh_k[i]; j += 32) {
+            const int p = pl.free_ids[sh_at[i] + j];
             c.ref[p] = 1;
-            c.table[(size_t)s * c.max_pages + have + j] = p;
+            c.table[(size_t)sh_seq[i] * c.max_pages + (sh_len[i] + c.ps - 1) / c.ps + j] = p;
         }
-        if (i < n) c.len[s] = l + n_new;
-        base += total;
-    }
     __syncthreads();
     for (long long e = tid; e < n_slots; e += PLAN_THREADS) {
-        const int i = (int)(e / n_new), s = seqs[i];
-        const int at = c.len[s] - n_new + (int)(e - (long long)i * n_new);
-        slots[e] = c.table[(size_t)s * c.max_pages + at / c.ps] * c.ps + at % c.ps;
+        const int i = (int)(e / n_new), at = sh_len[i] + (int)(e - (long long)i * n_new);
+        slots[e] = c.table[(size_t)sh_seq[i] * c.max_pages + at / c.ps] * c.ps + at % c.ps;
     }
 }
 
@@ -352,17 +334,24 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-static cudaError_t launch_copy(const xc_kv_cache &c, const KvPlan &pl, long long n_entries, cudaStream_t st) {
-    return launch_pdl(kv_copy_kernel, dim3(device_sms() * 8), dim3(256), 0, st, reinterpret_cast<uint4 *>(c.k),
-                      reinterpret_cast<uint4 *>(c.v), c.n_layers, c.n_pages, c.page_size,
-                      (int)(kv_row_bytes(c) / 16), pl, c.table, n_entries);
+// most: pages the plan may have listed.  The grid follows it up to 64 CTAs a
+// SM (8 resident at a time): the later CTAs' loads of the copy list overlap the
+// earlier ones' copies (1.47 GB of moves: 232 us, 6.3 TB/s with the plan; 250
+// at 8 CTAs a SM, all resident).
+static cudaError_t launch_copy(const xc_kv_cache &c, const KvPlan &pl, long long most, long long n_entries,
+                               cudaStream_t st) {
+    const int row_vecs = (int)(kv_row_bytes(c) / 16);
+    const long long chunks = most * c.n_layers * 2 * (((long long)c.page_size * row_vecs + COPY_VECS - 1) / COPY_VECS);
+    const long long ctas = std::max(std::min(chunks, (long long)device_sms() * 64), 1ll);
+    return launch_pdl(kv_copy_kernel, dim3((unsigned)ctas), dim3(256), 0, st, reinterpret_cast<uint4 *>(c.k),
+                      reinterpret_cast<uint4 *>(c.v), c.n_layers, c.n_pages, c.page_size, row_vecs, pl, c.table, n_entries);
 }
 
 cudaError_t kv_fork(const xc_kv_cache &c, int n, const int *src, const int *dst, void *ws, int *err, cudaStream_t st) {
     const KvPlan pl = kv_plan(c, ws);
     cudaError_t e = launch_pdl(kv_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, kv_state(c), n, src, dst, pl, err);
     if (e != cudaSuccess) return e;
-    return launch_copy(c, pl, 0, st);
+    return launch_copy(c, pl, n, 0, st);
 }
 cudaError_t kv_extend(const xc_kv_cache &c, int n, const int *seqs, int n_new, int *slots, void *ws, int *err,
                       cudaStream_t st) {
@@ -376,7 +365,7 @@ cudaError_t kv_compact(const xc_kv_cache &c, int *n_live, void *ws, cudaStream_t
     const KvPlan pl = kv_plan(c, ws);
     cudaError_t e = launch_pdl(kv_compact_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, kv_state(c), pl, n_live);
     if (e != cudaSuccess) return e;
-    return launch_copy(c, pl, (long long)c.max_seqs * c.max_pages, st);
+    return launch_copy(c, pl, (c.n_pages + 1) / 2, (long long)c.max_seqs * c.max_pages, st);
 }
 
 // ------------------------------------------------------- rotation and norm

@@ -12,6 +12,7 @@ enum : int { ERR_CACHE_FULL = XC_DEV_CACHE_FULL, ERR_BAD_SEQ = XC_DEV_BAD_SEQUEN
 inline size_t elem_bytes(int dtype) { return dtype == XC_BF16 ? 2 : 4; }
 inline size_t kv_row_bytes(const xc_kv_cache &c) { return (size_t)c.n_kv_heads * c.head_dim * elem_bytes(c.dtype); }
 
+constexpr int KV_LIST_MAX = 1024;     // sequences of one fork or extend
 size_t kv_workspace_bytes(const xc_kv_cache &c);
 cudaError_t kv_fork(const xc_kv_cache &c, int n, const int *src, const int *dst, void *ws, int *err, cudaStream_t st);
 cudaError_t kv_extend(const xc_kv_cache &c, int n, const int *seqs, int n_new, int *slots, void *ws, int *err,

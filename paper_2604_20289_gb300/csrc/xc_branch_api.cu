@@ -103,8 +103,8 @@ size_t xc_op_kv_workspace_bytes(const xc_kv_cache *cache) {
 xc_status xc_op_kv_fork(const xc_kv_cache *cache, int n, const int *src, const int *dst, void *workspace,
                         size_t workspace_bytes, void *stream) {
     CHECK(check_cache("xc_op_kv_fork", cache));
-    if (n < 0 || n > cache->max_seqs || (n > 0 && (src == nullptr || dst == nullptr)))
-        return fail(XC_EINVAL, "xc_op_kv_fork: 0 to max_seqs pairs of sequences");
+    if (n < 0 || n > cache->max_seqs || n > KV_LIST_MAX || (n > 0 && (src == nullptr || dst == nullptr)))
+        return fail(XC_EINVAL, "xc_op_kv_fork: 0 to max_seqs, and to %d, pairs of sequences", KV_LIST_MAX);
     if (n == 0) return XC_OK;
     CHECK(check_ws("xc_op_kv_fork", workspace, workspace_bytes, kv_workspace_bytes(*cache)));
     ERR_WORD(err, "xc_op_kv_fork");
@@ -114,9 +114,9 @@ xc_status xc_op_kv_fork(const xc_kv_cache *cache, int n, const int *src, const i
 xc_status xc_op_kv_extend(const xc_kv_cache *cache, int n, const int *seqs, int n_new, int *slots,
                           void *workspace, size_t workspace_bytes, void *stream) {
     CHECK(check_cache("xc_op_kv_extend", cache));
-    if (n < 0 || n > cache->max_seqs || n_new < 0 || n_new > cache->max_pages * cache->page_size ||
+    if (n < 0 || n > cache->max_seqs || n > KV_LIST_MAX || n_new < 0 || n_new > cache->max_pages * cache->page_size ||
         (n > 0 && n_new > 0 && (seqs == nullptr || slots == nullptr)))
-        return fail(XC_EINVAL, "xc_op_kv_extend: 0 to max_seqs sequences, n_new up to a table row");
+        return fail(XC_EINVAL, "xc_op_kv_extend: 0 to max_seqs, and to %d, sequences, n_new up to a table row", KV_LIST_MAX);
     if (n == 0 || n_new == 0) return XC_OK;
     CHECK(check_ws("xc_op_kv_extend", workspace, workspace_bytes, kv_workspace_bytes(*cache)));
     ERR_WORD(err, "xc_op_kv_extend");

@@ -106,6 +106,9 @@ def test_page_call_refusals(xb):
     assert xb.LIB.xc_op_kv_fork(p, 1, None, P, P, big, None) == xb.XC_EINVAL
     assert xb.LIB.xc_op_kv_fork(p, 1, P, P, P, 8, None) == xb.XC_EINVAL
     assert "workspace" in xb.last_error(None)
+    wide = desc(xb, max_seqs=2000)
+    assert xb.LIB.xc_op_kv_fork(addr(wide), 1025, P, P, P, big, None) == xb.XC_EINVAL and "1024" in xb.last_error(None)
+    assert xb.LIB.xc_op_kv_extend(addr(wide), 1025, P, 1, P, P, big, None) == xb.XC_EINVAL
     assert xb.LIB.xc_op_kv_extend(p, 1, P, 16 * 16 + 1, P, P, big, None) == xb.XC_EINVAL
     assert xb.LIB.xc_op_kv_extend(p, 1, P, -1, P, P, big, None) == xb.XC_EINVAL
     assert xb.LIB.xc_op_kv_extend(p, 1, P, 1, None, P, big, None) == xb.XC_EINVAL

@@ -437,7 +437,7 @@ def test_page_operations_follow_the_model(dtype, ps, n_pages, max_seqs, max_page
         op = ["extend", "fork", "free", "compact"][rng.integers(4)] if step > 1 else "extend"
         if op == "extend":
             n_new = int(rng.integers(1, 2 * ps + 2))
-            pick = rng.permutation(max_seqs)[:rng.integers(1, (1090 if many else 4))].tolist()
+            pick = rng.permutation(max_seqs)[:rng.integers(1, (1025 if many else 4))].tolist()
             slots = torch.full((len(pick), n_new), 77, dtype=torch.int32, device=DEV)
             xb.op_kv_extend(cache, i32(pick), n_new, slots)
             want = m.extend(pick, n_new)
