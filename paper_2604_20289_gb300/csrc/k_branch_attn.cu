@@ -21,7 +21,7 @@
 
 namespace xc {
 
-constexpr int LEN_CACHE = 128;   // branches whose table row and length are kept in shared memory
+constexpr int LEN_CACHE = 64;    // branches whose table row and length are kept in shared memory
 
 struct BranchSched {
     int B, n_q, grp, Hk;
@@ -244,10 +244,13 @@ struct BranchTile {
     static constexpr int NR = HD / 64;                 // 64-wide swizzle regions per row
     static constexpr int REGION = 128 * 128;           // [128 rows][64 bf16]
     static constexpr int Q_BYTES = NR * REGION, KV_BYTES = NR * REGION;
-    static constexpr int STAGES = HD == 64 ? (QT == 2 ? 4 : 5) : (QT == 2 ? 2 : 3);
-    static constexpr int OFF_K = QT * Q_BYTES, OFF_V = OFF_K + STAGES * KV_BYTES;
-    static constexpr int OFF_BAR = OFF_V + STAGES * KV_BYTES;
-    static constexpr int SMEM_BYTES = OFF_BAR + 384 + 1024;
+    // K and V tiles share a ring of SLOTS in the order K0 V0 K1 V1 ...: as many
+    // as fit beside Q (with 2 + 2 slots instead of 5 the loads of a tile were
+    // requested one tile before its use, about the latency under load).
+    static constexpr int SLOTS = HD == 64 ? 10 : (QT == 2 ? 5 : 6);
+    static constexpr int PAIRS = 8;                    // barriers of (V_g, K_g+1), more than the ring can hold
+    static constexpr int OFF_KV = QT * Q_BYTES, OFF_BAR = OFF_KV + SLOTS * KV_BYTES;
+    static constexpr int SMEM_BYTES = OFF_BAR + 448 + 1024;
     static constexpr bool SEP_P = HD == 64 || QT == 1;     // P has TMEM columns of its own
     static constexpr int ISSUERS = SEP_P ? QT : 1;
     static constexpr int S_COL(int i) { return 128 * i; }
@@ -256,7 +259,6 @@ struct BranchTile {
     static constexpr int TMEM_COLS = HD == 64 && QT == 1 ? 256 : 512;
     static constexpr int W_TMA = 4 * QT, W_MMA = W_TMA + 1, W_TAIL = W_MMA + ISSUERS;
     static constexpr int THREADS = 32 * (W_TAIL + 1);
-    static constexpr bool HALVES = SEP_P;              // P V in two halves of 64 keys
     static constexpr bool TURNS = HD == 64 && QT == 2;
     static constexpr float LAZY = 8.0f;                // rescale threshold (log2 units)
 };
@@ -326,19 +328,18 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
     __shared__ BranchStart sh_start;
     __shared__ BranchWarpWalk sh_walk[4 * QT];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    uint8_t *sQ = smem, *sK = smem + A::OFF_K, *sV = smem + A::OFF_V;
+    uint8_t *sQ = smem, *sKV = smem + A::OFF_KV;
     uint64_t *bar = reinterpret_cast<uint64_t *>(smem + A::OFF_BAR);
     uint64_t *q_full = bar;                    // Q of piece p landed
     uint64_t *q_empty = bar + 1;               // every S of piece p done
-    uint64_t *k_full = bar + 2;
-    uint64_t *k_empty = k_full + A::STAGES;
-    uint64_t *v_full = k_empty + A::STAGES;    // landed, and cleared past the last key
-    uint64_t *v_empty = v_full + A::STAGES;
-    uint64_t *v_tail = v_empty + A::STAGES;    // a unit's last V tile landed
-    uint64_t *s_full = v_tail + A::STAGES;     // [QT] S_i computed
+    uint64_t *k0_full = bar + 2;               // the first K tile landed
+    uint64_t *pair = bar + 3;                  // [PAIRS] V_g (cleared past the last key) and K_g+1 landed
+    uint64_t *v_tail = pair + A::PAIRS;        // [PAIRS] V_g landed, where it is to be cleared
+    uint64_t *empty = v_tail + A::PAIRS;       // [SLOTS] slot read by every issuer
+    uint64_t *s_full = empty + A::SLOTS;     // [QT] S_i computed
     uint64_t *s_cons = s_full + QT;            // [QT] S_i read (SEP_P)
     uint64_t *p_full = s_cons + QT;            // [QT] P_i written, O_i corrected
-    uint64_t *p_half = p_full + QT;            // [QT] first 64 keys of P_i written, O_i corrected
+    uint64_t *p_half = p_full + QT;            // [QT] first 64 keys of P_i written, O_i corrected (SEP_P)
     uint64_t *pv_done = p_half + QT;           // [QT] P_i V done (SEP_P: every tile; else last of a piece)
     uint64_t *o_free = pv_done + QT;           // [QT] O_i of piece p read out
     uint64_t *turn = o_free + QT;              // [2][4] exponential-phase hand-off (TURNS)
@@ -348,13 +349,12 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, A::ISSUERS);
-        for (int s = 0; s < A::STAGES; ++s) {
-            mbar_init(&k_full[s], 1);
-            mbar_init(&k_empty[s], A::ISSUERS);
-            mbar_init(&v_full[s], 1);
-            mbar_init(&v_empty[s], A::ISSUERS);
+        mbar_init(k0_full, 1);
+        for (int s = 0; s < A::PAIRS; ++s) {
+            mbar_init(&pair[s], 2);
             mbar_init(&v_tail[s], 1);
         }
+        for (int s = 0; s < A::SLOTS; ++s) mbar_init(&empty[s], A::ISSUERS);
         for (int i = 0; i < QT; ++i) {
             mbar_init(&s_full[i], 1);
             mbar_init(&s_cons[i], 128);
@@ -385,7 +385,9 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         const int box = min(sc.ps, 128), log_ps = 31 - __clz(sc.ps);
         const int q_bytes = QT * A::NR * tt1 * sc.grp * 128;
         int p = 0, g = 0;
-        uint32_t tails = 0, tail_ph = 0;       // stages whose last use was a tail, parity of their tail uses
+        int slot = 0;
+        uint32_t turn_ph = 0;                  // parity of the ring's turn
+        uint32_t tails = 0, tail_ph = 0;       // pairs whose last use was a tail, parity of their tail uses
         bool ok = true;
         while (ok && walk.next(sc, sh_len, pc)) {
             if (p > 0) ok = mbar_wait(q_empty, (p - 1) & 1, err, ERR_WAIT_PRODUCER);
@@ -415,40 +417,44 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             for (int kt = pc.kt0; kt < pc.kt1; ++kt, ++g) {
                 const int row = nrow;
                 if (kt + 1 < pc.kt1) nrow = page_row(kt + 1);
-                const int st = g % A::STAGES;
-                const uint32_t ph = ((g / A::STAGES) & 1) ^ 1;
                 const int n_pg = __popc(__ballot_sync(0xffffffffu, row >= 0));
                 const uint32_t bytes = n_pg * box * 128 * A::NR;
                 const bool tail = pc.keys < (kt + 1) * 128;
-                ok = mbar_wait(&k_empty[st], ph, err, ERR_WAIT_PRODUCER);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                if (lane == 0) mbar_expect_tx(&k_full[st], bytes);
-                __syncwarp();
-                if (row >= 0)
-                    for (int r = 0; r < A::NR; ++r)
-                        tma_load_2d(sK + st * A::KV_BYTES + r * A::REGION + lane * box * 128, &tmK, &k_full[st],
-                                    pc.h * HD + 64 * r, row);
-                ok = mbar_wait(&v_empty[st], ph, err, ERR_WAIT_PRODUCER);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                uint64_t *vb = tail ? &v_tail[st] : &v_full[st];
-                if (lane == 0) mbar_expect_tx(vb, bytes);
-                __syncwarp();
-                if (row >= 0)
-                    for (int r = 0; r < A::NR; ++r)
-                        tma_load_2d(sV + st * A::KV_BYTES + r * A::REGION + lane * box * 128, &tmV, vb,
-                                    pc.h * HD + 64 * r, row);
-                if (tail) tail_ph ^= 1u << st;
-                tails = tail ? tails | 1u << st : tails & ~(1u << st);
+                auto load = [&](const CUtensorMap *tm, uint64_t *b) -> bool {      // the next slot
+                    const bool r = mbar_wait(&empty[slot], turn_ph ^ 1, err, ERR_WAIT_PRODUCER);
+                    if (!__all_sync(0xffffffffu, r)) return false;
+                    if (lane == 0) mbar_expect_tx(b, bytes);
+                    __syncwarp();
+                    if (row >= 0)
+                        for (int r2 = 0; r2 < A::NR; ++r2)
+                            tma_load_2d(sKV + slot * A::KV_BYTES + r2 * A::REGION + lane * box * 128, tm, b,
+                                        pc.h * HD + 64 * r2, row);
+                    if (++slot == A::SLOTS) {
+                        slot = 0;
+                        turn_ph ^= 1;
+                    }
+                    return true;
+                };
+                const int pi = g % A::PAIRS;
+                ok = load(&tmK, g == 0 ? k0_full : &pair[(g - 1) % A::PAIRS]);
+                if (!ok) break;
+                ok = load(&tmV, tail ? &v_tail[pi] : &pair[pi]);
+                if (!ok) break;
+                if (tail) tail_ph ^= 1u << pi;
+                tails = tail ? tails | 1u << pi : tails & ~(1u << pi);
             }
         }
         // every copy this warp started has landed before the CTA exits
         if (lane == 0) {
+            if (g > 0) {
+                mbar_arrive(&pair[(g - 1) % A::PAIRS]);        // the last V tile is not followed by a K tile
+                mbar_wait(k0_full, 0, err, ERR_WAIT_PRODUCER);
+            }
             if (p > 0) mbar_wait(q_full, (p - 1) & 1, err, ERR_WAIT_PRODUCER);
-            for (int x = max(g - A::STAGES, 0); x < g; ++x) {
-                const int st = x % A::STAGES;
-                mbar_wait(&k_full[st], (x / A::STAGES) & 1, err, ERR_WAIT_PRODUCER);
-                if (tails >> st & 1u) mbar_wait(&v_tail[st], (tail_ph >> st & 1u) ^ 1u, err, ERR_WAIT_PRODUCER);
-                else mbar_wait(&v_full[st], (x / A::STAGES) & 1, err, ERR_WAIT_PRODUCER);
+            for (int x = max(g - A::PAIRS, 0); x < g; ++x) {
+                const int pi = x % A::PAIRS;
+                if (tails >> pi & 1u) mbar_wait(&v_tail[pi], (tail_ph >> pi & 1u) ^ 1u, err, ERR_WAIT_PRODUCER);
+                mbar_wait(&pair[pi], (x / A::PAIRS) & 1, err, ERR_WAIT_PRODUCER);
             }
         }
     } else if (warp == A::W_TAIL) {
@@ -461,18 +467,18 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             g += pc.kt1 - pc.kt0;
             const int valid = pc.keys - kt * 128;
             if (valid >= 128) continue;
-            const int st = (g - 1) % A::STAGES;
-            ok = mbar_wait(&v_tail[st], ph >> st & 1u, err, ERR_WAIT_PRODUCER);
+            const int pi = (g - 1) % A::PAIRS, slot = (2 * g - 1) % A::SLOTS;
+            ok = mbar_wait(&v_tail[pi], ph >> pi & 1u, err, ERR_WAIT_PRODUCER);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            ph ^= 1u << st;
+            ph ^= 1u << pi;
             // rows are 128 bytes in each region whatever the swizzle of their 16-byte pieces
             for (int r = 0; r < A::NR; ++r)
                 for (int x = max(valid, 0) * 8 + lane; x < 128 * 8; x += 32)
-                    *reinterpret_cast<uint4 *>(sV + st * A::KV_BYTES + r * A::REGION + x * 16) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(sKV + slot * A::KV_BYTES + r * A::REGION + x * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&v_full[st]);
+            if (lane == 0) mbar_arrive(&pair[pi]);
         }
     } else if (warp >= A::W_MMA) {
         // ------------------------------------------------------ MMA issue
@@ -480,13 +486,13 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         constexpr uint32_t idesc_s = idesc_bf16(128, 128, false, false);
         constexpr uint32_t idesc_o = idesc_bf16(128, HD, false, true);
         const uint64_t dQ0 = sdesc_sw128(smem_u32(sQ), 16, 1024);
-        const uint64_t dK0 = sdesc_sw128(smem_u32(sK), 16, 1024);
-        const uint64_t dV0 = sdesc_sw128(smem_u32(sV), A::REGION, 1024);
+        const uint64_t dK0 = sdesc_sw128(smem_u32(sKV), 16, 1024);
+        const uint64_t dV0 = sdesc_sw128(smem_u32(sKV), A::REGION, 1024);
         // (issued for both tiles also where a unit has rows in the first only: a
         // branch around the instructions cost 3 % on the large shapes)
-        auto issue_s = [&](int i, int g) {             // S_i = Q_i K_g^T
+        auto issue_s = [&](int i, int slot) {          // S_i = Q_i K^T
             const uint64_t dq = dQ0 + (uint64_t)((i * A::Q_BYTES) >> 4);
-            const uint64_t dk = dK0 + (uint64_t)(((g % A::STAGES) * A::KV_BYTES) >> 4);
+            const uint64_t dk = dK0 + (uint64_t)((slot * A::KV_BYTES) >> 4);
 #pragma unroll
             for (int ks = 0; ks < HD / 16; ++ks) {
                 const uint32_t off = ((ks >> 2) * A::REGION + (ks & 3) * 32) >> 4;
@@ -494,8 +500,8 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             }
             tc_commit_warp(&s_full[i]);
         };
-        auto issue_pv = [&](int i, int g, bool fresh, int half) {   // O_i (+)= P_i V_g over 64 keys, P_i in TMEM
-            const uint64_t dv = dV0 + (uint64_t)(((g % A::STAGES) * A::KV_BYTES) >> 4);
+        auto issue_pv = [&](int i, int slot, bool fresh, int half) {   // O_i (+)= P_i V over 64 keys, P_i in TMEM
+            const uint64_t dv = dV0 + (uint64_t)((slot * A::KV_BYTES) >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int ks = 4 * half + k;
@@ -504,108 +510,89 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             }
         };
         auto wait = [&](uint64_t *b, int parity) -> bool {
+            if (__all_sync(0xffffffffu, mbar_try_wait(smem_u32(b), parity & 1))) return true;
             const bool r = mbar_wait(b, parity & 1, err, ERR_WAIT_MMA);
             return __all_sync(0xffffffffu, r) != 0;
         };
-        // The key tiles of the CTA as two walks, S one tile ahead of P V.
-        struct Tile {
-            int g, p;                                  // tile and piece of the CTA
-            bool first, last;                          // of its piece
-        };
-        BranchWalk<128> walk_s = walk;
-        BranchPiece ps{}, pv{};
-        Tile ts{-1, -1, false, true}, tv{-1, -1, false, true};
-        auto step = [&](BranchWalk<128> &w, BranchPiece &c, Tile &t) -> bool {
-            if (t.last) {
-                if (!w.next(sc, sh_len, c)) return false;
-                ++t.p;
-                t.first = true;
+        // S runs one key tile ahead of P V.  The tensor core drains what is
+        // queued (about 8 products) while this warp looks at barriers, and each
+        // look costs ~150 cycles next to the busy softmax warps, so there are
+        // few: V_g and K_g+1 share one, the queries' and the output's only stand at
+        // a piece's first tile (12 heads x 128, 2 x 4320 queries, 30240 keys:
+        // 3000 cycles a key tile with separate ones and a tile cursor).
+        bool ok = walk.next(sc, sh_len, pc) && wait(q_full, 0) && wait(k0_full, 0);
+        const int i_own = warp - A::W_MMA;                 // SEP_P: the row tile of this warp
+        int g = 0, p = 0, left = pc.kt1 - pc.kt0;          // left: key tiles of the piece from g on
+        bool fresh = true;                                 // g is the piece's first
+        int sk = 0, sv = 1;                                // slots of K_g+1 and V_g
+        auto two_on = [&](int s) { return s + 2 >= A::SLOTS ? s + 2 - A::SLOTS : s + 2; };
+        if (ok) {
+            tc_fence_after();
+            issue_s(A::SEP_P ? i_own : 0, 0);
+            if constexpr (!A::SEP_P) issue_s(1, 0);
+            tc_commit_warp(&empty[0]);
+            if (left == 1) tc_commit_warp(q_empty);
+        }
+        while (ok) {
+            sk = two_on(sk);
+            const bool last = left == 1;
+            bool more = true;
+            if (last) {
+                more = walk.next(sc, sh_len, pc);
+                left = more ? pc.kt1 - pc.kt0 : 0;
+                if (more && !wait(q_full, p + 1)) break;
             } else {
-                ++c.kt0;
-                t.first = false;
+                --left;
             }
-            ++t.g;
-            t.last = c.kt0 == c.kt1 - 1;
-            return true;
-        };
-        auto s_ready = [&](const Tile &t) -> bool {
-            if (t.first && !wait(q_full, t.p)) return false;
-            return wait(&k_full[t.g % A::STAGES], t.g / A::STAGES);
-        };
-        // P_i V of a tile; in two halves, the first while the softmax is still
-        // at the exponentials of the second
-        auto do_pv = [&](int i, const Tile &t) -> bool {
-            if (t.first && t.p > 0 && !wait(&o_free[i], t.p - 1)) return false;
-            if (A::HALVES) {
-                if (!wait(&v_full[t.g % A::STAGES], t.g / A::STAGES) || !wait(&p_half[i], t.g)) return false;
-                tc_fence_after();
-                issue_pv(i, t.g, t.first, 0);
-                if (!wait(&p_full[i], t.g)) return false;
-                tc_fence_after();
-                issue_pv(i, t.g, t.first, 1);
-            } else {
-                if (!wait(&p_full[i], t.g) || !wait(&v_full[t.g % A::STAGES], t.g / A::STAGES)) return false;
-                tc_fence_after();
-                issue_pv(i, t.g, t.first, 0);
-                issue_pv(i, t.g, t.first, 1);
-            }
-            return true;
-        };
-        if constexpr (A::SEP_P) {
-            // S_i of the next tile as soon as the softmax has read S_i, then
-            // P_i V once P_i is ready
-            const int i = warp - A::W_MMA;
-            bool more = step(walk_s, ps, ts);
-            bool ok = more && s_ready(ts);
-            if (ok) {
-                tc_fence_after();
-                issue_s(i, 0);
-                tc_commit_warp(&k_empty[0]);
-                if (ts.last) tc_commit_warp(q_empty);
-            }
-            while (ok && step(walk, pv, tv)) {
-                more = more && step(walk_s, ps, ts);
+            if (!wait(&pair[g % A::PAIRS], g / A::PAIRS)) break;
+            if constexpr (A::SEP_P) {
+                // S_i of the next tile as soon as the softmax has read S_i, then
+                // P_i V, its first half while the softmax is at the second
+                const int i = i_own;
                 if (more) {
-                    if (!(wait(&s_cons[i], tv.g) && s_ready(ts))) break;
+                    if (!wait(&s_cons[i], g)) break;
                     tc_fence_after();
-                    issue_s(i, ts.g);
-                    tc_commit_warp(&k_empty[ts.g % A::STAGES]);
-                    if (ts.last) tc_commit_warp(q_empty);
+                    issue_s(i, sk);
+                    tc_commit_warp(&empty[sk]);
+                    if (left == 1) tc_commit_warp(q_empty);
                 }
-                if (!do_pv(i, tv)) break;
+                if (fresh && p > 0 && !wait(&o_free[i], p - 1)) break;
+                if (!wait(&p_half[i], g)) break;
+                tc_fence_after();
+                issue_pv(i, sv, fresh, 0);
+                if (!wait(&p_full[i], g)) break;
+                tc_fence_after();
+                issue_pv(i, sv, fresh, 1);
                 tc_commit_warp(&pv_done[i]);
-                tc_commit_warp(&v_empty[tv.g % A::STAGES]);
-            }
-        } else {
-            // P_i overwrites S_i: P0 V, next S0, P1 V, next S1 -- the order in
-            // which the warpgroups finish
-            bool more = step(walk_s, ps, ts);
-            bool ok = more && s_ready(ts);
-            if (ok) {
+                tc_commit_warp(&empty[sv]);
+            } else {
+                // P_i overwrites S_i: P0 V, next S0, P1 V, next S1 -- the order
+                // in which the warpgroups finish
+                if (fresh && p > 0 && !wait(&o_free[0], p - 1)) break;
+                if (!wait(&p_full[0], g)) break;
                 tc_fence_after();
-                issue_s(0, 0);
-                issue_s(1, 0);
-                tc_commit_warp(&k_empty[0]);
-                if (ts.last) tc_commit_warp(q_empty);
-            }
-            while (ok && step(walk, pv, tv)) {
-                more = more && step(walk_s, ps, ts);
-                if (!do_pv(0, tv)) break;
-                if (tv.last) tc_commit_warp(&pv_done[0]);
+                issue_pv(0, sv, fresh, 0);
+                issue_pv(0, sv, fresh, 1);
+                if (more) issue_s(0, sk);
+                if (last) tc_commit_warp(&pv_done[0]);
+                if (fresh && p > 0 && !wait(&o_free[1], p - 1)) break;
+                if (!wait(&p_full[1], g)) break;
+                tc_fence_after();
+                issue_pv(1, sv, fresh, 0);
+                issue_pv(1, sv, fresh, 1);
+                tc_commit_warp(&empty[sv]);
+                if (last) tc_commit_warp(&pv_done[1]);
                 if (more) {
-                    if (!s_ready(ts)) break;
-                    tc_fence_after();
-                    issue_s(0, ts.g);
-                }
-                if (!do_pv(1, tv)) break;
-                tc_commit_warp(&v_empty[tv.g % A::STAGES]);
-                if (tv.last) tc_commit_warp(&pv_done[1]);
-                if (more) {
-                    issue_s(1, ts.g);
-                    tc_commit_warp(&k_empty[ts.g % A::STAGES]);
-                    if (ts.last) tc_commit_warp(q_empty);
+                    issue_s(1, sk);
+                    tc_commit_warp(&empty[sk]);
+                    if (left == 1) tc_commit_warp(q_empty);
                 }
             }
+            if (!more) break;
+            sv = two_on(sv);
+            fresh = last;
+            p += last ? 1 : 0;
+            ++g;
         }
     } else {
         // ------------------------------------------------------------ softmax
@@ -702,7 +689,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                     w[k + 1] = *reinterpret_cast<const uint32_t *>(&h1);
                 }
                 tmem_st16u_sync(tP + 16 * qt, w);
-                if (A::HALVES && qt == 1) {
+                if (A::SEP_P && qt == 1) {
                     tc_fence_before();
                     mbar_arrive(&p_half[wg]);
                 }
@@ -727,7 +714,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                 if (wg == 1 || g > 0)
                     ok = ok && mbar_wait(&turn[4 * wg + q], (wg == 1 ? g : g - 1) & 1, err, ERR_WAIT_SOFTMAX);
             ok = __all_sync(0xffffffffu, ok);
-            if constexpr (A::HALVES) mbar_arrive(&p_half[wg]);
+            if constexpr (A::SEP_P) mbar_arrive(&p_half[wg]);
             mbar_arrive(&p_full[wg]);
             if constexpr (A::TURNS)
                 if (lane == 0) mbar_arrive(&turn[4 * (wg ^ 1) + q]);
