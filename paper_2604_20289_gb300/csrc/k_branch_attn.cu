@@ -145,10 +145,9 @@ struct BranchWalk {
 };
 
 // This CTA's share of the line.  Every thread calls it; lens (2 LEN_CACHE ints)
-// receives the branches' lengths, then their table rows.  CTA 0 also leaves the entries' scan for
-// the combine kernel, and checks what the host could not see.
+// receives the branches' lengths, then their table rows.
 template <int KT>
-__device__ BranchStart branch_start(const BranchSched &s, int *lens, int *sh, BranchStart *out, int *err) {
+__device__ BranchStart branch_start(const BranchSched &s, int *lens, int *sh, BranchStart *out) {
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = nt >> 5;
     const int c = blockIdx.x;
     for (int b = tid; b < min(s.B, LEN_CACHE); b += nt) {
@@ -176,19 +175,6 @@ __device__ BranchStart branch_start(const BranchSched &s, int *lens, int *sh, Br
     }
     const int excl = before + x - mine;
     const unsigned PP = (unsigned)s.n_pr * s.line_len(s.n_pt), Th = PP + S, T = Th * s.Hk;
-    if (c == 0) {
-        int a = excl;
-        for (int e = e0; e < e1; ++e) {
-            s.ws_off[e] = a;
-            a += s.line_len((s.own_keys(e, lens) + KT - 1) / KT);
-        }
-        if (tid == 0) s.ws_off[s.E] = S;
-        for (int b = tid; b < s.B; b += nt) {
-            const int q = s.seqs[b];
-            if (err && (q < 0 || q >= s.max_seqs || s.len[q] < 0 || s.len[q] > s.max_pages * s.ps || s.len[q] < s.P))
-                atomicOr(err, ERR_BAD_SEQ);
-        }
-    }
     const BranchLine line(T, s.G);
     const unsigned g0 = line.begin(c), g1 = line.begin(c + 1);
     if (g1 > g0) {
@@ -209,6 +195,32 @@ __device__ BranchStart branch_start(const BranchSched &s, int *lens, int *sh, Br
     }
     __syncthreads();
     return *out;
+}
+
+// One warp of one CTA: the entries' scan for the combine kernel, and a check of
+// what the host could not see.
+template <int KT>
+__device__ void branch_publish(const BranchSched &s, const int *lens, int *err) {
+    const int lane = threadIdx.x & 31;
+    int base = 0;
+    for (int e0 = 0; e0 < s.E; e0 += 32) {
+        const int e = e0 + lane;
+        const int mine = e < s.E ? s.line_len((s.own_keys(e, lens) + KT - 1) / KT) : 0;
+        int x = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        if (e < s.E) s.ws_off[e] = base + x - mine;
+        base += __shfl_sync(0xffffffffu, x, 31);
+    }
+    if (lane == 0) s.ws_off[s.E] = base;
+    for (int b = lane; b < s.B; b += 32) {
+        const int q = s.seqs[b];
+        if (err && (q < 0 || q >= s.max_seqs || s.len[q] < 0 || s.len[q] > s.max_pages * s.ps || s.len[q] < s.P))
+            atomicOr(err, ERR_BAD_SEQ);
+    }
 }
 
 // Entries without a key to read: their rows are zero (with prefix units the
@@ -369,12 +381,13 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
     if (warp == A::W_MMA) tmem_alloc(tmem_slot, A::TMEM_COLS);
     // nothing above depends on the kernels before this one
     pdl_wait();
-    const BranchStart start = branch_start<128>(sc, sh_len, sh_scan, &sh_start, err);
+    const BranchStart start = branch_start<128>(sc, sh_len, sh_scan, &sh_start);
     branch_zero_rows<bf16>(sc, sh_len, o, o_ld, sc.Hk * sc.grp * HD);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    if (blockIdx.x == 0 && warp == A::W_TAIL) branch_publish<128>(sc, sh_len, err);
     BranchWalk<128> walk(sc, start);
     BranchPiece pc;
 
@@ -847,8 +860,9 @@ __global__ void __launch_bounds__(256)
     extern __shared__ __align__(16) float sm[];
     __shared__ int sh_len[2 * LEN_CACHE], sh_scan[32];
     __shared__ BranchStart sh_start;
-    const BranchStart start = branch_start<64>(sc, sh_len, sh_scan, &sh_start, err);
+    const BranchStart start = branch_start<64>(sc, sh_len, sh_scan, &sh_start);
     branch_zero_rows<float>(sc, sh_len, o, o_ld, sc.Hk * sc.grp * HD);
+    if (blockIdx.x == 0 && threadIdx.x < 32) branch_publish<64>(sc, sh_len, err);
     float *sQ = sm, *sK = sQ + 64 * A::LD, *sV = sK + 64 * A::LD, *sP = sV + 64 * A::LD;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int log_ps = 31 - __clz(sc.ps);
@@ -884,26 +898,37 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
             for (int j = 0; j < NC; ++j) acc[i][j] = 0.0f;
         }
-        for (int kt = pc.kt0; kt < pc.kt1; ++kt) {
-            __syncthreads();
-            for (int x = tid; x < 64 * V4; x += 256) {
-                const int r = x / V4, c = x % V4, key = kt * 64 + r;
-                float4 fk = make_float4(0, 0, 0, 0), fv = fk;
+        // the next tile's rows come into registers while this one is at work
+        float4 nk[NC], nv[NC];
+        auto fetch = [&](int kt) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const int x = tid + 256 * i, r = x / V4, c = x % V4, key = kt * 64 + r;
+                nk[i] = nv[i] = make_float4(0, 0, 0, 0);
                 if (key < pc.keys && row_id >= 0) {
                     const int at = pc.key0 + key;
                     const int id = sc.table[(size_t)row_id * sc.max_pages + (at >> log_ps)];
                     if (id >= 0 && id < sc.n_pages) {
                         const size_t off = ((size_t)id * sc.ps + (at & (sc.ps - 1))) * ld + pc.h * HD + 4 * c;
-                        fk = *reinterpret_cast<const float4 *>(k + off);
-                        fv = *reinterpret_cast<const float4 *>(v + off);
+                        nk[i] = *reinterpret_cast<const float4 *>(k + off);
+                        nv[i] = *reinterpret_cast<const float4 *>(v + off);
                     } else if (err) {
                         atomicOr(err, ERR_BAD_SEQ);
                     }
                 }
-                *reinterpret_cast<float4 *>(sK + r * A::LD + 4 * c) = fk;
-                *reinterpret_cast<float4 *>(sV + r * A::LD + 4 * c) = fv;
+            }
+        };
+        fetch(pc.kt0);
+        for (int kt = pc.kt0; kt < pc.kt1; ++kt) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const int x = tid + 256 * i, r = x / V4, c = x % V4;
+                *reinterpret_cast<float4 *>(sK + r * A::LD + 4 * c) = nk[i];
+                *reinterpret_cast<float4 *>(sV + r * A::LD + 4 * c) = nv[i];
             }
             __syncthreads();
+            if (kt + 1 < pc.kt1) fetch(kt + 1);
             if (4 * (ty & ~1) < rows) {                    // the warp (thread rows 2 w, 2 w + 1) has rows
                 float s[4][4];
 #pragma unroll
@@ -1007,8 +1032,9 @@ __global__ void __launch_bounds__(256)
 // of the unit.  A thread owns four columns of every RB-th row, neighbouring
 // threads neighbouring rows.  Latency bound, so nothing passes between
 // threads and the loads of NI rows x KB pieces are in flight together: one
-// row and 8 pieces where many pieces meet few rows (PREFIX), 4 rows and 2
-// pieces where few pieces meet many rows.
+// row and 8 pieces where many pieces meet few rows (PREFIX; 16 pieces take 140
+// registers and 12 % longer over 576 CTAs), 4 rows and 2 pieces where few
+// pieces meet many rows.
 template <typename T, int HD, bool PREFIX>
 __global__ void __launch_bounds__(256)
     branch_combine_kernel(T *o, const long o_ld, const __grid_constant__ BranchSched s) {
