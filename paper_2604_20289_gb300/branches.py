@@ -1,0 +1,176 @@
+"""Branched rollouts: several candidate futures from one history.
+
+``BranchedLayers`` runs a stack of causal self-attention layers
+
+    x <- x + W_o attn(rope(norm(W_q h)), cache) + b_o,   h = LN(x),
+
+over a paged key / value cache (``xcache.KVCache``) in which the branches of a
+rollout share the pages of their common history.  A planner that compares
+candidate actions runs the history once, forks it once per candidate without
+copying it, advances all candidates together -- the shared keys are read once
+for the whole batch -- and drops the ones it does not follow.  All arithmetic
+runs in the CUDA library; this module sequences calls and keeps, on the host,
+the lengths and which pages sequences have in common.
+
+``python -m paper_2604_20289_gb300.branches`` runs such a planning step on
+random weights.
+"""
+from __future__ import annotations
+
+import itertools
+
+import torch
+
+from . import xcache as xb
+
+
+class BranchedLayers:
+    """weights: per layer a dict of CUDA tensors -- ``qkv_w`` [(H + 2 Hk) hd, d] and
+    ``o_w`` [d, H hd] (K-major, the storage type), ``qkv_b``, ``o_b`` (float32),
+    ``gamma_q``, ``gamma_k`` [hd] (float32).  Calls go to the stream that is current
+    when the object is made."""
+
+    def __init__(self, weights, n_heads, n_kv_heads, head_dim, n_pages, page_size=64, max_seqs=64, max_len=4096,
+                 dtype="bf16", theta=10000.0, eps=1e-6):
+        self.weights, self.dtype, self.eps = weights, dtype, float(eps)
+        self.H, self.Hk, self.hd = n_heads, n_kv_heads, head_dim
+        self.d = weights[0]["o_w"].shape[0]
+        self.max_len = max_len
+        self.cache = xb.KVCache.empty(dtype, len(weights), n_pages, page_size, n_kv_heads, head_dim, max_seqs,
+                                      -(-max_len // page_size))
+        self.stream = xb._stream(None)
+        self.pairs, self.n_pos = [head_dim // 2], [max_len]
+        self.rotation = torch.empty(2 * self.pairs[0] * max_len, device="cuda")
+        xb.op_rope_table(self.pairs, self.n_pos, theta, self.rotation, stream=self.stream)
+        self.zeros = torch.zeros(self.d, device="cuda")
+        self.ones = torch.ones(self.d, device="cuda")
+        self.length = [0] * max_seqs
+        self._pages = [[] for _ in range(max_seqs)]       # a label per page; equal labels are the same page
+        self._label = itertools.count()
+        self._free = list(range(max_seqs - 1, -1, -1))
+
+    def _ids(self, seqs):
+        return torch.tensor(list(seqs), dtype=torch.int32, device="cuda")
+
+    def _take(self, n):
+        if n > len(self._free):
+            raise ValueError(f"{n} sequences asked for, {len(self._free)} free")
+        return [self._free.pop() for _ in range(n)]
+
+    def new(self) -> int:
+        """An empty sequence."""
+        return self._take(1)[0]
+
+    def fork(self, seq: int, n: int) -> list:
+        """n sequences that continue ``seq``; full pages are shared, not copied."""
+        ids = self._take(n)
+        xb.op_kv_fork(self.cache, self._ids([seq] * n), self._ids(ids), stream=self.stream)
+        full = self.length[seq] // self.cache.page_size
+        for i in ids:
+            self.length[i] = self.length[seq]
+            self._pages[i] = self._pages[seq][:full]
+            self._relabel(i)
+        return ids
+
+    def free(self, seqs):
+        xb.op_kv_free(self.cache, self._ids(seqs), stream=self.stream)
+        for s in seqs:
+            self.length[s], self._pages[s] = 0, []
+            self._free.append(s)
+
+    def compact(self) -> torch.Tensor:
+        """Moves the pages in use to the front of the pool; returns their count (on the device)."""
+        live = torch.empty(1, dtype=torch.int32, device="cuda")
+        xb.op_kv_compact(self.cache, live, stream=self.stream)
+        return live
+
+    def _relabel(self, s):
+        while len(self._pages[s]) * self.cache.page_size < self.length[s]:
+            self._pages[s].append(next(self._label))
+
+    def shared_len(self, seqs) -> int:
+        """Tokens whose pages all of these sequences have in common."""
+        rows = [self._pages[s] for s in seqs]
+        n = 0
+        for labels in zip(*rows):
+            if any(x != labels[0] for x in labels):
+                break
+            n += 1
+        return min(n * self.cache.page_size, min(self.length[s] for s in seqs) // self.cache.page_size *
+                   self.cache.page_size)
+
+    def step(self, seqs, x):
+        """Appends x [len(seqs), n, d] to the sequences and returns the layers' output
+        of the new tokens (same shape).  Every new token sees its sequence up to itself."""
+        B, n, d = x.shape
+        if B != len(seqs) or d != self.d:
+            raise ValueError(f"x: [{len(seqs)}, n, {self.d}] expected")
+        if n == 0 or B == 0:
+            return x
+        if any(self.length[s] + n > self.max_len for s in seqs):
+            raise ValueError(f"sequences hold at most {self.max_len} tokens")
+        c, st, T = self.cache, self.stream, B * n
+        dt = c.k.dtype
+        dq, dk = self.H * self.hd, self.Hk * self.hd
+        ids = self._ids(seqs)
+        slots = torch.empty(B, n, dtype=torch.int32, device="cuda")
+        xb.op_kv_extend(c, ids, n, slots, stream=st)
+        pos = torch.tensor([[self.length[s] + i] for s in seqs for i in range(n)], dtype=torch.int32, device="cuda")
+        for s in seqs:
+            self.length[s] += n
+            self._relabel(s)
+        shared = self.shared_len(seqs) if B > 1 else 0
+        x = x.reshape(T, d).to(dt).contiguous()
+        h = torch.empty_like(x)
+        qkv = torch.empty(T, dq + 2 * dk, dtype=dt, device="cuda")
+        q = torch.empty(T, dq, dtype=dt, device="cuda")
+        o = torch.empty_like(q)
+        for layer, w in enumerate(self.weights):
+            xb.op_ln_mod(self.dtype, x, self.zeros, self.zeros, h, eps=self.eps, stream=st)
+            xb.op_linear(self.dtype, xb.XC_EPI_BIAS, h, w["qkv_w"], w["qkv_b"], qkv, stream=st)
+            xb.op_qk_norm_rope(c, layer, qkv[:, :dq], qkv[:, dq:dq + dk], qkv[:, dq + dk:], w["gamma_q"], w["gamma_k"],
+                               pos, self.pairs, self.n_pos, self.rotation, slots.view(-1), q, eps=self.eps, stream=st)
+            xb.op_branch_attention(c, layer, ids, n, q, o, shared_len=shared, causal=True, stream=st)
+            y = torch.empty_like(x)
+            xb.op_linear(self.dtype, xb.XC_EPI_RESID_GATE, o, w["o_w"], w["o_b"], y, gate=self.ones, resid=x, stream=st)
+            x = y
+        return x.view(B, n, d)
+
+
+def random_layers(n_layers, d, n_heads, n_kv_heads, head_dim, dtype="bf16", seed=0):
+    """Random weights of the shapes BranchedLayers takes."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rows = (n_heads + 2 * n_kv_heads) * head_dim
+
+    def r(*shape, std=1.0):
+        return std * torch.randn(*shape, generator=g, device="cuda")
+
+    return [dict(qkv_w=r(rows, d, std=d ** -0.5).to(dt), qkv_b=r(rows, std=0.05),
+                 o_w=r(d, n_heads * head_dim, std=(n_heads * head_dim) ** -0.5).to(dt), o_b=r(d, std=0.05),
+                 gamma_q=1.0 + 0.1 * r(head_dim), gamma_k=1.0 + 0.1 * r(head_dim)) for _ in range(n_layers)]
+
+
+def main():
+    d, H, Hk, hd, candidates = 512, 8, 8, 64, 6
+    m = BranchedLayers(random_layers(4, d, H, Hk, hd), H, Hk, hd, n_pages=256, page_size=64, max_seqs=16, max_len=8192)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    history = m.new()
+    m.step([history], torch.randn(1, 2016, d, generator=g, device="cuda"))
+    kids = m.fork(history, candidates)
+    pages = int((m.cache.ref > 0).sum())
+    first = torch.randn(candidates, 1, d, generator=g, device="cuda")
+    x = first
+    for _ in range(8):                                    # one token at a time, all candidates together
+        x = m.step(kids, x)
+    score = x.float().square().mean(dim=(1, 2))
+    best = int(score.argmin())
+    m.free([k for i, k in enumerate(kids) if i != best] + [history])
+    live = int(m.compact())
+    xb.check(xb.XC_OK if xb.op_device_error() == 0 else xb.XC_ECUDA)
+    print(f"history 2016 tokens, {candidates} candidates on {pages} pages (shared {m.shared_len(kids[best:best + 1])} "
+          f"tokens); kept candidate {best}: {m.length[kids[best]]} tokens on {live} pages")
+
+
+if __name__ == "__main__":
+    main()

@@ -138,6 +138,8 @@ TOKEN_CASES = [
     (64, 1, 64, 16, [700, 900], 640),
     (128, 1, 128, 16, [200, 220, 240], 192),             # a whole tile per token
     (2, 2, 64, 1024, [3000, 2050], 2048),
+    (2, 2, 64, 16, [64 + (37 * b) % 90 for b in range(130)], 64),   # more branches than lengths in shared memory
+    (1, 1, 128, 64, [19968 + 5 * b for b in range(3)], 19968),      # one head: a row in as many pieces as CTAs
 ]
 
 
@@ -160,6 +162,8 @@ MULTI_CASES = [
     (10, 2, 128, 32, [96 + 24] * 16, 24, 96),
     (4, 4, 128, 128, [128 * 5, 128 * 6], 128, 512),
     (100, 1, 64, 16, [70, 90], 5, 64),                   # 100 query heads of one key head
+    (2, 2, 128, 16, [100 + (13 * b) % 61 for b in range(70)], 3, 0),
+    (1, 1, 64, 32, [160 + b % 30 for b in range(40)], 20, 128),      # packed rows fill several row tiles
 ]
 
 
@@ -259,6 +263,49 @@ def test_attention_flags_what_the_host_cannot_see():
     cache.len[1] = 16                                                         # shorter than the shared part
     xb.op_branch_attention(cache, 0, i32([0, 1]), 1, q, o, shared_len=32)
     assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
+    assert xb.op_device_error() == 0
+
+
+def test_one_workspace_for_calls_in_turn():
+    """Two shapes through one workspace, back to back and again: nothing is kept between calls."""
+    a = make_cache("bf16", 2, 64, 16, [300, 310, 290], 256)
+    b = make_cache("bf16", 4, 128, 32, [700, 500], 0, seed=9)
+    qa, qb = rand((3, 8 * 64), "bf16", 1), rand((2 * 90, 4 * 128), "bf16", 2)
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device=DEV)
+    outs = []
+    for _ in range(3):
+        oa, ob = torch.empty_like(qa), torch.empty_like(qb)
+        xb.op_branch_attention(a, 0, i32([0, 1, 2]), 1, qa, oa, shared_len=256, causal=True, workspace=ws)
+        xb.op_branch_attention(b, 0, i32([0, 1]), 90, qb, ob, causal=True, workspace=ws)
+        outs.append((oa, ob))
+    for oa, ob in outs[1:]:
+        assert torch.equal(oa, outs[0][0]) and torch.equal(ob, outs[0][1])
+    assert rel_l2(host(outs[0][0]), ref_attention(a, 0, [0, 1, 2], 1, qa, True)) <= 5e-3
+    assert rel_l2(host(outs[0][1]), ref_attention(b, 0, [0, 1], 90, qb, True)) <= 5e-3
+
+
+def test_replayed_in_a_graph_with_new_lengths():
+    """A captured planning step (extend, attend) follows the lengths on the device."""
+    cache = make_cache("bf16", 2, 64, 16, [100, 130], 96, max_pages=20, dead=0.0)
+    free = xb.KVCache("bf16", 2, 64, torch.cat([cache.k, cache.k], 1), torch.cat([cache.v, cache.v], 1),
+                      torch.cat([cache.ref, torch.zeros_like(cache.ref)]), cache.table, cache.len)
+    q, seqs, slots = rand((2, 4 * 64), "bf16", 3), i32([0, 1]), torch.empty(2, 1, dtype=torch.int32, device=DEV)
+    o = torch.empty_like(q)
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):                           # workspaces and one-time set-up before the capture
+        xb.op_kv_extend(free, seqs, 1, slots)
+        xb.op_branch_attention(free, 0, seqs, 1, q, o, shared_len=96, causal=True)
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        xb.op_kv_extend(free, seqs, 1, slots)
+        xb.op_branch_attention(free, 0, seqs, 1, q, o, shared_len=96, causal=True)
+    for n in range(1, 30, 7):
+        while free.len[0].item() < 101 + n:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert free.len.tolist() == [101 + n, 131 + n]
+        assert rel_l2(host(o), ref_attention(free, 0, [0, 1], 1, q, True)) <= 5e-3
     assert xb.op_device_error() == 0
 
 
@@ -535,3 +582,75 @@ def test_offsets_past_32_bits():
     xb.op_qk_norm_rope(cache, 0, x, x, x, g, g, i32([[0]]), [64], [1], table, i32([last * ps + 63]), torch.empty_like(x))
     assert torch.equal(cache.v[0, last, 63], x[0])
     assert xb.op_device_error() == 0
+
+
+# ---------------------------------------------------------------- together
+def plain_layers(weights, H, hk, hd, x, eps=1e-6, theta=1e4):
+    """The causal layers of one whole sequence x [n, d], in 64 bits."""
+    n = x.shape[0]
+    for w in weights:
+        h = (x - x.mean(1, keepdims=True)) / np.sqrt(x.var(1, keepdims=True) + eps)
+        qkv = h @ host(w["qkv_w"]).T + host(w["qkv_b"])
+        pos = np.arange(n)[:, None]
+        q = ref_rotate(qkv[:, :H * hd], H, hd, host(w["gamma_q"]), pos, [hd // 2], theta, False, eps).reshape(n, H, hd)
+        k = ref_rotate(qkv[:, H * hd:(H + hk) * hd], hk, hd, host(w["gamma_k"]), pos, [hd // 2], theta, False,
+                       eps).reshape(n, hk, hd).repeat(H // hk, axis=1)
+        v = qkv[:, (H + hk) * hd:].reshape(n, hk, hd).repeat(H // hk, axis=1)
+        s = np.einsum("ihd,jhd->hij", q, k) / math.sqrt(hd)
+        s[:, np.triu(np.ones((n, n), bool), 1)] = -np.inf
+        p = np.exp(s - s.max(-1, keepdims=True))
+        o = np.einsum("hij,jhd->ihd", p / p.sum(-1, keepdims=True), v).reshape(n, H * hd)
+        x = x + o @ host(w["o_w"]).T + host(w["o_b"])
+    return x
+
+
+@pytest.mark.parametrize("dtype,H,hk,hd,tol", [("f32", 4, 2, 32, 2e-5), ("bf16", 8, 4, 64, 2e-2)])
+def test_branched_layers_match_whole_sequences(dtype, H, hk, hd, tol):
+    """History once, forked, branches advanced together, freed, compacted, forked
+    again: every output equals the layers run on that branch's whole sequence.
+    fp32: a few 1e-6 per layer; bf16: some ten roundings of 2^-9 per layer."""
+    from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
+    d = 256
+    weights = random_layers(2, d, H, hk, hd, dtype, seed=4)
+    m = BranchedLayers(weights, H, hk, hd, n_pages=40, page_size=16, max_seqs=8, max_len=160, dtype=dtype)
+    rng = np.random.default_rng(2)
+    text = {}                                             # tokens of every sequence
+
+    def step(seqs, n):
+        x = torch.from_numpy(rng.standard_normal((len(seqs), n, d))).to(DEV).to(tdt(dtype))
+        for i, s in enumerate(seqs):
+            text[s] = np.concatenate([text[s], host(x[i])])
+        y = host(m.step(seqs, x))
+        assert xb.op_device_error() == 0
+        for i, s in enumerate(seqs):
+            want = plain_layers(weights, H, hk, hd, text[s])[-n:]
+            assert rel_l2(y[i], want) <= tol, rel_l2(y[i], want)
+
+    root = m.new()
+    text[root] = np.zeros((0, d))
+    step([root], 37)
+    kids = m.fork(root, 3)
+    for k in kids:
+        text[k] = text[root]
+    assert m.shared_len(kids) == 32
+    step(kids, 1)
+    step(kids, 12)
+    step([kids[2], root], 5)
+    grand = m.fork(kids[1], 2)
+    for k in grand:
+        text[k] = text[kids[1]]
+    assert m.shared_len(grand) == 48 and m.shared_len([grand[0], root]) == 32
+    m.free([kids[0], kids[1]])
+    live = int(m.compact())
+    assert live == int((m.cache.ref > 0).sum()) and bool((m.cache.ref[:live] > 0).all())
+    step(grand + [root, kids[2]], 3)
+    step(grand, 17)
+    m.free(grand + [root, kids[2]])
+    assert int(m.cache.ref.sum()) == 0
+    with pytest.raises(ValueError):
+        m.fork(root, 9)
+
+
+def test_example_runs():
+    from paper_2604_20289_gb300 import branches
+    branches.main()
