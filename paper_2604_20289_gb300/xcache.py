@@ -170,10 +170,16 @@ def _ptr(t) -> int | None:
     return t.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream) -> int | None:
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        global _raw_stream
+        if _raw_stream is None:                   # the handle alone: a Stream object costs 3 us a call
+            import torch
+            _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        return _raw_stream[0](_raw_stream[1]())
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -407,11 +413,12 @@ class KVCache:
         self.k, self.v, self.ref, self.table, self.len = k, v, ref, table, length
         self.dtype, self.n_kv_heads, self.head_dim = dtype, n_kv_heads, head_dim
         self.page_size = k.shape[2]
+        self.torch_dtype, self._int32 = want, torch.int32
         self.desc = KVCacheDesc(dtype_code(dtype), k.shape[0], k.shape[1], k.shape[2], n_kv_heads, head_dim,
                                 table.shape[0], table.shape[1], k.data_ptr(), v.data_ptr(), ref.data_ptr(),
                                 table.data_ptr(), length.data_ptr())
         self.ptr = ctypes.addressof(self.desc)
-        self._ws = {}
+        self._ws = {}                             # stream -> (tensor, pointer, bytes)
         self._attn_bytes, self._axes = {}, {}
         self._page_bytes = LIB.xc_op_kv_workspace_bytes(self.ptr)
 
@@ -427,58 +434,50 @@ class KVCache:
                    torch.zeros(max_seqs, dtype=torch.int32, device=device))
 
     def workspace(self, nbytes: int, stream: int):
-        """Device workspace of at least nbytes for calls on this stream (cudaStream_t)."""
+        """(tensor, pointer, bytes) of a device workspace for calls on this stream (cudaStream_t)."""
         ws = self._ws.get(stream)
-        if ws is None or ws.numel() < nbytes:
+        if ws is None or ws[2] < nbytes:
             import torch
             ext = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
             with torch.cuda.stream(ext):       # freed memory is reused in this stream's order
-                ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.k.device)
-            self._ws[stream] = ws
+                buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.k.device)
+            ws = self._ws[stream] = buf, buf.data_ptr(), buf.numel()
         return ws
 
-
-def _row_stride(t) -> int:
-    """Elements between the rows of a [rows, columns] tensor with unit column stride."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("rows must have unit column stride")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _int32(t, n):
-    import torch
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"expected a contiguous int32 tensor of {n} elements")
-    return t.data_ptr()
+    def int32(self, t, n: int) -> int:
+        """Device pointer of a contiguous int32 tensor of n elements."""
+        if t.dtype is not self._int32 or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"expected a contiguous int32 tensor of {n} elements")
+        return t.data_ptr()
 
 
 def op_kv_fork(cache: KVCache, src, dst, stream=None):
     """Sequence dst[i] becomes a copy of src[i] (int32 CUDA tensors)."""
     st = _stream(stream)
     n = src.numel()
-    ws = cache.workspace(cache._page_bytes, st)
-    check(LIB.xc_op_kv_fork(cache.ptr, n, _int32(src, n), _int32(dst, n), ws.data_ptr(), ws.numel(), st))
+    _, ws, nbytes = cache.workspace(cache._page_bytes, st)
+    check(LIB.xc_op_kv_fork(cache.ptr, n, cache.int32(src, n), cache.int32(dst, n), ws, nbytes, st))
 
 
 def op_kv_extend(cache: KVCache, seqs, n_new: int, slots, stream=None):
     """Appends n_new tokens to every listed sequence; slots [n, n_new] int32 receives their cache slots."""
     st = _stream(stream)
     n = seqs.numel()
-    ws = cache.workspace(cache._page_bytes, st)
-    check(LIB.xc_op_kv_extend(cache.ptr, n, _int32(seqs, n), n_new, _int32(slots, n * n_new), ws.data_ptr(),
-                              ws.numel(), st))
+    _, ws, nbytes = cache.workspace(cache._page_bytes, st)
+    check(LIB.xc_op_kv_extend(cache.ptr, n, cache.int32(seqs, n), n_new, cache.int32(slots, n * n_new), ws, nbytes,
+                              st))
 
 
 def op_kv_free(cache: KVCache, seqs, stream=None):
     n = seqs.numel()
-    check(LIB.xc_op_kv_free(cache.ptr, n, _int32(seqs, n), _stream(stream)))
+    check(LIB.xc_op_kv_free(cache.ptr, n, cache.int32(seqs, n), _stream(stream)))
 
 
 def op_kv_compact(cache: KVCache, n_live, stream=None):
     """n_live: int32 CUDA tensor of one element, receives the pages in use."""
     st = _stream(stream)
-    ws = cache.workspace(cache._page_bytes, st)
-    check(LIB.xc_op_kv_compact(cache.ptr, _int32(n_live, 1), ws.data_ptr(), ws.numel(), st))
+    _, ws, nbytes = cache.workspace(cache._page_bytes, st)
+    check(LIB.xc_op_kv_compact(cache.ptr, cache.int32(n_live, 1), ws, nbytes, st))
 
 
 def op_rope_table(axis_pairs, n_pos, theta, out, stream=None):
@@ -494,9 +493,9 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
                     eps=1e-6, half_split=False, stream=None):
     """q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] (row-strided views allowed), pos [T, axes]
     and slots [T] int32, table from op_rope_table; axis_pairs, n_pos: host sequences."""
-    T = q.shape[0]
-    hd = cache.head_dim
-    wide = cache.n_kv_heads * hd
+    T, dq = q.shape
+    hd, dt = cache.head_dim, cache.torch_dtype
+    dk = cache.n_kv_heads * hd
     key = (len(axis_pairs), *axis_pairs, *n_pos)
     axes = cache._axes.get(key)
     if axes is None:
@@ -505,17 +504,24 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
         axes = cache._axes[key] = (len(axis_pairs), (_I * len(axis_pairs))(*axis_pairs), (_I * len(n_pos))(*n_pos),
                                    2 * sum(a * b for a, b in zip(axis_pairs, n_pos)))
     n, c_pairs, c_pos, entries = axes
-    if q.shape[1] % hd or q_out.shape != q.shape or k.shape != (T, wide) or v.shape != (T, wide) or \
-            not (q.dtype == k.dtype == v.dtype == q_out.dtype == cache.k.dtype):
+    if dq % hd or q_out.shape != q.shape or k.shape != (T, dk) or v.shape != (T, dk) or q.dtype is not dt or \
+            k.dtype is not dt or v.dtype is not dt or q_out.dtype is not dt:
         raise ValueError("q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] of the cache's dtype")
-    if gamma_q.numel() != hd or gamma_k.numel() != hd or table.numel() != entries or \
-            any(x.element_size() != 4 or not x.is_contiguous() for x in (gamma_q, gamma_k, table)):
+    if gamma_q.numel() != hd or gamma_k.numel() != hd or table.numel() != entries or gamma_q.element_size() != 4 or \
+            gamma_k.element_size() != 4 or table.element_size() != 4 or not gamma_q.is_contiguous() or \
+            not gamma_k.is_contiguous() or not table.is_contiguous():
         raise ValueError("float32 gamma_q, gamma_k [head_dim]; table: one (cos, sin) pair per position and pair of every axis")
-    check(LIB.xc_op_qk_norm_rope(cache.ptr, layer, T, q.shape[1] // hd, q.data_ptr(), _row_stride(q), k.data_ptr(),
-                                 _row_stride(k), v.data_ptr(), _row_stride(v), gamma_q.data_ptr(),
-                                 gamma_k.data_ptr(), eps, n, c_pairs, c_pos,
-                                 _int32(pos, T * n), table.data_ptr(), int(half_split), _int32(slots, T),
-                                 q_out.data_ptr(), _row_stride(q_out), _stream(stream)))
+    (sq, u0), (sk, u1), (sv, u2), (so, u3) = q.stride(), k.stride(), v.stride(), q_out.stride()
+    if u0 != 1 or u1 != 1 or u2 != 1 or u3 != 1:
+        raise ValueError("rows must have unit column stride")
+    if T == 1:
+        sq, sk, sv, so = dq, dk, dk, dq
+    st = LIB.xc_op_qk_norm_rope(cache.ptr, layer, T, dq // hd, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv,
+                                gamma_q.data_ptr(), gamma_k.data_ptr(), eps, n, c_pairs, c_pos,
+                                cache.int32(pos, T * n), table.data_ptr(), half_split, cache.int32(slots, T),
+                                q_out.data_ptr(), so, _stream(stream))
+    if st:
+        check(st)
 
 
 def op_branch_attention_workspace_bytes(cache: KVCache, n_branches, n_q, n_heads, shared_len=0) -> int:
@@ -526,18 +532,25 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
                         workspace=None, stream=None):
     """q, o [len(seqs) * n_q, n_heads * head_dim] (row-strided views allowed); seqs int32 CUDA tensor.
     workspace: a device tensor of op_branch_attention_workspace_bytes, or None for the cache's own."""
-    B, hd = seqs.numel(), cache.head_dim
-    st = _stream(stream)
-    if q.shape[0] != B * n_q or q.shape[1] % hd or o.shape != q.shape or \
-            not (q.dtype == o.dtype == cache.k.dtype):
+    B, hd, dt = seqs.numel(), cache.head_dim, cache.torch_dtype
+    T, dq = q.shape
+    if T != B * n_q or dq % hd or o.shape != q.shape or q.dtype is not dt or o.dtype is not dt:
         raise ValueError("q, o [len(seqs) * n_q, n_heads * head_dim] of the cache's dtype")
-    H = q.shape[1] // hd
+    (sq, u0), (so, u1) = q.stride(), o.stride()
+    if u0 != 1 or u1 != 1:
+        raise ValueError("rows must have unit column stride")
+    if T == 1:
+        sq = so = dq
+    cuda = _stream(stream)
     if workspace is None:
-        key = (B, n_q, H, shared_len)
+        key = (B, n_q, dq, shared_len)
         need = cache._attn_bytes.get(key)
         if need is None:
-            need = cache._attn_bytes[key] = op_branch_attention_workspace_bytes(cache, B, n_q, H, shared_len)
-        workspace = cache.workspace(need, st)
-    check(LIB.xc_op_branch_attention(cache.ptr, layer, B, _int32(seqs, B), n_q, H, q.data_ptr(), _row_stride(q),
-                                     shared_len, int(causal), scale, o.data_ptr(), _row_stride(o),
-                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
+            need = cache._attn_bytes[key] = op_branch_attention_workspace_bytes(cache, B, n_q, dq // hd, shared_len)
+        _, ws, nbytes = cache.workspace(need, cuda)
+    else:
+        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = LIB.xc_op_branch_attention(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
+                                    shared_len, causal, scale, o.data_ptr(), so, ws, nbytes, cuda)
+    if st:
+        check(st)
