@@ -1029,17 +1029,18 @@ __global__ void __launch_bounds__(256)
 // PREFIX: grid.x is (key head, own entry), and every row is merged.  Else
 // grid.x is the CTA boundaries, of which the first one inside a unit merges
 // it (units that one CTA ran whole are written already).  grid.y: NI RB rows
-// of the unit.  A thread owns four columns of every RB-th row, neighbouring
-// threads neighbouring rows.  Latency bound, so nothing passes between
-// threads and the loads of NI rows x KB pieces are in flight together: one
-// row and 8 pieces where many pieces meet few rows (PREFIX; 16 pieces take 140
-// registers and 12 % longer over 576 CTAs), 4 rows and 2 pieces where few
-// pieces meet many rows.
+// of the unit.  A thread owns four columns of a row, neighbouring threads
+// neighbouring rows.  Latency bound, so the loads of NI rows x KB pieces are
+// in flight together: 4 rows and 2 pieces where few pieces meet many rows;
+// with PREFIX, where many pieces meet few rows, one row and 8 pieces, and the
+// row slots that a short tile leaves idle take a share of the pieces each
+// (their sums meet in shared memory, in a fixed order).
+constexpr int COMBINE_THREADS = 256;
 template <typename T, int HD, bool PREFIX>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(COMBINE_THREADS, PREFIX ? 3 : 0)
     branch_combine_kernel(T *o, const long o_ld, const __grid_constant__ BranchSched s) {
     pdl_wait();
-    constexpr int RB = 256 / (HD / 4), NI = PREFIX ? 1 : 4, KB = PREFIX ? 8 : 2;
+    constexpr int RB = COMBINE_THREADS / (HD / 4), NI = PREFIX ? 1 : 4, KB = PREFIX ? 8 : 2;
     const unsigned PP = PREFIX ? (unsigned)s.n_pr * s.line_len(s.n_pt) : 0;
     int h, e, off, len;                                    // own unit: position in its head's line, line length
     if (PREFIX) {
@@ -1074,13 +1075,22 @@ __global__ void __launch_bounds__(256)
     }
     const int b = e / s.n_st, i0 = (e - b * s.n_st) * s.tt;
     const int rows = min(s.tt, s.n_q - i0) * s.grp;
-    const int ch = threadIdx.x / RB, r0 = blockIdx.y * (NI * RB) + threadIdx.x % RB;
-    if (r0 >= rows) return;
+    const int ch = threadIdx.x / RB, slot_r = threadIdx.x % RB, first_row = blockIdx.y * (NI * RB);
+    if (first_row >= rows) return;
+    // PREFIX: 2^lg row slots hold the rows that are left, the others shares of the pieces
+    int lg = 0;
+    if (PREFIX)
+        while ((1 << lg) < RB && (1 << lg) < rows - first_row) ++lg;
+    const int share = PREFIX ? slot_r >> lg : 0, n_share = PREFIX ? RB >> lg : 1;
+    const int r0 = first_row + (PREFIX ? slot_r & ((1 << lg) - 1) : slot_r);
+    const bool there = r0 < rows;
+    if (!PREFIX && !there) return;
     int np = 0;
     const float4 *px = nullptr;                            // first prefix piece: this row's float4, (m, l)
     const float2 *pml = nullptr;
     if (PREFIX) {
-        const int t = b * s.n_q + i0 + r0 / s.grp, pi = t / s.tt, in = (t - pi * s.tt) * s.grp + r0 % s.grp;
+        const int rr = min(r0, rows - 1), t = b * s.n_q + i0 + rr / s.grp, pi = t / s.tt;
+        const int in = (t - pi * s.tt) * s.grp + rr % s.grp;
         const unsigned s0 = h * Th + (unsigned)pi * s.line_len(s.n_pt) + s.lead;
         const int cp = line.owner(s0);
         np = line.owner(s0 + s.n_pt - 1) - cp + 1;
@@ -1098,12 +1108,13 @@ __global__ void __launch_bounds__(256)
         den[i] = 0.0f;
         acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int k0 = 0; k0 < n; k0 += KB) {
+#pragma unroll 1
+    for (int k0 = share; k0 < n; k0 += KB * n_share) {
         float4 x[NI][KB];
         float2 ml[NI][KB];
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
-            const int kk = min(k0 + k, n - 1);             // a piece that exists: its loads are always sound
+            const int at = k0 + k * n_share, kk = min(at, n - 1);   // a piece that exists: its loads are always sound
             const bool pre = PREFIX && kk < np;
             long slot = 0;                                 // the own slot's first row
             if (!pre) slot = PREFIX ? own0 + (long)(kk - np) * s.pitch_o : (2l * (co + kk) + (line.begin(co + kk) >= so ? 0 : 1)) * s.pitch_o;
@@ -1113,7 +1124,7 @@ __global__ void __launch_bounds__(256)
                 x[i][k] = pre ? px[(size_t)kk * s.pitch_p * (HD / 4)]
                               : reinterpret_cast<const float4 *>(s.ws_o + slot * HD)[(size_t)ch * s.pitch_o + r];
                 ml[i][k] = pre ? pml[(size_t)kk * s.pitch_p] : s.ws_ml[slot + r];
-                if (k0 + k >= n) ml[i][k] = make_float2(-INFINITY, 0.0f);
+                if (at >= n) ml[i][k] = make_float2(-INFINITY, 0.0f);
             }
         }
 #pragma unroll
@@ -1137,6 +1148,32 @@ __global__ void __launch_bounds__(256)
                 acc[i].w = fmaf(w, x[i][k].w, acc[i].w);
             }
         }
+    }
+    if constexpr (PREFIX) {
+        __shared__ float4 sh_x[COMBINE_THREADS];
+        __shared__ float2 sh_ml[COMBINE_THREADS];
+        if (n_share > 1) {
+            sh_x[threadIdx.x] = acc[0];
+            sh_ml[threadIdx.x] = make_float2(m[0], den[0]);
+            __syncthreads();
+            if (share > 0) return;
+            float top = m[0];
+            for (int j = 1; j < n_share; ++j) top = fmaxf(top, sh_ml[threadIdx.x + (j << lg)].x);
+            const float use = top == -INFINITY ? 0.0f : top;
+            den[0] = 0.0f;
+            acc[0] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int j = 0; j < n_share; ++j) {
+                const float2 ml = sh_ml[threadIdx.x + (j << lg)];
+                const float4 x = sh_x[threadIdx.x + (j << lg)];
+                const float w = exp2f(ml.x - use);         // 0 for a share without keys, whose sums are 0
+                den[0] = fmaf(w, ml.y, den[0]);
+                acc[0].x = fmaf(w, x.x, acc[0].x);
+                acc[0].y = fmaf(w, x.y, acc[0].y);
+                acc[0].z = fmaf(w, x.z, acc[0].z);
+                acc[0].w = fmaf(w, x.w, acc[0].w);
+            }
+        }
+        if (!there) return;
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -1250,14 +1287,16 @@ static cudaError_t launch_f32(const BranchAttnArgs &a, const BranchPlan &p, floa
 }
 template <typename T, int HD>
 static cudaError_t launch_combine(const BranchAttnArgs &a, const BranchPlan &p, cudaStream_t st) {
-    constexpr int RB = 256 / (HD / 4);
     T *o = reinterpret_cast<T *>(a.o);
-    if (p.s.n_pr > 0)
+    if (p.s.n_pr > 0) {
+        constexpr int RB = COMBINE_THREADS / (HD / 4);
         return launch_pdl(branch_combine_kernel<T, HD, true>, dim3((unsigned)(p.s.Hk * p.s.E), (p.s.pitch_o + RB - 1) / RB),
-                          dim3(256), 0, st, o, a.o_ld, p.s);
+                          dim3(COMBINE_THREADS), 0, st, o, a.o_ld, p.s);
+    }
+    constexpr int ROWS = 4 * COMBINE_THREADS / (HD / 4);
     if (p.s.G == 1) return cudaSuccess;
-    return launch_pdl(branch_combine_kernel<T, HD, false>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + 4 * RB - 1) / (4 * RB)),
-                      dim3(256), 0, st, o, a.o_ld, p.s);
+    return launch_pdl(branch_combine_kernel<T, HD, false>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + ROWS - 1) / ROWS),
+                      dim3(COMBINE_THREADS), 0, st, o, a.o_ld, p.s);
 }
 
 cudaError_t branch_attn(const xc_kv_cache &c, const BranchAttnArgs &a, void *ws, int *err, cudaStream_t st) {
