@@ -90,19 +90,27 @@ struct BranchPiece {
     int b;                   // branch whose table row holds the keys
     int key0, keys;          // first key and keys of the unit
     int kt0, kt1, n_kt;      // key tiles of the piece and of the unit
+    int first;               // key tile that the tensor-core kernel begins with
     int idx;                 // unit of the head: prefix tiles, then entries
 };
 struct BranchStart {
     int h, idx, off, n;      // first unit, position in it, line length of this CTA
 };
 
+//
+// Order of the key tiles.  A softmax may take its keys in any order, so CTAs
+// that read the same keys take them in step, and one read from DRAM serves all
+// of them through L2: after `done` key tiles a CTA begins a whole unit of n at
+// tile done mod n and goes around.  A cut unit's tiles count from its end, so
+// that the CTA it is cut to -- whose clock is at 0 -- begins at tile 0, and all
+// CTAs end at tile n - 1.
 template <int KT>
 struct BranchWalk {
-    int h, idx, off, left;
+    int h, idx, off, left, done;
     int b, j;                // entry idx - n_pr (idx >= n_pr)
     BranchWalk() = default;
     __host__ __device__ __forceinline__ BranchWalk(const BranchSched &s, const BranchStart &st)
-        : h(st.h), idx(st.idx), off(st.off), left(st.n) {
+        : h(st.h), idx(st.idx), off(st.off), left(st.n), done(0) {
         const int e = max(idx - s.n_pr, 0);
         b = e / s.n_st;
         j = e - b * s.n_st;
@@ -126,7 +134,11 @@ struct BranchWalk {
                 p.kt1 = max(end - s.lead, 0);
                 left -= end - off;
                 off = end;
-                if (p.kt1 > p.kt0) return true;
+                if (p.kt1 > p.kt0) {
+                    p.first = p.kt1 - p.kt0 == n ? done % n : n - p.kt1;
+                    done += p.kt1 - p.kt0;
+                    return true;
+                }
                 continue;
             }
             off = 0;
@@ -335,8 +347,10 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                        const __grid_constant__ CUtensorMap tmV, bf16 *o, const long o_ld, const float sl2,
                        const int tt1, const __grid_constant__ BranchSched sc, int *err) {
     using A = BranchTile<HD, QT>;
+    static_assert(A::SMEM_BYTES + sizeof(BranchWarpWalk) * 4 * QT + 4 * (2 * LEN_CACHE + 16) + 32 <= 232448,
+                  "227 KB of shared memory a CTA");
     extern __shared__ uint8_t smem_raw[];
-    __shared__ int sh_len[2 * LEN_CACHE], sh_scan[32];
+    __shared__ int sh_len[2 * LEN_CACHE], sh_scan[16];
     __shared__ BranchStart sh_start;
     __shared__ BranchWarpWalk sh_walk[4 * QT];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -426,13 +440,14 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                 }
                 return id * sc.ps + (key & (sc.ps - 1));
             };
-            int nrow = page_row(pc.kt0);
-            for (int kt = pc.kt0; kt < pc.kt1; ++kt, ++g) {
+            int kt = pc.first, nrow = page_row(kt);
+            for (int i = pc.kt1 - pc.kt0; i > 0; --i, ++g) {
                 const int row = nrow;
-                if (kt + 1 < pc.kt1) nrow = page_row(kt + 1);
+                const bool tail = pc.keys < (kt + 1) * 128;
+                kt = kt + 1 == pc.n_kt ? 0 : kt + 1;
+                if (i > 1) nrow = page_row(kt);
                 const int n_pg = __popc(__ballot_sync(0xffffffffu, row >= 0));
                 const uint32_t bytes = n_pg * box * 128 * A::NR;
-                const bool tail = pc.keys < (kt + 1) * 128;
                 auto load = [&](const CUtensorMap *tm, uint64_t *b) -> bool {      // the next slot
                     const bool r = mbar_wait(&empty[slot], turn_ph ^ 1, err, ERR_WAIT_PRODUCER);
                     if (!__all_sync(0xffffffffu, r)) return false;
@@ -476,11 +491,11 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         int g = 0;
         bool ok = true;
         while (ok && walk.next(sc, sh_len, pc)) {
-            const int kt = pc.kt1 - 1;
-            g += pc.kt1 - pc.kt0;
-            const int valid = pc.keys - kt * 128;
-            if (valid >= 128) continue;
-            const int pi = (g - 1) % A::PAIRS, slot = (2 * g - 1) % A::SLOTS;
+            const int tiles = pc.kt1 - pc.kt0, valid = pc.keys - (pc.n_kt - 1) * 128;
+            const int gt = g + pc.n_kt - 1 - pc.first;         // when the unit's last key tile comes
+            g += tiles;
+            if (valid >= 128 || gt >= g) continue;
+            const int pi = gt % A::PAIRS, slot = (2 * gt + 1) % A::SLOTS;
             ok = mbar_wait(&v_tail[pi], ph >> pi & 1u, err, ERR_WAIT_PRODUCER);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -647,8 +662,8 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
 #pragma unroll
             for (int k = 0; k < 5; ++k) mx[k] = max3(mx[k], mx[k + 5], mx[k + 10]);
             const float m_new = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[15]), mx[0]) * sl2;
-            // a row that sees no key of a piece's first tile sees none of the
-            // piece: m stays -inf, every weight 0
+            // a row that has seen no key yet: m = -inf, every weight 0; its first
+            // key scales the (zero) sums by 2^-inf = 0
             if (fresh) m = m_new;
             const bool grow = !fresh && m_new > m + A::LAZY;
             const float alpha = grow ? exp2_mufu(m - m_new) : 1.0f;
@@ -761,15 +776,18 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                 see = min(sc.limit(sc.seq_len(b, sh_len), t - b * sc.n_q) - cur.key0, cur.keys);
             }
             float m = -INFINITY, l = 0.0f;
-            const int kt0 = cur.kt0, kt1 = cur.kt1;
+            const int g_end = g + cur.kt1 - cur.kt0, wrap = cur.n_kt * 128;
+            bool fresh = true;
             if (live) {
                 const int least = __reduce_min_sync(0xffffffffu, see);
-                for (int kt = kt0; kt < kt1; ++kt, ++g) {
-                    ok = tile(g, see - kt * 128, least < (kt + 1) * 128, kt == kt0, m, l);
+                for (int key = cur.first * 128; g < g_end; ++g) {
+                    ok = tile(g, see - key, least < key + 128, fresh, m, l);
                     if (!ok) break;
+                    fresh = false;
+                    key = key + 128 == wrap ? 0 : key + 128;
                 }
             } else {
-                for (int kt = kt0; ok && kt < kt1; ++kt, ++g) ok = idle_tile(g);
+                for (; ok && g < g_end; ++g) ok = idle_tile(g);
             }
             if (!ok) break;
             advance((p + 1) & 1);                          // while the last P V runs
@@ -858,7 +876,7 @@ __global__ void __launch_bounds__(256)
     using A = BranchTileF32<HD>;
     pdl_wait();
     extern __shared__ __align__(16) float sm[];
-    __shared__ int sh_len[2 * LEN_CACHE], sh_scan[32];
+    __shared__ int sh_len[2 * LEN_CACHE], sh_scan[16];
     __shared__ BranchStart sh_start;
     const BranchStart start = branch_start<64>(sc, sh_len, sh_scan, &sh_start);
     branch_zero_rows<float>(sc, sh_len, o, o_ld, sc.Hk * sc.grp * HD);

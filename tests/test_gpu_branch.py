@@ -164,6 +164,9 @@ MULTI_CASES = [
     (100, 1, 64, 16, [70, 90], 5, 64),                   # 100 query heads of one key head
     (2, 2, 128, 16, [100 + (13 * b) % 61 for b in range(70)], 3, 0),
     (1, 1, 64, 32, [160 + b % 30 for b in range(40)], 20, 128),      # packed rows fill several row tiles
+    # several whole units per CTA, each begun at another key tile: causal rows meet their first visible key late
+    (10, 10, 64, 16, [210 + (31 * b) % 400 for b in range(40)], 40, 0),
+    (9, 9, 128, 64, [150 + (53 * b) % 700 for b in range(24)], 130, 0),
 ]
 
 
