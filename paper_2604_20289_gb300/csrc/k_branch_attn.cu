@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
     uint64_t *pair = bar + 3;                  // [PAIRS] V_g (cleared past the last key) and K_g+1 landed
     uint64_t *v_tail = pair + A::PAIRS;        // [PAIRS] V_g landed, where it is to be cleared
     uint64_t *empty = v_tail + A::PAIRS;       // [SLOTS] slot read by every issuer
-    uint64_t *s_full = empty + A::SLOTS;     // [QT] S_i computed
+    uint64_t *s_full = empty + A::SLOTS;       // [QT] S_i computed
     uint64_t *s_cons = s_full + QT;            // [QT] S_i read (SEP_P)
     uint64_t *p_full = s_cons + QT;            // [QT] P_i written, O_i corrected
     uint64_t *p_half = p_full + QT;            // [QT] first 64 keys of P_i written, O_i corrected (SEP_P)
@@ -418,6 +418,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
         bool ok = true;
         while (ok && walk.next(sc, sh_len, pc)) {
             if (p > 0) ok = mbar_wait(q_empty, (p - 1) & 1, err, ERR_WAIT_PRODUCER);
+            ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             if (lane == 0) {
                 mbar_expect_tx(q_full, q_bytes);
@@ -1247,11 +1248,10 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
         s.n_pr = (int)packed;
         s.n_pt = (shared + KT - 1) / KT;
     }
-    // A unit's query load, pipeline ramp and output take about as long as one
-    // key tile where its rows are few, two where they fill the tile (measured:
-    // 1 against 2 with prefix units 64.9 / 67.1 us for 32 single tokens over
-    // 38880 keys, without them 74.6 / 70.2 us for 6 prompts of 1031 tokens).
-    s.lead = s.n_pr > 0 ? 1 : 2;
+    // A unit's query load, pipeline ramp and output take about as long as two
+    // key tiles (counted 1: 6 prompts of 1031 tokens 74.6 us, counted 2: 70.2;
+    // 16 branches of 20 tokens over 12960 keys 56.1 and 52.2).
+    s.lead = 2;
     s.pitch_p = (int)(tokens < s.tt ? tokens : s.tt) * s.grp;
     s.pitch_o = (n_q < s.tt ? n_q : s.tt) * s.grp;
     s.slots_p = s.n_pr > 0 ? (long)s.Hk * s.n_pr + s.G : 0;
