@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(PLAN_THREADS)
     pdl_release();
     __shared__ int sh[32], sh_seq[PLAN_THREADS], sh_len[PLAN_THREADS], sh_at[PLAN_THREADS], sh_k[PLAN_THREADS], why;
     __shared__ unsigned long long want;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     const long long n_slots = (long long)n * n_new;
     const bool mine = tid < n;
     const int s = mine ? seqs[tid] : 0;
@@ -228,17 +228,24 @@ __global__ void __launch_bounds__(PLAN_THREADS)
     sh_len[tid] = l;
     if (mine) c.len[s] = l + n_new;
     __syncthreads();
-    for (int i = warp; i < n; i += PLAN_THREADS / 32)
-        for (int j = lane; j < sh_k[i]; j += 32) {
+    // 2^lg threads a sequence: its new pages, then its slots
+    const int lg = 31 - __clz(PLAN_THREADS / n), i = tid >> lg, per = 1 << lg, j0 = tid & (per - 1);
+    const int log_ps = 31 - __clz(c.ps);
+    int *row = c.table + (size_t)(i < n ? sh_seq[i] : 0) * c.max_pages;
+    if (i < n) {
+        const int at = (sh_len[i] + c.ps - 1) >> log_ps;
+        for (int j = j0; j < sh_k[i]; j += per) {
             const int p = pl.free_ids[sh_at[i] + j];
             c.ref[p] = 1;
-            c.table[(size_t)sh_seq[i] * c.max_pages + (sh_len[i] + c.ps - 1) / c.ps + j] = p;
+            row[at + j] = p;
         }
-    __syncthreads();
-    for (long long e = tid; e < n_slots; e += PLAN_THREADS) {
-        const int i = (int)(e / n_new), at = sh_len[i] + (int)(e - (long long)i * n_new);
-        slots[e] = c.table[(size_t)sh_seq[i] * c.max_pages + at / c.ps] * c.ps + at % c.ps;
     }
+    __syncthreads();
+    if (i < n)
+        for (int j = j0; j < n_new; j += per) {
+            const int at = sh_len[i] + j;
+            slots[(size_t)i * n_new + j] = (row[at >> log_ps] << log_ps) + (at & (c.ps - 1));
+        }
 }
 
 // One CTA per listed sequence.  The exchange of len makes a sequence that is

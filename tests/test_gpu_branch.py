@@ -551,6 +551,20 @@ def test_page_calls_change_nothing_on_bad_input():
     assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
 
 
+@pytest.mark.parametrize("n,n_new", [(1, 5000), (3, 1700), (700, 17), (1024, 1)])
+def test_extend_many_tokens_or_sequences(n, n_new):
+    ps, rows = 16, -(-n_new // 16) + 1
+    cache = xb.KVCache.empty("bf16", 1, n * rows, ps, 1, 16, n, rows)
+    order = np.random.default_rng(3).permutation(n).tolist()
+    m = PageModel(n * rows, ps, n, rows, np.zeros((1, 1)))
+    for step in (n_new, 3):
+        slots = torch.empty(n, step, dtype=torch.int32, device=DEV)
+        xb.op_kv_extend(cache, i32(order), step, slots)
+        assert xb.op_device_error() == 0
+        assert slots.tolist() == m.extend(order, step)
+    assert cache.ref.tolist() == m.ref and cache.len.tolist() == m.len
+
+
 def test_offsets_past_32_bits():
     """A pool whose element offsets pass 2^31: pages at both ends, copied, filled and read."""
     ps, hk, hd, n_pages = 64, 8, 128, 40000                     # 2.6e9 elements, 5.2 GB each
