@@ -1241,12 +1241,17 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     s.tt = p.tt1 * p.qt;
     s.n_st = (n_q + s.tt - 1) / s.tt;
     s.E = B * s.n_st;
-    // prefix units where packing the branches' rows saves a tenth of the row tiles
-    const long long packed = (tokens + s.tt - 1) / s.tt;
-    if (shared > 0 && packed * 10 <= (long long)s.E * 9) {
+    // Prefix units where the tiles saved by packing the branches' rows outweigh
+    // what they bring: a lead each, and partials of every row (about two key
+    // tiles a unit, written and read), where whole units write their output.
+    // 46 branches of 440 tokens over 864 shared keys, 2 x 8 heads x 128: 572 us
+    // with prefix units, 232 without; 16 branches of 20 tokens over 12960: 54 and
+    // 186 us.
+    const long long packed = (tokens + s.tt - 1) / s.tt, n_pt = (shared + KT - 1) / KT;
+    if (shared > 0 && s.E * (n_pt - 2) > packed * (n_pt + 4)) {
         s.P = shared;
         s.n_pr = (int)packed;
-        s.n_pt = (shared + KT - 1) / KT;
+        s.n_pt = (int)n_pt;
     }
     // A unit's query load, pipeline ramp and output take about as long as two
     // key tiles (counted 1: 6 prompts of 1031 tokens 74.6 us, counted 2: 70.2;
