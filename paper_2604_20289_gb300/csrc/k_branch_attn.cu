@@ -29,6 +29,7 @@ struct BranchSched {
     int n_pr, n_pt;          // prefix row tiles and key tiles (n_pr = 0: no prefix units)
     int n_st, E;             // own row tiles per branch, of all branches
     int P;                   // keys of the prefix units: own keys begin there
+    int shared;              // the caller's shared_len, which no sequence may be shorter than
     int causal, G;           // G: CTAs
     int lead;                // what a unit costs beside its key tiles, in key tiles (see branch_plan)
     int max_seqs, max_pages, ps, n_pages;
@@ -230,7 +231,7 @@ __device__ void branch_publish(const BranchSched &s, const int *lens, int *err) 
     if (lane == 0) s.ws_off[s.E] = base;
     for (int b = lane; b < s.B; b += 32) {
         const int q = s.seqs[b];
-        if (err && (q < 0 || q >= s.max_seqs || s.len[q] < 0 || s.len[q] > s.max_pages * s.ps || s.len[q] < s.P))
+        if (err && (q < 0 || q >= s.max_seqs || s.len[q] < 0 || s.len[q] > s.max_pages * s.ps || s.len[q] < s.shared))
             atomicOr(err, ERR_BAD_SEQ);
     }
 }
@@ -1326,6 +1327,7 @@ cudaError_t branch_attn(const xc_kv_cache &c, const BranchAttnArgs &a, void *ws,
     BranchPlan p = branch_plan(c, a.B, a.n_q, a.H, a.shared);
     p.s.seqs = a.seqs;
     p.s.causal = a.causal;
+    p.s.shared = a.shared;
     p.s.ws_start = reinterpret_cast<int4 *>(ws);
     p.s.ws_o = reinterpret_cast<float *>(p.s.ws_start + p.s.G);
     p.s.ws_ml = reinterpret_cast<float2 *>(p.s.ws_o + p.rows * c.head_dim);
