@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             if (last) {
                 more = walk.next(sc, sh_len, pc);
                 left = more ? pc.kt1 - pc.kt0 : 0;
-                if (more && !wait(q_full, p + 1)) break;
+                if (A::SEP_P && more && !wait(q_full, p + 1)) break;
             } else {
                 --left;
             }
@@ -597,14 +597,16 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
                 tc_commit_warp(&empty[sv]);
             } else {
                 // P_i overwrites S_i: P0 V, next S0, P1 V, next S1 -- the order
-                // in which the warpgroups finish
+                // in which the warpgroups finish (the next piece's queries, on
+                // their way, hold up its S0 only)
                 if (fresh && p > 0 && !wait(&o_free[0], p - 1)) break;
                 if (!wait(&p_full[0], g)) break;
                 tc_fence_after();
                 issue_pv(0, sv, fresh, 0);
                 issue_pv(0, sv, fresh, 1);
-                if (more) issue_s(0, sk);
                 if (last) tc_commit_warp(&pv_done[0]);
+                if (last && more && !wait(q_full, p + 1)) break;
+                if (more) issue_s(0, sk);
                 if (fresh && p > 0 && !wait(&o_free[1], p - 1)) break;
                 if (!wait(&p_full[1], g)) break;
                 tc_fence_after();
