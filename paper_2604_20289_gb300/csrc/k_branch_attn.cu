@@ -544,10 +544,9 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             const bool r = mbar_wait(b, parity & 1, err, ERR_WAIT_MMA);
             return __all_sync(0xffffffffu, r) != 0;
         };
-        // S runs one key tile ahead of P V.  The tensor core drains what is
-        // queued (about 8 products) while this warp looks at barriers, and each
-        // look costs ~150 cycles next to the busy softmax warps, so there are
-        // few: V_g and K_g+1 share one, the queries' and the output's only stand at
+        // S runs one key tile ahead of P V.  A look at a barrier that has long
+        // completed costs 150 cycles and more next to the busy softmax warps,
+        // in which nothing is issued, so there are few: V_g and K_g+1 share one, the queries' and the output's only stand at
         // a piece's first tile (12 heads x 128, 2 x 4320 queries, 30240 keys:
         // 3000 cycles a key tile with separate ones and a tile cursor).
         bool ok = walk.next(sc, sh_len, pc) && wait(q_full, 0) && wait(k0_full, 0);
@@ -866,15 +865,34 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
 
 // ------------------------------------------------------------ fp32 kernel
 // 64-row x 64-key tiles, 256 threads as 16 x 16: thread (ty, tx) computes
-// scores of rows 4 ty.. and keys tx + 16 j, and the same rows' output columns
-// tx + 16 j.  fp32 FMA bound; exact exp2f, no bf16 anywhere.
+// scores of rows 4 ty.. and keys tx + 16 j, and of the same rows' output one or
+// two groups of four columns, over one of KS interleaved shares of the keys
+// where a row has fewer than 16 groups (the shares meet at a piece's end): 12
+// shared-memory accesses per 64 FMAs in either product.  The next tile's keys
+// and values come by asynchronous copies.  exp2f, no bf16 anywhere.  8 heads, 4
+// x 512 causal queries over 4096 + 512..1024 keys: 171 / 507 / 1031 us at head
+// size 16 / 64 / 128, 28 / 38 / 37.5 TFLOP/s of about 80 (issue slots of the
+// softmax and the accesses beside the FMAs; one CTA of 8 warps at head size
+// 128).  Short calls are a few tiles of 3 to 6 us each: 4 x 232 tokens, 4
+// heads x 16, 696 keys 19.4 us.
+// CTAs an SM where a call has work for them (what fits in shared memory): 2
+// against 1 take 171 / 203 and 507 / 591 us above, but 18.6 / 15.7 us where 2 x
+// 77 queries over some 380 keys leave a CTA one tile or none.
+constexpr int branch_f32_ctas(int hd) { return hd <= 64 ? 2 : 1; }
 template <int HD>
 struct BranchTileF32 {
     static constexpr int RT = 64, KT = 64, LD = HD + 4, LDP = KT + 4;
-    static constexpr int SMEM_BYTES = (3 * 64 * LD + 64 * LDP) * (int)sizeof(float);
+    static constexpr int SMEM_BYTES = (5 * 64 * LD + 64 * LDP) * (int)sizeof(float);
+    static constexpr int CG = HD / 4 < 16 ? HD / 4 : 16;   // column groups side by side
+    static constexpr int KS = 16 / CG, NV = HD / (4 * CG); // shares of the keys, column groups of a thread
+    static constexpr int CTAS = branch_f32_ctas(HD);       // resident on an SM
 };
+// 16 bytes to shared memory, of which `bytes` are read and the rest are zero
+__device__ __forceinline__ void cp_async16(uint32_t dst, const float *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 template <int HD>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, BranchTileF32<HD>::CTAS)
     branch_attn_f32_kernel(const float *q, const long q_ld, const float *__restrict__ k, const float *__restrict__ v,
                            float *o, const long o_ld, const float sl2, const __grid_constant__ BranchSched sc, int *err) {
     using A = BranchTileF32<HD>;
@@ -885,12 +903,13 @@ __global__ void __launch_bounds__(256)
     const BranchStart start = branch_start<64>(sc, sh_len, sh_scan, &sh_start);
     branch_zero_rows<float>(sc, sh_len, o, o_ld, sc.Hk * sc.grp * HD);
     if (blockIdx.x == 0 && threadIdx.x < 32) branch_publish<64>(sc, sh_len, err);
-    float *sQ = sm, *sK = sQ + 64 * A::LD, *sV = sK + 64 * A::LD, *sP = sV + 64 * A::LD;
+    float *sQ = sm, *sKV = sQ + 64 * A::LD, *sP = sKV + 4 * 64 * A::LD;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int log_ps = 31 - __clz(sc.ps);
     const size_t ld = (size_t)sc.Hk * HD;
     constexpr int V4 = HD / 4;                             // float4 of a row
-    constexpr int NC = HD / 16;                            // output columns of a thread
+    constexpr int NC = HD / 16;                            // float4 of K and of V that a thread loads
+    const int cg = tx % A::CG, ks = tx / A::CG;
     BranchWalk<64> walk(sc, start);
     BranchPiece pc;
     int np = 0;
@@ -906,7 +925,8 @@ __global__ void __launch_bounds__(256)
             *reinterpret_cast<float4 *>(sQ + r * A::LD + 4 * c) = f;
         }
         int see[4];
-        float m[4], l[4], acc[4][NC];
+        float m[4], l[4];                                  // l: of this thread's keys
+        float4 acc[4][A::NV];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = 4 * ty + i;
@@ -918,39 +938,37 @@ __global__ void __launch_bounds__(256)
             m[i] = -INFINITY;
             l[i] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < NC; ++j) acc[i][j] = 0.0f;
+            for (int j = 0; j < A::NV; ++j) acc[i][j] = make_float4(0, 0, 0, 0);
         }
-        // the next tile's rows come into registers while this one is at work
-        float4 nk[NC], nv[NC];
+        // the next tile's rows are on their way while this one is at work
         auto fetch = [&](int kt) {
+            float *dst = sKV + ((kt - pc.kt0) & 1) * (2 * 64 * A::LD);
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 const int x = tid + 256 * i, r = x / V4, c = x % V4, key = kt * 64 + r;
-                nk[i] = nv[i] = make_float4(0, 0, 0, 0);
+                size_t off = 0;
+                int bytes = 0;                             // 0: the row is filled with zeros
                 if (key < pc.keys && row_id >= 0) {
                     const int at = pc.key0 + key;
                     const int id = sc.table[(size_t)row_id * sc.max_pages + (at >> log_ps)];
                     if (id >= 0 && id < sc.n_pages) {
-                        const size_t off = ((size_t)id * sc.ps + (at & (sc.ps - 1))) * ld + pc.h * HD + 4 * c;
-                        nk[i] = *reinterpret_cast<const float4 *>(k + off);
-                        nv[i] = *reinterpret_cast<const float4 *>(v + off);
+                        off = ((size_t)id * sc.ps + (at & (sc.ps - 1))) * ld + pc.h * HD + 4 * c;
+                        bytes = 16;
                     } else if (err) {
                         atomicOr(err, ERR_BAD_SEQ);
                     }
                 }
+                cp_async16(smem_u32(dst + r * A::LD + 4 * c), k + off, bytes);
+                cp_async16(smem_u32(dst + (64 + r) * A::LD + 4 * c), v + off, bytes);
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
         fetch(pc.kt0);
         for (int kt = pc.kt0; kt < pc.kt1; ++kt) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const int x = tid + 256 * i, r = x / V4, c = x % V4;
-                *reinterpret_cast<float4 *>(sK + r * A::LD + 4 * c) = nk[i];
-                *reinterpret_cast<float4 *>(sV + r * A::LD + 4 * c) = nv[i];
-            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncthreads();
             if (kt + 1 < pc.kt1) fetch(kt + 1);
+            const float *sK = sKV + ((kt - pc.kt0) & 1) * (2 * 64 * A::LD), *sV = sK + 64 * A::LD;
             if (4 * (ty & ~1) < rows) {                    // the warp (thread rows 2 w, 2 w + 1) has rows
                 float s[4][4];
 #pragma unroll
@@ -993,33 +1011,52 @@ __global__ void __launch_bounds__(256)
                         sum += pj;
                         sP[(4 * ty + i) * A::LDP + tx + 16 * j] = pj;
                     }
-#pragma unroll
-                    for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
                     l[i] = l[i] * alpha + sum;
                     m[i] = mn;
 #pragma unroll
-                    for (int j = 0; j < NC; ++j) acc[i][j] *= alpha;
+                    for (int j = 0; j < A::NV; ++j) {
+                        acc[i][j].x *= alpha;
+                        acc[i][j].y *= alpha;
+                        acc[i][j].z *= alpha;
+                        acc[i][j].w *= alpha;
+                    }
                 }
                 __syncwarp();                              // a warp reads only its own rows of P
 #pragma unroll 2
-                for (int c = 0; c < 64; c += 4) {
-                    float4 a[4];
+                for (int c = 4 * ks; c < 64; c += 4 * A::KS) {
+                    float pr[4][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4 *>(sP + (4 * ty + i) * A::LDP + c);
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<float4 *>(pr[i]) = *reinterpret_cast<const float4 *>(sP + (4 * ty + i) * A::LDP + c);
 #pragma unroll
-                    for (int j = 0; j < NC; ++j) {
-                        const float *b = sV + c * A::LD + tx + 16 * j;
-                        const float b0 = b[0], b1 = b[A::LD], b2 = b[2 * A::LD], b3 = b[3 * A::LD];
+                    for (int j = 0; j < A::NV; ++j)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            acc[i][j] = fmaf(a[i].x, b0, acc[i][j]);
-                            acc[i][j] = fmaf(a[i].y, b1, acc[i][j]);
-                            acc[i][j] = fmaf(a[i].z, b2, acc[i][j]);
-                            acc[i][j] = fmaf(a[i].w, b3, acc[i][j]);
+                        for (int x = 0; x < 4; ++x) {
+                            const float4 b = *reinterpret_cast<const float4 *>(sV + (c + x) * A::LD + 4 * (cg + A::CG * j));
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                acc[i][j].x = fmaf(pr[i][x], b.x, acc[i][j].x);
+                                acc[i][j].y = fmaf(pr[i][x], b.y, acc[i][j].y);
+                                acc[i][j].z = fmaf(pr[i][x], b.z, acc[i][j].z);
+                                acc[i][j].w = fmaf(pr[i][x], b.w, acc[i][j].w);
+                            }
                         }
-                    }
                 }
             }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+#pragma unroll
+            for (int d = 8; d >= A::CG; d >>= 1)
+#pragma unroll
+                for (int j = 0; j < A::NV; ++j) {
+                    acc[i][j].x += __shfl_xor_sync(0xffffffffu, acc[i][j].x, d);
+                    acc[i][j].y += __shfl_xor_sync(0xffffffffu, acc[i][j].y, d);
+                    acc[i][j].z += __shfl_xor_sync(0xffffffffu, acc[i][j].z, d);
+                    acc[i][j].w += __shfl_xor_sync(0xffffffffu, acc[i][j].w, d);
+                }
         }
         const bool whole = sc.n_pr == 0 && pc.kt1 - pc.kt0 == pc.n_kt;
         const long row0 = whole ? 0 : branch_slot_row(sc, pc, blockIdx.x, np == 0);
@@ -1028,17 +1065,20 @@ __global__ void __launch_bounds__(256)
         for (int i = 0; i < 4; ++i) {
             const int r = 4 * ty + i;
             if (r >= rows) continue;
+            const bool mine = i % A::KS == ks;             // every share holds the sums: row by row another writes
             if (whole) {
                 const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
                 float *dst = o + (size_t)(pc.t0 + r / sc.grp) * o_ld + (pc.h * sc.grp + r % sc.grp) * HD;
 #pragma unroll
-                for (int j = 0; j < NC; ++j) dst[tx + 16 * j] = acc[i][j] * inv;
+                for (int j = 0; j < A::NV; ++j)
+                    if (mine)
+                        *reinterpret_cast<float4 *>(dst + 4 * (cg + A::CG * j)) =
+                            make_float4(acc[i][j].x * inv, acc[i][j].y * inv, acc[i][j].z * inv, acc[i][j].w * inv);
             } else {
 #pragma unroll
-                for (int j = 0; j < NC; ++j) {
-                    const int col = tx + 16 * j;
-                    sc.ws_o[row0 * HD + ((size_t)(col >> 2) * pitch + r) * 4 + (col & 3)] = acc[i][j];
-                }
+                for (int j = 0; j < A::NV; ++j)
+                    if (mine)
+                        *reinterpret_cast<float4 *>(sc.ws_o + row0 * HD + ((size_t)(cg + A::CG * j) * pitch + r) * 4) = acc[i][j];
                 if (tx == 0) sc.ws_ml[row0 + r] = make_float2(m[i], l[i]);
             }
         }
@@ -1244,6 +1284,8 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     s.tt = p.tt1 * p.qt;
     s.n_st = (n_q + s.tt - 1) / s.tt;
     s.E = B * s.n_st;
+    // (keys that the host knows of: a CTA on every SM has 8 tiles or more)
+    if (f32 && (double)s.E * s.Hk * ((shared + n_q + KT - 1) / KT) >= 8.0 * s.G) s.G *= branch_f32_ctas(c.head_dim);
     // Prefix units where the tiles saved by packing the branches' rows outweigh
     // what they bring: a lead each, and partials of every row (about two key
     // tiles a unit, written and read), where whole units write their output.
