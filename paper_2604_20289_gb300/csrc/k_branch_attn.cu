@@ -871,10 +871,10 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
 // shared-memory accesses per 64 FMAs in either product.  The next tile's keys
 // and values come by asynchronous copies.  exp2f, no bf16 anywhere.  8 heads, 4
 // x 512 causal queries over 4096 + 512..1024 keys: 171 / 507 / 1031 us at head
-// size 16 / 64 / 128, 28 / 38 / 37.5 TFLOP/s of about 80 (issue slots of the
-// softmax and the accesses beside the FMAs; one CTA of 8 warps at head size
-// 128).  Short calls are a few tiles of 3 to 6 us each: 4 x 232 tokens, 4
-// heads x 16, 696 keys 19.4 us.
+// size 16 / 64 / 128, 28 / 38 / 37.5 TFLOP/s of about 80: the shared-memory
+// pipe is 64 / 77 / 68 % and the issue slots 71 / 71 / 63 % busy, the FMA pipe 48
+// / 56 / 52 %.  Short calls are a few tiles a CTA: 4 x 232 tokens, 4 heads x 16,
+// 696 keys 19.4 us.
 // CTAs an SM where a call has work for them (what fits in shared memory): 2
 // against 1 take 171 / 203 and 507 / 591 us above, but 18.6 / 15.7 us where 2 x
 // 77 queries over some 380 keys leave a CTA one tile or none.

@@ -188,6 +188,26 @@ def test_float32(H, hk, hd, ps, lens, n_q, shared, causal):
     check_attention("f32", H, hk, hd, ps, lens, n_q, shared, causal)
 
 
+@pytest.mark.parametrize("H,hk,hd,lens,n_q,shared", [
+    (8, 8, 16, [1344, 1501], 300, 1024),          # two CTAs an SM, prefix units
+    (16, 8, 32, [1040, 903, 700], 211, 0),        # whole and cut units
+    (8, 4, 64, [2500, 2307], 257, 2048),
+    (8, 8, 128, [1344, 1501], 300, 1024),
+])
+def test_float32_long_calls(H, hk, hd, lens, n_q, shared):
+    check_attention("f32", H, hk, hd, 16, lens, n_q, shared, True)
+
+
+def test_float32_flags_a_bad_page_and_reads_on():
+    cache = make_cache("f32", 2, 32, 16, [100, 90], 0, dead=0.0)
+    q = rand((2, 4 * 32), "f32", 4)
+    o = torch.empty_like(q)
+    cache.table[1, 2] = 1 << 20
+    xb.op_branch_attention(cache, 0, i32([0, 1]), 1, q, o)
+    assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
+    assert torch.isfinite(o).all()
+
+
 def test_more_key_tiles_than_ctas_and_long_tables():
     """Lines of many key tiles per CTA, cut inside units, with a table row longer than its sequence."""
     check_attention("bf16", 2, 2, 128, 16, [9000, 5000, 7001], 300, 0, True, max_pages=1000)
