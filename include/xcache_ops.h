@@ -171,7 +171,8 @@ xc_status xc_op_gate_static(int dtype, int n_cams, int tokens_per_cam, int d, co
  * value sets a bit of the word xc_op_device_error() returns --
  * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, which then
  * change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
- * whose token is then skipped. */
+ * whose token is then skipped.  The first operator call of a process sets up
+ * that word; it should come before any stream capture. */
 typedef struct {
     int dtype, n_layers, n_pages, page_size, n_kv_heads, head_dim, max_seqs, max_pages;
     void *k, *v;
@@ -260,7 +261,7 @@ xc_status xc_op_qk_norm_rope(const xc_kv_cache *cache, int layer, int n_tokens, 
  * Cache rows that no sequence has reached (the rest of a last page) may hold
  * anything.  A key that the causal limit hides from a row but that is part of
  * the sequence must be finite, as must its value.  XC_BF16 needs head_dim 64
- * or 128.  At most 128 query heads per key head. */
+ * or 128.  At most 128 query heads per key head (XC_F32: 64). */
 size_t xc_op_branch_attention_workspace_bytes(const xc_kv_cache *cache, int n_branches, int n_q, int n_heads,
                                               int shared_len);
 xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q,

@@ -445,9 +445,9 @@ class KVCache:
         return ws
 
     def int32(self, t, n: int) -> int:
-        """Device pointer of a contiguous int32 tensor of n elements."""
-        if t.dtype is not self._int32 or t.numel() != n or not t.is_contiguous():
-            raise ValueError(f"expected a contiguous int32 tensor of {n} elements")
+        """Device pointer of a contiguous int32 CUDA tensor of n elements."""
+        if t.dtype is not self._int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"expected a contiguous int32 CUDA tensor of {n} elements")
         return t.data_ptr()
 
 
@@ -483,7 +483,8 @@ def op_kv_compact(cache: KVCache, n_live, stream=None):
 def op_rope_table(axis_pairs, n_pos, theta, out, stream=None):
     """out: contiguous float32 CUDA tensor of 2 * sum(axis_pairs * n_pos) elements."""
     n = len(axis_pairs)
-    if len(n_pos) != n or out.numel() != 2 * sum(a * b for a, b in zip(axis_pairs, n_pos)) or not out.is_contiguous():
+    if len(n_pos) != n or out.numel() != 2 * sum(a * b for a, b in zip(axis_pairs, n_pos)) or \
+            not out.is_contiguous() or not out.is_cuda or out.element_size() != 4:
         raise ValueError("out: one (cos, sin) pair per position and pair of every axis")
     check(LIB.xc_op_rope_table(n, (_I * n)(*axis_pairs), (_I * n)(*n_pos), float(theta), out.data_ptr(),
                                _stream(stream)))
@@ -514,6 +515,9 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
     (sq, u0), (sk, u1), (sv, u2), (so, u3) = q.stride(), k.stride(), v.stride(), q_out.stride()
     if u0 != 1 or u1 != 1 or u2 != 1 or u3 != 1:
         raise ValueError("rows must have unit column stride")
+    if not (q.is_cuda and k.is_cuda and v.is_cuda and q_out.is_cuda and gamma_q.is_cuda and gamma_k.is_cuda and
+            table.is_cuda):
+        raise ValueError("expected CUDA tensors")
     if T == 1:
         sq, sk, sv, so = dq, dk, dk, dq
     st = LIB.xc_op_qk_norm_rope(cache.ptr, layer, T, dq // hd, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv,
@@ -539,6 +543,8 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
     (sq, u0), (so, u1) = q.stride(), o.stride()
     if u0 != 1 or u1 != 1:
         raise ValueError("rows must have unit column stride")
+    if not (q.is_cuda and o.is_cuda and (workspace is None or workspace.is_cuda)):
+        raise ValueError("expected CUDA tensors")
     if T == 1:
         sq = so = dq
     cuda = _stream(stream)

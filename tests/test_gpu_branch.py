@@ -289,6 +289,32 @@ def test_attention_flags_what_the_host_cannot_see():
     assert xb.op_device_error() == 0
 
 
+def test_host_tensors_are_refused():
+    """A host address never reaches a kernel: every operand of every call is refused before the launch."""
+    cache = make_cache("bf16", 2, 64, 16, [40, 50], 32, dead=0.0)
+    q, seqs = rand((2, 128), "bf16", 4), i32([0, 1])
+    o = torch.empty_like(q)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    args = [seqs, q, o, ws]
+    for i in range(4):
+        a = [x.cpu() if j == i else x for j, x in enumerate(args)]
+        with pytest.raises(ValueError):
+            xb.op_branch_attention(cache, 0, a[0], 1, a[1], a[2], workspace=a[3])
+    for call in (lambda: xb.op_kv_fork(cache, seqs.cpu(), seqs), lambda: xb.op_kv_fork(cache, seqs, seqs.cpu()),
+                 lambda: xb.op_kv_extend(cache, seqs, 1, i32([0, 0]).cpu()), lambda: xb.op_kv_free(cache, seqs.cpu()),
+                 lambda: xb.op_kv_compact(cache, i32([0]).cpu()),
+                 lambda: xb.op_rope_table([32], [64], 1e4, torch.empty(2 * 32 * 64))):
+        with pytest.raises(ValueError):
+            call()
+    gamma, table = torch.ones(64, device=DEV), torch.empty(2 * 32 * 64, device=DEV)
+    args = [q, q, q, gamma, gamma, seqs, table, seqs, o]
+    for i in range(9):
+        a = [x.cpu() if j == i else x for j, x in enumerate(args)]
+        with pytest.raises(ValueError):
+            xb.op_qk_norm_rope(cache, 0, *a[:6], [32], [64], *a[6:])
+    assert xb.op_device_error() == 0
+
+
 def test_one_workspace_for_calls_in_turn():
     """Two shapes through one workspace, back to back and again: nothing is kept between calls."""
     a = make_cache("bf16", 2, 64, 16, [300, 310, 290], 256)
