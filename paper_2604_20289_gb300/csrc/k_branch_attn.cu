@@ -1278,26 +1278,37 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     s.table = c.table;
     s.G = device_sms();
     p.tt1 = RT / s.grp;
-    // two row tiles per CTA where a unit's rows can fill them
-    const long long tokens = (long long)B * n_q;
-    p.qt = !f32 && (shared > 0 ? tokens : (long long)n_q) > p.tt1 ? 2 : 1;
-    s.tt = p.tt1 * p.qt;
-    s.n_st = (n_q + s.tt - 1) / s.tt;
-    s.E = B * s.n_st;
-    // (keys that the host knows of: a CTA on every SM has 8 tiles or more)
-    if (f32 && (double)s.E * s.Hk * ((shared + n_q + KT - 1) / KT) >= 8.0 * s.G) s.G *= branch_f32_ctas(c.head_dim);
     // Prefix units where the tiles saved by packing the branches' rows outweigh
     // what they bring: a lead each, and partials of every row (about two key
     // tiles a unit, written and read), where whole units write their output.
     // 46 branches of 440 tokens over 864 shared keys, 2 x 8 heads x 128: 572 us
     // with prefix units, 232 without; 16 branches of 20 tokens over 12960: 54 and
     // 186 us.
-    const long long packed = (tokens + s.tt - 1) / s.tt, n_pt = (shared + KT - 1) / KT;
-    if (shared > 0 && s.E * (n_pt - 2) > packed * (n_pt + 4)) {
-        s.P = shared;
-        s.n_pr = (int)packed;
-        s.n_pt = (int)n_pt;
+    // Two row tiles per CTA where that makes the shorter line: a key tile of one
+    // counts 2 against 3, a branch's own keys (the host does not know them) as one
+    // key tile and its new tokens.  One against two tiles: 200 single tokens over
+    // 256 + 16..120 keys, 32 / 8 heads x 64 74.5 and 110.9 us, 16 branches of 20
+    // tokens 50.6 and 52.9; but 32 single tokens over 38880 + 1..1500 keys, 40 / 8
+    // heads x 128 75.5 and 63.4, 6 prompts of 1031 tokens 71.0 and 65.7.
+    const long long tokens = (long long)B * n_q, n_pt = (shared + KT - 1) / KT, own = 1 + n_q / KT;
+    long long least = 0;
+    for (int qt = 1; qt <= (f32 ? 1 : 2); ++qt) {
+        const int tt = p.tt1 * qt, n_st = (n_q + tt - 1) / tt;
+        const long long E = (long long)B * n_st, packed = (tokens + tt - 1) / tt;
+        const bool prefix = shared > 0 && E * (n_pt - 2) > packed * (n_pt + 4);
+        const long long line = prefix ? packed * (n_pt + 2) + E * (own + 2) : E * (n_pt + own + 2);
+        if (qt == 2 && 3 * line >= 2 * least) break;
+        least = line;
+        p.qt = qt;
+        s.tt = tt;
+        s.n_st = n_st;
+        s.E = (int)E;
+        s.P = prefix ? shared : 0;
+        s.n_pr = prefix ? (int)packed : 0;
+        s.n_pt = prefix ? (int)n_pt : 0;
     }
+    // (keys that the host knows of: a CTA on every SM has 8 tiles or more)
+    if (f32 && (double)s.E * s.Hk * ((shared + n_q + KT - 1) / KT) >= 8.0 * s.G) s.G *= branch_f32_ctas(c.head_dim);
     // A unit's query load, pipeline ramp and output take about as long as two
     // key tiles (counted 1: 6 prompts of 1031 tokens 74.6 us, counted 2: 70.2;
     // 16 branches of 20 tokens over 12960 keys 56.1 and 52.2).

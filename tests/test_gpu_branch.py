@@ -176,6 +176,20 @@ def test_several_tokens(H, hk, hd, ps, lens, n_q, shared, causal):
     check_attention("bf16", H, hk, hd, ps, lens, n_q, shared, causal)
 
 
+@pytest.mark.parametrize("H,hk,hd,ps,lens,n_q,shared", [
+    # long shared parts: prefix units of two row tiles
+    (2, 2, 128, 32, [2760, 2700], 128, 2560),
+    (4, 2, 64, 16, [2760, 2700, 2690, 2800], 64, 2560),
+    (40, 8, 128, 128, [16384 + (61 * b) % 300 for b in range(32)], 1, 16384),
+    # packed rows just past whole pairs of row tiles
+    (3, 3, 128, 16, [1040 + 40 * b for b in range(5)], 65, 960),
+    (8, 1, 64, 32, [320 + 7 * b for b in range(33)], 1, 320),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_one_or_two_row_tiles(H, hk, hd, ps, lens, n_q, shared, causal):
+    check_attention("bf16", H, hk, hd, ps, lens, n_q, shared, causal)
+
+
 F32_CASES = [
     (4, 4, 16, 16, [464 + 232] * 2, 58, 464), (4, 2, 32, 16, [50, 1, 0, 33], 1, 0), (6, 1, 64, 32, [200, 130], 70, 96),
     (8, 8, 128, 64, [64, 65, 400], 3, 64), (64, 1, 16, 16, [40, 50], 2, 32), (3, 3, 64, 16, [10, 40, 0], 25, 0),
