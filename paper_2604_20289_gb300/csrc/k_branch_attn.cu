@@ -1278,12 +1278,13 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     s.table = c.table;
     s.G = device_sms();
     p.tt1 = RT / s.grp;
-    // Prefix units where the tiles saved by packing the branches' rows outweigh
-    // what they bring: a lead each, and partials of every row (about two key
-    // tiles a unit, written and read), where whole units write their output.
-    // 46 branches of 440 tokens over 864 shared keys, 2 x 8 heads x 128: 572 us
-    // with prefix units, 232 without; 16 branches of 20 tokens over 12960: 54 and
-    // 186 us.
+    // Prefix units where the tiles saved by packing the branches' rows (the shared
+    // keys of every entry) outweigh what they bring: a lead each, and partials,
+    // where whole units write their output: about two key tiles for the rows of
+    // a prefix tile and as much, by the rows it has, for an entry.  With them and
+    // without, 46 branches of 440 tokens over 864 shared keys, 2 x 8 heads x 128:
+    // 572 and 232 us; 16 branches of 20 tokens over 12960: 54 and 186; 200 single
+    // tokens over 256, 32 / 8 heads x 128: 71 and 98.
     // Two row tiles per CTA where that makes the shorter line: a key tile of one
     // counts 2 against 3, a branch's own keys (the host does not know them) as one
     // key tile and its new tokens.  One against two tiles: 200 single tokens over
@@ -1295,7 +1296,8 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     for (int qt = 1; qt <= (f32 ? 1 : 2); ++qt) {
         const int tt = p.tt1 * qt, n_st = (n_q + tt - 1) / tt;
         const long long E = (long long)B * n_st, packed = (tokens + tt - 1) / tt;
-        const bool prefix = shared > 0 && E * (n_pt - 2) > packed * (n_pt + 4);
+        const long long rows = std::min(n_q, tt) * s.grp;
+        const bool prefix = shared > 0 && E * shared > packed * (n_pt + 4) * KT + 2 * E * rows / qt;
         const long long line = prefix ? packed * (n_pt + 2) + E * (own + 2) : E * (n_pt + own + 2);
         if (qt == 2 && 3 * line >= 2 * least) break;
         least = line;
