@@ -1097,12 +1097,12 @@ __global__ void __launch_bounds__(256, BranchTileF32<HD>::CTAS)
 // with PREFIX, where many pieces meet few rows, one row and 8 pieces, and the
 // row slots that a short tile leaves idle take a share of the pieces each
 // (their sums meet in shared memory, in a fixed order).
-constexpr int COMBINE_THREADS = 256;
-template <typename T, int HD, bool PREFIX>
-__global__ void __launch_bounds__(COMBINE_THREADS, PREFIX ? 3 : 0)
+constexpr int COMBINE_THREADS = 256, COMBINE_SMALL = 64;
+template <typename T, int HD, bool PREFIX, int THREADS>
+__global__ void __launch_bounds__(THREADS, PREFIX ? 3 * COMBINE_THREADS / THREADS : 0)
     branch_combine_kernel(T *o, const long o_ld, const __grid_constant__ BranchSched s) {
     pdl_wait();
-    constexpr int RB = COMBINE_THREADS / (HD / 4), NI = PREFIX ? 1 : 4, KB = PREFIX ? 8 : 2;
+    constexpr int RB = THREADS / (HD / 4), NI = PREFIX ? 1 : 4, KB = PREFIX ? 8 : 2;
     const unsigned PP = PREFIX ? (unsigned)s.n_pr * s.line_len(s.n_pt) : 0;
     int h, e, off, len;                                    // own unit: position in its head's line, line length
     if (PREFIX) {
@@ -1212,8 +1212,8 @@ __global__ void __launch_bounds__(COMBINE_THREADS, PREFIX ? 3 : 0)
         }
     }
     if constexpr (PREFIX) {
-        __shared__ float4 sh_x[COMBINE_THREADS];
-        __shared__ float2 sh_ml[COMBINE_THREADS];
+        __shared__ float4 sh_x[THREADS];
+        __shared__ float2 sh_ml[THREADS];
         if (n_share > 1) {
             sh_x[threadIdx.x] = acc[0];
             sh_ml[threadIdx.x] = make_float2(m[0], den[0]);
@@ -1370,13 +1370,23 @@ template <typename T, int HD>
 static cudaError_t launch_combine(const BranchAttnArgs &a, const BranchPlan &p, cudaStream_t st) {
     T *o = reinterpret_cast<T *>(a.o);
     if (p.s.n_pr > 0) {
-        constexpr int RB = COMBINE_THREADS / (HD / 4);
-        return launch_pdl(branch_combine_kernel<T, HD, true>, dim3((unsigned)(p.s.Hk * p.s.E), (p.s.pitch_o + RB - 1) / RB),
+        constexpr int RB = COMBINE_THREADS / (HD / 4), RS = COMBINE_SMALL / (HD / 4);
+        const unsigned units = (unsigned)(p.s.Hk * p.s.E);
+        // CTAs of 64 threads where an entry's rows would leave half of 256 idle,
+        // if the entries are more than one round of CTAs, or a row's pieces few
+        // enough (8 a thread) for the few shares: 200 single tokens over 256 keys,
+        // 32 / 8 heads x 128 69 -> 63 us, 16 / 8 heads x 64 58 -> 49; but 4 single
+        // tokens over 32768 keys, one head x 128 16.8 -> 21.5.
+        const int shares = p.s.pitch_o < RS ? RS / p.s.pitch_o : 1;
+        if (2 * p.s.pitch_o <= RB && (units > 3u * device_sms() || p.s.G <= 8l * shares * p.s.Hk * p.s.n_pr))
+            return launch_pdl(branch_combine_kernel<T, HD, true, COMBINE_SMALL>, dim3(units, (p.s.pitch_o + RS - 1) / RS),
+                              dim3(COMBINE_SMALL), 0, st, o, a.o_ld, p.s);
+        return launch_pdl(branch_combine_kernel<T, HD, true, COMBINE_THREADS>, dim3(units, (p.s.pitch_o + RB - 1) / RB),
                           dim3(COMBINE_THREADS), 0, st, o, a.o_ld, p.s);
     }
     constexpr int ROWS = 4 * COMBINE_THREADS / (HD / 4);
     if (p.s.G == 1) return cudaSuccess;
-    return launch_pdl(branch_combine_kernel<T, HD, false>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + ROWS - 1) / ROWS),
+    return launch_pdl(branch_combine_kernel<T, HD, false, COMBINE_THREADS>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + ROWS - 1) / ROWS),
                       dim3(COMBINE_THREADS), 0, st, o, a.o_ld, p.s);
 }
 

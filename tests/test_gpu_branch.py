@@ -190,6 +190,19 @@ def test_one_or_two_row_tiles(H, hk, hd, ps, lens, n_q, shared, causal):
     check_attention("bf16", H, hk, hd, ps, lens, n_q, shared, causal)
 
 
+@pytest.mark.parametrize("dtype,H,hk,hd,ps,lens,shared", [
+    # entries of few rows, merged by small CTAs: many of them; few with few pieces a row
+    ("bf16", 16, 8, 64, 16, [256 + (29 * b) % 90 for b in range(90)], 256),
+    ("bf16", 32, 8, 128, 16, [256 + (29 * b) % 90 for b in range(70)], 256),
+    ("bf16", 16, 16, 128, 64, [2048 + 17 * b for b in range(4)], 2048),
+    ("bf16", 3, 3, 128, 64, [4096 + 17 * b for b in range(4)], 4096),      # many pieces a row
+    ("f32", 8, 8, 16, 16, [256 + (29 * b) % 90 for b in range(90)], 256),
+    ("f32", 24, 8, 128, 16, [256 + (29 * b) % 90 for b in range(70)], 256),
+])
+def test_merge_of_short_entries(dtype, H, hk, hd, ps, lens, shared):
+    check_attention(dtype, H, hk, hd, ps, lens, 1, shared, True)
+
+
 F32_CASES = [
     (4, 4, 16, 16, [464 + 232] * 2, 58, 464), (4, 2, 32, 16, [50, 1, 0, 33], 1, 0), (6, 1, 64, 32, [200, 130], 70, 96),
     (8, 8, 128, 64, [64, 65, 400], 3, 64), (64, 1, 16, 16, [40, 50], 2, 32), (3, 3, 64, 16, [10, 40, 0], 25, 0),
