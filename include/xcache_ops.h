@@ -169,8 +169,8 @@ xc_status xc_op_gate_static(int dtype, int n_cams, int tokens_per_cam, int d, co
  *
  * What the host cannot see is checked on the device: a call that finds a bad
  * value sets a bit of the word xc_op_device_error() returns --
- * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, which then
- * change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
+ * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, of which fork
+ * and extend then change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
  * whose token is then skipped.  The first operator call of a process sets up
  * that word; it should come before any stream capture. */
 typedef struct {
@@ -205,7 +205,8 @@ xc_status xc_op_kv_extend(const xc_kv_cache *cache, int n, const int *seqs, int 
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /* Empties the n listed sequences: ref - 1 of their pages, table entries -1,
- * len 0.  An empty sequence stays as it is. */
+ * len 0.  An empty sequence stays as it is.  An id out of range is flagged and
+ * skipped; the others are emptied. */
 xc_status xc_op_kv_free(const xc_kv_cache *cache, int n, const int *seqs, void *stream);
 
 /* Moves the pages in use to ids 0 .. n_live - 1: the k-th page in use with an

@@ -624,6 +624,14 @@ def test_page_calls_change_nothing_on_bad_input():
     assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
 
 
+def test_free_skips_a_bad_id_and_empties_the_others():
+    cache = xb.KVCache.empty("bf16", 1, 8, 16, 1, 16, 4, 4)
+    xb.op_kv_extend(cache, i32([0, 2]), 20, i32([[0] * 20] * 2))
+    xb.op_kv_free(cache, i32([9, 0, -1]))
+    assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
+    assert cache.len.tolist() == [0, 0, 20, 0] and cache.ref.sum().item() == 2
+
+
 @pytest.mark.parametrize("n,n_new", [(1, 5000), (3, 1700), (700, 17), (1024, 1)])
 def test_extend_many_tokens_or_sequences(n, n_new):
     ps, rows = 16, -(-n_new // 16) + 1
