@@ -1094,15 +1094,15 @@ __global__ void __launch_bounds__(256, BranchTileF32<HD>::CTAS)
 // of the unit.  A thread owns four columns of a row, neighbouring threads
 // neighbouring rows.  Latency bound, so the loads of NI rows x KB pieces are
 // in flight together: 4 rows and 2 pieces where few pieces meet many rows;
-// with PREFIX, where many pieces meet few rows, one row and 8 pieces, and the
-// row slots that a short tile leaves idle take a share of the pieces each
-// (their sums meet in shared memory, in a fixed order).
+// with PREFIX one row and 8 pieces, or 4 with more CTAs resident where a row
+// has few, and the row slots that a short tile leaves idle take a share of the
+// pieces each (their sums meet in shared memory, in a fixed order).
 constexpr int COMBINE_THREADS = 256, COMBINE_SMALL = 64;
-template <typename T, int HD, bool PREFIX, int THREADS>
-__global__ void __launch_bounds__(THREADS, PREFIX ? 3 * COMBINE_THREADS / THREADS : 0)
+template <typename T, int HD, bool PREFIX, int THREADS, int KB>
+__global__ void __launch_bounds__(THREADS, PREFIX ? (KB == 8 ? 3 : 4) * COMBINE_THREADS / THREADS : 0)
     branch_combine_kernel(T *o, const long o_ld, const __grid_constant__ BranchSched s) {
     pdl_wait();
-    constexpr int RB = THREADS / (HD / 4), NI = PREFIX ? 1 : 4, KB = PREFIX ? 8 : 2;
+    constexpr int RB = THREADS / (HD / 4), NI = PREFIX ? 1 : 4;
     const unsigned PP = PREFIX ? (unsigned)s.n_pr * s.line_len(s.n_pt) : 0;
     int h, e, off, len;                                    // own unit: position in its head's line, line length
     if (PREFIX) {
@@ -1372,21 +1372,29 @@ static cudaError_t launch_combine(const BranchAttnArgs &a, const BranchPlan &p, 
     if (p.s.n_pr > 0) {
         constexpr int RB = COMBINE_THREADS / (HD / 4), RS = COMBINE_SMALL / (HD / 4);
         const unsigned units = (unsigned)(p.s.Hk * p.s.E);
+        const long prefixes = (long)p.s.Hk * p.s.n_pr;
+        auto launch = [&](auto kernel, int threads, int rb) {
+            return launch_pdl(kernel, dim3(units, (p.s.pitch_o + rb - 1) / rb), dim3(threads), 0, st, o, a.o_ld, p.s);
+        };
+        // 4 pieces at a time where a prefix row has 5 or fewer: 8 branches of 600
+        // tokens over 16000 keys, 16 / 8 heads x 128 539 -> 521 us, 32 of 40 over 2048
+        // 94 -> 85; but 32 single tokens over 38880 (19 pieces) 63.7 -> 64.9.
+        const bool few = p.s.G <= 5 * prefixes;
         // CTAs of 64 threads where an entry's rows would leave half of 256 idle,
         // if the entries are more than one round of CTAs, or a row's pieces few
         // enough (8 a thread) for the few shares: 200 single tokens over 256 keys,
         // 32 / 8 heads x 128 69 -> 63 us, 16 / 8 heads x 64 58 -> 49; but 4 single
         // tokens over 32768 keys, one head x 128 16.8 -> 21.5.
         const int shares = p.s.pitch_o < RS ? RS / p.s.pitch_o : 1;
-        if (2 * p.s.pitch_o <= RB && (units > 3u * device_sms() || p.s.G <= 8l * shares * p.s.Hk * p.s.n_pr))
-            return launch_pdl(branch_combine_kernel<T, HD, true, COMBINE_SMALL>, dim3(units, (p.s.pitch_o + RS - 1) / RS),
-                              dim3(COMBINE_SMALL), 0, st, o, a.o_ld, p.s);
-        return launch_pdl(branch_combine_kernel<T, HD, true, COMBINE_THREADS>, dim3(units, (p.s.pitch_o + RB - 1) / RB),
-                          dim3(COMBINE_THREADS), 0, st, o, a.o_ld, p.s);
+        if (2 * p.s.pitch_o <= RB && (units > 3u * device_sms() || p.s.G <= 8 * shares * prefixes))
+            return few ? launch(branch_combine_kernel<T, HD, true, COMBINE_SMALL, 4>, COMBINE_SMALL, RS)
+                       : launch(branch_combine_kernel<T, HD, true, COMBINE_SMALL, 8>, COMBINE_SMALL, RS);
+        return few ? launch(branch_combine_kernel<T, HD, true, COMBINE_THREADS, 4>, COMBINE_THREADS, RB)
+                   : launch(branch_combine_kernel<T, HD, true, COMBINE_THREADS, 8>, COMBINE_THREADS, RB);
     }
     constexpr int ROWS = 4 * COMBINE_THREADS / (HD / 4);
     if (p.s.G == 1) return cudaSuccess;
-    return launch_pdl(branch_combine_kernel<T, HD, false, COMBINE_THREADS>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + ROWS - 1) / ROWS),
+    return launch_pdl(branch_combine_kernel<T, HD, false, COMBINE_THREADS, 2>, dim3((unsigned)(p.s.G - 1), (p.s.pitch_o + ROWS - 1) / ROWS),
                       dim3(COMBINE_THREADS), 0, st, o, a.o_ld, p.s);
 }
 
