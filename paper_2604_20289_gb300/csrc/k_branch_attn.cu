@@ -1282,15 +1282,15 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     // keys of every entry) outweigh what they bring: a lead each, and partials,
     // where whole units write their output: about two key tiles for the rows of
     // a prefix tile and as much, by the rows it has, for an entry.  With them and
-    // without, 46 branches of 440 tokens over 864 shared keys, 2 x 8 heads x 128:
-    // 572 and 232 us; 16 branches of 20 tokens over 12960: 54 and 186; 200 single
-    // tokens over 256, 32 / 8 heads x 128: 71 and 98.
+    // without, 46 branches of 440 tokens over 864 shared keys, 16 / 8 heads x 128:
+    // 565 and 229 us; 16 branches of 20 tokens over 12960: 51 and 154; 200 single
+    // tokens over 256, 32 / 8 heads x 128: 63 and 97.
     // Two row tiles per CTA where that makes the shorter line: a key tile of one
     // counts 2 against 3, a branch's own keys (the host does not know them) as one
     // key tile and its new tokens.  One against two tiles: 200 single tokens over
-    // 256 + 16..120 keys, 32 / 8 heads x 64 74.5 and 110.9 us, 16 branches of 20
-    // tokens 50.6 and 52.9; but 32 single tokens over 38880 + 1..1500 keys, 40 / 8
-    // heads x 128 75.5 and 63.4, 6 prompts of 1031 tokens 71.0 and 65.7.
+    // 256 + 16..120 keys, 32 / 8 heads x 64 48 and 58 us, 16 branches of 20 tokens
+    // over 12960 keys 50.8 and 52.9; but 32 single tokens over 38880 + 1..1500
+    // keys, 40 / 8 heads x 128 76.6 and 63.4, 6 prompts of 1031 tokens 70.7 and 65.9.
     const long long tokens = (long long)B * n_q, n_pt = (shared + KT - 1) / KT, own = 1 + n_q / KT;
     long long least = 0;
     for (int qt = 1; qt <= (f32 ? 1 : 2); ++qt) {
@@ -1312,8 +1312,8 @@ static BranchPlan branch_plan(const xc_kv_cache &c, int B, int n_q, int H, int s
     // (keys that the host knows of: a CTA on every SM has 8 tiles or more)
     if (f32 && (double)s.E * s.Hk * ((shared + n_q + KT - 1) / KT) >= 8.0 * s.G) s.G *= branch_f32_ctas(c.head_dim);
     // A unit's query load, pipeline ramp and output take about as long as two
-    // key tiles (counted 1: 6 prompts of 1031 tokens 74.6 us, counted 2: 70.2;
-    // 16 branches of 20 tokens over 12960 keys 56.1 and 52.2).
+    // key tiles (counted 1: 6 prompts of 1031 tokens 71.2 us, counted 2: 65.7; 16
+    // branches of 20 tokens over 12960 keys 53.3 and 50.7).
     s.lead = 2;
     s.pitch_p = (int)(tokens < s.tt ? tokens : s.tt) * s.grp;
     s.pitch_o = (n_q < s.tt ? n_q : s.tt) * s.grp;
