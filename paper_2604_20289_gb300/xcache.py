@@ -178,6 +178,7 @@ def _stream(stream) -> int | None:
         global _raw_stream
         if _raw_stream is None:                   # the handle alone: a Stream object costs 3 us a call
             import torch
+            torch.cuda.current_stream()           # sets torch's CUDA state up, or says why it cannot
             _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         return _raw_stream[0](_raw_stream[1]())
     return getattr(stream, "cuda_stream", stream)
