@@ -253,7 +253,9 @@ xc_status xc_op_qk_norm_rope(const xc_kv_cache *cache, int layer, int n_tokens, 
  *   shared_len  the first shared_len tokens (a multiple of page_size) of every
  *               listed sequence are the same pages, as after a fork: they are
  *               read once for all branches, from the row of seqs[0].  Which
- *               keys a row sees does not depend on it.
+ *               keys a row sees does not depend on it.  Keys and values
+ *               behind a page id out of range, or in the row of a seqs[0]
+ *               out of range, count as 0, and the call is flagged.
  *   scale       > 0, or 0 for 1 / sqrt(head_dim)
  *   q, o        [n_branches * n_q][n_heads * head_dim], rows q_stride / o_stride
  *               elements apart, 16-byte aligned

@@ -441,8 +441,8 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             // first pool row of this lane's page in key tile kt (lane < pages of a tile)
             auto page_row = [&](int kt) {
                 const int key = pc.key0 + kt * 128 + lane * box;
-                if (lane * box >= 128 || kt * 128 + lane * box >= pc.keys || row_id < 0) return -1;
-                const int id = pages[key >> log_ps];
+                if (lane * box >= 128 || kt * 128 + lane * box >= pc.keys) return -1;
+                const int id = row_id < 0 ? -1 : pages[key >> log_ps];   // (a prefix unit of a bad first sequence)
                 if (id < 0 || id >= sc.n_pages) {
                     if (err) atomicOr(err, ERR_BAD_SEQ);
                     return sc.n_pages * sc.ps;         // out of range: TMA fills zeros
