@@ -272,6 +272,11 @@ xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_bran
                                  float scale, void *o, long o_stride, void *workspace, size_t workspace_bytes,
                                  void *stream);
 
+/* 1 while work given to `stream` is captured into a graph, else 0.  A captured
+ * call uses its pointers again at every replay: its workspace must live as long
+ * as the graph, and must not be shared with calls that overlap a replay. */
+int xc_op_stream_capturing(void *stream);
+
 /* Reads and clears the process-wide device error word of operator calls
  * (synchronising).  0 = no error. */
 int xc_op_device_error(void);

@@ -262,4 +262,14 @@ xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_bran
     return launched(who, branch_attn(c, a, workspace, err, as_stream(stream)));
 }
 
+int xc_op_stream_capturing(void *stream) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (stream == nullptr) return 0;                       // the legacy default stream is never captured
+    if (cudaStreamIsCapturing(as_stream(stream), &status) != cudaSuccess) {
+        cudaGetLastError();                                // cleared: the stream's next call reports it
+        return 0;
+    }
+    return status != cudaStreamCaptureStatusNone;
+}
+
 }  // extern "C"

@@ -132,6 +132,7 @@ SIGNATURES = {
     "xc_op_rope_table": (_I, [_I, _P, _P, ctypes.c_double, _P, _P]),
     "xc_op_qk_norm_rope": (_I, [_P, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _P, _F, _I, _P, _P, _P, _P, _I, _P, _P,
                                 _L, _P]),
+    "xc_op_stream_capturing": (_I, [_P]),
     "xc_op_branch_attention_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I, _I, _I]),
     "xc_op_branch_attention": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _I, _I, _F, _P, _L, _P, ctypes.c_size_t, _P]),
 }
@@ -395,7 +396,12 @@ class KVCache:
     CUDA tensors: k, v [n_layers, n_pages, page_size, n_kv_heads * head_dim]
     (float32 or bfloat16), ref [n_pages], table [max_seqs, max_pages] and len
     [max_seqs] int32, all contiguous.  Keeps the tensors, and one workspace per
-    stream that grows to the largest call.  ``empty`` allocates them."""
+    stream that grows to the largest call.  ``empty`` allocates them.
+
+    A call that torch captures into a graph (``torch.cuda.graph``) takes a
+    workspace of its own from the graph's memory instead: it lives as long as the
+    graph, whatever larger calls follow, and replays may overlap other calls'
+    workspaces.  Calls in a capture that torch does not run need ``workspace=``."""
 
     def __init__(self, dtype, n_kv_heads, head_dim, k, v, ref, table, length):
         import torch
@@ -435,14 +441,17 @@ class KVCache:
                    torch.zeros(max_seqs, dtype=torch.int32, device=device))
 
     def workspace(self, nbytes: int, stream: int):
-        """(tensor, pointer, bytes) of a device workspace for calls on this stream (cudaStream_t)."""
-        ws = self._ws.get(stream)
+        """(tensor, pointer, bytes) of a device workspace for one call on this stream (cudaStream_t)."""
+        capturing = LIB.xc_op_stream_capturing(stream)
+        ws = None if capturing else self._ws.get(stream)
         if ws is None or ws[2] < nbytes:
             import torch
             ext = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
             with torch.cuda.stream(ext):       # freed memory is reused in this stream's order
                 buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.k.device)
-            ws = self._ws[stream] = buf, buf.data_ptr(), buf.numel()
+            ws = buf, buf.data_ptr(), buf.numel()
+            if not capturing:                  # a graph's memory is the graph's: never kept, never handed to other calls
+                self._ws[stream] = ws
         return ws
 
     def int32(self, t, n: int) -> int:
@@ -452,19 +461,32 @@ class KVCache:
         return t.data_ptr()
 
 
-def op_kv_fork(cache: KVCache, src, dst, stream=None):
+def _given(workspace):
+    """(tensor, pointer, bytes) of the caller's own workspace."""
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous CUDA tensor")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def op_kv_workspace_bytes(cache: KVCache) -> int:
+    """Bytes of a workspace for op_kv_fork, op_kv_extend and op_kv_compact, whose ``workspace`` is a device tensor of
+    that size, or None for the cache's own."""
+    return cache._page_bytes
+
+
+def op_kv_fork(cache: KVCache, src, dst, stream=None, workspace=None):
     """Sequence dst[i] becomes a copy of src[i] (int32 CUDA tensors)."""
     st = _stream(stream)
     n = src.numel()
-    _, ws, nbytes = cache.workspace(cache._page_bytes, st)
+    buf, ws, nbytes = cache.workspace(cache._page_bytes, st) if workspace is None else _given(workspace)
     check(LIB.xc_op_kv_fork(cache.ptr, n, cache.int32(src, n), cache.int32(dst, n), ws, nbytes, st))
 
 
-def op_kv_extend(cache: KVCache, seqs, n_new: int, slots, stream=None):
+def op_kv_extend(cache: KVCache, seqs, n_new: int, slots, stream=None, workspace=None):
     """Appends n_new tokens to every listed sequence; slots [n, n_new] int32 receives their cache slots."""
     st = _stream(stream)
     n = seqs.numel()
-    _, ws, nbytes = cache.workspace(cache._page_bytes, st)
+    buf, ws, nbytes = cache.workspace(cache._page_bytes, st) if workspace is None else _given(workspace)
     check(LIB.xc_op_kv_extend(cache.ptr, n, cache.int32(seqs, n), n_new, cache.int32(slots, n * n_new), ws, nbytes,
                               st))
 
@@ -474,10 +496,10 @@ def op_kv_free(cache: KVCache, seqs, stream=None):
     check(LIB.xc_op_kv_free(cache.ptr, n, cache.int32(seqs, n), _stream(stream)))
 
 
-def op_kv_compact(cache: KVCache, n_live, stream=None):
+def op_kv_compact(cache: KVCache, n_live, stream=None, workspace=None):
     """n_live: int32 CUDA tensor of one element, receives the pages in use."""
     st = _stream(stream)
-    _, ws, nbytes = cache.workspace(cache._page_bytes, st)
+    buf, ws, nbytes = cache.workspace(cache._page_bytes, st) if workspace is None else _given(workspace)
     check(LIB.xc_op_kv_compact(cache.ptr, cache.int32(n_live, 1), ws, nbytes, st))
 
 
@@ -544,7 +566,7 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
     (sq, u0), (so, u1) = q.stride(), o.stride()
     if u0 != 1 or u1 != 1:
         raise ValueError("rows must have unit column stride")
-    if not (q.is_cuda and o.is_cuda and (workspace is None or workspace.is_cuda)):
+    if not (q.is_cuda and o.is_cuda):
         raise ValueError("expected CUDA tensors")
     if T == 1:
         sq = so = dq
@@ -554,9 +576,9 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
         need = cache._attn_bytes.get(key)
         if need is None:
             need = cache._attn_bytes[key] = op_branch_attention_workspace_bytes(cache, B, n_q, dq // hd, shared_len)
-        _, ws, nbytes = cache.workspace(need, cuda)
+        buf, ws, nbytes = cache.workspace(need, cuda)
     else:
-        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        buf, ws, nbytes = _given(workspace)
     st = LIB.xc_op_branch_attention(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
                                     shared_len, causal, scale, o.data_ptr(), so, ws, nbytes, cuda)
     if st:

@@ -42,3 +42,153 @@ def test_shared_keys_of_a_bad_first_sequence_are_zeros(dtype, H, hk, hd, n_q, ba
     got = host(o)
     assert (got[:n_q] == 0).all()
     assert rel_l2(got[n_q:], want[n_q:]) <= (5e-3 if dtype == "bf16" else 5e-6)
+
+
+def test_captured_calls_have_workspaces_of_their_own():
+    """A larger call on the capture's stream and replays on another stream leave a graph's results,
+    the other calls' results and other memory as they are."""
+    small = make_cache("bf16", 2, 64, 16, [700 + 9 * b for b in range(8)], 640, dead=0.0)
+    cache = xb.KVCache("bf16", 2, 64, torch.cat([small.k] * 2, 1), torch.cat([small.v] * 2, 1),
+                       torch.cat([small.ref, torch.zeros_like(small.ref)]),
+                       torch.nn.functional.pad(small.table, (0, 8), value=-1).contiguous(), small.len)
+    q, seqs = rand((8, 8 * 64), "bf16", 3), i32(list(range(8)))
+    qs, few = rand((8 * 300, 8 * 64), "bf16", 4), i32(list(range(8)))
+    o, big = torch.empty_like(q), torch.empty_like(qs)
+    want, want_big = torch.empty_like(q), torch.empty_like(qs)
+    xb.op_branch_attention(cache, 0, seqs, 1, q, want, shared_len=640, causal=True)
+    xb.op_branch_attention(cache, 0, few, 300, qs, want_big, causal=True)
+    st, other = torch.cuda.Stream(), torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    slots = torch.empty(8, 1, dtype=torch.int32, device=DEV)
+    with torch.cuda.stream(st):
+        xb.op_branch_attention(cache, 0, seqs, 1, q, o, shared_len=640, causal=True)
+    st.synchronize()
+    kept = cache._ws[st.cuda_stream]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        xb.op_kv_extend(cache, seqs, 0, slots[:, :0])      # no work, no page taken
+        xb.op_branch_attention(cache, 0, seqs, 1, q, o, shared_len=640, causal=True)
+    assert cache._ws[st.cuda_stream] is kept               # the capture has put nothing in its place
+    with torch.cuda.stream(st):
+        xb.op_branch_attention(cache, 0, few, 300, qs, big, causal=True)
+    st.synchronize()
+    assert cache._ws[st.cuda_stream][2] > kept[2]
+    size = kept[2]
+    del kept
+    fresh = []
+    for s in (st, other, torch.cuda.current_stream()):     # what the allocator hands out now is not the graph's
+        with torch.cuda.stream(s):
+            fresh += [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        o.fill_(float("nan"))
+        big.fill_(float("nan"))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            graph.replay()
+        with torch.cuda.stream(st):
+            xb.op_branch_attention(cache, 0, few, 300, qs, big, causal=True)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want) and torch.equal(big, want_big)
+    assert all(bool((f == 7).all()) for f in fresh)
+    assert xb.op_device_error() == 0
+
+
+def test_workspaces_of_the_caller():
+    cache = xb.KVCache.empty("bf16", 1, 12, 16, 1, 64, 4, 4)
+    cache.k.zero_()
+    cache.v.zero_()
+    need = xb.op_kv_workspace_bytes(cache)
+    ws = torch.full((need + 16,), 0x5A, dtype=torch.uint8, device=DEV)
+    slots, live = i32([[0] * 20]), i32([0])
+    xb.op_kv_extend(cache, i32([0]), 20, slots, workspace=ws[:need])
+    xb.op_kv_fork(cache, i32([0]), i32([1]), workspace=ws[:need])
+    xb.op_kv_free(cache, i32([0]))
+    xb.op_kv_compact(cache, live, workspace=ws[:need])
+    assert xb.op_device_error() == 0 and live.item() == 2 and cache.table[1].tolist() == [0, 1, -1, -1]
+    assert bool((ws[need:] == 0x5A).all()) and not cache._ws
+    q = rand((1, 64), "bf16", 1)
+    o = torch.empty_like(q)
+    calls = [lambda w: xb.op_kv_extend(cache, i32([1]), 1, i32([[0]]), workspace=w),
+             lambda w: xb.op_kv_fork(cache, i32([1]), i32([2]), workspace=w),
+             lambda w: xb.op_kv_compact(cache, live, workspace=w),
+             lambda w: xb.op_branch_attention(cache, 0, i32([1]), 1, q, o, workspace=w)]
+    state = [t.clone() for t in (cache.ref, cache.table, cache.len)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(ws.cpu())
+        with pytest.raises(ValueError):
+            call(ws[:16].expand(1 << 20, 16))              # 16 bytes that look like 16 MB
+        with pytest.raises(xb.XCacheError):
+            call(ws[:32])
+    for a, b in zip(state, (cache.ref, cache.table, cache.len)):
+        assert torch.equal(a, b)
+    assert xb.op_device_error() == 0
+
+
+def test_a_whole_planning_step_in_one_graph():
+    """fork, extend, norm and append, attention, free: captured once, replayed with other inputs and
+    a history that grew in between."""
+    hk, Hq, hd, ps, eps, n = 2, 4, 64, 16, 1e-6, 3
+    cache = xb.KVCache.empty("bf16", 2, 64, ps, hk, hd, 6, 8)
+    cache.k.zero_()
+    cache.v.zero_()
+    table = torch.empty(2 * 32 * 128, device=DEV)
+    xb.op_rope_table([32], [128], 1e4, table)
+    gq, gk = rand((hd,), "f32", 1), rand((hd,), "f32", 2)
+    root, kids = i32([0]), i32([3, 1, 4])
+    qkv = torch.empty(n, (Hq + 2 * hk) * hd, dtype=torch.bfloat16, device=DEV)
+    pos, slots = i32([[0]] * n), torch.empty(n, 1, dtype=torch.int32, device=DEV)
+    q, o = (torch.empty(n, Hq * hd, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    heads = (qkv[:, :Hq * hd], qkv[:, Hq * hd:(Hq + hk) * hd], qkv[:, (Hq + hk) * hd:])
+
+    def grow(m, seed):                                    # m tokens of history, keys and values at random
+        s = torch.empty(1, m, dtype=torch.int32, device=DEV)
+        xb.op_kv_extend(cache, root, m, s)
+        for t, x in ((cache.k, seed), (cache.v, seed + 1)):
+            t[1].view(-1, hk * hd)[s.long().view(-1)] = rand((m, hk * hd), "bf16", x)
+
+    def plan():
+        xb.op_kv_fork(cache, root.expand(n).contiguous(), kids)
+        xb.op_kv_extend(cache, kids, 1, slots)
+        xb.op_qk_norm_rope(cache, 1, *heads, gq, gk, pos, [32], [128], table, slots.view(-1), q, eps=eps)
+        xb.op_branch_attention(cache, 1, kids, 1, q, o, shared_len=32, causal=True)
+        xb.op_kv_free(cache, kids)
+
+    grow(41, 10)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        plan()
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        plan()
+    for i in range(4):
+        length = int(cache.len[0])
+        qkv.copy_(rand(tuple(qkv.shape), "bf16", 20 + i))
+        pos.fill_(length)
+        o.fill_(float("nan"))
+        graph.replay()
+        assert xb.op_device_error() == 0
+        at = slots.view(-1).tolist()
+        assert len(set(at)) == n
+        ang = np.full((n, 1), length)
+        assert rel_l2(host(q), ref_rotate(host(heads[0]), Hq, hd, host(gq), ang, [32], 1e4, False, eps)) <= 2.3e-3
+        k, v = (host(t[1]).reshape(-1, hk * hd) for t in (cache.k, cache.v))
+        assert rel_l2(k[at], ref_rotate(host(heads[1]), hk, hd, host(gk), ang, [32], 1e4, False, eps)) <= 2.3e-3
+        np.testing.assert_array_equal(v[at], host(heads[2]))
+        j = np.arange(length)
+        rows = cache.table[0].cpu().numpy()[j // ps] * ps + j % ps
+        got = host(o).reshape(n, Hq, hd)
+        for b in range(n):
+            kk = np.concatenate([k[rows], k[at[b]][None]]).reshape(-1, hk, hd)
+            vv = np.concatenate([v[rows], v[at[b]][None]]).reshape(-1, hk, hd)
+            w = np.einsum("hd,jhd->hj", host(q)[b].reshape(Hq, hd), kk.repeat(Hq // hk, axis=1)) / np.sqrt(hd)
+            w = np.exp(w - w.max(1, keepdims=True))
+            want = np.einsum("hj,jhd->hd", w / w.sum(1, keepdims=True), vv.repeat(Hq // hk, axis=1))
+            assert rel_l2(got[b], want) <= 5e-3
+        assert cache.len.tolist() == [length] + [0] * 5
+        assert int(cache.ref.sum()) == -(-length // ps)
+        grow(6 + i, 50 + 2 * i)
+        assert xb.op_device_error() == 0
