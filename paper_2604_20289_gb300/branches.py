@@ -27,8 +27,8 @@ from . import xcache as xb
 class BranchedLayers:
     """weights: per layer a dict of CUDA tensors -- ``qkv_w`` [(H + 2 Hk) hd, d] and
     ``o_w`` [d, H hd] (K-major, the storage type), ``qkv_b``, ``o_b`` (float32),
-    ``gamma_q``, ``gamma_k`` [hd] (float32).  Calls go to the stream that is current
-    when the object is made."""
+    ``gamma_q``, ``gamma_k`` [hd] (float32).  A call runs on the stream that is
+    current when it is made, after the object's earlier calls on whatever stream."""
 
     def __init__(self, weights, n_heads, n_kv_heads, head_dim, n_pages, page_size=64, max_seqs=64, max_len=4096,
                  dtype="bf16", theta=10000.0, eps=1e-6):
@@ -38,16 +38,31 @@ class BranchedLayers:
         self.max_len = max_len
         self.cache = xb.KVCache.empty(dtype, len(weights), n_pages, page_size, n_kv_heads, head_dim, max_seqs,
                                       -(-max_len // page_size))
-        self.stream = xb._stream(None)
         self.pairs, self.n_pos = [head_dim // 2], [max_len]
         self.rotation = torch.empty(2 * self.pairs[0] * max_len, device="cuda")
-        xb.op_rope_table(self.pairs, self.n_pos, theta, self.rotation, stream=self.stream)
+        xb.op_rope_table(self.pairs, self.n_pos, theta, self.rotation)
         self.zeros = torch.zeros(self.d, device="cuda")
         self.ones = torch.ones(self.d, device="cuda")
+        self._last = torch.cuda.current_stream()          # stream of the last call
+        self._streams = {self._last.cuda_stream}          # streams that have used the tensors kept here
         self.length = [0] * max_seqs
         self._pages = [[] for _ in range(max_seqs)]       # a label per page; equal labels are the same page
         self._label = itertools.count()
         self._free = list(range(max_seqs - 1, -1, -1))
+
+    def _on_current_stream(self):
+        """Orders the current stream after the object's earlier calls.  Every method that
+        launches work begins with it: its temporaries and its launches are then of one stream."""
+        st = torch.cuda.current_stream()
+        if st != self._last:
+            st.wait_stream(self._last)
+            self._last = st
+        if st.cuda_stream not in self._streams:           # memory kept here is not reused under work of this stream
+            self._streams.add(st.cuda_stream)
+            c = self.cache
+            for t in (c.k, c.v, c.ref, c.table, c.len, self.rotation, self.zeros, self.ones,
+                      *(t for w in self.weights for t in w.values())):
+                t.record_stream(st)
 
     def _ids(self, seqs):
         return torch.tensor(list(seqs), dtype=torch.int32, device="cuda")
@@ -64,7 +79,8 @@ class BranchedLayers:
     def fork(self, seq: int, n: int) -> list:
         """n sequences that continue ``seq``; full pages are shared, not copied."""
         ids = self._take(n)
-        xb.op_kv_fork(self.cache, self._ids([seq] * n), self._ids(ids), stream=self.stream)
+        self._on_current_stream()
+        xb.op_kv_fork(self.cache, self._ids([seq] * n), self._ids(ids))
         full = self.length[seq] // self.cache.page_size
         for i in ids:
             self.length[i] = self.length[seq]
@@ -73,15 +89,17 @@ class BranchedLayers:
         return ids
 
     def free(self, seqs):
-        xb.op_kv_free(self.cache, self._ids(seqs), stream=self.stream)
+        self._on_current_stream()
+        xb.op_kv_free(self.cache, self._ids(seqs))
         for s in seqs:
             self.length[s], self._pages[s] = 0, []
             self._free.append(s)
 
     def compact(self) -> torch.Tensor:
         """Moves the pages in use to the front of the pool; returns their count (on the device)."""
+        self._on_current_stream()
         live = torch.empty(1, dtype=torch.int32, device="cuda")
-        xb.op_kv_compact(self.cache, live, stream=self.stream)
+        xb.op_kv_compact(self.cache, live)
         return live
 
     def _relabel(self, s):
@@ -109,7 +127,8 @@ class BranchedLayers:
             return x
         if any(self.length[s] + n > self.max_len for s in seqs):
             raise ValueError(f"sequences hold at most {self.max_len} tokens")
-        c, st, T = self.cache, self.stream, B * n
+        self._on_current_stream()
+        c, st, T = self.cache, self._last.cuda_stream, B * n
         dt = c.k.dtype
         dq, dk = self.H * self.hd, self.Hk * self.hd
         ids = self._ids(seqs)

@@ -18,6 +18,51 @@ from paper_2604_20289_gb300 import xcache as xb  # noqa: E402
 from test_gpu_branch import (DEV, PageModel, check_attention, host, i32, make_cache, plain_layers, rand,  # noqa: E402
                              ref_attention, ref_rotate, rel_l2, tdt)
 
+D, H, HK, HD = 256, 4, 2, 32
+
+
+class Rollout:
+    """BranchedLayers (fp32, two layers) with the tokens of every sequence kept on the host."""
+
+    def __init__(self, n_pages, max_seqs=8, max_len=160):
+        from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
+        self.weights = random_layers(2, D, H, HK, HD, "f32", seed=4)
+        self.m = BranchedLayers(self.weights, H, HK, HD, n_pages=n_pages, page_size=16, max_seqs=max_seqs,
+                                max_len=max_len, dtype="f32")
+        self.rng = np.random.default_rng(2)
+        self.text = {}
+
+    def tokens(self, n_seqs, n):
+        return torch.from_numpy(self.rng.standard_normal((n_seqs, n, D))).float().to(DEV)
+
+    def new(self):
+        s = self.m.new()
+        self.text[s] = np.zeros((0, D))
+        return s
+
+    def fork(self, seq, n):
+        kids = self.m.fork(seq, n)
+        for k in kids:
+            self.text[k] = self.text[seq]
+        return kids
+
+    def step(self, seqs, n):
+        x = self.tokens(len(seqs), n)
+        y = self.m.step(seqs, x)
+        self.check(seqs, x, y)
+
+    def check(self, seqs, x, y):
+        n = x.shape[1]
+        for i, s in enumerate(seqs):
+            self.text[s] = np.concatenate([self.text[s], host(x[i])])
+            err = rel_l2(host(y[i]), plain_layers(self.weights, H, HK, HD, self.text[s])[-n:])
+            assert err <= 2e-5, err
+        assert xb.op_device_error() == 0
+
+    def state(self):
+        c, m = self.m.cache, self.m
+        return [t.tolist() for t in (c.ref, c.table, c.len)] + [list(m.length), list(m._free)]
+
 
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
@@ -124,6 +169,49 @@ def test_workspaces_of_the_caller():
     for a, b in zip(state, (cache.ref, cache.table, cache.len)):
         assert torch.equal(a, b)
     assert xb.op_device_error() == 0
+
+
+def test_steps_on_other_streams():
+    """Built on one stream, called on others, each behind a delay, with no event of the caller's
+    between the calls: the object orders them, and inputs and outputs are of the calling stream."""
+    main, a, b = torch.cuda.current_stream(), torch.cuda.Stream(), torch.cuda.Stream()
+    r = Rollout(n_pages=40)
+    m = r.m
+    torch.cuda.synchronize()
+    raw = [r.tokens(1, 37), r.tokens(3, 2), r.tokens(3, 5), r.tokens(2, 3)]
+    torch.cuda.synchronize()
+    got = []
+
+    def step(seqs, i):
+        torch.cuda._sleep(20_000_000)                     # some 10 ms: what was not ordered would run before it
+        x = raw[i] + 1.0                                  # made on this stream, behind the delay
+        y = m.step(seqs, x)
+        got.append((seqs, x, y, y + 0.0))                 # read on this stream
+        del x
+        torch.full((1 << 20,), float("nan"), device=DEV)  # memory that the call has let go of
+
+    with torch.cuda.stream(a):
+        root = r.new()
+        step([root], 0)
+    with torch.cuda.stream(b):
+        kids = r.fork(root, 3)
+        step(kids, 1)
+    torch.full((1 << 20,), float("nan"), device=DEV)      # on the stream that the object was made on
+    step(kids, 2)
+    with torch.cuda.stream(a):
+        m.free([root, kids[2]])
+        live = m.compact()
+        step(kids[:2], 3)
+    torch.cuda.synchronize()
+    assert m.cache.len.tolist() == [{k: 47 for k in kids[:2]}.get(s, 0) for s in range(8)]
+    assert int(live) == int((m.cache.ref > 0).sum())      # (the last step stays within its pages)
+    for i, (seqs, x, y, z) in enumerate(got):
+        assert torch.equal(y, z)
+        if i == 1:
+            for k in kids:
+                r.text[k] = r.text[root]
+        r.check(seqs, x, y)
+    assert main == torch.cuda.current_stream()
 
 
 def test_a_whole_planning_step_in_one_graph():
