@@ -10,7 +10,8 @@ candidate actions runs the history once, forks it once per candidate without
 copying it, advances all candidates together -- the shared keys are read once
 for the whole batch -- and drops the ones it does not follow.  All arithmetic
 runs in the CUDA library; this module sequences calls and keeps, on the host,
-the lengths and which pages sequences have in common.
+the lengths and which pages sequences have in common, so that a call the pool
+has no pages for is refused before anything changes.
 
 ``python -m paper_2604_20289_gb300.branches`` runs such a planning step on
 random weights.
@@ -48,6 +49,7 @@ class BranchedLayers:
         self.length = [0] * max_seqs
         self._pages = [[] for _ in range(max_seqs)]       # a label per page; equal labels are the same page
         self._label = itertools.count()
+        self._holders = {}                                # sequences per label; a page without any is free
         self._free = list(range(max_seqs - 1, -1, -1))
 
     def _on_current_stream(self):
@@ -72,12 +74,18 @@ class BranchedLayers:
             raise ValueError(f"{n} sequences asked for, {len(self._free)} free")
         return [self._free.pop() for _ in range(n)]
 
+    def _room(self, pages):
+        free = self.cache.ref.numel() - len(self._holders)
+        if pages > free:
+            raise ValueError(f"{pages} pages asked for, {free} free")
+
     def new(self) -> int:
         """An empty sequence."""
         return self._take(1)[0]
 
     def fork(self, seq: int, n: int) -> list:
         """n sequences that continue ``seq``; full pages are shared, not copied."""
+        self._room(n if self.length[seq] % self.cache.page_size else 0)
         ids = self._take(n)
         self._on_current_stream()
         xb.op_kv_fork(self.cache, self._ids([seq] * n), self._ids(ids))
@@ -85,6 +93,8 @@ class BranchedLayers:
         for i in ids:
             self.length[i] = self.length[seq]
             self._pages[i] = self._pages[seq][:full]
+            for p in self._pages[i]:
+                self._holders[p] += 1
             self._relabel(i)
         return ids
 
@@ -92,6 +102,10 @@ class BranchedLayers:
         self._on_current_stream()
         xb.op_kv_free(self.cache, self._ids(seqs))
         for s in seqs:
+            for p in self._pages[s]:
+                self._holders[p] -= 1
+                if self._holders[p] == 0:
+                    del self._holders[p]
             self.length[s], self._pages[s] = 0, []
             self._free.append(s)
 
@@ -105,6 +119,7 @@ class BranchedLayers:
     def _relabel(self, s):
         while len(self._pages[s]) * self.cache.page_size < self.length[s]:
             self._pages[s].append(next(self._label))
+            self._holders[self._pages[s][-1]] = 1
 
     def shared_len(self, seqs) -> int:
         """Tokens whose pages all of these sequences have in common."""
@@ -127,6 +142,7 @@ class BranchedLayers:
             return x
         if any(self.length[s] + n > self.max_len for s in seqs):
             raise ValueError(f"sequences hold at most {self.max_len} tokens")
+        self._room(sum(-(-(self.length[s] + n) // self.cache.page_size) - len(self._pages[s]) for s in seqs))
         self._on_current_stream()
         c, st, T = self.cache, self._last.cuda_stream, B * n
         dt = c.k.dtype

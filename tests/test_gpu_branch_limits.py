@@ -64,6 +64,37 @@ class Rollout:
         return [t.tolist() for t in (c.ref, c.table, c.len)] + [list(m.length), list(m._free)]
 
 
+def test_a_full_pool_is_refused_before_anything_changes():
+    r = Rollout(n_pages=5)
+    m = r.m
+    root = r.new()
+    r.step([root], 37)                                    # 3 pages of 5
+    before = r.state()
+    with pytest.raises(ValueError):
+        m.fork(root, 3)                                   # 3 copies of the last page
+    with pytest.raises(ValueError):
+        m.step([root], r.tokens(1, 44))                   # 81 tokens: 6 pages
+    assert r.state() == before and xb.op_device_error() == 0
+    kids = r.fork(root, 2)                                # the pool is full
+    before = r.state()
+    with pytest.raises(ValueError):
+        m.step(kids, r.tokens(2, 12))                     # 49 tokens each: a fourth page
+    with pytest.raises(ValueError):
+        m.step([root], r.tokens(1, 12))
+    assert r.state() == before and xb.op_device_error() == 0
+    r.step(kids, 11)                                      # what still fits
+    m.free([root])                                        # its last page only: the others are the children's
+    r.step([kids[0]], 1)
+    with pytest.raises(ValueError):
+        m.step([kids[1]], r.tokens(1, 1))
+    m.free([kids[0]])
+    r.step([kids[1]], 17)
+    m.free([kids[1]])
+    assert int(m.cache.ref.sum()) == 0
+    other = r.new()
+    r.step([other], 80)                                   # the whole pool again
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
