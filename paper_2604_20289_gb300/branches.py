@@ -19,6 +19,7 @@ random weights.
 from __future__ import annotations
 
 import itertools
+import operator
 
 import torch
 
@@ -79,12 +80,24 @@ class BranchedLayers:
         if pages > free:
             raise ValueError(f"{pages} pages asked for, {free} free")
 
+    def _in_use(self, seqs, once=True):
+        """The sequences as a list of ints, each handed out and (once) listed once."""
+        ids = [operator.index(s) for s in seqs]
+        idle = set(self._free)
+        for s in ids:
+            if not 0 <= s < len(self.length) or s in idle:
+                raise ValueError(f"sequence {s} is not in use")
+        if once and len(set(ids)) != len(ids):
+            raise ValueError("a sequence is listed twice")
+        return ids
+
     def new(self) -> int:
         """An empty sequence."""
         return self._take(1)[0]
 
     def fork(self, seq: int, n: int) -> list:
         """n sequences that continue ``seq``; full pages are shared, not copied."""
+        seq, = self._in_use([seq])
         self._room(n if self.length[seq] % self.cache.page_size else 0)
         ids = self._take(n)
         self._on_current_stream()
@@ -99,6 +112,7 @@ class BranchedLayers:
         return ids
 
     def free(self, seqs):
+        seqs = self._in_use(seqs)
         self._on_current_stream()
         xb.op_kv_free(self.cache, self._ids(seqs))
         for s in seqs:
@@ -123,6 +137,7 @@ class BranchedLayers:
 
     def shared_len(self, seqs) -> int:
         """Tokens whose pages all of these sequences have in common."""
+        seqs = self._in_use(seqs, once=False)
         rows = [self._pages[s] for s in seqs]
         n = 0
         for labels in zip(*rows):
@@ -135,6 +150,7 @@ class BranchedLayers:
     def step(self, seqs, x):
         """Appends x [len(seqs), n, d] to the sequences and returns the layers' output
         of the new tokens (same shape).  Every new token sees its sequence up to itself."""
+        seqs = self._in_use(seqs)
         B, n, d = x.shape
         if B != len(seqs) or d != self.d:
             raise ValueError(f"x: [{len(seqs)}, n, {self.d}] expected")

@@ -95,6 +95,37 @@ def test_a_full_pool_is_refused_before_anything_changes():
     r.step([other], 80)                                   # the whole pool again
 
 
+def test_ids_are_refused_before_anything_changes():
+    r = Rollout(n_pages=20)
+    m = r.m
+    a = r.new()
+    r.step([a], 20)
+    b = r.fork(a, 1)[0]
+    x = r.tokens(2, 1)
+    before = r.state()
+    for ids in ([a, a], [a, 7], [b, -1], [b, 8]):         # twice, not in use, out of range
+        with pytest.raises(ValueError):
+            m.step(ids, x)
+        with pytest.raises(ValueError):
+            m.free(ids)
+        assert r.state() == before
+    for s in (7, -1, 8):
+        with pytest.raises(ValueError):
+            m.fork(s, 1)
+        with pytest.raises(ValueError):
+            m.shared_len([a, s])
+    assert m.shared_len([a, b, a]) == 16
+    assert r.state() == before and xb.op_device_error() == 0
+    m.free(s for s in [b])
+    with pytest.raises(ValueError):
+        m.free([b])                                       # no longer in use
+    ids = [r.new() for _ in range(7)]
+    assert len(set(ids + [a])) == 8                       # no id is handed out twice
+    with pytest.raises(ValueError):
+        m.new()
+    r.step([a, ids[3]], 2)
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
