@@ -101,7 +101,11 @@ class BranchedLayers:
         self._room(n if self.length[seq] % self.cache.page_size else 0)
         ids = self._take(n)
         self._on_current_stream()
-        xb.op_kv_fork(self.cache, self._ids([seq] * n), self._ids(ids))
+        try:
+            xb.op_kv_fork(self.cache, self._ids([seq] * n), self._ids(ids))
+        except Exception:                                 # nothing was launched
+            self._free += reversed(ids)
+            raise
         full = self.length[seq] // self.cache.page_size
         for i in ids:
             self.length[i] = self.length[seq]

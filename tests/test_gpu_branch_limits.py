@@ -126,6 +126,19 @@ def test_ids_are_refused_before_anything_changes():
     r.step([a, ids[3]], 2)
 
 
+def test_a_refused_call_takes_no_sequences():
+    """More children than one fork call of the library takes."""
+    r = Rollout(n_pages=40, max_seqs=1500)
+    root = r.new()
+    r.step([root], 16)
+    before = r.state()
+    with pytest.raises((ValueError, xb.XCacheError)):
+        r.m.fork(root, 1400)
+    assert r.state() == before
+    kids = r.fork(root, 3)
+    r.step(kids, 2)
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
