@@ -167,26 +167,29 @@ class BranchedLayers:
         c, st, T = self.cache, self._last.cuda_stream, B * n
         dt = c.k.dtype
         dq, dk = self.H * self.hd, self.Hk * self.hd
+        # What can fail for want of memory comes before the extension, which the host's lengths follow.  (No page
+        # that the new tokens go to is shared, so the shared part is the same before and after.)
+        shared = self.shared_len(seqs) if B > 1 else 0
         ids = self._ids(seqs)
         slots = torch.empty(B, n, dtype=torch.int32, device="cuda")
-        xb.op_kv_extend(c, ids, n, slots, stream=st)
         pos = torch.tensor([[self.length[s] + i] for s in seqs for i in range(n)], dtype=torch.int32, device="cuda")
-        for s in seqs:
-            self.length[s] += n
-            self._relabel(s)
-        shared = self.shared_len(seqs) if B > 1 else 0
         x = x.reshape(T, d).to(dt).contiguous()
-        h = torch.empty_like(x)
+        h, out = torch.empty_like(x), [torch.empty_like(x) for _ in self.weights[:2]]
         qkv = torch.empty(T, dq + 2 * dk, dtype=dt, device="cuda")
         q = torch.empty(T, dq, dtype=dt, device="cuda")
         o = torch.empty_like(q)
+        c.workspace(xb.op_branch_attention_workspace_bytes(c, B, n, self.H, shared), st)
+        xb.op_kv_extend(c, ids, n, slots, stream=st)
+        for s in seqs:
+            self.length[s] += n
+            self._relabel(s)
         for layer, w in enumerate(self.weights):
             xb.op_ln_mod(self.dtype, x, self.zeros, self.zeros, h, eps=self.eps, stream=st)
             xb.op_linear(self.dtype, xb.XC_EPI_BIAS, h, w["qkv_w"], w["qkv_b"], qkv, stream=st)
             xb.op_qk_norm_rope(c, layer, qkv[:, :dq], qkv[:, dq:dq + dk], qkv[:, dq + dk:], w["gamma_q"], w["gamma_k"],
                                pos, self.pairs, self.n_pos, self.rotation, slots.view(-1), q, eps=self.eps, stream=st)
             xb.op_branch_attention(c, layer, ids, n, q, o, shared_len=shared, causal=True, stream=st)
-            y = torch.empty_like(x)
+            y = out[layer % 2]
             xb.op_linear(self.dtype, xb.XC_EPI_RESID_GATE, o, w["o_w"], w["o_b"], y, gate=self.ones, resid=x, stream=st)
             x = y
         return x.view(B, n, d)

@@ -139,6 +139,42 @@ def test_a_refused_call_takes_no_sequences():
     r.step(kids, 2)
 
 
+def test_a_step_without_memory_changes_nothing(monkeypatch):
+    """Whichever allocation fails, the object and the device stay as they were, and the step can be made again."""
+    r = Rollout(n_pages=40)
+    root = r.new()
+    r.step([root], 37)
+    kids = r.fork(root, 3)
+    x = r.tokens(3, 9)
+    before = r.state()
+    made = {name: getattr(torch, name) for name in ("empty", "empty_like", "tensor")}
+    fails = 0
+    while True:
+        left = [fails]
+
+        def limited(name):
+            def make(*args, **kw):
+                if left[0] == 0:
+                    raise torch.cuda.OutOfMemoryError(name)
+                left[0] -= 1
+                return made[name](*args, **kw)
+            return make
+
+        for name in made:
+            monkeypatch.setattr(torch, name, limited(name))
+        try:
+            y = r.m.step(kids, x)
+        except torch.cuda.OutOfMemoryError:
+            y = None
+        monkeypatch.undo()
+        if y is not None:
+            break
+        assert r.state() == before and xb.op_device_error() == 0
+        fails += 1
+    assert fails >= 8
+    r.check(kids, x, y)
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
