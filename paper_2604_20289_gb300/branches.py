@@ -155,9 +155,9 @@ class BranchedLayers:
         """Appends x [len(seqs), n, d] to the sequences and returns the layers' output
         of the new tokens (same shape).  Every new token sees its sequence up to itself."""
         seqs = self._in_use(seqs)
+        if x.dim() != 3 or x.shape[0] != len(seqs) or x.shape[2] != self.d or not x.is_cuda:
+            raise ValueError(f"x: CUDA tensor [{len(seqs)}, n, {self.d}] expected")
         B, n, d = x.shape
-        if B != len(seqs) or d != self.d:
-            raise ValueError(f"x: [{len(seqs)}, n, {self.d}] expected")
         if n == 0 or B == 0:
             return x
         if any(self.length[s] + n > self.max_len for s in seqs):

@@ -175,6 +175,18 @@ def test_a_step_without_memory_changes_nothing(monkeypatch):
     r.check(kids, x, y)
 
 
+def test_a_step_of_a_host_tensor_is_refused():
+    r = Rollout(n_pages=20)
+    root = r.new()
+    r.step([root], 20)
+    before = r.state()
+    for x in (r.tokens(1, 2).cpu(), r.tokens(1, 2)[0], r.tokens(2, 2), r.tokens(1, 2)[..., :-1]):
+        with pytest.raises(ValueError):
+            r.m.step([root], x)
+    assert r.state() == before and xb.op_device_error() == 0
+    r.step([root], 2)
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
