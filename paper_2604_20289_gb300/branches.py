@@ -37,6 +37,7 @@ class BranchedLayers:
         self.weights, self.dtype, self.eps = weights, dtype, float(eps)
         self.H, self.Hk, self.hd = n_heads, n_kv_heads, head_dim
         self.d = weights[0]["o_w"].shape[0]
+        self._check_weights()
         self.max_len = max_len
         self.cache = xb.KVCache.empty(dtype, len(weights), n_pages, page_size, n_kv_heads, head_dim, max_seqs,
                                       -(-max_len // page_size))
@@ -52,6 +53,17 @@ class BranchedLayers:
         self._label = itertools.count()
         self._holders = {}                                # sequences per label; a page without any is free
         self._free = list(range(max_seqs - 1, -1, -1))
+
+    def _check_weights(self):
+        rows, dt = (self.H + 2 * self.Hk) * self.hd, torch.bfloat16 if self.dtype == "bf16" else torch.float32
+        want = dict(qkv_w=((rows, self.d), dt), o_w=((self.d, self.H * self.hd), dt), qkv_b=((rows,), torch.float32),
+                    o_b=((self.d,), torch.float32), gamma_q=((self.hd,), torch.float32),
+                    gamma_k=((self.hd,), torch.float32))
+        for layer, w in enumerate(self.weights):
+            for name, (shape, dtype) in want.items():
+                t = w[name]
+                if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+                    raise ValueError(f"layer {layer}: {name}: contiguous CUDA tensor {list(shape)} of {dtype} expected")
 
     def _on_current_stream(self):
         """Orders the current stream after the object's earlier calls.  Every method that

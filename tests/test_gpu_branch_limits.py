@@ -187,6 +187,23 @@ def test_a_step_of_a_host_tensor_is_refused():
     r.step([root], 2)
 
 
+@pytest.mark.parametrize("name", ["qkv_w", "o_w", "qkv_b", "o_b", "gamma_q", "gamma_k"])
+def test_weights_of_other_shapes_or_types_are_refused(name):
+    from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
+
+    def build(weights, dtype="f32"):
+        return BranchedLayers(weights, H, HK, HD, n_pages=8, page_size=16, max_seqs=2, max_len=64, dtype=dtype)
+
+    good = random_layers(2, D, H, HK, HD, "f32", seed=1)
+    build(good)
+    t = good[1][name]
+    for wrong in (t[:-1], t.double(), t.cpu(), torch.cat([t, t]), t.repeat_interleave(2, dim=-1)[..., ::2]):
+        with pytest.raises(ValueError):
+            build([good[0], {**good[1], name: wrong}])
+    with pytest.raises(ValueError):
+        build(good, "bf16")                               # fp32 weights of a bf16 stack
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
