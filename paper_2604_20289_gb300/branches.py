@@ -37,7 +37,6 @@ class BranchedLayers:
         self.weights, self.dtype, self.eps = weights, dtype, float(eps)
         self.H, self.Hk, self.hd = n_heads, n_kv_heads, head_dim
         self.d = weights[0]["o_w"].shape[0]
-        self._check_weights()
         self.max_len = max_len
         self.cache = xb.KVCache.empty(dtype, len(weights), n_pages, page_size, n_kv_heads, head_dim, max_seqs,
                                       -(-max_len // page_size))
@@ -46,6 +45,7 @@ class BranchedLayers:
         xb.op_rope_table(self.pairs, self.n_pos, theta, self.rotation)
         self.zeros = torch.zeros(self.d, device="cuda")
         self.ones = torch.ones(self.d, device="cuda")
+        self._check_weights()
         self._last = torch.cuda.current_stream()          # stream of the last call
         self._streams = {self._last.cuda_stream}          # streams that have used the tensors kept here
         self.length = [0] * max_seqs
@@ -55,7 +55,7 @@ class BranchedLayers:
         self._free = list(range(max_seqs - 1, -1, -1))
 
     def _check_weights(self):
-        rows, dt = (self.H + 2 * self.Hk) * self.hd, torch.bfloat16 if self.dtype == "bf16" else torch.float32
+        rows, dt = (self.H + 2 * self.Hk) * self.hd, self.cache.torch_dtype
         want = dict(qkv_w=((rows, self.d), dt), o_w=((self.d, self.H * self.hd), dt), qkv_b=((rows,), torch.float32),
                     o_b=((self.d,), torch.float32), gamma_q=((self.hd,), torch.float32),
                     gamma_k=((self.hd,), torch.float32))

@@ -204,6 +204,15 @@ def test_weights_of_other_shapes_or_types_are_refused(name):
         build(good, "bf16")                               # fp32 weights of a bf16 stack
 
 
+@pytest.mark.parametrize("dtype,name", [(xb.XC_F32, "f32"), (xb.XC_BF16, "bf16")])
+def test_types_by_their_codes(dtype, name):
+    from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
+    m = BranchedLayers(random_layers(1, D, H, HK, 64, name), H, HK, 64, n_pages=8, page_size=16, max_seqs=2, max_len=64,
+                       dtype=dtype)
+    y = m.step([m.new()], torch.ones(1, 3, D, device=DEV))
+    assert y.dtype == tdt(name) and bool(torch.isfinite(y).all()) and xb.op_device_error() == 0
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
