@@ -420,7 +420,7 @@ class KVCache:
         self.k, self.v, self.ref, self.table, self.len = k, v, ref, table, length
         self.dtype, self.n_kv_heads, self.head_dim = dtype, n_kv_heads, head_dim
         self.page_size = k.shape[2]
-        self.torch_dtype, self._int32 = want, torch.int32
+        self.torch_dtype, self._int32, self._float32 = want, torch.int32, torch.float32
         self.desc = KVCacheDesc(dtype_code(dtype), k.shape[0], k.shape[1], k.shape[2], n_kv_heads, head_dim,
                                 table.shape[0], table.shape[1], k.data_ptr(), v.data_ptr(), ref.data_ptr(),
                                 table.data_ptr(), length.data_ptr())
@@ -507,8 +507,9 @@ def op_rope_table(axis_pairs, n_pos, theta, out, stream=None):
     """out: contiguous float32 CUDA tensor of 2 * sum(axis_pairs * n_pos) elements."""
     n = len(axis_pairs)
     if len(n_pos) != n or out.numel() != 2 * sum(a * b for a, b in zip(axis_pairs, n_pos)) or \
-            not out.is_contiguous() or not out.is_cuda or out.element_size() != 4:
-        raise ValueError("out: one (cos, sin) pair per position and pair of every axis")
+            not out.is_contiguous() or not out.is_cuda or out.element_size() != 4 or \
+            not out.is_floating_point():
+        raise ValueError("out: float32, one (cos, sin) pair per position and pair of every axis")
     check(LIB.xc_op_rope_table(n, (_I * n)(*axis_pairs), (_I * n)(*n_pos), float(theta), out.data_ptr(),
                                _stream(stream)))
 
@@ -531,8 +532,9 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
     if dq % hd or q_out.shape != q.shape or k.shape != (T, dk) or v.shape != (T, dk) or q.dtype is not dt or \
             k.dtype is not dt or v.dtype is not dt or q_out.dtype is not dt:
         raise ValueError("q, q_out [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] of the cache's dtype")
-    if gamma_q.numel() != hd or gamma_k.numel() != hd or table.numel() != entries or gamma_q.element_size() != 4 or \
-            gamma_k.element_size() != 4 or table.element_size() != 4 or not gamma_q.is_contiguous() or \
+    f32 = cache._float32
+    if gamma_q.numel() != hd or gamma_k.numel() != hd or table.numel() != entries or gamma_q.dtype is not f32 or \
+            gamma_k.dtype is not f32 or table.dtype is not f32 or not gamma_q.is_contiguous() or \
             not gamma_k.is_contiguous() or not table.is_contiguous():
         raise ValueError("float32 gamma_q, gamma_k [head_dim]; table: one (cos, sin) pair per position and pair of every axis")
     (sq, u0), (sk, u1), (sv, u2), (so, u3) = q.stride(), k.stride(), v.stride(), q_out.stride()

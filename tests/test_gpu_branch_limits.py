@@ -238,6 +238,21 @@ def test_shared_keys_of_a_bad_first_sequence_are_zeros(dtype, H, hk, hd, n_q, ba
     assert rel_l2(got[n_q:], want[n_q:]) <= (5e-3 if dtype == "bf16" else 5e-6)
 
 
+def test_integers_in_place_of_float_operands_are_refused():
+    """Four-byte integers have the size of a float, not its meaning."""
+    cache = make_cache("bf16", 2, 64, 16, [40, 50], 32, dead=0.0)
+    x, out = rand((2, 128), "bf16", 4), rand((2, 128), "bf16", 5)
+    gamma, table = torch.ones(64, device=DEV), torch.zeros(2 * 32 * 64, device=DEV)
+    args = [gamma, gamma, table]
+    for i in range(3):
+        a = [t.int() if j == i else t for j, t in enumerate(args)]
+        with pytest.raises(ValueError):
+            xb.op_qk_norm_rope(cache, 0, x, x, x, a[0], a[1], i32([0, 1]), [32], [64], a[2], i32([0, 1]), out)
+    with pytest.raises(ValueError):
+        xb.op_rope_table([32], [64], 1e4, table.int())
+    assert xb.op_device_error() == 0
+
+
 def test_captured_calls_have_workspaces_of_their_own():
     """A larger call on the capture's stream and replays on another stream leave a graph's results,
     the other calls' results and other memory as they are."""
