@@ -378,6 +378,47 @@ def test_steps_on_other_streams():
     assert main == torch.cuda.current_stream()
 
 
+@pytest.mark.parametrize("n,sources,pages", [(1, 1, 8400), (16, 1, 600), (16, 3, 530), (64, 4, 150), (1000, 7, 13),
+                                             (1024, 1, 12)])
+@pytest.mark.parametrize("part", [0, 5])
+def test_forks_of_long_rows_and_many_pairs(n, sources, pages, part):
+    """Rows longer than what the plan's threads keep in registers, several children per source."""
+    ps, max_seqs, n_pages = 16, n + sources, sources * (pages + 1) + n + 9
+    cache = xb.KVCache.empty("bf16", 1, n_pages, ps, 1, 16, max_seqs, pages + 1)
+    n_rows = n_pages * ps
+    cache.k.copy_(rand(tuple(cache.k.shape), "bf16", 1))
+    cache.v.copy_(rand(tuple(cache.v.shape), "bf16", 2))
+    first = [host(t[0]).reshape(n_rows, -1) for t in (cache.k, cache.v)]
+    m = PageModel(n_pages, ps, max_seqs, pages + 1, np.arange(n_rows).reshape(n_pages, ps))
+    src = list(range(sources))
+    n_new = pages * ps + part
+    slots = torch.empty(sources, n_new, dtype=torch.int32, device=DEV)
+    xb.op_kv_extend(cache, i32(src), n_new, slots)
+    assert slots.tolist() == m.extend(src, n_new)
+    rng = np.random.default_rng(7)
+    pairs = [(int(rng.integers(sources)), sources + int(d)) for d in rng.permutation(n)]
+    a, b = i32([p[0] for p in pairs]), i32([p[1] for p in pairs])
+    tail = int(cache.table[pairs[-1][0], pages - 1])
+    for wrong in (n_pages, -3):                           # a bad page id in the row's last part: nothing changes
+        cache.table[pairs[-1][0], pages - 1] = wrong
+        xb.op_kv_fork(cache, a, b)
+        assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
+        assert cache.ref.tolist() == m.ref and cache.len.tolist() == m.len
+    cache.table[pairs[-1][0], pages - 1] = tail
+    xb.op_kv_fork(cache, a, b)
+    assert m.fork(pairs) and xb.op_device_error() == 0
+    m.check(cache, lambda layer, x: first[x])
+    xb.op_kv_free(cache, b)
+    m.free([p[1] for p in pairs])
+    assert cache.ref.tolist() == m.ref and xb.op_device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_thousands_of_branches(dtype):
+    check_attention(dtype, 2, 1, 64, 16, [32 + (7 * b) % 30 for b in range(3000)], 1, 32, True)
+    check_attention(dtype, 2, 2, 64, 16, [(11 * b) % 37 for b in range(2500)], 2, 0, True)
+
+
 def test_a_whole_planning_step_in_one_graph():
     """fork, extend, norm and append, attention, free: captured once, replayed with other inputs and
     a history that grew in between."""
