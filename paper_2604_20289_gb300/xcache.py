@@ -426,7 +426,7 @@ class KVCache:
                                 table.data_ptr(), length.data_ptr())
         self.ptr = ctypes.addressof(self.desc)
         self._ws = {}                             # stream -> (tensor, pointer, bytes)
-        self._attn_bytes, self._axes = {}, {}
+        self._attn_bytes, self._axes = {}, {}     # workspace sizes by shape, axis arrays by value
         self._page_bytes = LIB.xc_op_kv_workspace_bytes(self.ptr)
 
     @classmethod
@@ -439,6 +439,13 @@ class KVCache:
                    torch.zeros(n_pages, dtype=torch.int32, device=device),
                    torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
                    torch.zeros(max_seqs, dtype=torch.int32, device=device))
+
+    def note(self, memo: dict, key, value):
+        """Keeps value under key in one of the handle's two dicts, which hold 4096 shapes at most."""
+        if len(memo) >= 4096:
+            memo.clear()
+        memo[key] = value
+        return value
 
     def workspace(self, nbytes: int, stream: int):
         """(tensor, pointer, bytes) of a device workspace for one call on this stream (cudaStream_t)."""
@@ -526,8 +533,8 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
     if axes is None:
         if len(n_pos) != len(axis_pairs):
             raise ValueError("one n_pos per axis")
-        axes = cache._axes[key] = (len(axis_pairs), (_I * len(axis_pairs))(*axis_pairs), (_I * len(n_pos))(*n_pos),
-                                   2 * sum(a * b for a, b in zip(axis_pairs, n_pos)))
+        axes = cache.note(cache._axes, key, (len(axis_pairs), (_I * len(axis_pairs))(*axis_pairs),
+                                             (_I * len(n_pos))(*n_pos), 2 * sum(a * b for a, b in zip(axis_pairs, n_pos))))
     n, c_pairs, c_pos, entries = axes
     if dq % hd or q_out.shape != q.shape or k.shape != (T, dk) or v.shape != (T, dk) or q.dtype is not dt or \
             k.dtype is not dt or v.dtype is not dt or q_out.dtype is not dt:
@@ -577,7 +584,8 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
         key = (B, n_q, dq, shared_len)
         need = cache._attn_bytes.get(key)
         if need is None:
-            need = cache._attn_bytes[key] = op_branch_attention_workspace_bytes(cache, B, n_q, dq // hd, shared_len)
+            need = cache.note(cache._attn_bytes, key,
+                              op_branch_attention_workspace_bytes(cache, B, n_q, dq // hd, shared_len))
         buf, ws, nbytes = cache.workspace(need, cuda)
     else:
         buf, ws, nbytes = _given(workspace)

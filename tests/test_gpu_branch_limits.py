@@ -335,6 +335,17 @@ def test_workspaces_of_the_caller():
     assert xb.op_device_error() == 0
 
 
+def test_a_handle_does_not_grow_with_the_shapes_it_has_seen():
+    cache = xb.KVCache.empty("bf16", 1, 8, 16, 1, 64, 2, 4)
+    q, none = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV), i32([])
+    table, gamma = torch.zeros(64 * 9000, device=DEV), torch.ones(64, device=DEV)
+    for n in range(1, 9000):
+        xb.op_qk_norm_rope(cache, 0, q, q, q, gamma, gamma, none, [32], [n], table[:64 * n], none, q)
+        xb.op_branch_attention(cache, 0, none, n, q, q)
+    assert len(cache._axes) <= 4096 and len(cache._attn_bytes) <= 4096
+    assert xb.op_device_error() == 0
+
+
 def test_steps_on_other_streams():
     """Built on one stream, called on others, each behind a delay, with no event of the caller's
     between the calls: the object orders them, and inputs and outputs are of the calling stream."""
