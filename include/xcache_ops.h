@@ -164,7 +164,8 @@ xc_status xc_op_gate_static(int dtype, int n_cams, int tokens_per_cam, int d, co
  * An empty cache has ref = 0, table = -1, len = 0.  A partly filled last page
  * belongs to one sequence (the calls below keep it so), so appending never
  * writes to a shared page.  dtype XC_F32 / XC_BF16; head_dim 16, 32, 64 or
- * 128; page_size a power of two from 16 to 1024; n_pages * page_size < 2^31.
+ * 128 (the attention reads XC_BF16 caches of 64 and 128); page_size a power of
+ * two from 16 to 1024; n_pages * page_size < 2^31.
  * Calls on one cache must be ordered (one stream, or events).
  *
  * What the host cannot see is checked on the device: a call that finds a bad
@@ -264,7 +265,16 @@ xc_status xc_op_qk_norm_rope(const xc_kv_cache *cache, int layer, int n_tokens, 
  * Cache rows that no sequence has reached (the rest of a last page) may hold
  * anything.  A key that the causal limit hides from a row but that is part of
  * the sequence must be finite, as must its value.  XC_BF16 needs head_dim 64
- * or 128.  At most 128 query heads per key head (XC_F32: 64). */
+ * or 128.  At most 128 query heads per key head (XC_F32: 64).  Every branch has
+ * n_q new tokens, and only one common part is read once: the children of two
+ * parents read each parent's pages once a branch.
+ * Scores, maxima, sums and partial results are fp32.  For XC_BF16 the weights
+ * p_j are rounded to bf16 for the product with v, and the output once: rel-L2
+ * 2.3e-3 against 64 bits on long sequences, where rounding the exact output
+ * alone gives 1.7e-3.  XC_F32 rounds nothing to fewer bits.
+ * A call is refused when the line of key tiles would not fit 32 bits with every
+ * table row full, since the lengths are the device's and may have grown when a
+ * captured call is replayed. */
 size_t xc_op_branch_attention_workspace_bytes(const xc_kv_cache *cache, int n_branches, int n_q, int n_heads,
                                               int shared_len);
 xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q,

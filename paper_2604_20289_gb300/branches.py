@@ -11,7 +11,9 @@ copying it, advances all candidates together -- the shared keys are read once
 for the whole batch -- and drops the ones it does not follow.  All arithmetic
 runs in the CUDA library; this module sequences calls and keeps, on the host,
 the lengths and which pages sequences have in common, so that a call the pool
-has no pages for is refused before anything changes.
+has no pages for is refused before anything changes.  Ids and positions are
+uploaded from host lists in every call, so these calls cannot be captured into
+a graph; the operators they make can.
 
 ``python -m paper_2604_20289_gb300.branches`` runs such a planning step on
 random weights.
@@ -30,7 +32,8 @@ class BranchedLayers:
     """weights: per layer a dict of CUDA tensors -- ``qkv_w`` [(H + 2 Hk) hd, d] and
     ``o_w`` [d, H hd] (K-major, the storage type), ``qkv_b``, ``o_b`` (float32),
     ``gamma_q``, ``gamma_k`` [hd] (float32).  A call runs on the stream that is
-    current when it is made, after the object's earlier calls on whatever stream."""
+    current when it is made, after the object's earlier calls on whatever stream.
+    ``cache`` is for reading: its sequences change through this object alone."""
 
     def __init__(self, weights, n_heads, n_kv_heads, head_dim, n_pages, page_size=64, max_seqs=64, max_len=4096,
                  dtype="bf16", theta=10000.0, eps=1e-6):

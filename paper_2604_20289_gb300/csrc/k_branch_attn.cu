@@ -343,8 +343,9 @@ struct BranchWarpWalk {
 // and one that clears the value rows past a unit's last key, whose weights are
 // zero but whose bytes may be anything.
 // Measured, with the merge: 2 x 4320 queries over 30240 keys, 12 heads x 128,
-// 913-929 us, 1.74 PFLOP/s, the tensor pipe 76 % busy (2620 cycles a key tile of
-// 256 rows); 32 single tokens over 38880 shared + 1..1500 own keys, 40 / 8 heads
+// 1008-1030 us back to back (1.6 PFLOP/s, at the power cap), 913-929 after a pause
+// with the tensor pipe 76 % busy (2620 cycles a key tile of 256 rows); the same of
+// 12 heads x 64, 728 us; 32 single tokens over 38880 shared + 1..1500 own keys, 40 / 8 heads
 // x 128, 63 us for 258 MB, of which 7 until the first tile and 7 the merge.  Where
 // units are short the latency of a piece bounds it: 200 single tokens over 256 +
 // 16..120 keys, 32 / 8 heads x 128, 62 us, 10 or 11 pieces of one key tile a CTA at
