@@ -20,7 +20,6 @@ random weights.
 """
 from __future__ import annotations
 
-import itertools
 import operator
 
 import torch
@@ -52,9 +51,10 @@ class BranchedLayers:
         self._last = torch.cuda.current_stream()          # stream of the last call
         self._streams = {self._last.cuda_stream}          # streams that have used the tensors kept here
         self.length = [0] * max_seqs
-        self._pages = [[] for _ in range(max_seqs)]       # a label per page; equal labels are the same page
-        self._label = itertools.count()
-        self._holders = {}                                # sequences per label; a page without any is free
+        # The pages of a sequence: runs that it has in common with its forks, [pages, sequences that hold the run],
+        # then pages of its own.
+        self._runs = [[] for _ in range(max_seqs)]
+        self._used = 0                                    # pages in use
         self._free = list(range(max_seqs - 1, -1, -1))
 
     def _check_weights(self):
@@ -90,8 +90,14 @@ class BranchedLayers:
             raise ValueError(f"{n} sequences asked for, {len(self._free)} free")
         return [self._free.pop() for _ in range(n)]
 
+    def _n_pages(self, length):
+        return -(-length // self.cache.page_size)
+
+    def _own_pages(self, s):
+        return self._n_pages(self.length[s]) - sum(pages for pages, _ in self._runs[s])
+
     def _room(self, pages):
-        free = self.cache.ref.numel() - len(self._holders)
+        free = self.cache.ref.numel() - self._used
         if pages > free:
             raise ValueError(f"{pages} pages asked for, {free} free")
 
@@ -113,7 +119,8 @@ class BranchedLayers:
     def fork(self, seq: int, n: int) -> list:
         """n sequences that continue ``seq``; full pages are shared, not copied."""
         seq, = self._in_use([seq])
-        self._room(n if self.length[seq] % self.cache.page_size else 0)
+        part = self.length[seq] % self.cache.page_size != 0
+        self._room(n if part else 0)
         ids = self._take(n)
         self._on_current_stream()
         try:
@@ -121,13 +128,14 @@ class BranchedLayers:
         except Exception:                                 # nothing was launched
             self._free += reversed(ids)
             raise
-        full = self.length[seq] // self.cache.page_size
+        full = self._own_pages(seq) - part                # pages of its own that it shares from now on
+        if ids and full > 0:
+            self._runs[seq].append([full, 1])
+        for run in self._runs[seq]:
+            run[1] += len(ids)
         for i in ids:
-            self.length[i] = self.length[seq]
-            self._pages[i] = self._pages[seq][:full]
-            for p in self._pages[i]:
-                self._holders[p] += 1
-            self._relabel(i)
+            self.length[i], self._runs[i] = self.length[seq], list(self._runs[seq])
+        self._used += len(ids) if part else 0
         return ids
 
     def free(self, seqs):
@@ -135,11 +143,11 @@ class BranchedLayers:
         self._on_current_stream()
         xb.op_kv_free(self.cache, self._ids(seqs))
         for s in seqs:
-            for p in self._pages[s]:
-                self._holders[p] -= 1
-                if self._holders[p] == 0:
-                    del self._holders[p]
-            self.length[s], self._pages[s] = 0, []
+            self._used -= self._own_pages(s)
+            for run in self._runs[s]:
+                run[1] -= 1
+                self._used -= run[0] if run[1] == 0 else 0
+            self.length[s], self._runs[s] = 0, []
             self._free.append(s)
 
     def compact(self) -> torch.Tensor:
@@ -149,22 +157,17 @@ class BranchedLayers:
         xb.op_kv_compact(self.cache, live)
         return live
 
-    def _relabel(self, s):
-        while len(self._pages[s]) * self.cache.page_size < self.length[s]:
-            self._pages[s].append(next(self._label))
-            self._holders[self._pages[s][-1]] = 1
-
     def shared_len(self, seqs) -> int:
         """Tokens whose pages all of these sequences have in common."""
         seqs = self._in_use(seqs, once=False)
-        rows = [self._pages[s] for s in seqs]
-        n = 0
-        for labels in zip(*rows):
-            if any(x != labels[0] for x in labels):
+        if len(set(seqs)) == 1:
+            return self.length[seqs[0]] // self.cache.page_size * self.cache.page_size
+        pages = 0
+        for runs in zip(*(self._runs[s] for s in seqs)):
+            if any(run is not runs[0] for run in runs):
                 break
-            n += 1
-        return min(n * self.cache.page_size, min(self.length[s] for s in seqs) // self.cache.page_size *
-                   self.cache.page_size)
+            pages += runs[0][0]
+        return pages * self.cache.page_size
 
     def step(self, seqs, x):
         """Appends x [len(seqs), n, d] to the sequences and returns the layers' output
@@ -177,7 +180,8 @@ class BranchedLayers:
             return x
         if any(self.length[s] + n > self.max_len for s in seqs):
             raise ValueError(f"sequences hold at most {self.max_len} tokens")
-        self._room(sum(-(-(self.length[s] + n) // self.cache.page_size) - len(self._pages[s]) for s in seqs))
+        new_pages = sum(self._n_pages(self.length[s] + n) - self._n_pages(self.length[s]) for s in seqs)
+        self._room(new_pages)
         self._on_current_stream()
         c, st, T = self.cache, self._last.cuda_stream, B * n
         dt = c.k.dtype
@@ -195,9 +199,9 @@ class BranchedLayers:
         o = torch.empty_like(q)
         c.workspace(xb.op_branch_attention_workspace_bytes(c, B, n, self.H, shared), st)
         xb.op_kv_extend(c, ids, n, slots, stream=st)
+        self._used += new_pages
         for s in seqs:
             self.length[s] += n
-            self._relabel(s)
         for layer, w in enumerate(self.weights):
             xb.op_ln_mod(self.dtype, x, self.zeros, self.zeros, h, eps=self.eps, stream=st)
             xb.op_linear(self.dtype, xb.XC_EPI_BIAS, h, w["qkv_w"], w["qkv_b"], qkv, stream=st)

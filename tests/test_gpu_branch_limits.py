@@ -95,6 +95,41 @@ def test_a_full_pool_is_refused_before_anything_changes():
     r.step([other], 80)                                   # the whole pool again
 
 
+def test_shared_parts_and_pages_in_use_follow_the_tables():
+    """Forks of forks, grown and freed in any order: what the host counts is what the device's tables hold."""
+    r = Rollout(n_pages=60, max_seqs=10)
+    m, rng = r.m, np.random.default_rng(6)
+    live = [m.new()]
+    for _ in range(80):
+        op = rng.integers(4)
+        some = [int(s) for s in rng.permutation(live)[:rng.integers(1, 4)]]
+        if op == 0 and len(live) < 9:
+            live += m.fork(some[0], int(rng.integers(0, 3)))
+        elif op == 1 and len(live) > 3:
+            m.free(some[:2])
+            live = [s for s in live if s not in some[:2]]
+        else:
+            n = int(rng.integers(1, 21))
+            if max(m.length[s] for s in some) + n <= m.max_len:
+                try:
+                    m.step(some, r.tokens(len(some), n))
+                except ValueError:
+                    m.free([live.pop()])
+        table, ref = m.cache.table.tolist(), m.cache.ref
+        pages = 60 - int((ref > 0).sum())                 # what is free: one page more is refused
+        if m.length[live[0]] % 16 == 0 and m.length[live[0]] + 16 * pages + 16 <= m.max_len:
+            with pytest.raises(ValueError):
+                m.step(live[:1], r.tokens(1, 16 * pages + 1))
+        for a in live:
+            for b in live:
+                n = min(m.length[a], m.length[b]) // 16
+                same = next((i for i in range(n) if table[a][i] != table[b][i]), n)
+                assert m.shared_len([a, b]) == 16 * same
+        assert m.cache.len.tolist() == m.length and xb.op_device_error() == 0
+    m.free(live)
+    assert int(m.cache.ref.sum()) == 0
+
+
 def test_ids_are_refused_before_anything_changes():
     r = Rollout(n_pages=20)
     m = r.m
