@@ -48,6 +48,7 @@ class BranchedLayers:
         self.zeros = torch.zeros(self.d, device="cuda")
         self.ones = torch.ones(self.d, device="cuda")
         self._check_weights()
+        self._check_sizes()
         self._last = torch.cuda.current_stream()          # stream of the last call
         self._streams = {self._last.cuda_stream}          # streams that have used the tensors kept here
         self.length = [0] * max_seqs
@@ -67,6 +68,17 @@ class BranchedLayers:
                 t = w[name]
                 if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
                     raise ValueError(f"layer {layer}: {name}: contiguous CUDA tensor {list(shape)} of {dtype} expected")
+
+    def _check_sizes(self):
+        """What the library refuses of these sizes, it refuses here: one row through the operators of a layer."""
+        c, w, dt = self.cache, self.weights[0], self.cache.torch_dtype
+        if xb.op_branch_attention_workspace_bytes(c, 1, 1, self.H) == 0:
+            raise xb.XCacheError(xb.XC_EINVAL, xb.last_error())
+        x, o = (torch.zeros(1, n, dtype=dt, device="cuda") for n in (self.d, self.H * self.hd))
+        y, qkv = torch.empty_like(x), torch.empty(1, w["qkv_w"].shape[0], dtype=dt, device="cuda")
+        xb.op_ln_mod(self.dtype, x, self.zeros, self.zeros, y, eps=self.eps)
+        xb.op_linear(self.dtype, xb.XC_EPI_BIAS, y, w["qkv_w"], w["qkv_b"], qkv)
+        xb.op_linear(self.dtype, xb.XC_EPI_RESID_GATE, o, w["o_w"], w["o_b"], y, gate=self.ones, resid=x)
 
     def _on_current_stream(self):
         """Orders the current stream after the object's earlier calls.  Every method that

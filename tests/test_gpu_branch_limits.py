@@ -248,6 +248,19 @@ def test_types_by_their_codes(dtype, name):
     assert y.dtype == tdt(name) and bool(torch.isfinite(y).all()) and xb.op_device_error() == 0
 
 
+@pytest.mark.parametrize("dtype,d,h,hk,hd,page", [
+    ("bf16", 128, 4, 4, 64, 16), ("bf16", 256, 3, 1, 64, 16),     # widths that the bf16 linear operator does not take
+    ("bf16", 256, 8, 8, 32, 16),                                  # a head size that the bf16 attention does not read
+    ("f32", 256, 3, 2, 32, 16), ("f32", 256, 130, 2, 16, 16),     # heads that are not shared evenly, or by too many
+    ("f32", 40, 4, 2, 32, 16), ("f32", 256, 4, 2, 48, 16), ("f32", 256, 4, 2, 32, 24)])
+def test_sizes_that_a_step_would_refuse_are_refused_at_once(dtype, d, h, hk, hd, page):
+    from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
+    with pytest.raises(xb.XCacheError):
+        BranchedLayers(random_layers(1, d, h, hk, hd, dtype), h, hk, hd, n_pages=8, page_size=page, max_seqs=2,
+                       max_len=64, dtype=dtype)
+    assert xb.op_device_error() == 0
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
