@@ -209,7 +209,10 @@ class BranchedLayers:
         qkv = torch.empty(T, dq + 2 * dk, dtype=dt, device="cuda")
         q = torch.empty(T, dq, dtype=dt, device="cuda")
         o = torch.empty_like(q)
-        c.workspace(xb.op_branch_attention_workspace_bytes(c, B, n, self.H, shared), st)
+        need = xb.op_branch_attention_workspace_bytes(c, B, n, self.H, shared)
+        if need == 0:                                     # more rows than the attention takes
+            raise xb.XCacheError(xb.XC_EINVAL, xb.last_error())
+        c.workspace(need, st)
         xb.op_kv_extend(c, ids, n, slots, stream=st)
         self._used += new_pages
         for s in seqs:

@@ -222,6 +222,19 @@ def test_a_step_of_a_host_tensor_is_refused():
     r.step([root], 2)
 
 
+def test_a_step_that_the_attention_refuses_changes_nothing(monkeypatch):
+    r = Rollout(n_pages=20)
+    root = r.new()
+    r.step([root], 20)
+    before = r.state()
+    monkeypatch.setattr(xb, "op_branch_attention_workspace_bytes", lambda *a: 0)   # as for too many query rows
+    with pytest.raises(xb.XCacheError):
+        r.m.step([root], r.tokens(1, 2))
+    monkeypatch.undo()
+    assert r.state() == before
+    r.step([root], 2)
+
+
 @pytest.mark.parametrize("name", ["qkv_w", "o_w", "qkv_b", "o_b", "gamma_q", "gamma_k"])
 def test_weights_of_other_shapes_or_types_are_refused(name):
     from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
