@@ -78,6 +78,9 @@ class BranchedLayers:
         y, qkv = torch.empty_like(x), torch.empty(1, w["qkv_w"].shape[0], dtype=dt, device="cuda")
         xb.op_ln_mod(self.dtype, x, self.zeros, self.zeros, y, eps=self.eps)
         xb.op_linear(self.dtype, xb.XC_EPI_BIAS, y, w["qkv_w"], w["qkv_b"], qkv)
+        dq, dk, none = o.shape[1], self.Hk * self.hd, self._ids([-1])      # slot -1: no keys are kept
+        xb.op_qk_norm_rope(c, 0, qkv[:, :dq], qkv[:, dq:dq + dk], qkv[:, dq + dk:], w["gamma_q"], w["gamma_k"],
+                           self._ids([0]), self.pairs, self.n_pos, self.rotation, none, o, eps=self.eps)
         xb.op_linear(self.dtype, xb.XC_EPI_RESID_GATE, o, w["o_w"], w["o_b"], y, gate=self.ones, resid=x)
 
     def _on_current_stream(self):

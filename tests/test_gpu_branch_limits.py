@@ -274,6 +274,16 @@ def test_sizes_that_a_step_would_refuse_are_refused_at_once(dtype, d, h, hk, hd,
     assert xb.op_device_error() == 0
 
 
+@pytest.mark.parametrize("eps", [-1e-6, float("nan"), float("inf")])
+def test_an_eps_that_the_norm_refuses_is_refused_at_once(eps):
+    from paper_2604_20289_gb300.branches import BranchedLayers, random_layers
+    weights = random_layers(1, D, H, HK, HD, "f32")
+    with pytest.raises(xb.XCacheError):
+        BranchedLayers(weights, H, HK, HD, n_pages=8, page_size=16, max_seqs=2, max_len=64, dtype="f32", eps=eps)
+    m = BranchedLayers(weights, H, HK, HD, n_pages=8, page_size=16, max_seqs=2, max_len=64, dtype="f32", eps=0.0)
+    assert xb.op_device_error() == 0 and int(m.cache.ref.sum()) == 0
+
+
 @pytest.mark.parametrize("dtype,H,hk,hd,n_q", [("bf16", 8, 1, 64, 1), ("bf16", 8, 1, 128, 1), ("bf16", 4, 4, 64, 9),
                                                ("f32", 8, 1, 32, 1)])
 @pytest.mark.parametrize("bad", [-1, 33, 1 << 30])
