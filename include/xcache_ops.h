@@ -38,6 +38,32 @@ xc_status xc_op_linear(int dtype, int epilogue, int M, int N, int K, const void 
                        const void *resid, const void *xin, void *out, void *rhat,
                        void *stream);
 
+/* 8-bit integers with a scale for each row, for xc_op_linear_i8: of row m of x
+ * [M][K], a = max_k |x|, scale[m] = a / 127 (float32 division) and q[m][k] =
+ * 127 x / a rounded to the nearest whole number, halves to even (decided as the
+ * exact quotient would be); a = 0 gives zeros.  A row that holds an infinity
+ * or NaN gets scale NaN and zeros, so that its products are NaN.  The rows of
+ * a K-major weight are its channels: the same call quantises weights.
+ * x is XC_F32 or XC_BF16, rows contiguous, x and q 16-byte aligned, K a
+ * multiple of 16 up to 131072, 0 <= M < 2^24. */
+xc_status xc_op_quantize_rows(int dtype, int M, int K, const void *x, signed char *q, float *scale, void *stream);
+
+/* out = epilogue(s_a[m] w_scale[n] sum_k qa[m][k] Wt[n][k] + bias[n]): a
+ * projection in 8-bit integers.  The activations A [M][K] of `dtype` are
+ * quantised by the call as by xc_op_quantize_rows; with a_scale [M] not NULL, A
+ * is 8-bit already (Wt, A: [-128, 127]) and dtype is that of resid and out.  The sums are those of
+ * the integers while they stay below 2^24 in magnitude, rounded to fp32 above.
+ * out, resid [M][N] contiguous; epilogue XC_EPI_BIAS, XC_EPI_GELU or
+ * XC_EPI_RESID_GATE as in xc_op_linear; out may be resid.  Any M from 0 below 2^24 and any N from 1;
+ * K a multiple of 16 up to 131072.
+ *   workspace  device, 256-byte aligned, at least
+ *              xc_op_linear_i8_workspace_bytes(); contents on entry are
+ *              ignored; not shared by overlapping calls */
+size_t xc_op_linear_i8_workspace_bytes(int M, int N, int K);
+xc_status xc_op_linear_i8(int dtype, int epilogue, int M, int N, int K, const void *A, const float *a_scale,
+                          const signed char *Wt, const float *w_scale, const float *bias, const float *gate,
+                          const void *resid, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* QKV projection with RoPE (Section 2.1 block, reading of RoPE over
  * (camera, absolute frame, h, w)).  A [M][d] with M = n_cams*frames*gh*gw,
  * Wt [3d][d], bias [3d]; writes q, k, v [M][d] (heads interleaved by column:

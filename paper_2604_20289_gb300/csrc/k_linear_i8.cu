@@ -1,0 +1,611 @@
+// Matrix product in 8-bit integers with a scale for each token and each channel.
+//
+//   y[m][n] = epilogue(s_a[m] s_w[n] sum_k qa[m][k] qw[n][k] + b[n]),
+//   s_a[m] = max_k |x[m][k]| / 127,   qa[m][k] = round(127 x[m][k] / max_k |x[m][k]|)
+//
+// The tensor core of this part has no fast 8-bit integer kind.  Whole numbers
+// up to 127 are exact in fp16, their products and, below 2^24, their sums in
+// fp32, so the product runs at the fp16 rate with the integer's result; the
+// weights stay 8 bits wide in memory, which is what a step of few tokens
+// waits for.  The tokens are quantised by a kernel of their own (as fp16 whole
+// numbers, ready for TMA); the weights are widened on their way into tensor
+// memory, where they are the MMA's A operand: 128 channels are its rows, up to
+// 256 tokens its columns.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "xc_branch.cuh"
+#include "xc_kernels.cuh"
+#include "xc_ptx.cuh"
+
+namespace xc {
+
+// ------------------------------------------------------------- quantisation
+// Eight elements of a row.
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const bf16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
+    // largest magnitude of the eight and m, as bits (NaN above infinity above the rest)
+    __device__ __forceinline__ unsigned top(unsigned m) const {
+        unsigned x = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+        x = max(x << 16, x & 0xffff0000u);
+        return max(m, x);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+};
+template <> struct Vec8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = reinterpret_cast<const float4 *>(p)[0];
+        b = reinterpret_cast<const float4 *>(p)[1];
+    }
+    __device__ __forceinline__ unsigned top(unsigned m) const {
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+};
+
+constexpr float ROUND_MAGIC = 12582912.0f;   // 1.5 * 2^23: adding it rounds to whole numbers, held in the low bits
+
+// 127 x / a rounded to the nearest whole number, halves to even, decided as
+// the exact quotient would be.  r = 127 / a is off by 2^-24 and the product by
+// as much, 2e-5 in all: only a quotient that near to a half is divided.  (bf16:
+// 127 x is exact in fp32, and a quotient of a 15-bit by an 8-bit number that is
+// not a half is 2^-17 or more from one, which the division keeps apart.  fp32: the same of
+// 31 and 24 bits in double.)
+template <typename T> __device__ __forceinline__ float quant(float x, float r, float a) {
+    const float t = x * r;
+    float q = (t + ROUND_MAGIC) - ROUND_MAGIC;
+    if (fabsf(t - q) > 0.4999f) {
+        if constexpr (sizeof(T) == 2) q = rintf(__fdiv_rn(127.0f * x, a));
+        else q = (float)rint(127.0 * (double)x / (double)a);
+    }
+    return q;
+}
+
+// TPR threads a row; each keeps its first four vectors of eight elements in
+// registers and reads the others again (rows of more than 32 TPR elements).
+// HBM bound.  A row without a finite largest magnitude gets scale NaN and zeros.
+template <typename T, typename Q, int TPR>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
+    quantize_rows_kernel(const T *__restrict__ x, Q *__restrict__ q, float *__restrict__ scale, const int M, const int K) {
+    pdl_wait();
+    pdl_release();
+    constexpr int CTA = TPR < 128 ? 128 : TPR, KEEP = 4;
+    __shared__ unsigned sh[CTA / 32];
+    const int row = blockIdx.x * (CTA / TPR) + threadIdx.x / TPR, t = threadIdx.x % TPR;
+    if (TPR == 32 && row >= M) return;
+    const T *src = x + (size_t)row * K;
+    const int nv = K / 8;
+    Vec8<T> keep[KEEP];
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (t + i * TPR < nv) keep[i].load(src + 8 * (t + i * TPR));
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (t + i * TPR < nv) top = keep[i].top(top);
+    for (int v = t + KEEP * TPR; v < nv; v += TPR) {
+        Vec8<T> z;
+        z.load(src + 8 * v);
+        top = z.top(top);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (TPR > 32) {
+        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = top;
+        __syncthreads();
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < CTA / 32; ++w) top = max(top, sh[w]);
+    }
+    const bool finite = top < 0x7f800000u;
+    const float a = __uint_as_float(top);
+    if (t == 0) scale[row] = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
+    // far from 1, both sides of the quotient times a power of two, so that nothing over- or underflows
+    const float f = a > 0x1p100f ? 0x1p-100f : (a < 0x1p-60f ? 0x1p80f : 1.0f), as = a * f;
+    const float r = finite && a > 0.0f ? __fdiv_rn(127.0f, as) : 0.0f;
+    Q *dst = q + (size_t)row * K;
+    auto put = [&](const Vec8<T> &z, int v) {
+        float e[8];
+        z.get(e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = finite ? quant<T>(e[i] * f, r, as) : 0.0f;
+        if constexpr (sizeof(Q) == 1) {
+            unsigned w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                unsigned b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(e[4 * h + i] + ROUND_MAGIC);
+                w[h] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            }
+            *reinterpret_cast<uint2 *>(dst + 8 * v) = make_uint2(w[0], w[1]);
+        } else {
+            __half2 h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(e[2 * i], e[2 * i + 1]);
+            *reinterpret_cast<uint4 *>(dst + 8 * v) = *reinterpret_cast<uint4 *>(h);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (t + i * TPR < nv) put(keep[i], t + i * TPR);
+    for (int v = t + KEEP * TPR; v < nv; v += TPR) {
+        Vec8<T> z;
+        z.load(src + 8 * v);
+        put(z, v);
+    }
+}
+
+template <typename T, typename Q>
+static cudaError_t quantize_launch(const T *x, Q *q, float *scale, int M, int K, cudaStream_t st) {
+    const int nv = K / 8;
+    if (nv <= 32 * 4) return launch_pdl(quantize_rows_kernel<T, Q, 32>, dim3((M + 3) / 4), dim3(128), 0, st, x, q, scale, M, K);
+    if (nv <= 128 * 4) return launch_pdl(quantize_rows_kernel<T, Q, 128>, dim3(M), dim3(128), 0, st, x, q, scale, M, K);
+    if (nv <= 256 * 4) return launch_pdl(quantize_rows_kernel<T, Q, 256>, dim3(M), dim3(256), 0, st, x, q, scale, M, K);
+    return launch_pdl(quantize_rows_kernel<T, Q, 512>, dim3(M), dim3(512), 0, st, x, q, scale, M, K);
+}
+cudaError_t quantize_rows(int dtype, int M, int K, const void *x, signed char *q, float *scale, cudaStream_t st) {
+    return dtype == XC_BF16 ? quantize_launch(reinterpret_cast<const bf16 *>(x), q, scale, M, K, st)
+                            : quantize_launch(reinterpret_cast<const float *>(x), q, scale, M, K, st);
+}
+
+// Two whole numbers in [-128, 127] out of four bytes, as fp16: the byte plus 128
+// in the low bits of 1024 is 1152 more than the number.
+__device__ __forceinline__ void widen4(unsigned w, unsigned &lo, unsigned &hi) {
+    const __half2 off = __half2half2(__ushort_as_half(0x6480));
+    const unsigned u = w ^ 0x80808080u;
+    unsigned a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
+    lo = *reinterpret_cast<const unsigned *>(&x);
+    hi = *reinterpret_cast<const unsigned *>(&y);
+}
+
+// Tokens that the caller quantised: 8-bit whole numbers to fp16, scales to where the product reads them.
+__global__ void __launch_bounds__(256) widen_kernel(const uint4 *q, uint4 *out, const long n, const float *scale, float *scale_out,
+                                                     const int M) {
+    pdl_wait();
+    pdl_release();
+    const long stride = (long)gridDim.x * 256, i0 = (long)blockIdx.x * 256 + threadIdx.x;
+    for (long i = i0; i < n; i += stride) {
+        const uint4 v = q[i];
+        uint4 a, b;
+        widen4(v.x, a.x, a.y);
+        widen4(v.y, a.z, a.w);
+        widen4(v.z, b.x, b.y);
+        widen4(v.w, b.z, b.w);
+        out[2 * i] = a;
+        out[2 * i + 1] = b;
+    }
+    for (long i = i0; i < M; i += stride) scale_out[i] = scale[i];
+}
+
+// ------------------------------------------------------------------ product
+constexpr int I8_BM = 128, I8_BK = 128;        // channels and depth of a weight tile
+constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_W = 12, I8_MAX_B = 24, I8_A = 8;
+constexpr int I8_THREADS = 640;
+constexpr int I8_A_COL = 256;                  // widened weights: 8 slots of depth 64, 32 columns each, behind the sums
+
+struct I8Sched {
+    int M, N, NT;              // tokens, channels, tokens of a tile (a multiple of 16)
+    int m_tiles, n_tiles, KT;  // tiles of tokens and channels, weight tiles along the depth
+    int n_full, G;             // tiles that CTAs run whole, in rounds; the rest is cut
+    int wst, bst;              // ring slots: weights of depth 128, tokens of depth 64
+    int acc2;                  // two sets of sums (NT <= 128)
+    int epi;
+    const float *a_scale, *w_scale, *bias, *gate;
+    const void *resid;
+    void *out;
+    float *part;               // [2 G][NT][128] sums of cut tiles
+
+    __host__ __device__ __forceinline__ unsigned line() const { return (unsigned)(m_tiles * n_tiles - n_full) * KT; }
+};
+
+// Tiles in super-rows of 16 channel blocks, channels fastest: the tiles that run
+// at one time share their weights and tokens in L2.
+__host__ __device__ __forceinline__ void i8_tile(const I8Sched &s, int tile, int &mb, int &nb) {
+    const int per = 16 * s.m_tiles, grp = tile / per, first = 16 * grp, loc = tile - grp * per;
+    const int gn = s.n_tiles - first < 16 ? s.n_tiles - first : 16;
+    nb = first + loc % gn;
+    mb = loc / gn;
+}
+// The cut tiles' depth as one line over the CTAs.
+struct I8Line {
+    unsigned q, r;
+    __host__ __device__ __forceinline__ I8Line(unsigned T, unsigned G) : q(T / G), r(T - q * G) {}
+    __host__ __device__ __forceinline__ unsigned begin(unsigned c) const { return q * c + (c < r ? c : r); }
+    __host__ __device__ __forceinline__ unsigned owner(unsigned x) const {
+        const unsigned longer = r * (q + 1);
+        return x < longer ? x / (q + 1) : r + (x - longer) / q;
+    }
+};
+// The pieces of a CTA, as each of its roles walks them: whole tiles c, c + G, ...,
+// then its share of the line, which touches two tiles at most.
+struct I8Walk {
+    int tile, k0, k1, slot;    // slot: of the sums of a cut piece, -1: a whole tile
+    int next_full;
+    unsigned x, end;
+    int first;
+    __device__ __forceinline__ I8Walk(const I8Sched &s, int c) : tile(0), k0(0), k1(0), slot(-1), next_full(c), first(1) {
+        const I8Line l(s.line(), s.G);
+        x = l.begin(c);
+        end = l.begin(c + 1);
+    }
+    __device__ __forceinline__ bool next(const I8Sched &s) {
+        if (next_full < s.n_full) {
+            tile = next_full;
+            next_full += s.G;
+            k0 = 0;
+            k1 = s.KT;
+            return true;
+        }
+        if (x >= end) return false;
+        const int t = x / s.KT;
+        tile = s.n_full + t;
+        k0 = x - t * s.KT;
+        k1 = min(s.KT, k0 + (int)(end - x));
+        x += k1 - k0;
+        slot = k1 - k0 == s.KT ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
+        first = 0;
+        return true;
+    }
+};
+
+template <typename T> __device__ __forceinline__ float i8_gelu(float y) {
+    // y (1 + tanh u) / 2 = y / (1 + exp(-2 u)): no cancellation where tanh is near -1
+    const float u2 = -1.5957691216057308f * (y + 0.044715f * y * y * y);
+    if constexpr (sizeof(T) == 2) return __fdividef(y, 1.0f + __expf(u2));
+    else return y / (1.0f + expf(u2));
+}
+// One output of channel n (its scale, bias, gate in registers).
+template <typename T>
+__device__ __forceinline__ float i8_epilogue(int epi, float acc, float sa, float sw, float b, float g, float resid) {
+    const float y = fmaf(acc * sa, sw, b);
+    if (epi == EPI_GELU) return i8_gelu<T>(y);
+    if (epi == EPI_RESID_GATE) return fmaf(g, y, resid);
+    return y;
+}
+
+// Warps: 0 loads weights, 1 issues the products, 2 loads tokens, 4-11 widen the
+// weights (thread = channel = TMEM lane, a half of each tile's depth to either four
+// warps), 12-19 write the outputs (two per TMEM quadrant, 16 tokens in turn).
+template <typename T>
+__global__ void __launch_bounds__(I8_THREADS, 1)
+    linear_i8_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
+                     const __grid_constant__ I8Sched s, int *err) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * I8_MAX_W + 2 * I8_MAX_B + 2 * I8_A + 5];
+    __shared__ uint32_t tmem_slot;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const int b_bytes = s.NT * 128;
+    uint8_t *sW = smem, *sB = smem + s.wst * I8_W_BYTES;
+    uint64_t *w_full = bars, *w_empty = w_full + I8_MAX_W, *b_full = w_empty + I8_MAX_W, *b_empty = b_full + I8_MAX_B;
+    uint64_t *a_full = b_empty + I8_MAX_B, *a_empty = a_full + I8_A, *acc_full = a_empty + I8_A, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < s.wst; ++i) {
+            mbar_init(&w_full[i], 1);
+            mbar_init(&w_empty[i], 256);
+        }
+        for (int i = 0; i < s.bst; ++i) {
+            mbar_init(&b_full[i], 1);
+            mbar_init(&b_empty[i], 1);
+        }
+        for (int i = 0; i < I8_A; ++i) {
+            mbar_init(&a_full[i], 128);
+            mbar_init(&a_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&acc_full[i], 1);
+            mbar_init(&acc_empty[i], 256);
+        }
+        mbar_init(drained, 1);
+        mbar_fence_init();
+    }
+    if (warp == 1) tmem_alloc(&tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    I8Walk w(s, blockIdx.x);
+
+    if (warp == 0) {
+        // The kernel before this one in the stream (the quantisation) began after
+        // everything before it had ended, so the weights need no wait.
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            while (ok && w.next(s)) {
+                int mb, nb;
+                i8_tile(s, w.tile, mb, nb);
+                for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
+                    const int i = it % s.wst;
+                    if (!(ok = mbar_wait(&w_empty[i], ((it / s.wst) & 1) ^ 1, err, ERR_WAIT_PRODUCER))) break;
+                    mbar_expect_tx(&w_full[i], I8_W_BYTES);
+                    tma_load_2d(sW + i * I8_W_BYTES, &tmW, &w_full[i], kt * I8_BK, nb * I8_BM);
+                }
+            }
+            for (int j = max(it - s.wst, 0); j < it; ++j)         // every copy has landed before the CTA exits
+                mbar_wait(&w_full[j % s.wst], (j / s.wst) & 1, err, ERR_WAIT_PRODUCER);
+        }
+    } else if (warp == 2) {
+        if (lane == 0) {
+            pdl_wait();
+            int it = 0;
+            bool ok = true;
+            while (ok && w.next(s)) {
+                int mb, nb;
+                i8_tile(s, w.tile, mb, nb);
+                for (int kt = 2 * w.k0; kt < 2 * w.k1; ++kt, ++it) {
+                    const int i = it % s.bst;
+                    if (!(ok = mbar_wait(&b_empty[i], ((it / s.bst) & 1) ^ 1, err, ERR_WAIT_PRODUCER))) break;
+                    mbar_expect_tx(&b_full[i], b_bytes);
+                    tma_load_2d(sB + i * b_bytes, &tmA, &b_full[i], kt * 64, mb * s.NT);
+                }
+            }
+            for (int j = max(it - s.bst, 0); j < it; ++j)
+                mbar_wait(&b_full[j % s.bst], (j / s.bst) & 1, err, ERR_WAIT_PRODUCER);
+        }
+    } else if (warp == 1) {
+        // D f32, A and B f16, N = NT, M = 128
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(s.NT >> 3) << 17) | ((uint32_t)(I8_BM >> 4) << 24);
+        const uint64_t d0 = sdesc_sw128(smem_u32(sB), 16, 1024);
+        auto wait = [&](uint64_t *b, uint32_t parity) {
+            return __all_sync(0xffffffffu, mbar_wait(b, parity & 1, err, ERR_WAIT_MMA)) != 0;
+        };
+        int it = 0, local = 0, bi = 0, b_ph = 0;
+        bool ok = true;
+        while (ok && w.next(s)) {
+            const int buf = s.acc2 ? local & 1 : 0, use = s.acc2 ? local >> 1 : local;
+            ++local;
+            if (!(ok = wait(&acc_empty[buf], use ^ 1))) break;
+            tc_fence_after();
+            const uint32_t acc = tmem + buf * 128;
+            for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    const int a = (2 * it + h) % I8_A;
+                    if (!(ok = wait(&a_full[a], (2 * it + h) / I8_A) && wait(&b_full[bi], b_ph))) break;
+                    tc_fence_after();
+                    const uint64_t db = d0 + (uint64_t)((bi * b_bytes) >> 4);
+                    const uint32_t ta = tmem + I8_A_COL + 32 * a;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma_tmem_a_warp(acc, ta + 8 * k, db + 2 * k, idesc, (kt > w.k0 || h > 0 || k > 0) ? 1u : 0u);
+                    tc_commit_warp(&b_empty[bi]);
+                    tc_commit_warp(&a_empty[a]);
+                    if (++bi == s.bst) {
+                        bi = 0;
+                        b_ph ^= 1;
+                    }
+                }
+                if (!ok) break;
+            }
+            if (ok) tc_commit_warp(&acc_full[buf]);
+        }
+        if (!ok) {                                     // a wait ran out: no product is under way when the CTA ends
+            tc_commit_warp(drained);
+            wait(drained, 0);
+        }
+    } else if (warp >= 4 && warp < 12) {
+        const int g = (warp - 4) >> 2, q = warp & 3, r = 32 * q + lane;
+        const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + I8_A_COL;
+        int it = 0;
+        bool ok = true;
+        while (ok && w.next(s)) {
+            for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
+                const int i = it % s.wst, a = (2 * it + g) % I8_A;
+                ok = mbar_wait(&w_full[i], (it / s.wst) & 1, err, ERR_WAIT_TMA);
+                ok = ok && mbar_wait(&a_empty[a], (((2 * it + g) / I8_A) & 1) ^ 1, err, ERR_WAIT_MMA);
+                if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+                tc_fence_after();
+                const uint8_t *src = sW + i * I8_W_BYTES + r * 128;
+                uint32_t x[32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + (((4 * g + c) ^ (r & 7)) << 4));
+                    widen4(v.x, x[8 * c], x[8 * c + 1]);
+                    widen4(v.y, x[8 * c + 2], x[8 * c + 3]);
+                    widen4(v.z, x[8 * c + 4], x[8 * c + 5]);
+                    widen4(v.w, x[8 * c + 6], x[8 * c + 7]);
+                }
+                mbar_arrive(&w_empty[i]);
+                tmem_st32_sync(t0 + 32 * a, x);
+                tc_fence_before();
+                mbar_arrive(&a_full[a]);
+            }
+        }
+    } else if (warp >= 12) {
+        pdl_wait();                                    // the tokens' scales
+        const int q = warp & 3, half = (warp - 12) >> 2;
+        const uint32_t tq = tmem + ((uint32_t)(32 * q) << 16);
+        const T *resid = reinterpret_cast<const T *>(s.resid);
+        T *out = reinterpret_cast<T *>(s.out);
+        int local = 0;
+        bool ok = true;
+        while (ok && w.next(s)) {
+            const int buf = s.acc2 ? local & 1 : 0, use = s.acc2 ? local >> 1 : local;
+            ++local;
+            int mb, nb;
+            i8_tile(s, w.tile, mb, nb);
+            const int m0 = mb * s.NT, ch = 32 * q + lane, n = nb * I8_BM + ch, nc = min(n, s.N - 1);
+            const int cols = min(s.NT, s.M - m0), chunks = (cols + 15) / 16;
+            const float sw = s.w_scale[nc], b = s.bias[nc], gt = s.epi == EPI_RESID_GATE ? s.gate[nc] : 0.0f;
+            ok = mbar_wait(&acc_full[buf], use & 1, err, ERR_WAIT_EPI);
+            if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+            tc_fence_after();
+            for (int c = half; c < chunks; c += 2) {
+                const int mc = m0 + 16 * c, left = cols - 16 * c;
+                float res[16];
+                if (s.epi == EPI_RESID_GATE && w.slot < 0) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) res[i] = i < left ? to_f(resid[(size_t)(mc + i) * s.N + nc]) : 0.0f;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) res[i] = 0.0f;
+                }
+                float v[16];
+                tmem_ld16_sync(tq + buf * 128 + 16 * c, v);
+                if (c + 2 >= chunks) {
+                    tc_fence_before();
+                    mbar_arrive(&acc_empty[buf]);
+                }
+                if (w.slot >= 0) {
+                    float *dst = s.part + ((size_t)w.slot * s.NT + 16 * c) * I8_BM + ch;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i < left) dst[i * I8_BM] = v[i];
+                } else if (n < s.N) {
+                    float sa[16];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(sa + 4 * i) = *reinterpret_cast<const float4 *>(s.a_scale + mc + 4 * i);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i < left)
+                            out[(size_t)(mc + i) * s.N + n] = from_f<T>(i8_epilogue<T>(s.epi, v[i], sa[i], sw, b, gt, res[i]));
+                }
+            }
+            if (half >= chunks) mbar_arrive(&acc_empty[buf]);
+        }
+    }
+    pdl_release();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Adds the pieces of a cut tile in CTA order: thread = channel, 8 tokens a CTA.
+template <typename T>
+__global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_constant__ I8Sched s) {
+    pdl_wait();
+    pdl_release();
+    constexpr int TOK = 8;
+    const I8Line l(s.line(), s.G);
+    const unsigned x0 = blockIdx.x * (unsigned)s.KT;
+    const int c0 = l.owner(x0), c1 = l.owner(x0 + s.KT - 1);
+    if (c0 == c1) return;                              // run whole
+    int mb, nb;
+    i8_tile(s, s.n_full + blockIdx.x, mb, nb);
+    const int t0 = blockIdx.y * TOK, m0 = mb * s.NT + t0, ch = threadIdx.x, n = nb * I8_BM + ch;
+    const int left = min(s.NT - t0, s.M - m0);
+    if (left <= 0 || n >= s.N) return;
+    float sum[TOK];
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) sum[i] = 0.0f;
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+        const float *src = s.part + ((size_t)(2 * c + (l.begin(c) >= x0 ? 0 : 1)) * s.NT + t0) * I8_BM + ch;
+#pragma unroll
+        for (int i = 0; i < TOK; ++i)
+            if (i < left) sum[i] += src[i * I8_BM];
+    }
+    const float sw = s.w_scale[n], b = s.bias[n], gt = s.epi == EPI_RESID_GATE ? s.gate[n] : 0.0f;
+    const T *resid = reinterpret_cast<const T *>(s.resid);
+    T *out = reinterpret_cast<T *>(s.out);
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+        if (i >= left) break;
+        const size_t at = (size_t)(m0 + i) * s.N + n;
+        const float r = s.epi == EPI_RESID_GATE ? to_f(resid[at]) : 0.0f;
+        out[at] = from_f<T>(i8_epilogue<T>(s.epi, sum[i], s.a_scale[m0 + i], sw, b, gt, r));
+    }
+}
+
+// ------------------------------------------------------------------- host
+struct I8Plan {
+    I8Sched s;
+    size_t off_scale, off_part, bytes;
+    int smem, cut;             // cut: whether a tile may be cut
+};
+static I8Plan i8_plan(int M, int N, int K) {
+    I8Plan p;
+    I8Sched &s = p.s;
+    s = I8Sched{};
+    s.M = M;
+    s.N = N;
+    const int mt = (M + 255) / 256;
+    s.NT = ((M + mt - 1) / mt + 15) / 16 * 16;         // the tiles of tokens as even as they come
+    s.m_tiles = (M + s.NT - 1) / s.NT;
+    s.n_tiles = (N + I8_BM - 1) / I8_BM;
+    s.KT = (K + I8_BK - 1) / I8_BK;
+    const int tiles = s.m_tiles * s.n_tiles, sms = device_sms();
+    s.G = (int)std::min<long long>(sms, (long long)tiles * s.KT);
+    s.n_full = tiles / s.G * s.G;
+    p.cut = s.n_full < tiles;
+    s.acc2 = s.NT <= 128;
+    const int budget = 222 * 1024;
+    s.wst = std::min(I8_MAX_W, std::max(3, budget / (I8_W_BYTES + 256 * s.NT)));
+    s.bst = std::min(std::min(I8_MAX_B, 2 * s.wst), (budget - s.wst * I8_W_BYTES) / (128 * s.NT));
+    p.smem = s.wst * I8_W_BYTES + s.bst * 128 * s.NT + 1024;
+    p.off_scale = ((size_t)M * K * 2 + 255) / 256 * 256;
+    p.off_part = p.off_scale + ((size_t)s.m_tiles * s.NT + 16) * sizeof(float);
+    p.off_part = (p.off_part + 255) / 256 * 256;
+    p.bytes = p.off_part + (p.cut ? (size_t)2 * s.G * s.NT * I8_BM * sizeof(float) : 0);
+    return p;
+}
+size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_plan(M, N, K).bytes; }
+
+template <typename T>
+static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUtensorMap &ta, int *err, cudaStream_t st) {
+    static bool done = false;
+    if (!done) {
+        const cudaError_t e = cudaFuncSetAttribute(linear_i8_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 223 * 1024 + 1024);
+        if (e != cudaSuccess) return e;
+        done = true;
+    }
+    cudaError_t e = launch_pdl(linear_i8_kernel<T>, dim3(p.s.G), dim3(I8_THREADS), p.smem, st, tw, ta, p.s, err);
+    if (e != cudaSuccess || !p.cut) return e;
+    return launch_pdl(linear_i8_merge_kernel<T>, dim3(p.s.m_tiles * p.s.n_tiles - p.s.n_full, (p.s.NT + 7) / 8), dim3(I8_BM), 0, st, p.s);
+}
+
+cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st) {
+    I8Plan p = i8_plan(a.M, a.N, a.K);
+    I8Sched &s = p.s;
+    char *w = reinterpret_cast<char *>(ws);
+    __half *tokens = reinterpret_cast<__half *>(w);
+    float *scale = reinterpret_cast<float *>(w + p.off_scale);
+    s.epi = a.epi;
+    s.a_scale = scale;
+    s.w_scale = a.w_scale;
+    s.bias = a.bias;
+    s.gate = a.gate;
+    s.resid = a.resid;
+    s.out = a.out;
+    s.part = reinterpret_cast<float *>(w + p.off_part);
+    CUtensorMap tw, ta;
+    if (!make_tmap_2d(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.W, a.N, a.K, I8_BM, 128) ||
+        !make_tmap_2d(&ta, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, tokens, a.M, a.K, s.NT, 64))
+        return cudaErrorInvalidValue;
+    cudaError_t e;
+    if (a.a_scale != nullptr) {
+        const long n = (long)a.M * a.K / 16;
+        const long ctas = std::min<long>((n + 255) / 256, (long)device_sms() * 8);
+        e = launch_pdl(widen_kernel, dim3((unsigned)ctas), dim3(256), 0, st, reinterpret_cast<const uint4 *>(a.A),
+                       reinterpret_cast<uint4 *>(tokens), n, a.a_scale, scale, a.M);
+    } else {
+        e = a.dtype == XC_BF16 ? quantize_launch(reinterpret_cast<const bf16 *>(a.A), tokens, scale, a.M, a.K, st)
+                               : quantize_launch(reinterpret_cast<const float *>(a.A), tokens, scale, a.M, a.K, st);
+    }
+    if (e != cudaSuccess) return e;
+    return a.dtype == XC_BF16 ? i8_launch<bf16>(p, tw, ta, err, st) : i8_launch<float>(p, tw, ta, err, st);
+}
+
+}  // namespace xc

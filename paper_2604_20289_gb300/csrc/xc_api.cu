@@ -1570,6 +1570,54 @@ xc_status xc_op_linear(int dtype, int epilogue, int M, int N, int K, const void 
     return XC_OK;
 }
 
+// ---- products in 8-bit integers ----
+static bool i8_aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+static bool i8_shape(int M, int N, int K) {
+    return M >= 0 && M < (1 << 24) && N >= 1 && N < (1 << 24) && K >= 16 && K <= (1 << 17) && K % 16 == 0 &&
+           ((M + 255ll) / 256 + 1) * ((N + 127ll) / 128) * ((K + 127ll) / 128) < (1ll << 31);
+}
+
+xc_status xc_op_quantize_rows(int dtype, int M, int K, const void *x, signed char *q, float *scale, void *stream) {
+    if (dtype != XC_F32 && dtype != XC_BF16) OP_FAIL(XC_EINVAL, "xc_op_quantize_rows: dtype");
+    if (!i8_shape(M, 1, K)) OP_FAIL(XC_EINVAL, "xc_op_quantize_rows: K a multiple of 16 up to 131072, M from 0 below 2^24");
+    if (M == 0) return XC_OK;
+    if (x == nullptr || q == nullptr || scale == nullptr || !i8_aligned(x) || !i8_aligned(q))
+        OP_FAIL(XC_EINVAL, "xc_op_quantize_rows: NULL or unaligned pointer");
+    OP_CK(quantize_rows(dtype, M, K, x, q, scale, reinterpret_cast<cudaStream_t>(stream)));
+    return XC_OK;
+}
+
+size_t xc_op_linear_i8_workspace_bytes(int M, int N, int K) {
+    if (!i8_shape(M, N, K)) {
+        set_err(nullptr, "xc_op_linear_i8_workspace_bytes: N from 1, K a multiple of 16 up to 131072, M from 0 below 2^24");
+        return 0;
+    }
+    return M == 0 ? 0 : linear_i8_workspace_bytes(M, N, K);
+}
+
+xc_status xc_op_linear_i8(int dtype, int epilogue, int M, int N, int K, const void *A, const float *a_scale,
+                          const signed char *Wt, const float *w_scale, const float *bias, const float *gate,
+                          const void *resid, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (dtype != XC_F32 && dtype != XC_BF16) OP_FAIL(XC_EINVAL, "xc_op_linear_i8: dtype");
+    if (epilogue != XC_EPI_BIAS && epilogue != XC_EPI_GELU && epilogue != XC_EPI_RESID_GATE)
+        OP_FAIL(XC_EINVAL, "xc_op_linear_i8: epilogue: bias, GELU or gated residual");
+    if (!i8_shape(M, N, K)) OP_FAIL(XC_EINVAL, "xc_op_linear_i8: N from 1, K a multiple of 16 up to 131072, M from 0 below 2^24");
+    if (M == 0) return XC_OK;
+    if (A == nullptr || Wt == nullptr || w_scale == nullptr || bias == nullptr || out == nullptr)
+        OP_FAIL(XC_EINVAL, "xc_op_linear_i8: NULL pointer");
+    if (epilogue == XC_EPI_RESID_GATE && (gate == nullptr || resid == nullptr))
+        OP_FAIL(XC_EINVAL, "xc_op_linear_i8: gated residual needs gate and resid");
+    if (!i8_aligned(A) || !i8_aligned(Wt)) OP_FAIL(XC_EINVAL, "xc_op_linear_i8: A and Wt must be 16-byte aligned");
+    const size_t need = linear_i8_workspace_bytes(M, N, K);
+    if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need)
+        OP_FAIL(XC_EINVAL, "xc_op_linear_i8: workspace of %zu bytes needed (256-byte aligned)", need);
+    int *err = op_err_word();
+    if (err == nullptr) OP_FAIL(XC_ECUDA, "xc_op_linear_i8: error word");
+    const LinearI8Args a{dtype, epilogue, M, N, K, A, a_scale, Wt, w_scale, bias, gate, resid, out};
+    OP_CK(linear_i8(a, workspace, err, reinterpret_cast<cudaStream_t>(stream)));
+    return XC_OK;
+}
+
 xc_status xc_op_qkv_rope(int dtype, int n_cams, int frames, int gh, int gw, int chunk, int d, int head_dim,
                          float rope_theta, const void *A, const void *Wt, const float *bias, void *q, void *k,
                          void *v, void *stream) {

@@ -108,6 +108,19 @@ cudaError_t residual_reuse(const T *x, const T *r, T *out, long n, const uint8_t
 cudaError_t euler_update(float *x, const float *v, float ds, long n, cudaStream_t st);
 template <typename T>
 cudaError_t convert_f32(const float *in, T *out, long n, int n_sm, cudaStream_t st);
+// Products in 8-bit integers (k_linear_i8.cu).
+struct LinearI8Args {
+    int dtype, epi, M, N, K;
+    const void *A;                // [M][K] activations, or with a_scale 8-bit whole numbers
+    const float *a_scale;         // [M] or NULL
+    const signed char *W;         // [N][K]
+    const float *w_scale, *bias, *gate;
+    const void *resid;
+    void *out;
+};
+size_t linear_i8_workspace_bytes(int M, int N, int K);
+cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st);
+cudaError_t quantize_rows(int dtype, int M, int K, const void *x, signed char *q, float *scale, cudaStream_t st);
 // Fused conditioning (three launches), see k_elem.cu.
 constexpr int COND_TEMB_MAX = 512;
 struct CondArgs {

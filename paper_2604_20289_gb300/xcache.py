@@ -113,6 +113,9 @@ SIGNATURES = {
     "xc_profile_start": (_I, [_P, ctypes.c_uint, _I]),
     "xc_profile_stop": (_I, [_P, ctypes.POINTER(ProfileRec), _I, ctypes.POINTER(_I)]),
     "xc_op_linear": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "xc_op_quantize_rows": (_I, [_I, _I, _I, _P, _P, _P, _P]),
+    "xc_op_linear_i8_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I]),
+    "xc_op_linear_i8": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "xc_op_qkv_rope": (_I, [_I, _I, _I, _I, _I, _I, _I, _I, _F, _P, _P, _P, _P, _P, _P, _P]),
     "xc_op_attention_workspace_bytes": (ctypes.c_size_t, [_I, _I]),
     "xc_op_attention": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
@@ -327,6 +330,69 @@ def op_linear(dtype, epilogue, A, Wt, bias, out, gate=None, resid=None, xin=None
                            _stream(stream)))
 
 
+def _torch_types(dtype):
+    """(the activations' torch type, torch)"""
+    import torch
+    return (torch.float32 if dtype_code(dtype) == XC_F32 else torch.bfloat16), torch
+
+
+def _on_device(*tensors):
+    """Refuses tensors that are not on the current CUDA device."""
+    import torch
+    dev = torch._C._cuda_getDevice() if tensors[0].is_cuda else -2
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("expected CUDA tensors on the current device")
+
+
+def op_quantize_rows(dtype, x, q, scale, stream=None):
+    """8-bit integers q [M, K] (int8) and scale [M] (float32) of the rows of x [M, K]; all contiguous."""
+    dt, torch = _torch_types(dtype)
+    _on_device(x, q, scale)
+    if x.dim() != 2 or x.dtype is not dt or q.shape != x.shape or q.dtype is not torch.int8 or \
+            scale.shape != x.shape[:1] or scale.dtype is not torch.float32 or \
+            not (x.is_contiguous() and q.is_contiguous() and scale.is_contiguous()):
+        raise ValueError("x [M, K] of dtype, q [M, K] int8, scale [M] float32, all contiguous")
+    M, K = x.shape
+    check(LIB.xc_op_quantize_rows(dtype_code(dtype), M, K, x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(stream)))
+
+
+def op_linear_i8_workspace_bytes(M, N, K) -> int:
+    return LIB.xc_op_linear_i8_workspace_bytes(M, N, K)
+
+
+def op_linear_i8(dtype, epilogue, A, Wq, w_scale, bias, out, gate=None, resid=None, a_scale=None, workspace=None,
+                 stream=None):
+    """out [M, N] = epilogue of A [M, K] by Wq [N, K] (int8) with w_scale [N] and bias [N] (float32).  A is of dtype and
+    quantised by the call, or with a_scale [M] (float32) int8.  gate [N] float32 and resid [M, N] of dtype for
+    XC_EPI_RESID_GATE.  All contiguous.  workspace: a device tensor of op_linear_i8_workspace_bytes, or None: allocated
+    for the call (in a capture: from the graph's memory)."""
+    dt, torch = _torch_types(dtype)
+    f32, i8 = torch.float32, torch.int8
+    _on_device(A, Wq, w_scale, bias, out, gate, resid, a_scale)
+    (M, K), N = A.shape, Wq.shape[0]
+    if A.dtype is not (dt if a_scale is None else i8) or Wq.dtype is not i8 or Wq.shape != (N, K) or \
+            out.shape != (M, N) or out.dtype is not dt or w_scale.shape != (N,) or bias.shape != (N,) or \
+            w_scale.dtype is not f32 or bias.dtype is not f32 or not (A.is_contiguous() and Wq.is_contiguous() and
+            w_scale.is_contiguous() and bias.is_contiguous() and out.is_contiguous()):
+        raise ValueError("A [M, K] of dtype (int8 with a_scale), Wq [N, K] int8, w_scale, bias [N] float32, out [M, N] of "
+                         "dtype, all contiguous")
+    if (gate is not None and (gate.shape != (N,) or gate.dtype is not f32 or not gate.is_contiguous())) or \
+            (resid is not None and (resid.shape != (M, N) or resid.dtype is not dt or not resid.is_contiguous())) or \
+            (a_scale is not None and (a_scale.shape != (M,) or a_scale.dtype is not f32 or not a_scale.is_contiguous())):
+        raise ValueError("gate [N] and a_scale [M] float32, resid [M, N] of dtype, all contiguous")
+    cuda = _stream(stream)
+    if workspace is None:
+        buf, ws, nbytes = _scratch(LIB.xc_op_linear_i8_workspace_bytes(M, N, K), stream, cuda, A.device)
+    else:
+        buf, ws, nbytes = _given(workspace)
+    st = LIB.xc_op_linear_i8(dtype_code(dtype), epilogue, M, N, K, A.data_ptr(), _ptr(a_scale), Wq.data_ptr(),
+                             w_scale.data_ptr(), bias.data_ptr(), _ptr(gate), _ptr(resid), out.data_ptr(), ws, nbytes,
+                             cuda)
+    if st:
+        check(st)
+
+
 def op_qkv_rope(dtype, n_cams, frames, gh, gw, chunk, head_dim, theta, A, Wt, bias, q, k, v,
                 stream=None):
     d = A.shape[1]
@@ -466,6 +532,17 @@ class KVCache:
         if t.dtype is not self._int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
             raise ValueError(f"expected a contiguous int32 CUDA tensor of {n} elements")
         return t.data_ptr()
+
+
+def _scratch(nbytes, stream, cuda, device):
+    """(tensor, pointer, bytes) of a workspace for one call, from the memory of the stream it runs on."""
+    import torch
+    if stream is None:
+        buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(torch.cuda.ExternalStream(cuda) if cuda else torch.cuda.default_stream()):
+            buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    return buf, buf.data_ptr(), buf.numel()
 
 
 def _given(workspace):

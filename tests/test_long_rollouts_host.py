@@ -1,0 +1,53 @@
+"""Host-side argument checks of the operators of long rollouts (8-bit products):
+every refusal comes before any CUDA call, so no GPU is needed."""
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2604_20289_gb300", "libxcache.so")
+P = 1 << 20          # a 256-byte aligned address that is never read
+
+
+@pytest.fixture(scope="module")
+def xb():
+    if not os.path.exists(LIB):
+        from paper_2604_20289_gb300 import build
+        build.build()
+    from paper_2604_20289_gb300 import xcache
+    return xcache
+
+
+@pytest.mark.parametrize("kw,msg", [
+    (dict(dtype=2), "dtype"), (dict(dtype=-1), "dtype"), (dict(M=-1), "K a multiple"), (dict(M=1 << 24), "K a multiple"),
+    (dict(K=0), "K a multiple"), (dict(K=24), "K a multiple"), (dict(K=-16), "K a multiple"),
+    (dict(K=(1 << 17) + 16), "K a multiple"), (dict(x=0), "pointer"), (dict(q=0), "pointer"), (dict(scale=0), "pointer"),
+    (dict(x=P + 8), "pointer"), (dict(q=P + 4), "pointer")])
+def test_quantise_refusals(xb, kw, msg):
+    a = dict(dtype=xb.XC_BF16, M=4, K=64, x=P, q=P, scale=P)
+    a.update(kw)
+    assert xb.LIB.xc_op_quantize_rows(a["dtype"], a["M"], a["K"], a["x"], a["q"], a["scale"], None) == xb.XC_EINVAL
+    assert msg in xb.last_error(None)
+
+
+@pytest.mark.parametrize("kw,msg", [
+    (dict(dtype=2), "dtype"), (dict(epi=3), "epilogue"), (dict(epi=-1), "epilogue"), (dict(epi=16), "epilogue"),
+    (dict(M=-1), "K a multiple"), (dict(N=0), "K a multiple"), (dict(K=40), "K a multiple"), (dict(N=1 << 24), "K a multiple"),
+    (dict(M=(1 << 24) - 1, N=(1 << 24) - 1, K=1 << 17), "K a multiple"), (dict(A=0), "NULL"), (dict(W=0), "NULL"),
+    (dict(ws=0), "NULL"), (dict(bias=0), "NULL"), (dict(out=0), "NULL"), (dict(epi=2), "residual"),
+    (dict(epi=2, gate=P), "residual"), (dict(A=P + 8), "aligned"), (dict(W=P + 8), "aligned"), (dict(work=0), "workspace"),
+    (dict(work=P + 16), "workspace"), (dict(bytes=100), "workspace")])
+def test_product_refusals(xb, kw, msg):
+    a = dict(dtype=xb.XC_BF16, epi=0, M=4, N=100, K=64, A=P, W=P, ws=P, bias=P, gate=0, resid=0, out=P, work=P, bytes=1 << 40)
+    a.update(kw)
+    st = xb.LIB.xc_op_linear_i8(a["dtype"], a["epi"], a["M"], a["N"], a["K"], a["A"], None, a["W"], a["ws"], a["bias"],
+                                a["gate"], a["resid"], a["out"], a["work"], a["bytes"], None)
+    assert st == xb.XC_EINVAL
+    assert msg in xb.last_error(None), xb.last_error(None)
+
+
+def test_nothing_to_do(xb):
+    assert xb.LIB.xc_op_quantize_rows(xb.XC_BF16, 0, 64, None, None, None, None) == xb.XC_OK
+    assert xb.LIB.xc_op_linear_i8(xb.XC_F32, 0, 0, 8, 64, *[None] * 8, None, 0, None) == xb.XC_OK
+    assert xb.op_linear_i8_workspace_bytes(0, 8, 64) == 0
+    assert xb.op_linear_i8_workspace_bytes(4, 8, 40) == 0 and "K a multiple" in xb.last_error(None)
