@@ -308,6 +308,14 @@ xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_bran
                                  float scale, void *o, long o_stride, void *workspace, size_t workspace_bytes,
                                  void *stream);
 
+/* The same call, and lse [n_branches * n_q][n_heads] (float, or NULL): the log of
+ * each row's sum of exp(scale * (q . k_j)) over the keys it sees, -infinity
+ * where it sees none. */
+xc_status xc_op_branch_attention_lse(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q,
+                                     int n_heads, const void *q, long q_stride, int shared_len, int causal,
+                                     float scale, void *o, long o_stride, float *lse, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
 /* 1 while work given to `stream` is captured into a graph, else 0.  A captured
  * call uses its pointers again at every replay: its workspace must live as long
  * as the graph, and must not be shared with calls that overlap a replay. */

@@ -39,6 +39,7 @@ struct BranchSched {
     float *ws_o;             // partial O, then (m, l) of each row, then the scan
     float2 *ws_ml;
     int *ws_off;             // [E + 1] line length before each entry (same for every head)
+    float *lse;              // [B n_q][Hk grp] log of each row's sum of exponentials, or NULL
     int4 *ws_start;          // [G] per CTA: its first unit (head, entry), position in it, key tiles of it
 
     __host__ __device__ __forceinline__ int seq(int b) const {
@@ -58,6 +59,10 @@ struct BranchSched {
     }
     // length on the line of a unit of n key tiles
     __host__ __device__ __forceinline__ int line_len(int n) const { return n > 0 ? n + lead : 0; }
+    // log sum_j exp(scale q . k_j) of a row, from its max m (log2 units) and sum l: -inf without keys
+    __device__ __forceinline__ void put_lse(int t, int head, float m, float l) const {
+        lse[(size_t)t * (Hk * grp) + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
     // keys that query i of a branch of length l sees
     __host__ __device__ __forceinline__ int limit(int l, int i) const {
         const int x = causal ? l - n_q + i + 1 : l;
@@ -247,6 +252,9 @@ __device__ void branch_zero_rows(const BranchSched &s, const int *lens, T *o, lo
         const int vecs = d * (int)sizeof(T) / 16;
         for (int x = threadIdx.x; x < nt * vecs; x += blockDim.x)
             reinterpret_cast<uint4 *>(o + (size_t)(b * s.n_q + i0 + x / vecs) * o_ld)[x % vecs] = make_uint4(0, 0, 0, 0);
+        if (s.lse != nullptr)
+            for (int x = threadIdx.x; x < nt * s.Hk * s.grp; x += blockDim.x)
+                s.lse[(size_t)(b * s.n_q + i0) * (s.Hk * s.grp) + x] = -INFINITY;
     }
 }
 
@@ -823,6 +831,7 @@ __global__ void __launch_bounds__(BranchTile<HD, QT>::THREADS, 1)
             mbar_arrive(&o_free[wg]);                      // the next piece may write O_i
             const BranchPiece c = cur;
             if (sc.n_pr == 0 && c.kt1 - c.kt0 == c.n_kt) {
+                if (sc.lse != nullptr && row_ok) sc.put_lse(c.t0 + tl_, c.h * sc.grp + gq, m, l);
                 // Whole unit: 32 columns (64 bytes) of a row at a time.  Each
                 // quad of lanes exchanges its four rows' 16-byte parts, so
                 // that a store covers 64 consecutive bytes of 8 rows.
@@ -1076,6 +1085,7 @@ __global__ void __launch_bounds__(256, BranchTileF32<HD>::CTAS)
             const bool mine = i % A::KS == ks;             // every share holds the sums: row by row another writes
             if (whole) {
                 const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
+                if (sc.lse != nullptr && tx == 0) sc.put_lse(pc.t0 + r / sc.grp, pc.h * sc.grp + r % sc.grp, m[i], l[i]);
                 float *dst = o + (size_t)(pc.t0 + r / sc.grp) * o_ld + (pc.h * sc.grp + r % sc.grp) * HD;
 #pragma unroll
                 for (int j = 0; j < A::NV; ++j)
@@ -1232,6 +1242,7 @@ __global__ void __launch_bounds__(THREADS, PREFIX ? (KB == 8 ? 3 : 4) * COMBINE_
             float top = m[0];
             for (int j = 1; j < n_share; ++j) top = fmaxf(top, sh_ml[threadIdx.x + (j << lg)].x);
             const float use = top == -INFINITY ? 0.0f : top;
+            m[0] = top;
             den[0] = 0.0f;
             acc[0] = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int j = 0; j < n_share; ++j) {
@@ -1253,6 +1264,7 @@ __global__ void __launch_bounds__(THREADS, PREFIX ? (KB == 8 ? 3 : 4) * COMBINE_
         if (r >= rows) break;
         const float inv = den[i] > 0.0f ? 1.0f / den[i] : 0.0f;
         const int tr = r / s.grp;
+        if (s.lse != nullptr && ch == 0) s.put_lse(b * s.n_q + i0 + tr, h * s.grp + r - tr * s.grp, m[i], den[i]);
         T *dst = o + (size_t)(b * s.n_q + i0 + tr) * o_ld + (h * s.grp + r - tr * s.grp) * HD + 4 * ch;
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<float4 *>(dst) = make_float4(acc[i].x * inv, acc[i].y * inv, acc[i].z * inv, acc[i].w * inv);
@@ -1413,6 +1425,7 @@ cudaError_t branch_attn(const xc_kv_cache &c, const BranchAttnArgs &a, void *ws,
     p.s.seqs = a.seqs;
     p.s.causal = a.causal;
     p.s.shared = a.shared;
+    p.s.lse = a.lse;
     p.s.ws_start = reinterpret_cast<int4 *>(ws);
     p.s.ws_o = reinterpret_cast<float *>(p.s.ws_start + p.s.G);
     p.s.ws_ml = reinterpret_cast<float2 *>(p.s.ws_o + p.rows * c.head_dim);

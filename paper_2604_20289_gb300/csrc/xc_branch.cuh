@@ -50,6 +50,7 @@ struct BranchAttnArgs {
     const void *q;
     long q_ld, o_ld;
     void *o;
+    float *lse;                       // [B n_q][H] or NULL
     const void *k, *v;                // the layer's pools
 };
 // Whether the line of key tiles fits the kernels' 32-bit counters.

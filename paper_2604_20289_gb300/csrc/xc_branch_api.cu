@@ -230,6 +230,14 @@ xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_bran
                                  int n_heads, const void *q, long q_stride, int shared_len, int causal,
                                  float scale, void *o, long o_stride, void *workspace, size_t workspace_bytes,
                                  void *stream) {
+    return xc_op_branch_attention_lse(cache, layer, n_branches, seqs, n_q, n_heads, q, q_stride, shared_len, causal, scale,
+                                      o, o_stride, nullptr, workspace, workspace_bytes, stream);
+}
+
+xc_status xc_op_branch_attention_lse(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q,
+                                     int n_heads, const void *q, long q_stride, int shared_len, int causal,
+                                     float scale, void *o, long o_stride, float *lse, void *workspace,
+                                     size_t workspace_bytes, void *stream) {
     const char *who = "xc_op_branch_attention";
     CHECK(check_cache(who, cache));
     const xc_kv_cache &c = *cache;
@@ -256,6 +264,7 @@ xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_bran
     a.q_ld = q_stride;
     a.o = o;
     a.o_ld = o_stride;
+    a.lse = lse;
     const size_t layer_off = (size_t)layer * c.n_pages * c.page_size * kv_row_bytes(c);
     a.k = reinterpret_cast<const char *>(c.k) + layer_off;
     a.v = reinterpret_cast<const char *>(c.v) + layer_off;

@@ -138,6 +138,7 @@ SIGNATURES = {
     "xc_op_stream_capturing": (_I, [_P]),
     "xc_op_branch_attention_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I, _I, _I]),
     "xc_op_branch_attention": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _I, _I, _F, _P, _L, _P, ctypes.c_size_t, _P]),
+    "xc_op_branch_attention_lse": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _I, _I, _F, _P, _L, _P, _P, ctypes.c_size_t, _P]),
 }
 
 
@@ -641,9 +642,16 @@ def op_branch_attention_workspace_bytes(cache: KVCache, n_branches, n_q, n_heads
     return LIB.xc_op_branch_attention_workspace_bytes(cache.ptr, n_branches, n_q, n_heads, shared_len)
 
 
+def _lse(cache: KVCache, lse, rows, heads) -> int:
+    if lse.shape != (rows, heads) or lse.dtype is not cache._float32 or not lse.is_contiguous() or not lse.is_cuda:
+        raise ValueError("lse: contiguous float32 CUDA tensor [len(seqs) * n_q, n_heads]")
+    return lse.data_ptr()
+
+
 def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, causal=False, scale=0.0,
-                        workspace=None, stream=None):
+                        workspace=None, stream=None, lse=None):
     """q, o [len(seqs) * n_q, n_heads * head_dim] (row-strided views allowed); seqs int32 CUDA tensor.
+    lse: float32 [len(seqs) * n_q, n_heads], receives the log of each row's sum of exponentials, or None.
     workspace: a device tensor of op_branch_attention_workspace_bytes, or None for the cache's own."""
     B, hd, dt = seqs.numel(), cache.head_dim, cache.torch_dtype
     T, dq = q.shape
@@ -656,6 +664,8 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
         raise ValueError("expected CUDA tensors")
     if T == 1:
         sq = so = dq
+    if lse is not None:
+        lse = _lse(cache, lse, T, dq // hd)
     cuda = _stream(stream)
     if workspace is None:
         key = (B, n_q, dq, shared_len)
@@ -666,7 +676,7 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
         buf, ws, nbytes = cache.workspace(need, cuda)
     else:
         buf, ws, nbytes = _given(workspace)
-    st = LIB.xc_op_branch_attention(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
-                                    shared_len, causal, scale, o.data_ptr(), so, ws, nbytes, cuda)
+    st = LIB.xc_op_branch_attention_lse(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
+                                        shared_len, causal, scale, o.data_ptr(), so, lse, ws, nbytes, cuda)
     if st:
         check(st)
