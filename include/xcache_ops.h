@@ -316,6 +316,27 @@ xc_status xc_op_branch_attention_lse(const xc_kv_cache *cache, int layer, int n_
                                      float scale, void *o, long o_stride, float *lse, void *workspace,
                                      size_t workspace_bytes, void *stream);
 
+/* The weight that one layer's attention gave to each cached key, added up over
+ * the query rows that see it (arguments as in xc_op_branch_attention, lse as that
+ * call left it):
+ *   weights[s][j] = decay * weights[s][j] + sum exp(scale * (q[t][h] . k_j) - lse[t][h])
+ * over the tokens t and heads h of branch b, s = seqs[b], j < len[s].  Every row
+ * adds 1 in all.  One array serves every layer of a step: decay of the step in the first
+ * layer's call, 1 in the others'.  decay = 0 does not read the old weights.  A row
+ * whose lse is -infinity adds nothing.
+ *   weights     device float [max_seqs][w_stride], w_stride >= max_pages * page_size;
+ *               entries past len[s] are neither read nor written, so those of new tokens must be 0
+ *               (or decay 0)
+ *   seqs        n_branches <= 1024 sequences; one listed again is flagged and takes no part
+ *               the second time
+ * Each of a row's keys counts as in the attention: page ids out of range as zeros,
+ * flagged.  The sums are fp32, in an order that does not change from run to run. */
+size_t xc_op_key_weights_workspace_bytes(const xc_kv_cache *cache, int n_branches, int n_q, int n_heads, int shared_len);
+xc_status xc_op_key_weights(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q, int n_heads,
+                            const void *q, long q_stride, const float *lse, int shared_len, int causal, float scale,
+                            float decay, float *weights, long w_stride, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
 /* 1 while work given to `stream` is captured into a graph, else 0.  A captured
  * call uses its pointers again at every replay: its workspace must live as long
  * as the graph, and must not be shared with calls that overlap a replay. */

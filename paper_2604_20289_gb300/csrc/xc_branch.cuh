@@ -58,6 +58,22 @@ bool branch_attn_fits(const xc_kv_cache &c, int B, int n_q, int H, int shared);
 size_t branch_attn_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, int shared);
 cudaError_t branch_attn(const xc_kv_cache &c, const BranchAttnArgs &a, void *ws, int *err, cudaStream_t st);
 
+// Weights of the cached keys (k_key_weights.cu).
+struct KeyWeightsArgs {
+    int B, n_q, H, shared, causal;
+    float scale, decay;
+    const int *seqs;
+    const void *q;
+    long q_ld;
+    const float *lse;
+    float *w;
+    long w_ld;
+    const void *k;                    // the layer's pool
+};
+bool key_weights_fit(const xc_kv_cache &c, int B, int n_q, int H, int shared);
+size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, int shared);
+cudaError_t key_weights(const xc_kv_cache &c, const KeyWeightsArgs &a, void *ws, int *err, cudaStream_t st);
+
 // 3-D bf16 map of a [tokens][heads * head_dim] matrix (rows ld elements
 // apart) with a box of 64 columns x box_heads heads x box_tokens tokens,
 // 128-byte swizzle.

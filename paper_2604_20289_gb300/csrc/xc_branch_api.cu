@@ -271,6 +271,56 @@ xc_status xc_op_branch_attention_lse(const xc_kv_cache *cache, int layer, int n_
     return launched(who, branch_attn(c, a, workspace, err, as_stream(stream)));
 }
 
+static xc_status check_weigh(const char *who, const xc_kv_cache *cache, int n_branches, int n_q, int n_heads, int shared_len) {
+    CHECK(check_branch(who, cache, n_branches, n_q, n_heads, shared_len));
+    if (n_branches > 0 && n_q > 0 && !key_weights_fit(*cache, n_branches, n_q, n_heads, shared_len))
+        return fail(XC_EINVAL, "%s: too many branches (%d at most) or query rows for tables this long", who, KV_LIST_MAX);
+    return XC_OK;
+}
+
+size_t xc_op_key_weights_workspace_bytes(const xc_kv_cache *cache, int n_branches, int n_q, int n_heads, int shared_len) {
+    if (check_weigh("xc_op_key_weights_workspace_bytes", cache, n_branches, n_q, n_heads, shared_len) != XC_OK) return 0;
+    if (n_branches == 0 || n_q == 0) return 0;
+    return key_weights_workspace_bytes(*cache, n_branches, n_q, n_heads, shared_len);
+}
+
+xc_status xc_op_key_weights(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q, int n_heads,
+                            const void *q, long q_stride, const float *lse, int shared_len, int causal, float scale,
+                            float decay, float *weights, long w_stride, void *workspace, size_t workspace_bytes,
+                            void *stream) {
+    const char *who = "xc_op_key_weights";
+    CHECK(check_cache(who, cache));
+    const xc_kv_cache &c = *cache;
+    if (layer < 0 || layer >= c.n_layers) return fail(XC_EINVAL, "%s: layer", who);
+    CHECK(check_weigh(who, cache, n_branches, n_q, n_heads, shared_len));
+    if (!(scale >= 0.0f) || !std::isfinite(scale)) return fail(XC_EINVAL, "%s: scale must be finite and not negative", who);
+    if (!(decay >= 0.0f) || !std::isfinite(decay)) return fail(XC_EINVAL, "%s: decay must be finite and not negative", who);
+    if (n_branches == 0 || n_q == 0) return XC_OK;
+    if (!rows_ok(q, q_stride, (long)n_heads * c.head_dim, c.dtype))
+        return fail(XC_EINVAL, "%s: rows must be 16-byte aligned and at least as far apart as they are wide", who);
+    if (seqs == nullptr || lse == nullptr || weights == nullptr) return fail(XC_EINVAL, "%s: NULL pointer", who);
+    if (w_stride < (long)c.max_pages * c.page_size)
+        return fail(XC_EINVAL, "%s: w_stride: a row of weights holds a table row's tokens", who);
+    CHECK(check_ws(who, workspace, workspace_bytes, key_weights_workspace_bytes(c, n_branches, n_q, n_heads, shared_len)));
+    ERR_WORD(err, "xc_op_key_weights");
+    KeyWeightsArgs a{};
+    a.B = n_branches;
+    a.n_q = n_q;
+    a.H = n_heads;
+    a.shared = shared_len;
+    a.causal = causal != 0;
+    a.scale = scale > 0.0f ? scale : 1.0f / sqrtf((float)c.head_dim);
+    a.decay = decay;
+    a.seqs = seqs;
+    a.q = q;
+    a.q_ld = q_stride;
+    a.lse = lse;
+    a.w = weights;
+    a.w_ld = w_stride;
+    a.k = reinterpret_cast<const char *>(c.k) + (size_t)layer * c.n_pages * c.page_size * kv_row_bytes(c);
+    return launched(who, key_weights(c, a, workspace, err, as_stream(stream)));
+}
+
 int xc_op_stream_capturing(void *stream) {
     cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
     if (stream == nullptr) return 0;                       // the legacy default stream is never captured

@@ -138,6 +138,8 @@ SIGNATURES = {
     "xc_op_stream_capturing": (_I, [_P]),
     "xc_op_branch_attention_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I, _I, _I]),
     "xc_op_branch_attention": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _I, _I, _F, _P, _L, _P, ctypes.c_size_t, _P]),
+    "xc_op_key_weights_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I, _I, _I]),
+    "xc_op_key_weights": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _P, _I, _I, _F, _F, _P, _L, _P, ctypes.c_size_t, _P]),
     "xc_op_branch_attention_lse": (_I, [_P, _I, _I, _P, _I, _I, _P, _L, _I, _I, _F, _P, _L, _P, _P, ctypes.c_size_t, _P]),
 }
 
@@ -494,6 +496,7 @@ class KVCache:
         self.ptr = ctypes.addressof(self.desc)
         self._ws = {}                             # stream -> (tensor, pointer, bytes)
         self._attn_bytes, self._axes = {}, {}     # workspace sizes by shape, axis arrays by value
+        self._weigh_bytes = {}
         self._page_bytes = LIB.xc_op_kv_workspace_bytes(self.ptr)
 
     @classmethod
@@ -508,7 +511,7 @@ class KVCache:
                    torch.zeros(max_seqs, dtype=torch.int32, device=device))
 
     def note(self, memo: dict, key, value):
-        """Keeps value under key in one of the handle's two dicts, which hold 4096 shapes at most."""
+        """Keeps value under key in one of the handle's dicts, which hold 4096 shapes at most."""
         if len(memo) >= 4096:
             memo.clear()
         memo[key] = value
@@ -678,5 +681,48 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
         buf, ws, nbytes = _given(workspace)
     st = LIB.xc_op_branch_attention_lse(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
                                         shared_len, causal, scale, o.data_ptr(), so, lse, ws, nbytes, cuda)
+    if st:
+        check(st)
+
+
+def op_key_weights_workspace_bytes(cache: KVCache, n_branches, n_q, n_heads, shared_len=0) -> int:
+    return LIB.xc_op_key_weights_workspace_bytes(cache.ptr, n_branches, n_q, n_heads, shared_len)
+
+
+def _weights(cache: KVCache, weights) -> tuple:
+    """(pointer, row stride) of the keys' weights."""
+    if weights.dim() != 2 or weights.shape[0] != cache.table.shape[0] or \
+            weights.shape[1] < cache.table.shape[1] * cache.page_size or weights.dtype is not cache._float32 or \
+            not weights.is_cuda or weights.stride(1) != 1 or (weights.shape[0] > 1 and weights.stride(0) < weights.shape[1]):
+        raise ValueError("weights: float32 CUDA tensor [max_seqs, max_pages * page_size] with unit column stride")
+    return weights.data_ptr(), max(weights.stride(0), weights.shape[1])
+
+
+def op_key_weights(cache: KVCache, layer, seqs, n_q, q, lse, weights, shared_len=0, causal=False, scale=0.0, decay=1.0,
+                   workspace=None, stream=None):
+    """Adds to weights [max_seqs, max_pages * page_size] (float32), after decaying them, the weight that the rows of q
+    gave to each key; lse [len(seqs) * n_q, n_heads] from op_branch_attention of the same q.  workspace: a device tensor
+    of op_key_weights_workspace_bytes, or None for the cache's own."""
+    B, hd = seqs.numel(), cache.head_dim
+    T, dq = q.shape
+    if T != B * n_q or dq % hd or q.dtype is not cache.torch_dtype or not q.is_cuda:
+        raise ValueError("q: CUDA tensor [len(seqs) * n_q, n_heads * head_dim] of the cache's dtype")
+    sq, u0 = q.stride()
+    if u0 != 1:
+        raise ValueError("rows must have unit column stride")
+    if T == 1:
+        sq = dq
+    w, sw = _weights(cache, weights)
+    cuda = _stream(stream)
+    if workspace is None:
+        key = (B, n_q, dq, shared_len)
+        need = cache._weigh_bytes.get(key)
+        if need is None:
+            need = cache.note(cache._weigh_bytes, key, op_key_weights_workspace_bytes(cache, B, n_q, dq // hd, shared_len))
+        buf, ws, nbytes = cache.workspace(need, cuda)
+    else:
+        buf, ws, nbytes = _given(workspace)
+    st = LIB.xc_op_key_weights(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
+                               _lse(cache, lse, T, dq // hd), shared_len, causal, scale, decay, w, sw, ws, nbytes, cuda)
     if st:
         check(st)

@@ -1,5 +1,6 @@
 """Host-side argument checks of the operators of long rollouts (8-bit products):
 every refusal comes before any CUDA call, so no GPU is needed."""
+import ctypes
 import os
 
 import pytest
@@ -51,3 +52,40 @@ def test_nothing_to_do(xb):
     assert xb.LIB.xc_op_linear_i8(xb.XC_F32, 0, 0, 8, 64, *[None] * 8, None, 0, None) == xb.XC_OK
     assert xb.op_linear_i8_workspace_bytes(0, 8, 64) == 0
     assert xb.op_linear_i8_workspace_bytes(4, 8, 40) == 0 and "K a multiple" in xb.last_error(None)
+
+
+# ------------------------------------------------------------ key weights
+def desc(xb, **kw):
+    f = dict(dtype=xb.XC_BF16, n_layers=2, n_pages=64, page_size=16, n_kv_heads=2, head_dim=64, max_seqs=4,
+             max_pages=16, k=P, v=P, ref=P, table=P, len=P)
+    f.update(kw)
+    return xb.KVCacheDesc(**f)
+
+
+@pytest.mark.parametrize("kw,msg", [
+    (dict(layer=2), "layer"), (dict(layer=-1), "layer"), (dict(n_heads=3), "n_heads"), (dict(n_heads=2 * 129), "n_heads"),
+    (dict(n_branches=-1), "n_branches"), (dict(n_branches=1025), "branches"), (dict(shared_len=8), "shared_len"),
+    (dict(scale=-1.0), "scale"), (dict(scale=float("nan")), "scale"), (dict(decay=-0.5), "decay"), (dict(decay=float("inf")), "decay"),
+    (dict(q=0), "rows"), (dict(q=P + 4), "rows"), (dict(q_stride=120), "rows"), (dict(lse=0), "NULL"), (dict(w=0), "NULL"),
+    (dict(seqs=0), "NULL"), (dict(w_stride=255), "w_stride"), (dict(ws=0), "workspace"), (dict(ws=P + 8), "workspace"),
+    (dict(ws_bytes=10), "workspace")])
+def test_key_weight_refusals(xb, kw, msg):
+    d = desc(xb)
+    a = dict(layer=0, n_branches=2, seqs=P, n_q=1, n_heads=2, q=P, q_stride=128, lse=P, shared_len=0, causal=1, scale=0.0, decay=1.0,
+             w=P, w_stride=256, ws=P, ws_bytes=1 << 40)
+    a.update(kw)
+    st = xb.LIB.xc_op_key_weights(ctypes.addressof(d), a["layer"], a["n_branches"], a["seqs"], a["n_q"], a["n_heads"], a["q"],
+                                  a["q_stride"], a["lse"], a["shared_len"], a["causal"], a["scale"], a["decay"], a["w"],
+                                  a["w_stride"], a["ws"], a["ws_bytes"], None)
+    assert st == xb.XC_EINVAL
+    assert msg in xb.last_error(None), xb.last_error(None)
+
+
+def test_key_weights_of_nothing_and_of_bad_caches(xb):
+    d = desc(xb)
+    assert xb.LIB.xc_op_key_weights(ctypes.addressof(d), 0, 0, None, 1, 2, None, 0, None, 0, 1, 0.0, 1.0, None, 0, None, 0, None) == 0
+    assert xb.LIB.xc_op_key_weights_workspace_bytes(None, 1, 1, 2, 0) == 0
+    for kw in (dict(head_dim=32), dict(page_size=24), dict(k=0)):
+        bad = desc(xb, **kw)
+        st = xb.LIB.xc_op_key_weights(ctypes.addressof(bad), 0, 1, P, 1, 2, P, 128, P, 0, 1, 0.0, 1.0, P, 256, P, 1 << 30, None)
+        assert st == xb.XC_EINVAL
