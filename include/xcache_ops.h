@@ -196,8 +196,8 @@ xc_status xc_op_gate_static(int dtype, int n_cams, int tokens_per_cam, int d, co
  *
  * What the host cannot see is checked on the device: a call that finds a bad
  * value sets a bit of the word xc_op_device_error() returns --
- * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, of which fork
- * and extend then change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
+ * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, of which fork,
+ * extend and evict then change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
  * whose token is then skipped.  The first operator call of a process sets up
  * that word; it should come before any stream capture. */
 typedef struct {
@@ -242,6 +242,25 @@ xc_status xc_op_kv_free(const xc_kv_cache *cache, int n, const int *seqs, void *
  * The contents of pages that become free are left as they are. */
 xc_status xc_op_kv_compact(const xc_kv_cache *cache, int *n_live, void *workspace, size_t workspace_bytes,
                            void *stream);
+
+/* Evicts tokens from each of the n <= 1024 listed sequences that is longer than keep >= 1:
+ * its first n_first and last n_last tokens stay (n_first + n_last <= keep) and, of those
+ * between, the ones of the largest weights[seq][token], of equal ones the
+ * earliest; a NaN counts below every number.  What stays keeps its order and moves to the
+ * sequence's first keep positions, in every layer, with its weights; len becomes
+ * keep, the weights behind it 0.  (Keys keep the rotation of the position they were
+ * written at.)  Sequences of keep tokens or fewer stay as they are.
+ *   weights  device float [max_seqs][w_stride], w_stride >= max_pages * page_size, as of
+ *            xc_op_key_weights; NULL if n_first + n_last == keep
+ *   kept     device int [n][keep] or NULL: the tokens that stayed, ascending (a shorter
+ *            sequence: its tokens, then -1); -1 everywhere when the call changes nothing
+ * The rows move within the sequence's own pages, so a full pool is enough.  Where other
+ * sequences hold a page whose rows change, or that ends up partly filled, it is replaced by the lowest
+ * free page ids, in list order, then page order; released pages become free afterwards. */
+size_t xc_op_kv_evict_workspace_bytes(const xc_kv_cache *cache, int n, int keep);
+xc_status xc_op_kv_evict(const xc_kv_cache *cache, int n, const int *seqs, int keep, int n_first, int n_last,
+                         float *weights, long w_stride, int *kept, void *workspace, size_t workspace_bytes,
+                         void *stream);
 
 /* Rotation table: for each axis a of n_axes (1 to 4), positions 0 ..
  * n_pos[a] - 1 and pairs 0 .. axis_pairs[a] - 1 (host arrays), (cos, sin) of

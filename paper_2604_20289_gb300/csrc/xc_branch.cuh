@@ -18,6 +18,9 @@ cudaError_t kv_fork(const xc_kv_cache &c, int n, const int *src, const int *dst,
 cudaError_t kv_extend(const xc_kv_cache &c, int n, const int *seqs, int n_new, int *slots, void *ws, int *err,
                       cudaStream_t st);
 cudaError_t kv_free(const xc_kv_cache &c, int n, const int *seqs, int *err, cudaStream_t st);
+size_t kv_evict_workspace_bytes(const xc_kv_cache &c, int n, int keep);
+cudaError_t kv_evict(const xc_kv_cache &c, int n, const int *seqs, int keep, int n_first, int n_last, float *weights,
+                     long w_ld, int *kept, void *ws, int *err, cudaStream_t st);
 cudaError_t kv_compact(const xc_kv_cache &c, int *n_live, void *ws, cudaStream_t st);
 
 constexpr int ROPE_AXES = 4;

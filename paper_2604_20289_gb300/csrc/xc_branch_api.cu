@@ -139,6 +139,37 @@ xc_status xc_op_kv_compact(const xc_kv_cache *cache, int *n_live, void *workspac
     return launched("xc_op_kv_compact", kv_compact(*cache, n_live, workspace, as_stream(stream)));
 }
 
+static xc_status check_evict(const char *who, const xc_kv_cache *cache, int n, int keep) {
+    if (!cache_shape_ok(cache)) return check_cache(who, cache);
+    if (n < 0 || n > cache->max_seqs || n > KV_LIST_MAX) return fail(XC_EINVAL, "%s: 0 to max_seqs, and to %d, sequences", who, KV_LIST_MAX);
+    if (keep < 1 || keep > cache->max_pages * cache->page_size) return fail(XC_EINVAL, "%s: keep: from 1 to a table row's tokens", who);
+    return XC_OK;
+}
+
+size_t xc_op_kv_evict_workspace_bytes(const xc_kv_cache *cache, int n, int keep) {
+    if (check_evict("xc_op_kv_evict_workspace_bytes", cache, n, keep) != XC_OK) return 0;
+    return n == 0 ? 0 : kv_evict_workspace_bytes(*cache, n, keep);
+}
+
+xc_status xc_op_kv_evict(const xc_kv_cache *cache, int n, const int *seqs, int keep, int n_first, int n_last, float *weights,
+                         long w_stride, int *kept, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *who = "xc_op_kv_evict";
+    CHECK(check_cache(who, cache));
+    CHECK(check_evict(who, cache, n, keep));
+    if (n_first < 0 || n_last < 0 || (long long)n_first + n_last > keep)
+        return fail(XC_EINVAL, "%s: n_first and n_last: from 0, keep in all at most", who);
+    if (weights == nullptr && n_first + n_last != keep)
+        return fail(XC_EINVAL, "%s: without weights n_first and n_last must add up to keep", who);
+    if (weights != nullptr && w_stride < (long)cache->max_pages * cache->page_size)
+        return fail(XC_EINVAL, "%s: w_stride: a row of weights holds a table row's tokens", who);
+    if (n == 0) return XC_OK;
+    if (seqs == nullptr) return fail(XC_EINVAL, "%s: seqs is NULL", who);
+    CHECK(check_ws(who, workspace, workspace_bytes, kv_evict_workspace_bytes(*cache, n, keep)));
+    ERR_WORD(err, "xc_op_kv_evict");
+    return launched(who, kv_evict(*cache, n, seqs, keep, n_first, n_last, weights, w_stride, kept, workspace, err,
+                                  as_stream(stream)));
+}
+
 xc_status xc_op_rope_table(int n_axes, const int *axis_pairs, const int *n_pos, double theta, float *table,
                            void *stream) {
     RopeAxes ax;

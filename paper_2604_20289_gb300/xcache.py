@@ -132,6 +132,8 @@ SIGNATURES = {
     "xc_op_kv_extend": (_I, [_P, _I, _P, _I, _P, _P, ctypes.c_size_t, _P]),
     "xc_op_kv_free": (_I, [_P, _I, _P, _P]),
     "xc_op_kv_compact": (_I, [_P, _P, _P, ctypes.c_size_t, _P]),
+    "xc_op_kv_evict_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I]),
+    "xc_op_kv_evict": (_I, [_P, _I, _P, _I, _I, _I, _P, _L, _P, _P, ctypes.c_size_t, _P]),
     "xc_op_rope_table": (_I, [_I, _P, _P, ctypes.c_double, _P, _P]),
     "xc_op_qk_norm_rope": (_I, [_P, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _P, _F, _I, _P, _P, _P, _P, _I, _P, _P,
                                 _L, _P]),
@@ -724,5 +726,28 @@ def op_key_weights(cache: KVCache, layer, seqs, n_q, q, lse, weights, shared_len
         buf, ws, nbytes = _given(workspace)
     st = LIB.xc_op_key_weights(cache.ptr, layer, B, cache.int32(seqs, B), n_q, dq // hd, q.data_ptr(), sq,
                                _lse(cache, lse, T, dq // hd), shared_len, causal, scale, decay, w, sw, ws, nbytes, cuda)
+    if st:
+        check(st)
+
+
+def op_kv_evict_workspace_bytes(cache: KVCache, n, keep) -> int:
+    return LIB.xc_op_kv_evict_workspace_bytes(cache.ptr, n, keep)
+
+
+def op_kv_evict(cache: KVCache, seqs, keep: int, weights=None, n_first=0, n_last=0, kept=None, workspace=None, stream=None):
+    """Shortens every listed sequence that is longer than keep to its first n_first tokens, its last n_last and those of
+    the largest weights between (weights as of op_key_weights; None if n_first + n_last == keep).  kept: int32 CUDA tensor
+    [len(seqs), keep], receives the tokens that stayed, or None.  workspace: a device tensor of
+    op_kv_evict_workspace_bytes, or None for the cache's own."""
+    n = seqs.numel()
+    w, sw = _weights(cache, weights) if weights is not None else (None, 0)
+    cuda = _stream(stream)
+    if workspace is None:
+        need = op_kv_evict_workspace_bytes(cache, n, keep)
+        buf, ws, nbytes = cache.workspace(need, cuda)
+    else:
+        buf, ws, nbytes = _given(workspace)
+    st = LIB.xc_op_kv_evict(cache.ptr, n, cache.int32(seqs, n), keep, n_first, n_last, w, sw,
+                            cache.int32(kept, n * keep) if kept is not None else None, ws, nbytes, cuda)
     if st:
         check(st)

@@ -89,3 +89,29 @@ def test_key_weights_of_nothing_and_of_bad_caches(xb):
         bad = desc(xb, **kw)
         st = xb.LIB.xc_op_key_weights(ctypes.addressof(bad), 0, 1, P, 1, 2, P, 128, P, 0, 1, 0.0, 1.0, P, 256, P, 1 << 30, None)
         assert st == xb.XC_EINVAL
+
+
+# --------------------------------------------------------------- eviction
+@pytest.mark.parametrize("kw,msg", [
+    (dict(n=-1), "max_seqs"), (dict(n=5), "max_seqs"), (dict(keep=0), "keep"), (dict(keep=257), "keep"), (dict(first=-1), "n_first"),
+    (dict(last=-1), "n_first"), (dict(first=30, last=11), "n_first"), (dict(first=1 << 30, last=1 << 30), "n_first"),
+    (dict(w=0), "without weights"), (dict(w_stride=255), "w_stride"), (dict(seqs=0), "seqs"), (dict(ws=0), "workspace"),
+    (dict(ws=P + 8), "workspace"), (dict(ws_bytes=10), "workspace")])
+def test_eviction_refusals(xb, kw, msg):
+    d = desc(xb)
+    a = dict(n=2, seqs=P, keep=40, first=2, last=3, w=P, w_stride=256, ws=P, ws_bytes=1 << 40)
+    a.update(kw)
+    st = xb.LIB.xc_op_kv_evict(ctypes.addressof(d), a["n"], a["seqs"], a["keep"], a["first"], a["last"], a["w"], a["w_stride"],
+                               None, a["ws"], a["ws_bytes"], None)
+    assert st == xb.XC_EINVAL
+    assert msg in xb.last_error(None), xb.last_error(None)
+
+
+def test_eviction_of_nothing_and_from_bad_caches(xb):
+    d = desc(xb)
+    assert xb.LIB.xc_op_kv_evict(ctypes.addressof(d), 0, None, 40, 0, 0, P, 256, None, None, 0, None) == xb.XC_OK
+    assert xb.LIB.xc_op_kv_evict_workspace_bytes(ctypes.addressof(d), 0, 40) == 0
+    assert xb.LIB.xc_op_kv_evict_workspace_bytes(None, 1, 40) == 0
+    for kw in (dict(page_size=24), dict(k=0), dict(table=0)):
+        bad = desc(xb, **kw)
+        assert xb.LIB.xc_op_kv_evict(ctypes.addressof(bad), 1, P, 40, 0, 0, P, 256, None, P, 1 << 30, None) == xb.XC_EINVAL
