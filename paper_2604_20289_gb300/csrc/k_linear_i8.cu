@@ -78,6 +78,9 @@ template <typename T> __device__ __forceinline__ float quant(float x, float r, f
     return q;
 }
 
+// Far from 1 both sides of the quotient are taken times a power of two, so that nothing over- or underflows.
+__device__ __forceinline__ float quant_factor(float a) { return a > 0x1p100f ? 0x1p-100f : (a < 0x1p-60f ? 0x1p80f : 1.0f); }
+
 // TPR threads a row; each keeps its first four vectors of eight elements in
 // registers and reads the others again (rows of more than 32 TPR elements).
 // HBM bound.  A row without a finite largest magnitude gets scale NaN and zeros.
@@ -116,8 +119,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
     const bool finite = top < 0x7f800000u;
     const float a = __uint_as_float(top);
     if (t == 0) scale[row] = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
-    // far from 1, both sides of the quotient times a power of two, so that nothing over- or underflows
-    const float f = a > 0x1p100f ? 0x1p-100f : (a < 0x1p-60f ? 0x1p80f : 1.0f), as = a * f;
+    const float f = quant_factor(a), as = a * f;
     const float r = finite && a > 0.0f ? __fdiv_rn(127.0f, as) : 0.0f;
     Q *dst = q + (size_t)row * K;
     auto put = [&](const Vec8<T> &z, int v) {
@@ -197,15 +199,15 @@ __global__ void __launch_bounds__(256) widen_kernel(const uint4 *q, uint4 *out, 
 
 // ------------------------------------------------------------------ product
 constexpr int I8_BM = 128, I8_BK = 128;        // channels and depth of a weight tile
-constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_W = 12, I8_MAX_B = 24, I8_A = 8;
+constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_W = 12, I8_MAX_S = 8;
 constexpr int I8_THREADS = 640;
-constexpr int I8_A_COL = 256;                  // widened weights: 8 slots of depth 64, 32 columns each, behind the sums
+constexpr int I8_A_COL = 256;                  // widened weights: slots of depth 64, 32 columns each, behind the sums
 
 struct I8Sched {
     int M, N, NT;              // tokens, channels, tokens of a tile (a multiple of 16)
     int m_tiles, n_tiles, KT;  // tiles of tokens and channels, weight tiles along the depth
     int n_full, G;             // tiles that CTAs run whole, in rounds; the rest is cut
-    int wst, bst;              // ring slots: weights of depth 128, tokens of depth 64
+    int wst, st;               // ring slots: weights of depth 128; tokens and widened weights of depth 64
     int acc2;                  // two sets of sums (NT <= 128)
     int epi;
     const float *a_scale, *w_scale, *bias, *gate;
@@ -289,26 +291,23 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
     linear_i8_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                      const __grid_constant__ I8Sched s, int *err) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * I8_MAX_W + 2 * I8_MAX_B + 2 * I8_A + 5];
+    __shared__ uint64_t bars[2 * I8_MAX_W + 2 * I8_MAX_S + 5];
     __shared__ uint32_t tmem_slot;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int b_bytes = s.NT * 128;
     uint8_t *sW = smem, *sB = smem + s.wst * I8_W_BYTES;
-    uint64_t *w_full = bars, *w_empty = w_full + I8_MAX_W, *b_full = w_empty + I8_MAX_W, *b_empty = b_full + I8_MAX_B;
-    uint64_t *a_full = b_empty + I8_MAX_B, *a_empty = a_full + I8_A, *acc_full = a_empty + I8_A, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
+    uint64_t *w_full = bars, *w_empty = w_full + I8_MAX_W;
+    uint64_t *full = w_empty + I8_MAX_W, *empty = full + I8_MAX_S;      // tokens landed and weights widened; both read
+    uint64_t *acc_full = empty + I8_MAX_S, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < s.wst; ++i) {
             mbar_init(&w_full[i], 1);
             mbar_init(&w_empty[i], 256);
         }
-        for (int i = 0; i < s.bst; ++i) {
-            mbar_init(&b_full[i], 1);
-            mbar_init(&b_empty[i], 1);
-        }
-        for (int i = 0; i < I8_A; ++i) {
-            mbar_init(&a_full[i], 128);
-            mbar_init(&a_empty[i], 1);
+        for (int i = 0; i < s.st; ++i) {
+            mbar_init(&full[i], 129);
+            mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
@@ -352,14 +351,14 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
                 int mb, nb;
                 i8_tile(s, w.tile, mb, nb);
                 for (int kt = 2 * w.k0; kt < 2 * w.k1; ++kt, ++it) {
-                    const int i = it % s.bst;
-                    if (!(ok = mbar_wait(&b_empty[i], ((it / s.bst) & 1) ^ 1, err, ERR_WAIT_PRODUCER))) break;
-                    mbar_expect_tx(&b_full[i], b_bytes);
-                    tma_load_2d(sB + i * b_bytes, &tmA, &b_full[i], kt * 64, mb * s.NT);
+                    const int i = it % s.st;
+                    if (!(ok = mbar_wait(&empty[i], ((it / s.st) & 1) ^ 1, err, ERR_WAIT_PRODUCER))) break;
+                    mbar_expect_tx(&full[i], b_bytes);
+                    tma_load_2d(sB + i * b_bytes, &tmA, &full[i], kt * 64, mb * s.NT);
                 }
             }
-            for (int j = max(it - s.bst, 0); j < it; ++j)
-                mbar_wait(&b_full[j % s.bst], (j / s.bst) & 1, err, ERR_WAIT_PRODUCER);
+            for (int j = max(it - s.st, 0); j < it; ++j)
+                mbar_wait(&full[j % s.st], (j / s.st) & 1, err, ERR_WAIT_PRODUCER);
         }
     } else if (warp == 1) {
         // D f32, A and B f16, N = NT, M = 128
@@ -368,7 +367,8 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
         auto wait = [&](uint64_t *b, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(b, parity & 1, err, ERR_WAIT_MMA)) != 0;
         };
-        int it = 0, local = 0, bi = 0, b_ph = 0;
+        int local = 0, i = 0;
+        uint32_t ph = 0;
         bool ok = true;
         while (ok && w.next(s)) {
             const int buf = s.acc2 ? local & 1 : 0, use = s.acc2 ? local >> 1 : local;
@@ -376,25 +376,19 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
             if (!(ok = wait(&acc_empty[buf], use ^ 1))) break;
             tc_fence_after();
             const uint32_t acc = tmem + buf * 128;
-            for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    const int a = (2 * it + h) % I8_A;
-                    if (!(ok = wait(&a_full[a], (2 * it + h) / I8_A) && wait(&b_full[bi], b_ph))) break;
-                    tc_fence_after();
-                    const uint64_t db = d0 + (uint64_t)((bi * b_bytes) >> 4);
-                    const uint32_t ta = tmem + I8_A_COL + 32 * a;
+            for (int n = 2 * (w.k1 - w.k0), first = 0; n > 0; --n, first = 1) {
+                if (!(ok = wait(&full[i], ph))) break;
+                tc_fence_after();
+                const uint64_t db = d0 + (uint64_t)((i * b_bytes) >> 4);
+                const uint32_t ta = tmem + I8_A_COL + 32 * i;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        tc_mma_tmem_a_warp(acc, ta + 8 * k, db + 2 * k, idesc, (kt > w.k0 || h > 0 || k > 0) ? 1u : 0u);
-                    tc_commit_warp(&b_empty[bi]);
-                    tc_commit_warp(&a_empty[a]);
-                    if (++bi == s.bst) {
-                        bi = 0;
-                        b_ph ^= 1;
-                    }
+                for (int k = 0; k < 4; ++k) tc_mma_tmem_a_warp(acc, ta + 8 * k, db + 2 * k, idesc, k > 0 ? 1u : (uint32_t)first);
+                tc_commit_warp(&empty[i]);
+                if (++i == s.st) {
+                    i = 0;
+                    ph ^= 1;
                 }
-                if (!ok) break;
             }
             if (ok) tc_commit_warp(&acc_full[buf]);
         }
@@ -405,13 +399,18 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
     } else if (warp >= 4 && warp < 12) {
         const int g = (warp - 4) >> 2, q = warp & 3, r = 32 * q + lane;
         const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + I8_A_COL;
-        int it = 0;
+        // slots of the two rings and the parities of their turns: this group has every other slot of depth 64
+        int i = 0, a = g;
+        uint32_t w_ph = 0, a_ph = 1;
         bool ok = true;
         while (ok && w.next(s)) {
-            for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
-                const int i = it % s.wst, a = (2 * it + g) % I8_A;
-                ok = mbar_wait(&w_full[i], (it / s.wst) & 1, err, ERR_WAIT_TMA);
-                ok = ok && mbar_wait(&a_empty[a], (((2 * it + g) / I8_A) & 1) ^ 1, err, ERR_WAIT_MMA);
+            for (int kt = w.k0; kt < w.k1; ++kt) {
+                if (a >= s.st) {
+                    a -= s.st;
+                    a_ph ^= 1;
+                }
+                ok = mbar_wait(&w_full[i], w_ph, err, ERR_WAIT_TMA);
+                ok = ok && mbar_wait(&empty[a], a_ph, err, ERR_WAIT_MMA);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 tc_fence_after();
                 const uint8_t *src = sW + i * I8_W_BYTES + r * 128;
@@ -427,7 +426,12 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
                 mbar_arrive(&w_empty[i]);
                 tmem_st32_sync(t0 + 32 * a, x);
                 tc_fence_before();
-                mbar_arrive(&a_full[a]);
+                mbar_arrive(&full[a]);
+                a += 2;
+                if (++i == s.wst) {
+                    i = 0;
+                    w_ph ^= 1;
+                }
             }
         }
     } else if (warp >= 12) {
@@ -529,7 +533,242 @@ __global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_con
     }
 }
 
+// -------------------------------------------------------------- few tokens
+// A step of a few tokens waits for the weights' bytes, so everything else goes
+// into the one kernel: each CTA (one an SM) quantises all tokens into its shared
+// memory as fp16, in the order of the MMA's fragments, and streams its share of the
+// channels, N / G each.  The share is a line of (16 channels, depth 64) units that
+// its 16 warps split evenly; a lane loads 16 consecutive weights of two
+// channels straight into registers, I8S_AHEAD units ahead, and widens them there.  (An MMA may take its
+// depth in any order, so the 16 are its numbers 4 j .. 4 j + 3 of product j, and no lane
+// exchanges anything.)  The warps' sums meet in shared memory, in warp order.
+constexpr int I8S_THREADS = 512, I8S_WARPS = I8S_THREADS / 32, I8S_AHEAD = 8, I8S_GROUPS = 16;
+constexpr int I8S_MAX_M = 32, I8S_TOKEN_BYTES = 144 * 1024;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 load_stream(const void *p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+struct I8Small {
+    int M, N, K, KB, G;        // KB: units of depth 64
+    int epi;
+    const void *A;
+    const float *a_scale;      // or NULL: quantised here
+    const signed char *W;
+    const float *w_scale, *bias, *gate;
+    const void *resid;
+    void *out;
+};
+
+// Quantises (or widens) the tokens into dst: vector v of 8 numbers of token m at
+// [v / 8][v % 2][m][v / 2 % 4].
+template <typename T>
+__device__ __forceinline__ void i8_stage_tokens(const I8Small &s, uint4 *dst, float *sh_scale, unsigned *sh_top) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = s.K / 8, nvp = s.KB * 8;
+    auto place = [&](int m, int v) -> uint4 & { return dst[((size_t)((v >> 3) * 2 + (v & 1)) * s.M + m) * 4 + ((v >> 1) & 3)]; };
+    if (s.a_scale != nullptr) {
+        const uint2 *A = reinterpret_cast<const uint2 *>(s.A);
+        for (int x = tid; x < s.M * nvp; x += I8S_THREADS) {
+            const int m = x / nvp, v = x - m * nvp;
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (v < nv) {
+                const uint2 w = A[(size_t)m * nv + v];
+                widen4(w.x, u.x, u.y);
+                widen4(w.y, u.z, u.w);
+            }
+            place(m, v) = u;
+        }
+        if (tid < s.M) sh_scale[tid] = s.a_scale[tid];
+        return;
+    }
+    const T *A = reinterpret_cast<const T *>(s.A);
+    int wpr = 1;                                       // warps a token, a power of two
+    while (2 * wpr * s.M <= I8S_WARPS) wpr *= 2;
+    const int per = I8S_WARPS / wpr, part = warp % wpr;
+    if (tid < s.M) sh_top[tid] = 0;
+    __syncthreads();
+    for (int m = warp / wpr; m < s.M; m += per) {
+        unsigned top = 0;
+        for (int v = part * 32 + lane; v < nv; v += wpr * 32) {
+            Vec8<T> z;
+            z.load(A + (size_t)m * s.K + 8 * v);
+            top = z.top(top);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) atomicMax(&sh_top[m], top);
+    }
+    __syncthreads();
+    for (int m = warp / wpr; m < s.M; m += per) {
+        const unsigned top = sh_top[m];
+        const bool finite = top < 0x7f800000u;
+        const float a = __uint_as_float(top), f = quant_factor(a), as = a * f;
+        const float r = finite && a > 0.0f ? __fdiv_rn(127.0f, as) : 0.0f;
+        if (part == 0 && lane == 0) sh_scale[m] = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
+        for (int v = part * 32 + lane; v < nvp; v += wpr * 32) {
+            __half2 h[4];
+            float e[8] = {};
+            if (v < nv && finite) {
+                Vec8<T> z;
+                z.load(A + (size_t)m * s.K + 8 * v);
+                z.get(e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = quant<T>(e[i] * f, r, as);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(e[2 * i], e[2 * i + 1]);
+            place(m, v) = *reinterpret_cast<uint4 *>(h);
+        }
+    }
+}
+
+template <typename T, int NT8>
+__global__ void __launch_bounds__(I8S_THREADS, 1) linear_i8_small_kernel(const __grid_constant__ I8Small s) {
+    extern __shared__ __align__(16) uint4 sm_small[];
+    __shared__ float sh_scale[I8S_MAX_M];
+    __shared__ unsigned sh_top[I8S_MAX_M];
+    constexpr int MP = 8 * NT8;
+    uint4 *tok = sm_small;
+    float *part = reinterpret_cast<float *>(tok + (size_t)s.KB * 8 * s.M);        // [slot][16][MP]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
+    pdl_wait();
+    pdl_release();
+    const int row0 = (int)((long long)s.N * blockIdx.x / s.G), row1 = (int)((long long)s.N * (blockIdx.x + 1) / s.G);
+    bool staged = false;
+    for (int p0 = row0; p0 < row1; p0 += 16 * I8S_GROUPS) {
+        const int rows = min(row1 - p0, 16 * I8S_GROUPS), groups = (rows + 15) / 16;
+        const int U = groups * s.KB, q = U / I8S_WARPS, rem = U - q * I8S_WARPS;
+        const int u0 = warp * q + min(warp, rem), u1 = u0 + q + (warp < rem ? 1 : 0);
+        uint4 w[I8S_AHEAD][2];
+        // unit -> this lane's 16 weights of rows gid and gid + 8
+        int lg = u0 / s.KB, lk = u0 - lg * s.KB, lu = u0;      // next unit to load
+        auto fetch = [&](uint4 (&x)[2]) {
+            const int k = 64 * lk + 16 * tig;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 16 * lg + 8 * h + gid;
+                x[h] = lu < u1 && r < rows && k < s.K ? load_stream(s.W + (size_t)(p0 + r) * s.K + k) : make_uint4(0, 0, 0, 0);
+            }
+            ++lu;
+            if (++lk == s.KB) {
+                lk = 0;
+                ++lg;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < I8S_AHEAD; ++i) fetch(w[i]);
+        if (!staged) {
+            i8_stage_tokens<T>(s, tok, sh_scale, sh_top);
+            staged = true;
+        }
+        __syncthreads();                               // tokens staged; the last pass's sums read
+        int g = u0 / s.KB, k = u0 - g * s.KB;
+        float acc[NT8][4] = {};
+        // warp w's sums of group g: slot g + w (both only grow)
+        auto flush = [&]() {
+            float *dst = part + (size_t)(g + warp) * 16 * MP;
+#pragma unroll
+            for (int n = 0; n < NT8; ++n) {
+                *reinterpret_cast<float2 *>(dst + gid * MP + 8 * n + 2 * tig) = make_float2(acc[n][0], acc[n][1]);
+                *reinterpret_cast<float2 *>(dst + (gid + 8) * MP + 8 * n + 2 * tig) = make_float2(acc[n][2], acc[n][3]);
+                acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+            }
+        };
+        for (int u = u0; u < u1; u += I8S_AHEAD) {
+#pragma unroll
+            for (int i = 0; i < I8S_AHEAD; ++i) {
+                if (u + i >= u1) break;
+                const unsigned *x0 = reinterpret_cast<const unsigned *>(&w[i][0]), *x1 = reinterpret_cast<const unsigned *>(&w[i][1]);
+                unsigned a[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    widen4(x0[j], a[j][0], a[j][2]);
+                    widen4(x1[j], a[j][1], a[j][3]);
+                }
+                fetch(w[i]);
+#pragma unroll
+                for (int n = 0; n < NT8; ++n) {
+                    const int m = 8 * n + gid;
+                    uint4 b[2] = {};
+                    if (m < s.M) {
+                        const uint4 *t = tok + ((size_t)(2 * k) * s.M + m) * 4 + tig;
+                        b[0] = t[0];
+                        b[1] = t[4 * s.M];
+                    }
+                    mma_f16(acc[n], a[0][0], a[0][1], a[0][2], a[0][3], b[0].x, b[0].y);
+                    mma_f16(acc[n], a[1][0], a[1][1], a[1][2], a[1][3], b[0].z, b[0].w);
+                    mma_f16(acc[n], a[2][0], a[2][1], a[2][2], a[2][3], b[1].x, b[1].y);
+                    mma_f16(acc[n], a[3][0], a[3][1], a[3][2], a[3][3], b[1].z, b[1].w);
+                }
+                if (++k == s.KB) {
+                    flush();
+                    k = 0;
+                    ++g;
+                }
+            }
+        }
+        if (u1 > u0 && k > 0) flush();
+        __syncthreads();
+        // every output of the pass: its group's sums, in warp order
+        const T *resid = reinterpret_cast<const T *>(s.resid);
+        T *out = reinterpret_cast<T *>(s.out);
+        for (int x = tid; x < rows * s.M; x += I8S_THREADS) {
+            const int m = x / rows, r = x - m * rows, grp = r >> 4, n = p0 + r;
+            const int a0 = grp * s.KB, a1 = a0 + s.KB - 1, longer = rem * (q + 1);
+            const int w0 = a0 < longer ? a0 / (q + 1) : rem + (a0 - longer) / q, w1 = a1 < longer ? a1 / (q + 1) : rem + (a1 - longer) / q;
+            float v = 0.0f;
+            for (int y = w0; y <= w1; ++y) v += part[((size_t)(grp + y) * 16 + (r & 15)) * MP + m];
+            const size_t at = (size_t)m * s.N + n;
+            const float res = s.epi == EPI_RESID_GATE ? to_f(resid[at]) : 0.0f, gt = s.epi == EPI_RESID_GATE ? s.gate[n] : 0.0f;
+            out[at] = from_f<T>(i8_epilogue<T>(s.epi, v, sh_scale[m], s.w_scale[n], s.bias[n], gt, res));
+        }
+    }
+}
+
 // ------------------------------------------------------------------- host
+// Tokens that fit every CTA's shared memory go with the weights' stream.
+static bool i8_small(int M, int K) { return M <= I8S_MAX_M && (long)M * ((K + 63) / 64 * 64) * 2 <= I8S_TOKEN_BYTES; }
+
+template <typename T, int NT8>
+static cudaError_t i8_small_launch(const I8Small &s, cudaStream_t st) {
+    static bool done = false;
+    const int part = (I8S_GROUPS + I8S_WARPS) * 16 * 8 * NT8 * 4;
+    if (!done) {
+        const cudaError_t e = cudaFuncSetAttribute(linear_i8_small_kernel<T, NT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, I8S_TOKEN_BYTES + part);
+        if (e != cudaSuccess) return e;
+        done = true;
+    }
+    return launch_pdl(linear_i8_small_kernel<T, NT8>, dim3(s.G), dim3(I8S_THREADS), s.M * s.KB * 128 + part, st, s);
+}
+template <typename T>
+static cudaError_t i8_small_run(const LinearI8Args &a, cudaStream_t st) {
+    I8Small s{};
+    s.M = a.M;
+    s.N = a.N;
+    s.K = a.K;
+    s.KB = (a.K + 63) / 64;
+    s.G = std::min(device_sms(), (a.N + 7) / 8);
+    s.epi = a.epi;
+    s.A = a.A;
+    s.a_scale = a.a_scale;
+    s.W = a.W;
+    s.w_scale = a.w_scale;
+    s.bias = a.bias;
+    s.gate = a.gate;
+    s.resid = a.resid;
+    s.out = a.out;
+    if (a.M <= 8) return i8_small_launch<T, 1>(s, st);
+    if (a.M <= 16) return i8_small_launch<T, 2>(s, st);
+    return i8_small_launch<T, 4>(s, st);
+}
+
 struct I8Plan {
     I8Sched s;
     size_t off_scale, off_part, bytes;
@@ -551,17 +790,18 @@ static I8Plan i8_plan(int M, int N, int K) {
     s.n_full = tiles / s.G * s.G;
     p.cut = s.n_full < tiles;
     s.acc2 = s.NT <= 128;
-    const int budget = 222 * 1024;
-    s.wst = std::min(I8_MAX_W, std::max(3, budget / (I8_W_BYTES + 256 * s.NT)));
-    s.bst = std::min(std::min(I8_MAX_B, 2 * s.wst), (budget - s.wst * I8_W_BYTES) / (128 * s.NT));
-    p.smem = s.wst * I8_W_BYTES + s.bst * 128 * s.NT + 1024;
+    // a slot pair for every weight tile, up to the tensor memory's 8, and weights as deep as fit
+    const int budget = 222 * 1024, b_bytes = 128 * s.NT;
+    s.st = std::min(I8_MAX_S, std::max(4, budget / (I8_W_BYTES / 2 + b_bytes)));
+    s.wst = std::min(I8_MAX_W, (budget - s.st * b_bytes) / I8_W_BYTES);
+    p.smem = s.wst * I8_W_BYTES + s.st * b_bytes + 1024;
     p.off_scale = ((size_t)M * K * 2 + 255) / 256 * 256;
     p.off_part = p.off_scale + ((size_t)s.m_tiles * s.NT + 16) * sizeof(float);
     p.off_part = (p.off_part + 255) / 256 * 256;
     p.bytes = p.off_part + (p.cut ? (size_t)2 * s.G * s.NT * I8_BM * sizeof(float) : 0);
     return p;
 }
-size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_plan(M, N, K).bytes; }
+size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_small(M, K) ? 256 : i8_plan(M, N, K).bytes; }
 
 template <typename T>
 static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUtensorMap &ta, int *err, cudaStream_t st) {
@@ -577,6 +817,7 @@ static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUten
 }
 
 cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st) {
+    if (i8_small(a.M, a.K)) return a.dtype == XC_BF16 ? i8_small_run<bf16>(a, st) : i8_small_run<float>(a, st);
     I8Plan p = i8_plan(a.M, a.N, a.K);
     I8Sched &s = p.s;
     char *w = reinterpret_cast<char *>(ws);
