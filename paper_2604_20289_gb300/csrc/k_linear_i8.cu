@@ -10,7 +10,7 @@
 // waits for.  The tokens are quantised by a kernel of their own (as fp16 whole
 // numbers, ready for TMA); the weights are widened on their way into tensor
 // memory, where they are the MMA's A operand: 128 channels are its rows, up to
-// 256 tokens its columns.
+// 192 tokens its columns.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -199,71 +199,75 @@ __global__ void __launch_bounds__(256) widen_kernel(const uint4 *q, uint4 *out, 
 
 // ------------------------------------------------------------------ product
 constexpr int I8_BM = 128, I8_BK = 128;        // channels and depth of a weight tile
-constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_W = 12, I8_MAX_S = 8;
-constexpr int I8_THREADS = 640;
-constexpr int I8_A_COL = 256;                  // widened weights: slots of depth 64, 32 columns each, behind the sums
+constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_ST = 8, I8_MAX_A = 8;
+constexpr int I8_THREADS = 640, I8_SMEM = 220 * 1024;
+constexpr int I8_NT = 192;                     // most tokens of a tile: two sets of sums and four slots of widened weights
 
 struct I8Sched {
     int M, N, NT;              // tokens, channels, tokens of a tile (a multiple of 16)
-    int m_tiles, n_tiles, KT;  // tiles of tokens and channels, weight tiles along the depth
-    int n_full, G;             // tiles that CTAs run whole, in rounds; the rest is cut
-    int wst, st;               // ring slots: weights of depth 128; tokens and widened weights of depth 64
-    int acc2;                  // two sets of sums (NT <= 128)
-    int epi;
+    int m_tiles, n_pairs, KT;  // tiles of tokens, pairs of tiles of channels, tiles along the depth
+    int n_full, P;             // tile pairs that CTA pairs run whole, in rounds (the rest is cut); CTA pairs
+    int st, as, acs;           // stages of depth 128 in shared memory; slots of depth 64 in tensor memory; columns of a set of sums
+    int epi, vec;              // vec: 16-byte outputs
     const float *a_scale, *w_scale, *bias, *gate;
     const void *resid;
     void *out;
-    float *part;               // [2 G][NT][128] sums of cut tiles
+    float *part;               // [4 P][NT][128] sums of cut tiles
 
-    __host__ __device__ __forceinline__ unsigned line() const { return (unsigned)(m_tiles * n_tiles - n_full) * KT; }
+    __host__ __device__ __forceinline__ unsigned line() const { return (unsigned)(m_tiles * n_pairs - n_full) * KT; }
 };
 
-// Tiles in super-rows of 16 channel blocks, channels fastest: the tiles that run
-// at one time share their weights and tokens in L2.
-__host__ __device__ __forceinline__ void i8_tile(const I8Sched &s, int tile, int &mb, int &nb) {
-    const int per = 16 * s.m_tiles, grp = tile / per, first = 16 * grp, loc = tile - grp * per;
-    const int gn = s.n_tiles - first < 16 ? s.n_tiles - first : 16;
-    nb = first + loc % gn;
+// Tile pairs in super-rows of 8 pairs of channel blocks, channels fastest: the tiles that
+// run at one time share their weights and tokens in L2.
+__host__ __device__ __forceinline__ void i8_tile(const I8Sched &s, int tile, int &mb, int &pb) {
+    const int per = 8 * s.m_tiles, grp = tile / per, first = 8 * grp, loc = tile - grp * per;
+    const int gn = s.n_pairs - first < 8 ? s.n_pairs - first : 8;
+    pb = first + loc % gn;
     mb = loc / gn;
 }
-// The cut tiles' depth as one line over the CTAs.
+// The cut tiles' depth as one line over the CTA pairs.
 struct I8Line {
     unsigned q, r;
-    __host__ __device__ __forceinline__ I8Line(unsigned T, unsigned G) : q(T / G), r(T - q * G) {}
+    __host__ __device__ __forceinline__ I8Line(unsigned T, unsigned P) : q(T / P), r(T - q * P) {}
     __host__ __device__ __forceinline__ unsigned begin(unsigned c) const { return q * c + (c < r ? c : r); }
     __host__ __device__ __forceinline__ unsigned owner(unsigned x) const {
         const unsigned longer = r * (q + 1);
         return x < longer ? x / (q + 1) : r + (x - longer) / q;
     }
 };
-// The pieces of a CTA, as each of its roles walks them: whole tiles c, c + G, ...,
-// then its share of the line, which touches two tiles at most.
+// The pieces of a CTA pair, as each role walks them: whole tile pairs c, c + P, ..., then
+// its share of the line, which touches two tile pairs at most.
 struct I8Walk {
-    int tile, k0, k1, slot;    // slot: of the sums of a cut piece, -1: a whole tile
+    int mb, nb;                // tile of tokens, of channels (this CTA's of the pair)
+    int k0, k1, slot;          // slot: of the sums of a cut piece, -1: a whole tile
     int next_full;
     unsigned x, end;
     int first;
-    __device__ __forceinline__ I8Walk(const I8Sched &s, int c) : tile(0), k0(0), k1(0), slot(-1), next_full(c), first(1) {
-        const I8Line l(s.line(), s.G);
+    __device__ __forceinline__ I8Walk(const I8Sched &s, int c) : mb(0), nb(0), k0(0), k1(0), slot(-1), next_full(c), first(1) {
+        const I8Line l(s.line(), s.P);
         x = l.begin(c);
         end = l.begin(c + 1);
     }
     __device__ __forceinline__ bool next(const I8Sched &s) {
+        int tile;
         if (next_full < s.n_full) {
             tile = next_full;
-            next_full += s.G;
+            next_full += s.P;
             k0 = 0;
             k1 = s.KT;
-            return true;
+        } else {
+            if (x >= end) return false;
+            const int t = x / s.KT;
+            tile = s.n_full + t;
+            k0 = x - t * s.KT;
+            k1 = min(s.KT, k0 + (int)(end - x));
+            x += k1 - k0;
+            slot = k1 - k0 == s.KT ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
+            first = 0;
         }
-        if (x >= end) return false;
-        const int t = x / s.KT;
-        tile = s.n_full + t;
-        k0 = x - t * s.KT;
-        k1 = min(s.KT, k0 + (int)(end - x));
-        x += k1 - k0;
-        slot = k1 - k0 == s.KT ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
-        first = 0;
+        int pb;
+        i8_tile(s, tile, mb, pb);
+        nb = 2 * pb + ((int)blockIdx.x & 1);
         return true;
     }
 };
@@ -283,31 +287,84 @@ __device__ __forceinline__ float i8_epilogue(int epi, float acc, float sa, float
     return y;
 }
 
-// Warps: 0 loads weights, 1 issues the products, 2 loads tokens, 4-11 widen the
-// weights (thread = channel = TMEM lane, a half of each tile's depth to either four
-// warps), 12-19 write the outputs (two per TMEM quadrant, 16 tokens in turn).
+// Half of a tile of tokens into both CTAs of the pair: the bytes count on the barrier at the same place in either.
+__device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *tm, uint64_t *bar, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3}], [%4], %5;"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(smem_u32(bar)), "h"((unsigned short)3)
+        : "memory");
+}
+// Arrives at the barrier at this place in both CTAs of the pair when every product issued so far is done.
+__device__ __forceinline__ void tc_commit_pair_warp(uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t.reg .b32 r;\n\t"
+        "elect.sync r|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+        ::"r"(smem_u32(bar)), "h"((unsigned short)3)
+        : "memory");
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+}
+
+// Exchanges between lanes that turn a lane's 16 tokens of one channel into 8 consecutive
+// channels of two tokens: on return x[8 r + c] is channel 8 (lane / 8) + c of token 8 r + lane % 8.
+__device__ __forceinline__ void i8_turn(float (&x)[16], int lane) {
+    float y[16];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {                      // y[2 t + c]: channel pair of token 2 t + lane % 2
+        const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? x[2 * t] : x[2 * t + 1], 1);
+        y[2 * t] = (lane & 1) ? got : x[2 * t];
+        y[2 * t + 1] = (lane & 1) ? x[2 * t + 1] : got;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)                        // x[4 q + c]: 4 channels of token 4 q + lane % 4
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const float got = __shfl_xor_sync(0xffffffffu, (lane & 2) ? y[4 * q + c] : y[4 * q + 2 + c], 2);
+            x[4 * q + c] = (lane & 2) ? got : y[4 * q + c];
+            x[4 * q + 2 + c] = (lane & 2) ? y[4 * q + 2 + c] : got;
+        }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float got = __shfl_xor_sync(0xffffffffu, (lane & 4) ? x[8 * r + c] : x[8 * r + 4 + c], 4);
+            const float lo = (lane & 4) ? got : x[8 * r + c], hi = (lane & 4) ? x[8 * r + 4 + c] : got;
+            y[8 * r + c] = lo;
+            y[8 * r + 4 + c] = hi;
+        }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = y[i];
+}
+
+// Two CTAs run neighbouring tiles of channels with the same tokens: each loads half of the
+// tokens for both, which halves what they ask of L2 (a tile of 192 tokens and depth 64 is 32 KB
+// in 384 cycles of products, more than L2 hands an SM).
+// Warps: 0 loads, 1 issues the products, 4-11 widen the weights (thread = channel =
+// TMEM lane, a half of each tile's depth to either four warps), 12-19 write the outputs (two
+// per TMEM quadrant, half of the tokens each).
 template <typename T>
-__global__ void __launch_bounds__(I8_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     linear_i8_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                      const __grid_constant__ I8Sched s, int *err) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * I8_MAX_W + 2 * I8_MAX_S + 5];
+    __shared__ uint64_t bars[2 * I8_MAX_ST + 2 * I8_MAX_A + 5];
     __shared__ uint32_t tmem_slot;
+    __shared__ __align__(16) float sh_scale[8][I8_NT / 2 + 16];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    const int b_bytes = s.NT * 128;
-    uint8_t *sW = smem, *sB = smem + s.wst * I8_W_BYTES;
-    uint64_t *w_full = bars, *w_empty = w_full + I8_MAX_W;
-    uint64_t *full = w_empty + I8_MAX_W, *empty = full + I8_MAX_S;      // tokens landed and weights widened; both read
-    uint64_t *acc_full = empty + I8_MAX_S, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b_bytes = s.NT * 128, stage = I8_W_BYTES + 2 * b_bytes;      // weights, then tokens of depth 64 twice
+    uint64_t *full = bars, *empty = full + I8_MAX_ST, *a_full = empty + I8_MAX_ST, *a_empty = a_full + I8_MAX_A;
+    uint64_t *acc_full = a_empty + I8_MAX_A, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < s.wst; ++i) {
-            mbar_init(&w_full[i], 1);
-            mbar_init(&w_empty[i], 256);
-        }
         for (int i = 0; i < s.st; ++i) {
-            mbar_init(&full[i], 129);
-            mbar_init(&empty[i], 1);
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 2);                   // both CTAs have read their copy of the tokens
+        }
+        for (int i = 0; i < s.as; ++i) {
+            mbar_init(&a_full[i], 128);
+            mbar_init(&a_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
@@ -319,72 +376,82 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
     if (warp == 1) tmem_alloc(&tmem_slot, 512);
     tc_fence_before();
     __syncthreads();
+    cluster_sync_all();                                // the other CTA's barriers are set up too
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    I8Walk w(s, blockIdx.x);
+    const int a_col = 2 * s.acs;
+    I8Walk w(s, blockIdx.x >> 1);
 
     if (warp == 0) {
         // The kernel before this one in the stream (the quantisation) began after
         // everything before it had ended, so the weights need no wait.
         if (lane == 0) {
-            int it = 0;
-            bool ok = true;
-            while (ok && w.next(s)) {
-                int mb, nb;
-                i8_tile(s, w.tile, mb, nb);
-                for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
-                    const int i = it % s.wst;
-                    if (!(ok = mbar_wait(&w_empty[i], ((it / s.wst) & 1) ^ 1, err, ERR_WAIT_PRODUCER))) break;
-                    mbar_expect_tx(&w_full[i], I8_W_BYTES);
-                    tma_load_2d(sW + i * I8_W_BYTES, &tmW, &w_full[i], kt * I8_BK, nb * I8_BM);
-                }
-            }
-            for (int j = max(it - s.wst, 0); j < it; ++j)         // every copy has landed before the CTA exits
-                mbar_wait(&w_full[j % s.wst], (j / s.wst) & 1, err, ERR_WAIT_PRODUCER);
-        }
-    } else if (warp == 2) {
-        if (lane == 0) {
+            const int half = s.NT / 2 * rank;          // rows of the tile that this CTA loads for both
+            auto load_w = [&](const I8Walk &x, int i, int kt) {
+                mbar_expect_tx(&full[i], stage);
+                tma_load_2d(smem + i * stage, &tmW, &full[i], kt * I8_BK, x.nb * I8_BM);
+            };
+            int ahead = 0;
+            for (I8Walk x(s, blockIdx.x >> 1); ahead < s.st && x.next(s);)
+                for (int kt = x.k0; kt < x.k1 && ahead < s.st; ++kt, ++ahead) load_w(x, ahead, kt);
             pdl_wait();
-            int it = 0;
+            int i = 0, it = 0;
+            uint32_t ph = 1;
             bool ok = true;
             while (ok && w.next(s)) {
-                int mb, nb;
-                i8_tile(s, w.tile, mb, nb);
-                for (int kt = 2 * w.k0; kt < 2 * w.k1; ++kt, ++it) {
-                    const int i = it % s.st;
-                    if (!(ok = mbar_wait(&empty[i], ((it / s.st) & 1) ^ 1, err, ERR_WAIT_PRODUCER))) break;
-                    mbar_expect_tx(&full[i], b_bytes);
-                    tma_load_2d(sB + i * b_bytes, &tmA, &full[i], kt * 64, mb * s.NT);
+                for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
+                    if (it >= ahead) {
+                        if (!(ok = mbar_wait(&empty[i], ph, err, ERR_WAIT_PRODUCER))) break;
+                        load_w(w, i, kt);
+                    }
+                    for (int h = 0; h < 2; ++h)
+                        tma_load_2d_pair(smem + i * stage + I8_W_BYTES + h * b_bytes + half * 128, &tmA, &full[i], kt * I8_BK + 64 * h, w.mb * s.NT + half);
+                    if (++i == s.st) {
+                        i = 0;
+                        ph ^= 1;
+                    }
                 }
             }
-            for (int j = max(it - s.st, 0); j < it; ++j)
+            for (int j = max(it - s.st, 0); j < it; ++j)          // every copy has landed before the CTA exits
                 mbar_wait(&full[j % s.st], (j / s.st) & 1, err, ERR_WAIT_PRODUCER);
         }
     } else if (warp == 1) {
         // D f32, A and B f16, N = NT, M = 128
         const uint32_t idesc = (1u << 4) | ((uint32_t)(s.NT >> 3) << 17) | ((uint32_t)(I8_BM >> 4) << 24);
-        const uint64_t d0 = sdesc_sw128(smem_u32(sB), 16, 1024);
+        const uint64_t d0 = sdesc_sw128(smem_u32(smem) + I8_W_BYTES, 16, 1024);
         auto wait = [&](uint64_t *b, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(b, parity & 1, err, ERR_WAIT_MMA)) != 0;
         };
-        int local = 0, i = 0;
-        uint32_t ph = 0;
+        int local = 0, i = 0, a = 0;
+        uint32_t ph = 0, a_ph = 0;
         bool ok = true;
         while (ok && w.next(s)) {
-            const int buf = s.acc2 ? local & 1 : 0, use = s.acc2 ? local >> 1 : local;
+            const int buf = local & 1, use = local >> 1;
             ++local;
             if (!(ok = wait(&acc_empty[buf], use ^ 1))) break;
             tc_fence_after();
-            const uint32_t acc = tmem + buf * 128;
+            const uint32_t acc = tmem + buf * s.acs;
 #pragma unroll 1
-            for (int n = 2 * (w.k1 - w.k0), first = 0; n > 0; --n, first = 1) {
+            for (int kt = w.k0; kt < w.k1; ++kt) {
                 if (!(ok = wait(&full[i], ph))) break;
-                tc_fence_after();
-                const uint64_t db = d0 + (uint64_t)((i * b_bytes) >> 4);
-                const uint32_t ta = tmem + I8_A_COL + 32 * i;
+                const uint64_t db = d0 + (uint64_t)((i * stage) >> 4);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) tc_mma_tmem_a_warp(acc, ta + 8 * k, db + 2 * k, idesc, k > 0 ? 1u : (uint32_t)first);
-                tc_commit_warp(&empty[i]);
+                for (int h = 0; h < 2; ++h) {
+                    if (!(ok = wait(&a_full[a], a_ph))) break;
+                    tc_fence_after();
+                    const uint64_t dh = db + (uint64_t)((h * b_bytes) >> 4);
+                    const uint32_t ta = tmem + a_col + 32 * a;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma_tmem_a_warp(acc, ta + 8 * k, dh + 2 * k, idesc, h + k > 0 ? 1u : (kt > w.k0 ? 1u : 0u));
+                    tc_commit_warp(&a_empty[a]);
+                    if (++a == s.as) {
+                        a = 0;
+                        a_ph ^= 1;
+                    }
+                }
+                if (!ok) break;
+                tc_commit_pair_warp(&empty[i]);
                 if (++i == s.st) {
                     i = 0;
                     ph ^= 1;
@@ -398,22 +465,22 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
         }
     } else if (warp >= 4 && warp < 12) {
         const int g = (warp - 4) >> 2, q = warp & 3, r = 32 * q + lane;
-        const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + I8_A_COL;
-        // slots of the two rings and the parities of their turns: this group has every other slot of depth 64
+        const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + a_col;
+        // stage and slot, and the parities of their turns: this group has every other slot
         int i = 0, a = g;
-        uint32_t w_ph = 0, a_ph = 1;
+        uint32_t ph = 0, a_ph = 1;
         bool ok = true;
         while (ok && w.next(s)) {
             for (int kt = w.k0; kt < w.k1; ++kt) {
-                if (a >= s.st) {
-                    a -= s.st;
+                if (a >= s.as) {
+                    a -= s.as;
                     a_ph ^= 1;
                 }
-                ok = mbar_wait(&w_full[i], w_ph, err, ERR_WAIT_TMA);
-                ok = ok && mbar_wait(&empty[a], a_ph, err, ERR_WAIT_MMA);
+                ok = mbar_wait(&full[i], ph, err, ERR_WAIT_TMA);
+                ok = ok && mbar_wait(&a_empty[a], a_ph, err, ERR_WAIT_MMA);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 tc_fence_after();
-                const uint8_t *src = sW + i * I8_W_BYTES + r * 128;
+                const uint8_t *src = smem + i * stage + r * 128;
                 uint32_t x[32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -423,14 +490,13 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
                     widen4(v.z, x[8 * c + 4], x[8 * c + 5]);
                     widen4(v.w, x[8 * c + 6], x[8 * c + 7]);
                 }
-                mbar_arrive(&w_empty[i]);
                 tmem_st32_sync(t0 + 32 * a, x);
                 tc_fence_before();
-                mbar_arrive(&full[a]);
+                mbar_arrive(&a_full[a]);
                 a += 2;
-                if (++i == s.wst) {
+                if (++i == s.st) {
                     i = 0;
-                    w_ph ^= 1;
+                    ph ^= 1;
                 }
             }
         }
@@ -440,56 +506,91 @@ __global__ void __launch_bounds__(I8_THREADS, 1)
         const uint32_t tq = tmem + ((uint32_t)(32 * q) << 16);
         const T *resid = reinterpret_cast<const T *>(s.resid);
         T *out = reinterpret_cast<T *>(s.out);
+        float *scale = sh_scale[warp - 12];
+        const int nc = s.NT / 16, ch0 = half ? (nc + 1) / 2 : 0, ch1 = half ? nc : (nc + 1) / 2;   // this warp's tokens, by 16
         int local = 0;
         bool ok = true;
         while (ok && w.next(s)) {
-            const int buf = s.acc2 ? local & 1 : 0, use = s.acc2 ? local >> 1 : local;
+            const int buf = local & 1, use = local >> 1;
             ++local;
-            int mb, nb;
-            i8_tile(s, w.tile, mb, nb);
-            const int m0 = mb * s.NT, ch = 32 * q + lane, n = nb * I8_BM + ch, nc = min(n, s.N - 1);
-            const int cols = min(s.NT, s.M - m0), chunks = (cols + 15) / 16;
-            const float sw = s.w_scale[nc], b = s.bias[nc], gt = s.epi == EPI_RESID_GATE ? s.gate[nc] : 0.0f;
+            const int m0 = w.mb * s.NT, n_base = w.nb * I8_BM + 32 * q, n = n_base + lane, nl = min(n, s.N - 1);
+            const int cols = min(s.NT, s.M - m0), last = min(ch1, (cols + 15) / 16);
+            const float sw = s.w_scale[nl], b = s.bias[nl], gt = s.epi == EPI_RESID_GATE ? s.gate[nl] : 0.0f;
+            __syncwarp();
+            for (int x = lane; x < 16 * (last - ch0); x += 32) scale[x] = s.a_scale[min(m0 + 16 * ch0 + x, s.M - 1)];
+            __syncwarp();
             ok = mbar_wait(&acc_full[buf], use & 1, err, ERR_WAIT_EPI);
             if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
             tc_fence_after();
-            for (int c = half; c < chunks; c += 2) {
+            for (int c = ch0; c < last; ++c) {
                 const int mc = m0 + 16 * c, left = cols - 16 * c;
-                float res[16];
-                if (s.epi == EPI_RESID_GATE && w.slot < 0) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) res[i] = i < left ? to_f(resid[(size_t)(mc + i) * s.N + nc]) : 0.0f;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) res[i] = 0.0f;
-                }
                 float v[16];
-                tmem_ld16_sync(tq + buf * 128 + 16 * c, v);
-                if (c + 2 >= chunks) {
+                tmem_ld16_sync(tq + buf * s.acs + 16 * c, v);
+                if (c + 1 == last) {
                     tc_fence_before();
                     mbar_arrive(&acc_empty[buf]);
                 }
                 if (w.slot >= 0) {
-                    float *dst = s.part + ((size_t)w.slot * s.NT + 16 * c) * I8_BM + ch;
+                    float *dst = s.part + ((size_t)w.slot * s.NT + 16 * c) * I8_BM + 32 * q + lane;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (i < left) dst[i * I8_BM] = v[i];
-                } else if (n < s.N) {
-                    float sa[16];
+                    continue;
+                }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(sa + 4 * i) = *reinterpret_cast<const float4 *>(s.a_scale + mc + 4 * i);
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 sa = *reinterpret_cast<const float4 *>(scale + 16 * (c - ch0) + i);
+                    v[i] = fmaf(v[i] * sa.x, sw, b);
+                    v[i + 1] = fmaf(v[i + 1] * sa.y, sw, b);
+                    v[i + 2] = fmaf(v[i + 2] * sa.z, sw, b);
+                    v[i + 3] = fmaf(v[i + 3] * sa.w, sw, b);
+                }
+                if (s.epi == EPI_GELU) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = i8_gelu<T>(v[i]);
+                } else if (s.epi == EPI_RESID_GATE) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] *= gt;
+                }
+                if (sizeof(T) == 2 && s.vec) {         // whole 16 bytes: N is a multiple of 8
+                    i8_turn(v, lane);
+                    const int nv = n_base + (lane & ~7);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int i = 8 * r + (lane & 7);
+                        if (i >= left || nv >= s.N) continue;
+                        const size_t at = (size_t)(mc + i) * s.N + nv;
+                        float y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = v[8 * r + j];
+                        if (s.epi == EPI_RESID_GATE) {
+                            float x[8];
+                            loadW<T, 8>(resid + at, x);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) y[j] += x[j];
+                        }
+                        storeW<T, 8>(out + at, y);
+                    }
+                } else if (n < s.N) {
+                    float x[16];
+                    if (s.epi == EPI_RESID_GATE) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = i < left ? to_f(resid[(size_t)(mc + i) * s.N + n]) : 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] += x[i];
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (i < left)
-                            out[(size_t)(mc + i) * s.N + n] = from_f<T>(i8_epilogue<T>(s.epi, v[i], sa[i], sw, b, gt, res[i]));
+                        if (i < left) out[(size_t)(mc + i) * s.N + n] = from_f<T>(v[i]);
                 }
             }
-            if (half >= chunks) mbar_arrive(&acc_empty[buf]);
+            if (ch0 >= last) mbar_arrive(&acc_empty[buf]);
         }
     }
     pdl_release();
     tc_fence_before();
     __syncthreads();
+    cluster_sync_all();                                // the other CTA writes here no more
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -502,13 +603,14 @@ __global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_con
     pdl_wait();
     pdl_release();
     constexpr int TOK = 8;
-    const I8Line l(s.line(), s.G);
-    const unsigned x0 = blockIdx.x * (unsigned)s.KT;
+    const I8Line l(s.line(), s.P);
+    const int rank = blockIdx.x & 1;
+    const unsigned x0 = (blockIdx.x >> 1) * (unsigned)s.KT;
     const int c0 = l.owner(x0), c1 = l.owner(x0 + s.KT - 1);
     if (c0 == c1) return;                              // run whole
-    int mb, nb;
-    i8_tile(s, s.n_full + blockIdx.x, mb, nb);
-    const int t0 = blockIdx.y * TOK, m0 = mb * s.NT + t0, ch = threadIdx.x, n = nb * I8_BM + ch;
+    int mb, pb;
+    i8_tile(s, s.n_full + (blockIdx.x >> 1), mb, pb);
+    const int t0 = blockIdx.y * TOK, m0 = mb * s.NT + t0, ch = threadIdx.x, n = (2 * pb + rank) * I8_BM + ch;
     const int left = min(s.NT - t0, s.M - m0);
     if (left <= 0 || n >= s.N) return;
     float sum[TOK];
@@ -516,7 +618,7 @@ __global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_con
     for (int i = 0; i < TOK; ++i) sum[i] = 0.0f;
 #pragma unroll 4
     for (int c = c0; c <= c1; ++c) {
-        const float *src = s.part + ((size_t)(2 * c + (l.begin(c) >= x0 ? 0 : 1)) * s.NT + t0) * I8_BM + ch;
+        const float *src = s.part + ((size_t)(2 * (2 * c + rank) + (l.begin(c) >= x0 ? 0 : 1)) * s.NT + t0) * I8_BM + ch;
 #pragma unroll
         for (int i = 0; i < TOK; ++i)
             if (i < left) sum[i] += src[i * I8_BM];
@@ -780,25 +882,24 @@ static I8Plan i8_plan(int M, int N, int K) {
     s = I8Sched{};
     s.M = M;
     s.N = N;
-    const int mt = (M + 255) / 256;
+    const int mt = (M + I8_NT - 1) / I8_NT;
     s.NT = ((M + mt - 1) / mt + 15) / 16 * 16;         // the tiles of tokens as even as they come
     s.m_tiles = (M + s.NT - 1) / s.NT;
-    s.n_tiles = (N + I8_BM - 1) / I8_BM;
+    s.n_pairs = (N + 2 * I8_BM - 1) / (2 * I8_BM);
     s.KT = (K + I8_BK - 1) / I8_BK;
-    const int tiles = s.m_tiles * s.n_tiles, sms = device_sms();
-    s.G = (int)std::min<long long>(sms, (long long)tiles * s.KT);
-    s.n_full = tiles / s.G * s.G;
+    const int tiles = s.m_tiles * s.n_pairs;
+    s.P = (int)std::min<long long>(std::max(device_sms() / 2, 1), (long long)tiles * s.KT);
+    s.n_full = tiles / s.P * s.P;
     p.cut = s.n_full < tiles;
-    s.acc2 = s.NT <= 128;
-    // a slot pair for every weight tile, up to the tensor memory's 8, and weights as deep as fit
-    const int budget = 222 * 1024, b_bytes = 128 * s.NT;
-    s.st = std::min(I8_MAX_S, std::max(4, budget / (I8_W_BYTES / 2 + b_bytes)));
-    s.wst = std::min(I8_MAX_W, (budget - s.st * b_bytes) / I8_W_BYTES);
-    p.smem = s.wst * I8_W_BYTES + s.st * b_bytes + 1024;
+    s.acs = (s.NT + 31) / 32 * 32;
+    s.as = std::min(I8_MAX_A, (512 - 2 * s.acs) / 32);
+    const int stage = I8_W_BYTES + 256 * s.NT;
+    s.st = std::min(I8_MAX_ST, I8_SMEM / stage);
+    p.smem = s.st * stage + 1024;
     p.off_scale = ((size_t)M * K * 2 + 255) / 256 * 256;
     p.off_part = p.off_scale + ((size_t)s.m_tiles * s.NT + 16) * sizeof(float);
     p.off_part = (p.off_part + 255) / 256 * 256;
-    p.bytes = p.off_part + (p.cut ? (size_t)2 * s.G * s.NT * I8_BM * sizeof(float) : 0);
+    p.bytes = p.off_part + (p.cut ? (size_t)4 * s.P * s.NT * I8_BM * sizeof(float) : 0);
     return p;
 }
 size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_small(M, K) ? 256 : i8_plan(M, N, K).bytes; }
@@ -807,13 +908,13 @@ template <typename T>
 static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUtensorMap &ta, int *err, cudaStream_t st) {
     static bool done = false;
     if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(linear_i8_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 223 * 1024 + 1024);
+        const cudaError_t e = cudaFuncSetAttribute(linear_i8_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, I8_SMEM + 1024);
         if (e != cudaSuccess) return e;
         done = true;
     }
-    cudaError_t e = launch_pdl(linear_i8_kernel<T>, dim3(p.s.G), dim3(I8_THREADS), p.smem, st, tw, ta, p.s, err);
+    cudaError_t e = launch_pdl(linear_i8_kernel<T>, dim3(2 * p.s.P), dim3(I8_THREADS), p.smem, st, tw, ta, p.s, err);
     if (e != cudaSuccess || !p.cut) return e;
-    return launch_pdl(linear_i8_merge_kernel<T>, dim3(p.s.m_tiles * p.s.n_tiles - p.s.n_full, (p.s.NT + 7) / 8), dim3(I8_BM), 0, st, p.s);
+    return launch_pdl(linear_i8_merge_kernel<T>, dim3(2 * (p.s.m_tiles * p.s.n_pairs - p.s.n_full), (p.s.NT + 7) / 8), dim3(I8_BM), 0, st, p.s);
 }
 
 cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st) {
@@ -831,9 +932,10 @@ cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st
     s.resid = a.resid;
     s.out = a.out;
     s.part = reinterpret_cast<float *>(w + p.off_part);
+    s.vec = a.N % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.resid)) & 15) == 0;
     CUtensorMap tw, ta;
     if (!make_tmap_2d(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.W, a.N, a.K, I8_BM, 128) ||
-        !make_tmap_2d(&ta, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, tokens, a.M, a.K, s.NT, 64))
+        !make_tmap_2d(&ta, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, tokens, a.M, a.K, s.NT / 2, 64))
         return cudaErrorInvalidValue;
     cudaError_t e;
     if (a.a_scale != nullptr) {
