@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(256) widen_kernel(const uint4 *q, uint4 *out, 
 
 // ------------------------------------------------------------------ product
 constexpr int I8_BM = 128, I8_BK = 128;        // channels and depth of a weight tile
-constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_ST = 8, I8_MAX_A = 8;
+constexpr int I8_W_BYTES = I8_BM * I8_BK, I8_MAX_W = 8, I8_MAX_B = 16, I8_MAX_A = 8;
 constexpr int I8_THREADS = 640, I8_SMEM = 220 * 1024;
 constexpr int I8_NT = 192;                     // most tokens of a tile: two sets of sums and four slots of widened weights
 
@@ -207,7 +207,8 @@ struct I8Sched {
     int M, N, NT;              // tokens, channels, tokens of a tile (a multiple of 16)
     int m_tiles, n_pairs, KT;  // tiles of tokens, pairs of tiles of channels, tiles along the depth
     int n_full, P;             // tile pairs that CTA pairs run whole, in rounds (the rest is cut); CTA pairs
-    int st, as, acs;           // stages of depth 128 in shared memory; slots of depth 64 in tensor memory; columns of a set of sums
+    int wst, bst;              // slots in shared memory: weights of depth 128, tokens of depth 64
+    int as, acs;               // slots of depth 64 in tensor memory; columns of a set of sums
     int epi, vec;              // vec: 16-byte outputs
     const float *a_scale, *w_scale, *bias, *gate;
     const void *resid;
@@ -341,7 +342,7 @@ __device__ __forceinline__ void i8_turn(float (&x)[16], int lane) {
 // Two CTAs run neighbouring tiles of channels with the same tokens: each loads half of the
 // tokens for both, which halves what they ask of L2 (a tile of 192 tokens and depth 64 is 32 KB
 // in 384 cycles of products, more than L2 hands an SM).
-// Warps: 0 loads, 1 issues the products, 4-11 widen the weights (thread = channel =
+// Warps: 0 loads weights, 1 issues the products, 2 loads tokens, 4-11 widen the weights (thread = channel =
 // TMEM lane, a half of each tile's depth to either four warps), 12-19 write the outputs (two
 // per TMEM quadrant, half of the tokens each).
 template <typename T>
@@ -349,18 +350,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     linear_i8_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                      const __grid_constant__ I8Sched s, int *err) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * I8_MAX_ST + 2 * I8_MAX_A + 5];
+    __shared__ uint64_t bars[2 * I8_MAX_W + 2 * I8_MAX_B + 2 * I8_MAX_A + 5];
     __shared__ uint32_t tmem_slot;
     __shared__ __align__(16) float sh_scale[8][I8_NT / 2 + 16];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    const int b_bytes = s.NT * 128, stage = I8_W_BYTES + 2 * b_bytes;      // weights, then tokens of depth 64 twice
-    uint64_t *full = bars, *empty = full + I8_MAX_ST, *a_full = empty + I8_MAX_ST, *a_empty = a_full + I8_MAX_A;
+    const int b_bytes = s.NT * 128;
+    uint8_t *sW = smem, *sB = smem + s.wst * I8_W_BYTES;
+    uint64_t *w_full = bars, *w_empty = w_full + I8_MAX_W, *b_full = w_empty + I8_MAX_W, *b_empty = b_full + I8_MAX_B;
+    uint64_t *a_full = b_empty + I8_MAX_B, *a_empty = a_full + I8_MAX_A;
     uint64_t *acc_full = a_empty + I8_MAX_A, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < s.st; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 2);                   // both CTAs have read their copy of the tokens
+        for (int i = 0; i < s.wst; ++i) {
+            mbar_init(&w_full[i], 1);
+            mbar_init(&w_empty[i], 256);
+        }
+        for (int i = 0; i < s.bst; ++i) {
+            mbar_init(&b_full[i], 1);
+            mbar_init(&b_empty[i], 2);                 // both CTAs have read their copy of the tokens
         }
         for (int i = 0; i < s.as; ++i) {
             mbar_init(&a_full[i], 128);
@@ -386,39 +393,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
         // The kernel before this one in the stream (the quantisation) began after
         // everything before it had ended, so the weights need no wait.
         if (lane == 0) {
-            const int half = s.NT / 2 * rank;          // rows of the tile that this CTA loads for both
-            auto load_w = [&](const I8Walk &x, int i, int kt) {
-                mbar_expect_tx(&full[i], stage);
-                tma_load_2d(smem + i * stage, &tmW, &full[i], kt * I8_BK, x.nb * I8_BM);
-            };
-            int ahead = 0;
-            for (I8Walk x(s, blockIdx.x >> 1); ahead < s.st && x.next(s);)
-                for (int kt = x.k0; kt < x.k1 && ahead < s.st; ++kt, ++ahead) load_w(x, ahead, kt);
-            pdl_wait();
             int i = 0, it = 0;
             uint32_t ph = 1;
             bool ok = true;
             while (ok && w.next(s)) {
                 for (int kt = w.k0; kt < w.k1; ++kt, ++it) {
-                    if (it >= ahead) {
-                        if (!(ok = mbar_wait(&empty[i], ph, err, ERR_WAIT_PRODUCER))) break;
-                        load_w(w, i, kt);
-                    }
-                    for (int h = 0; h < 2; ++h)
-                        tma_load_2d_pair(smem + i * stage + I8_W_BYTES + h * b_bytes + half * 128, &tmA, &full[i], kt * I8_BK + 64 * h, w.mb * s.NT + half);
-                    if (++i == s.st) {
+                    if (!(ok = mbar_wait(&w_empty[i], ph, err, ERR_WAIT_PRODUCER))) break;
+                    mbar_expect_tx(&w_full[i], I8_W_BYTES);
+                    tma_load_2d(sW + i * I8_W_BYTES, &tmW, &w_full[i], kt * I8_BK, w.nb * I8_BM);
+                    if (++i == s.wst) {
                         i = 0;
                         ph ^= 1;
                     }
                 }
             }
-            for (int j = max(it - s.st, 0); j < it; ++j)          // every copy has landed before the CTA exits
-                mbar_wait(&full[j % s.st], (j / s.st) & 1, err, ERR_WAIT_PRODUCER);
+            for (int j = max(it - s.wst, 0); j < it; ++j)         // every copy has landed before the CTA exits
+                mbar_wait(&w_full[j % s.wst], (j / s.wst) & 1, err, ERR_WAIT_PRODUCER);
+        }
+    } else if (warp == 2) {
+        if (lane == 0) {
+            pdl_wait();
+            const int half = s.NT / 2 * rank;          // rows of the tile that this CTA loads for both
+            int i = 0, it = 0;
+            uint32_t ph = 1;
+            bool ok = true;
+            while (ok && w.next(s)) {
+                for (int kt = 2 * w.k0; kt < 2 * w.k1; ++kt, ++it) {
+                    if (!(ok = mbar_wait(&b_empty[i], ph, err, ERR_WAIT_PRODUCER))) break;
+                    mbar_expect_tx(&b_full[i], b_bytes);
+                    tma_load_2d_pair(sB + i * b_bytes + half * 128, &tmA, &b_full[i], 64 * kt, w.mb * s.NT + half);
+                    if (++i == s.bst) {
+                        i = 0;
+                        ph ^= 1;
+                    }
+                }
+            }
+            for (int j = max(it - s.bst, 0); j < it; ++j)
+                mbar_wait(&b_full[j % s.bst], (j / s.bst) & 1, err, ERR_WAIT_PRODUCER);
         }
     } else if (warp == 1) {
         // D f32, A and B f16, N = NT, M = 128
         const uint32_t idesc = (1u << 4) | ((uint32_t)(s.NT >> 3) << 17) | ((uint32_t)(I8_BM >> 4) << 24);
-        const uint64_t d0 = sdesc_sw128(smem_u32(smem) + I8_W_BYTES, 16, 1024);
+        const uint64_t d0 = sdesc_sw128(smem_u32(sB), 16, 1024);
         auto wait = [&](uint64_t *b, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(b, parity & 1, err, ERR_WAIT_MMA)) != 0;
         };
@@ -432,27 +448,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
             tc_fence_after();
             const uint32_t acc = tmem + buf * s.acs;
 #pragma unroll 1
-            for (int kt = w.k0; kt < w.k1; ++kt) {
-                if (!(ok = wait(&full[i], ph))) break;
-                const uint64_t db = d0 + (uint64_t)((i * stage) >> 4);
+            for (int n = 2 * (w.k1 - w.k0), first = 0; n > 0; --n, first = 1) {
+                if (!(ok = wait(&b_full[i], ph) && wait(&a_full[a], a_ph))) break;
+                tc_fence_after();
+                const uint64_t db = d0 + (uint64_t)((i * b_bytes) >> 4);
+                const uint32_t ta = tmem + a_col + 32 * a;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (!(ok = wait(&a_full[a], a_ph))) break;
-                    tc_fence_after();
-                    const uint64_t dh = db + (uint64_t)((h * b_bytes) >> 4);
-                    const uint32_t ta = tmem + a_col + 32 * a;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        tc_mma_tmem_a_warp(acc, ta + 8 * k, dh + 2 * k, idesc, h + k > 0 ? 1u : (kt > w.k0 ? 1u : 0u));
-                    tc_commit_warp(&a_empty[a]);
-                    if (++a == s.as) {
-                        a = 0;
-                        a_ph ^= 1;
-                    }
+                for (int k = 0; k < 4; ++k) tc_mma_tmem_a_warp(acc, ta + 8 * k, db + 2 * k, idesc, k > 0 ? 1u : (uint32_t)first);
+                tc_commit_warp(&a_empty[a]);
+                tc_commit_pair_warp(&b_empty[i]);
+                if (++a == s.as) {
+                    a = 0;
+                    a_ph ^= 1;
                 }
-                if (!ok) break;
-                tc_commit_pair_warp(&empty[i]);
-                if (++i == s.st) {
+                if (++i == s.bst) {
                     i = 0;
                     ph ^= 1;
                 }
@@ -466,7 +475,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     } else if (warp >= 4 && warp < 12) {
         const int g = (warp - 4) >> 2, q = warp & 3, r = 32 * q + lane;
         const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + a_col;
-        // stage and slot, and the parities of their turns: this group has every other slot
+        // slots of the two rings, and the parities of their turns: this group has every other slot
         int i = 0, a = g;
         uint32_t ph = 0, a_ph = 1;
         bool ok = true;
@@ -476,11 +485,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
                     a -= s.as;
                     a_ph ^= 1;
                 }
-                ok = mbar_wait(&full[i], ph, err, ERR_WAIT_TMA);
+                ok = mbar_wait(&w_full[i], ph, err, ERR_WAIT_TMA);
                 ok = ok && mbar_wait(&a_empty[a], a_ph, err, ERR_WAIT_MMA);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 tc_fence_after();
-                const uint8_t *src = smem + i * stage + r * 128;
+                const uint8_t *src = sW + i * I8_W_BYTES + r * 128;
                 uint32_t x[32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -491,10 +500,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
                     widen4(v.w, x[8 * c + 6], x[8 * c + 7]);
                 }
                 tmem_st32_sync(t0 + 32 * a, x);
+                // only now have the loads returned for certain: an arrival may overtake them, and the copy
+                // that follows it does not wait for loads of the other proxy
+                mbar_arrive(&w_empty[i]);
                 tc_fence_before();
                 mbar_arrive(&a_full[a]);
                 a += 2;
-                if (++i == s.st) {
+                if (++i == s.wst) {
                     i = 0;
                     ph ^= 1;
                 }
@@ -893,9 +905,11 @@ static I8Plan i8_plan(int M, int N, int K) {
     p.cut = s.n_full < tiles;
     s.acs = (s.NT + 31) / 32 * 32;
     s.as = std::min(I8_MAX_A, (512 - 2 * s.acs) / 32);
-    const int stage = I8_W_BYTES + 256 * s.NT;
-    s.st = std::min(I8_MAX_ST, I8_SMEM / stage);
-    p.smem = s.st * stage + 1024;
+    // as deep as fits, the weights' ring half a tile deeper than the tokens'
+    const int b_bytes = 128 * s.NT;
+    s.wst = std::min(I8_MAX_W, (I8_SMEM + I8_W_BYTES / 2) / (I8_W_BYTES + 2 * b_bytes) + 1);
+    s.bst = std::min(I8_MAX_B, (I8_SMEM - s.wst * I8_W_BYTES) / b_bytes);
+    p.smem = s.wst * I8_W_BYTES + s.bst * b_bytes + 1024;
     p.off_scale = ((size_t)M * K * 2 + 255) / 256 * 256;
     p.off_part = p.off_scale + ((size_t)s.m_tiles * s.NT + 16) * sizeof(float);
     p.off_part = (p.off_part + 255) / 256 * 256;

@@ -242,6 +242,21 @@ def test_weights_made_by_the_kernel_before_the_product():
             near(out, *plain_linear(dict(o), "bias"))
 
 
+def test_every_weight_reaches_its_token():
+    """One-hot tokens show each weight by itself; several rounds, as a slot refilled too early shows only now and then."""
+    M, N, K = 12960, 1536, 1536
+    w = operands("bf16", 1, N, K)["wq"]
+    x = torch.zeros(M, K, device=DEV)
+    m = torch.arange(M, device=DEV)
+    x[m, m % K] = 127.0
+    x = x.bfloat16()
+    one, zero, out = torch.full((N,), 1 / 127.0, device=DEV), torch.zeros(N, device=DEV), torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    want = w.t()[m % K].float()
+    for _ in range(10):
+        xb.op_linear_i8("bf16", xb.XC_EPI_BIAS, x, w, one, zero, out)
+        assert torch.equal(torch.round(out.float()), want)
+
+
 def test_streams_and_graphs():
     o = operands("bf16", 50, 640, 512)
     want = run_linear("bf16", o, "bias")
