@@ -295,13 +295,25 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *t
         ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(smem_u32(bar)), "h"((unsigned short)3)
         : "memory");
 }
-// Arrives at the barrier at this place in both CTAs of the pair when every product issued so far is done.
-__device__ __forceinline__ void tc_commit_pair_warp(uint64_t *bar) {
+// The products of one slot of depth 64 (A in tensor memory) and what their end tells: one
+// lane is elected for all of it (an election for each instruction took the issuing warp as long
+// as the products take).
+__device__ __forceinline__ void i8_issue_slot(uint32_t acc, uint32_t a, uint64_t b, uint32_t idesc, uint32_t first, uint64_t *a_empty,
+                                              uint64_t *b_empty) {
     asm volatile(
-        "{\n\t.reg .pred e;\n\t.reg .b32 r;\n\t"
+        "{\n\t.reg .pred e, p, t;\n\t.reg .b32 r, a1, a2, a3;\n\t.reg .b64 b1, b2, b3;\n\t"
         "elect.sync r|e, 0xffffffff;\n\t"
-        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
-        ::"r"(smem_u32(bar)), "h"((unsigned short)3)
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.eq.b32 t, %4, %4;\n\t"
+        "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"
+        "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, t;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, t;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, t;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%6], %7;\n\t}"
+        ::"r"(acc), "r"(a), "l"(b), "r"(idesc), "r"(first), "r"(smem_u32(a_empty)), "r"(smem_u32(b_empty)), "h"((unsigned short)3)
         : "memory");
 }
 __device__ __forceinline__ void cluster_sync_all() {
@@ -453,10 +465,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
                 tc_fence_after();
                 const uint64_t db = d0 + (uint64_t)((i * b_bytes) >> 4);
                 const uint32_t ta = tmem + a_col + 32 * a;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) tc_mma_tmem_a_warp(acc, ta + 8 * k, db + 2 * k, idesc, k > 0 ? 1u : (uint32_t)first);
-                tc_commit_warp(&a_empty[a]);
-                tc_commit_pair_warp(&b_empty[i]);
+                i8_issue_slot(acc, ta, db, idesc, first, &a_empty[a], &b_empty[i]);
                 if (++a == s.as) {
                     a = 0;
                     a_ph ^= 1;
