@@ -397,7 +397,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     __syncthreads();
     cluster_sync_all();                                // the other CTA's barriers are set up too
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = 0;                           // all 512 columns are this CTA's (a constant stays in uniform registers)
     const int a_col = 2 * s.acs;
     I8Walk w(s, blockIdx.x >> 1);
 
@@ -459,13 +459,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
             if (!(ok = wait(&acc_empty[buf], use ^ 1))) break;
             tc_fence_after();
             const uint32_t acc = tmem + buf * s.acs;
+            bool there = false;                        // the next slot has been seen to be ready
 #pragma unroll 1
             for (int n = 2 * (w.k1 - w.k0), first = 0; n > 0; --n, first = 1) {
-                if (!(ok = wait(&b_full[i], ph) && wait(&a_full[a], a_ph))) break;
+                if (!__all_sync(0xffffffffu, there) && !(ok = wait(&b_full[i], ph) && wait(&a_full[a], a_ph))) break;
                 tc_fence_after();
                 const uint64_t db = d0 + (uint64_t)((i * b_bytes) >> 4);
                 const uint32_t ta = tmem + a_col + 32 * a;
-                i8_issue_slot(acc, ta, db, idesc, first, &a_empty[a], &b_empty[i]);
+                uint64_t *a_done = &a_empty[a], *b_done = &b_empty[i];
                 if (++a == s.as) {
                     a = 0;
                     a_ph ^= 1;
@@ -474,6 +475,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
                     i = 0;
                     ph ^= 1;
                 }
+                there = mbar_test2(&b_full[i], ph, &a_full[a], a_ph);
+                i8_issue_slot(acc, ta, db, idesc, first, a_done, b_done);
             }
             if (ok) tc_commit_warp(&acc_full[buf]);
         }

@@ -46,6 +46,22 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t addr, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
+// Whether these phases of two barriers have completed: a look that nothing waits for.  An
+// issuing warp that looks at the next slot before it issues this one's products has the
+// answer when it needs it (a wait costs it 140 cycles also where the phase is over).
+__device__ __forceinline__ bool mbar_test2(uint64_t *x, uint32_t x_parity, uint64_t *y, uint32_t y_parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+        "and.pred p, p, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(x)), "r"(x_parity), "r"(smem_u32(y)), "r"(y_parity)
+        : "memory");
+    return ok != 0;
+}
 // Wait until the phase with the given parity has completed (bounded).
 __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, int *err, int code) {
     const uint32_t a = smem_u32(bar);
