@@ -62,105 +62,165 @@ template <> struct Vec8<float> {
 
 constexpr float ROUND_MAGIC = 12582912.0f;   // 1.5 * 2^23: adding it rounds to whole numbers, held in the low bits
 
-// 127 x / a rounded to the nearest whole number, halves to even, decided as
-// the exact quotient would be.  r = 127 / a is off by 2^-24 and the product by
-// as much, 2e-5 in all: only a quotient that near to a half is divided.  (bf16:
-// 127 x is exact in fp32, and a quotient of a 15-bit by an 8-bit number that is
-// not a half is 2^-17 or more from one, which the division keeps apart.  fp32: the same of
-// 31 and 24 bits in double.)
-template <typename T> __device__ __forceinline__ float quant(float x, float r, float a) {
-    const float t = x * r;
-    float q = (t + ROUND_MAGIC) - ROUND_MAGIC;
-    if (fabsf(t - q) > 0.4999f) {
-        if constexpr (sizeof(T) == 2) q = rintf(__fdiv_rn(127.0f * x, a));
-        else q = (float)rint(127.0 * (double)x / (double)a);
+// A row's divisor: the largest magnitude's bits, and what is made of them.
+struct QuantRow {
+    float a, r, f;             // divisor (times f), 127 / a; f: a power of two for both sides of the quotient
+    bool finite, plain;        // plain: f = 1
+
+    __device__ __forceinline__ QuantRow(unsigned top) {
+        finite = top < 0x7f800000u;
+        const float m = __uint_as_float(top);
+        // far from 1 both sides are scaled, so that nothing over- or underflows
+        f = m > 0x1p100f ? 0x1p-100f : (m < 0x1p-60f ? 0x1p80f : 1.0f);
+        plain = f == 1.0f;
+        a = m * f;
+        r = finite && m > 0.0f ? __fdiv_rn(127.0f, a) : 0.0f;
     }
-    return q;
+};
+__device__ __forceinline__ float quant_scale(unsigned top) {
+    return top < 0x7f800000u ? __fdiv_rn(__uint_as_float(top), 127.0f) : __uint_as_float(0x7fffffffu);
+}
+// 127 x / a of eight numbers, rounded to the nearest whole number, halves to even, decided as
+// the exact quotient would be.  r = 127 / a is off by 2^-24 and the product by
+// as much, 2e-5 in all: eight among which a quotient t is that near to a half are decided by the
+// sign of 127 x - (k + 1/2) a, k = floor(t), each product as a sum of two floats: near the half the
+// difference of the leading ones is exact, and that of the others is off by 2^-48, where sides that
+// differ do so by 2^-32 or more (31 and 32 bits).  One test for eight: with one each, 12960 rows of 5120 took 52 us instead of 40.
+template <typename T> __device__ __forceinline__ void quant8(const Vec8<T> &z, const QuantRow &row, float (&q)[8]) {
+    float x[8], far = row.plain ? 0.0f : 1.0f;
+    z.get(x);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const float2 t = __fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(row.r, row.r));
+        const float2 w = __fadd2_rn(__fadd2_rn(t, make_float2(ROUND_MAGIC, ROUND_MAGIC)), make_float2(-ROUND_MAGIC, -ROUND_MAGIC));
+        const float2 d = __fadd2_rn(t, make_float2(-w.x, -w.y));
+        far = fmaxf(far, fmaxf(fabsf(d.x), fabsf(d.y)));
+        q[i] = w.x;
+        q[i + 1] = w.y;
+    }
+    if (__builtin_expect(far > 0.4999f, 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = fabsf(x[i] * row.f), k = floorf(v * row.r), c = k + 0.5f;
+            const float p = 127.0f * v, h = c * row.a;
+            const float d = (p - h) + (fmaf(127.0f, v, -p) - fmaf(c, row.a, -h));
+            q[i] = copysignf(d > 0.0f ? k + 1.0f : d < 0.0f ? k : rintf(c), x[i]);
+        }
+        if (row.a == 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = 0.0f;
+        }
+    }
+    if (!row.finite) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = 0.0f;
+    }
 }
 
-// Far from 1 both sides of the quotient are taken times a power of two, so that nothing over- or underflows.
-__device__ __forceinline__ float quant_factor(float a) { return a > 0x1p100f ? 0x1p-100f : (a < 0x1p-60f ? 0x1p80f : 1.0f); }
+// Eight whole numbers as fp16, as bytes.
+__device__ __forceinline__ uint4 half8(const float (&e)[8]) {
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(e[2 * i], e[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned *>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint2 pack8(const float (&e)[8]) {
+    unsigned w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        unsigned b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(e[4 * h + i] + ROUND_MAGIC);
+        w[h] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    }
+    return make_uint2(w[0], w[1]);
+}
 
-// TPR threads a row; each keeps its first four vectors of eight elements in
-// registers and reads the others again (rows of more than 32 TPR elements).
-// HBM bound.  A row without a finite largest magnitude gets scale NaN and zeros.
-template <typename T, typename Q, int TPR>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
+// TPR threads a row, rows in turn; a thread keeps KEEP vectors of eight elements of its row in
+// registers, the next row's on their way meanwhile, and reads what a longer row has beyond
+// them again.  HBM bound.  A row without a finite largest magnitude gets scale NaN and zeros.
+template <typename T, typename Q, int TPR, int KEEP>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR == 512 ? 1 : TPR == 256 ? 3 : 5)
     quantize_rows_kernel(const T *__restrict__ x, Q *__restrict__ q, float *__restrict__ scale, const int M, const int K) {
     pdl_wait();
     pdl_release();
-    constexpr int CTA = TPR < 128 ? 128 : TPR, KEEP = 4;
-    __shared__ unsigned sh[CTA / 32];
-    const int row = blockIdx.x * (CTA / TPR) + threadIdx.x / TPR, t = threadIdx.x % TPR;
-    if (TPR == 32 && row >= M) return;
-    const T *src = x + (size_t)row * K;
-    const int nv = K / 8;
-    Vec8<T> keep[KEEP];
-    unsigned top = 0;
+    constexpr int CTA = TPR < 128 ? 128 : TPR, RPC = CTA / TPR;
+    __shared__ unsigned sh[2][CTA / 32];
+    const int t = threadIdx.x % TPR, nv = K / 8;
+    int row = blockIdx.x * RPC + threadIdx.x / TPR;
+    Vec8<T> next[KEEP];
+    auto load = [&](int r) {
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-        if (t + i * TPR < nv) keep[i].load(src + 8 * (t + i * TPR));
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-        if (t + i * TPR < nv) top = keep[i].top(top);
-    for (int v = t + KEEP * TPR; v < nv; v += TPR) {
-        Vec8<T> z;
-        z.load(src + 8 * v);
-        top = z.top(top);
-    }
-    top = __reduce_max_sync(0xffffffffu, top);
-    if constexpr (TPR > 32) {
-        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = top;
-        __syncthreads();
-        top = 0;
-#pragma unroll
-        for (int w = 0; w < CTA / 32; ++w) top = max(top, sh[w]);
-    }
-    const bool finite = top < 0x7f800000u;
-    const float a = __uint_as_float(top);
-    if (t == 0) scale[row] = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
-    const float f = quant_factor(a), as = a * f;
-    const float r = finite && a > 0.0f ? __fdiv_rn(127.0f, as) : 0.0f;
-    Q *dst = q + (size_t)row * K;
-    auto put = [&](const Vec8<T> &z, int v) {
-        float e[8];
-        z.get(e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = finite ? quant<T>(e[i] * f, r, as) : 0.0f;
-        if constexpr (sizeof(Q) == 1) {
-            unsigned w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                unsigned b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(e[4 * h + i] + ROUND_MAGIC);
-                w[h] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-            }
-            *reinterpret_cast<uint2 *>(dst + 8 * v) = make_uint2(w[0], w[1]);
-        } else {
-            __half2 h[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(e[2 * i], e[2 * i + 1]);
-            *reinterpret_cast<uint4 *>(dst + 8 * v) = *reinterpret_cast<uint4 *>(h);
-        }
+        for (int i = 0; i < KEEP; ++i)
+            if (r < M && t + i * TPR < nv) next[i].load(x + (size_t)r * K + 8 * (t + i * TPR));
     };
+    load(row);
+    for (int turn = 0; TPR > 32 ? row - (int)(threadIdx.x / TPR) < M : row < M; row += gridDim.x * RPC, turn ^= 1) {
+        Vec8<T> keep[KEEP];
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i)
-        if (t + i * TPR < nv) put(keep[i], t + i * TPR);
-    for (int v = t + KEEP * TPR; v < nv; v += TPR) {
-        Vec8<T> z;
-        z.load(src + 8 * v);
-        put(z, v);
+        for (int i = 0; i < KEEP; ++i) keep[i] = next[i];
+        load(row + gridDim.x * RPC);
+        const T *src = x + (size_t)row * K;
+        unsigned top = 0;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (t + i * TPR < nv) top = keep[i].top(top);
+        for (int v = t + KEEP * TPR; v < nv; v += TPR) {
+            Vec8<T> z;
+            z.load(src + 8 * v);
+            top = z.top(top);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if constexpr (TPR > 32) {                      // (two turns' maxima: one barrier a row)
+            if ((threadIdx.x & 31) == 0) sh[turn][threadIdx.x >> 5] = top;
+            __syncthreads();
+            top = 0;
+#pragma unroll
+            for (int w = 0; w < CTA / 32; ++w) top = max(top, sh[turn][w]);
+        }
+        if (t == 0) scale[row] = quant_scale(top);
+        const QuantRow qr(top);
+        Q *dst = q + (size_t)row * K;
+        auto put = [&](const Vec8<T> &z, int v) {
+            float e[8];
+            quant8<T>(z, qr, e);
+            if constexpr (sizeof(Q) == 1) {
+                *reinterpret_cast<uint2 *>(dst + 8 * v) = pack8(e);
+            } else {
+                *reinterpret_cast<uint4 *>(dst + 8 * v) = half8(e);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (t + i * TPR < nv) put(keep[i], t + i * TPR);
+        for (int v = t + KEEP * TPR; v < nv; v += TPR) {
+            Vec8<T> z;
+            z.load(src + 8 * v);
+            put(z, v);
+        }
     }
 }
 
 template <typename T, typename Q>
 static cudaError_t quantize_launch(const T *x, Q *q, float *scale, int M, int K, cudaStream_t st) {
-    const int nv = K / 8;
-    if (nv <= 32 * 4) return launch_pdl(quantize_rows_kernel<T, Q, 32>, dim3((M + 3) / 4), dim3(128), 0, st, x, q, scale, M, K);
-    if (nv <= 128 * 4) return launch_pdl(quantize_rows_kernel<T, Q, 128>, dim3(M), dim3(128), 0, st, x, q, scale, M, K);
-    if (nv <= 256 * 4) return launch_pdl(quantize_rows_kernel<T, Q, 256>, dim3(M), dim3(256), 0, st, x, q, scale, M, K);
-    return launch_pdl(quantize_rows_kernel<T, Q, 512>, dim3(M), dim3(512), 0, st, x, q, scale, M, K);
+    const int nv = K / 8, sms = device_sms();
+    constexpr int KEEP = sizeof(T) == 2 ? 5 : 3;
+    auto launch = [&](auto kernel, int tpr, int per_sm) {
+        const int cta = tpr < 128 ? 128 : tpr, ctas = (M + cta / tpr - 1) / (cta / tpr);
+        return launch_pdl(kernel, dim3(std::min(ctas, per_sm * sms)), dim3(cta), 0, st, x, q, scale, M, K);
+    };
+    // Few rows: the most threads a row with which all of them run at one time.  Many: the
+    // fewest that hold a row in registers, so that an SM has many rows' loads under way.
+    if (nv > 128 && M <= sms) return launch(quantize_rows_kernel<T, Q, 512, KEEP>, 512, 1);
+    if (nv > 64 && M <= 3 * sms) return launch(quantize_rows_kernel<T, Q, 256, KEEP>, 256, 3);
+    if (nv > 32 && M <= 5 * sms) return launch(quantize_rows_kernel<T, Q, 128, KEEP>, 128, 5);
+    if (nv <= 32 * KEEP) return launch(quantize_rows_kernel<T, Q, 32, KEEP>, 32, 5);
+    if (nv <= 128 * KEEP) return launch(quantize_rows_kernel<T, Q, 128, KEEP>, 128, 5);
+    if (nv <= 256 * KEEP) return launch(quantize_rows_kernel<T, Q, 256, KEEP>, 256, 3);
+    return launch(quantize_rows_kernel<T, Q, 512, KEEP>, 512, 1);
 }
 cudaError_t quantize_rows(int dtype, int M, int K, const void *x, signed char *q, float *scale, cudaStream_t st) {
     return dtype == XC_BF16 ? quantize_launch(reinterpret_cast<const bf16 *>(x), q, scale, M, K, st)
@@ -621,12 +681,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     }
 }
 
-// Adds the pieces of a cut tile in CTA order: thread = channel, 8 tokens a CTA.
+// Adds the pieces of a cut tile in CTA order: a thread has four channels of two tokens, a
+// CTA 16 tokens.
+constexpr int I8M_THREADS = 256, I8M_TOKENS = 16;
 template <typename T>
-__global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_constant__ I8Sched s) {
+__global__ void __launch_bounds__(I8M_THREADS) linear_i8_merge_kernel(const __grid_constant__ I8Sched s) {
     pdl_wait();
     pdl_release();
-    constexpr int TOK = 8;
     const I8Line l(s.line(), s.P);
     const int rank = blockIdx.x & 1;
     const unsigned x0 = (blockIdx.x >> 1) * (unsigned)s.KT;
@@ -634,28 +695,42 @@ __global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_con
     if (c0 == c1) return;                              // run whole
     int mb, pb;
     i8_tile(s, s.n_full + (blockIdx.x >> 1), mb, pb);
-    const int t0 = blockIdx.y * TOK, m0 = mb * s.NT + t0, ch = threadIdx.x, n = (2 * pb + rank) * I8_BM + ch;
-    const int left = min(s.NT - t0, s.M - m0);
-    if (left <= 0 || n >= s.N) return;
-    float sum[TOK];
-#pragma unroll
-    for (int i = 0; i < TOK; ++i) sum[i] = 0.0f;
+    const int ch = 4 * (threadIdx.x & 31), t0 = blockIdx.y * I8M_TOKENS + (threadIdx.x >> 5), n0 = (2 * pb + rank) * I8_BM + ch;
+    const int cols = min(s.NT, s.M - mb * s.NT);
+    if (t0 >= cols || n0 >= s.N) return;
+    const bool two = t0 + 8 < cols;
+    float4 sum[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll 4
     for (int c = c0; c <= c1; ++c) {
         const float *src = s.part + ((size_t)(2 * (2 * c + rank) + (l.begin(c) >= x0 ? 0 : 1)) * s.NT + t0) * I8_BM + ch;
-#pragma unroll
-        for (int i = 0; i < TOK; ++i)
-            if (i < left) sum[i] += src[i * I8_BM];
+        const float4 a = *reinterpret_cast<const float4 *>(src);
+        const float4 b = two ? *reinterpret_cast<const float4 *>(src + 8 * I8_BM) : make_float4(0.f, 0.f, 0.f, 0.f);
+        sum[0] = make_float4(sum[0].x + a.x, sum[0].y + a.y, sum[0].z + a.z, sum[0].w + a.w);
+        sum[1] = make_float4(sum[1].x + b.x, sum[1].y + b.y, sum[1].z + b.z, sum[1].w + b.w);
     }
-    const float sw = s.w_scale[n], b = s.bias[n], gt = s.epi == EPI_RESID_GATE ? s.gate[n] : 0.0f;
     const T *resid = reinterpret_cast<const T *>(s.resid);
     T *out = reinterpret_cast<T *>(s.out);
 #pragma unroll
-    for (int i = 0; i < TOK; ++i) {
-        if (i >= left) break;
-        const size_t at = (size_t)(m0 + i) * s.N + n;
-        const float r = s.epi == EPI_RESID_GATE ? to_f(resid[at]) : 0.0f;
-        out[at] = from_f<T>(i8_epilogue<T>(s.epi, sum[i], s.a_scale[m0 + i], sw, b, gt, r));
+    for (int t = 0; t < 2; ++t) {
+        if (t == 1 && !two) break;
+        const int m = mb * s.NT + t0 + 8 * t;
+        const float sa = s.a_scale[m], v[4] = {sum[t].x, sum[t].y, sum[t].z, sum[t].w};
+        const size_t at = (size_t)m * s.N + n0;
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int n = min(n0 + j, s.N - 1);
+            const float r = s.epi == EPI_RESID_GATE && n0 + j < s.N ? to_f(resid[at + j]) : 0.0f;
+            y[j] = i8_epilogue<T>(s.epi, v[j], sa, s.w_scale[n], s.bias[n], s.epi == EPI_RESID_GATE ? s.gate[n] : 0.0f, r);
+        }
+        if (sizeof(T) == 2 && s.vec) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(y[0], y[1]), b = __floats2bfloat162_rn(y[2], y[3]);
+            *reinterpret_cast<uint2 *>(out + at) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n0 + j < s.N) out[at + j] = from_f<T>(y[j]);
+        }
     }
 }
 
@@ -663,12 +738,16 @@ __global__ void __launch_bounds__(I8_BM) linear_i8_merge_kernel(const __grid_con
 // A step of a few tokens waits for the weights' bytes, so everything else goes
 // into the one kernel: each CTA (one an SM) quantises all tokens into its shared
 // memory as fp16, in the order of the MMA's fragments, and streams its share of the
-// channels, N / G each.  The share is a line of (16 channels, depth 64) units that
-// its 16 warps split evenly; a lane loads 16 consecutive weights of two
-// channels straight into registers, I8S_AHEAD units ahead, and widens them there.  (An MMA may take its
-// depth in any order, so the 16 are its numbers 4 j .. 4 j + 3 of product j, and no lane
-// exchanges anything.)  The warps' sums meet in shared memory, in warp order.
-constexpr int I8S_THREADS = 512, I8S_WARPS = I8S_THREADS / 32, I8S_AHEAD = 8, I8S_GROUPS = 16;
+// channels, N / G each.  The share is a line of (16 channels, depth 128) units that its 16 warps split evenly; a lane loads 16 consecutive
+// weights of two channels straight into registers, I8S_AHEAD units ahead, and widens them there.
+// (An MMA may take its depth in any order, so the 16 are its numbers 4 j .. 4 j + 3 of product j,
+// and no lane exchanges anything.  The tensor core's 8-bit integer products need no widening, but took
+// 18.8 us where these take 11 with 4 tokens, 15360 channels and depth 5120.)  The warps' sums
+// meet in shared memory, in warp order.  4 x 15360 x 5120: 18.3 us, of which some 3 until the
+// tokens are quantised and 2 the sums and outputs; the stream between them is near HBM's rate, and near that of
+// the half-rate integer pipe, which 3 of the 5 instructions that widen 4 weights share.  (Asking the weights into L2
+// at the kernel's start: 18.9 us.)
+constexpr int I8S_THREADS = 512, I8S_WARPS = I8S_THREADS / 32, I8S_AHEAD = 4, I8S_GROUPS = 16;
 constexpr int I8S_MAX_M = 32, I8S_TOKEN_BYTES = 144 * 1024;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
@@ -684,7 +763,7 @@ __device__ __forceinline__ uint4 load_stream(const void *p) {
 }
 
 struct I8Small {
-    int M, N, K, KB, G;        // KB: units of depth 64
+    int M, N, K, KB, G;        // KB: units of depth 128
     int epi;
     const void *A;
     const float *a_scale;      // or NULL: quantised here
@@ -695,10 +774,10 @@ struct I8Small {
 };
 
 // Quantises (or widens) the tokens into dst: vector v of 8 numbers of token m at
-// [v / 8][v % 2][m][v / 2 % 4].
+// [v / 8][v % 2][m][v / 2 % 4].  A token has 16 / M warps (a power of two, at least one).
 template <typename T>
 __device__ __forceinline__ void i8_stage_tokens(const I8Small &s, uint4 *dst, float *sh_scale, unsigned *sh_top) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = s.K / 8, nvp = s.KB * 8;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = s.K / 8, nvp = s.KB * 16;
     auto place = [&](int m, int v) -> uint4 & { return dst[((size_t)((v >> 3) * 2 + (v & 1)) * s.M + m) * 4 + ((v >> 1) & 3)]; };
     if (s.a_scale != nullptr) {
         const uint2 *A = reinterpret_cast<const uint2 *>(s.A);
@@ -715,43 +794,56 @@ __device__ __forceinline__ void i8_stage_tokens(const I8Small &s, uint4 *dst, fl
         if (tid < s.M) sh_scale[tid] = s.a_scale[tid];
         return;
     }
+    constexpr int KEEP = sizeof(T) == 2 ? 8 : 4;       // vectors of a lane's first token that stay in registers
     const T *A = reinterpret_cast<const T *>(s.A);
-    int wpr = 1;                                       // warps a token, a power of two
+    int wpr = 1;
     while (2 * wpr * s.M <= I8S_WARPS) wpr *= 2;
-    const int per = I8S_WARPS / wpr, part = warp % wpr;
-    if (tid < s.M) sh_top[tid] = 0;
-    __syncthreads();
-    for (int m = warp / wpr; m < s.M; m += per) {
+    const int per = I8S_WARPS / wpr, m0 = warp / wpr, v0 = (warp % wpr) * 32 + lane, dv = 32 * wpr;
+    Vec8<T> x[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+        if (m0 < s.M && v0 + i * dv < nv) x[i].load(A + (size_t)m0 * s.K + 8 * (v0 + i * dv));
+    for (int m = m0; m < s.M; m += per) {
+        const T *row = A + (size_t)m * s.K;
         unsigned top = 0;
-        for (int v = part * 32 + lane; v < nv; v += wpr * 32) {
+        int v = v0;
+        if (m == m0) {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if (v0 + i * dv < nv) top = x[i].top(top);
+            v = v0 + KEEP * dv;
+        }
+        for (; v < nv; v += dv) {
             Vec8<T> z;
-            z.load(A + (size_t)m * s.K + 8 * v);
+            z.load(row + 8 * v);
             top = z.top(top);
         }
         top = __reduce_max_sync(0xffffffffu, top);
         if (lane == 0) atomicMax(&sh_top[m], top);
     }
     __syncthreads();
-    for (int m = warp / wpr; m < s.M; m += per) {
-        const unsigned top = sh_top[m];
-        const bool finite = top < 0x7f800000u;
-        const float a = __uint_as_float(top), f = quant_factor(a), as = a * f;
-        const float r = finite && a > 0.0f ? __fdiv_rn(127.0f, as) : 0.0f;
-        if (part == 0 && lane == 0) sh_scale[m] = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
-        for (int v = part * 32 + lane; v < nvp; v += wpr * 32) {
-            __half2 h[4];
-            float e[8] = {};
-            if (v < nv && finite) {
-                Vec8<T> z;
-                z.load(A + (size_t)m * s.K + 8 * v);
-                z.get(e);
+    for (int m = m0; m < s.M; m += per) {
+        const T *row = A + (size_t)m * s.K;
+        const QuantRow qr(sh_top[m]);
+        if (v0 == 0) sh_scale[m] = quant_scale(sh_top[m]);
+        float e[8];
+        int v = v0;
+        if (m == m0) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = quant<T>(e[i] * f, r, as);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(e[2 * i], e[2 * i + 1]);
-            place(m, v) = *reinterpret_cast<uint4 *>(h);
+            for (int i = 0; i < KEEP; ++i)
+                if (v0 + i * dv < nv) {
+                    quant8<T>(x[i], qr, e);
+                    place(m, v0 + i * dv) = half8(e);
+                }
+            v = v0 + KEEP * dv;
         }
+        for (; v < nv; v += dv) {
+            Vec8<T> z;
+            z.load(row + 8 * v);
+            quant8<T>(z, qr, e);
+            place(m, v) = half8(e);
+        }
+        for (v = nv + v0; v < nvp; v += dv) place(m, v) = make_uint4(0, 0, 0, 0);      // depth past K
     }
 }
 
@@ -761,88 +853,113 @@ __global__ void __launch_bounds__(I8S_THREADS, 1) linear_i8_small_kernel(const _
     __shared__ float sh_scale[I8S_MAX_M];
     __shared__ unsigned sh_top[I8S_MAX_M];
     constexpr int MP = 8 * NT8;
-    uint4 *tok = sm_small;
-    float *part = reinterpret_cast<float *>(tok + (size_t)s.KB * 8 * s.M);        // [slot][16][MP]
+    uint4 *tok = sm_small;                             // [2 KB][2][M][4]
+    float *part = reinterpret_cast<float *>(tok + (size_t)s.KB * 16 * s.M);       // [slot][16][MP]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
+    const int row0 = (int)((long long)s.N * blockIdx.x / s.G), row1 = (int)((long long)s.N * (blockIdx.x + 1) / s.G);
+    if (tid < I8S_MAX_M) sh_top[tid] = 0;
+    __syncthreads();
     pdl_wait();
     pdl_release();
-    const int row0 = (int)((long long)s.N * blockIdx.x / s.G), row1 = (int)((long long)s.N * (blockIdx.x + 1) / s.G);
-    bool staged = false;
+    i8_stage_tokens<T>(s, tok, sh_scale, sh_top);
+    const bool tail = s.K % 128 != 0;
     for (int p0 = row0; p0 < row1; p0 += 16 * I8S_GROUPS) {
         const int rows = min(row1 - p0, 16 * I8S_GROUPS), groups = (rows + 15) / 16;
         const int U = groups * s.KB, q = U / I8S_WARPS, rem = U - q * I8S_WARPS;
         const int u0 = warp * q + min(warp, rem), u1 = u0 + q + (warp < rem ? 1 : 0);
-        uint4 w[I8S_AHEAD][2];
-        // unit -> this lane's 16 weights of rows gid and gid + 8
-        int lg = u0 / s.KB, lk = u0 - lg * s.KB, lu = u0;      // next unit to load
-        auto fetch = [&](uint4 (&x)[2]) {
-            const int k = 64 * lk + 16 * tig;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = 16 * lg + 8 * h + gid;
-                x[h] = lu < u1 && r < rows && k < s.K ? load_stream(s.W + (size_t)(p0 + r) * s.K + k) : make_uint4(0, 0, 0, 0);
+        uint4 w[I8S_AHEAD][4];
+        // The next unit to load: this lane's 16 weights of rows gid and gid + 8 in either half of the depth.  Rows
+        // and depth that do not exist are read as others that do: no output takes those rows, and the
+        // tokens are zero there.
+        int g = u0 / s.KB, k = u0 - g * s.KB, lu = u0, lk = k, lg = g;
+        const signed char *pa, *pb;
+        auto rows_of = [&]() {
+            const int r = 16 * lg + gid, off = 128 * lk + 16 * tig;
+            pa = s.W + (size_t)(p0 + min(r, rows - 1)) * s.K + off;
+            pb = s.W + (size_t)(p0 + min(r + 8, rows - 1)) * s.K + off;
+        };
+        rows_of();
+        auto fetch = [&](uint4 (&x)[4]) {
+            if (lu >= u1) return;
+            int o0 = 0, o1 = 64;
+            if (tail && lk + 1 == s.KB) {
+                const int most = s.K - 16 - (128 * lk + 16 * tig);
+                o0 = min(o0, most);
+                o1 = min(o1, most);
             }
+            x[0] = load_stream(pa + o0);
+            x[1] = load_stream(pb + o0);
+            x[2] = load_stream(pa + o1);
+            x[3] = load_stream(pb + o1);
             ++lu;
+            pa += 128;
+            pb += 128;
             if (++lk == s.KB) {
                 lk = 0;
                 ++lg;
+                rows_of();
             }
         };
 #pragma unroll
         for (int i = 0; i < I8S_AHEAD; ++i) fetch(w[i]);
-        if (!staged) {
-            i8_stage_tokens<T>(s, tok, sh_scale, sh_top);
-            staged = true;
-        }
         __syncthreads();                               // tokens staged; the last pass's sums read
-        int g = u0 / s.KB, k = u0 - g * s.KB;
-        float acc[NT8][4] = {};
+        const uint4 *t = tok + (size_t)k * 16 * s.M + 4 * gid + tig;
+        // four products a half: sums of their own where registers allow, as each waits for the one it adds to
+        constexpr int SETS = NT8 == 1 ? 4 : NT8 == 2 ? 2 : 1;
+        float acc[SETS][NT8][4] = {};
         // warp w's sums of group g: slot g + w (both only grow)
         auto flush = [&]() {
             float *dst = part + (size_t)(g + warp) * 16 * MP;
 #pragma unroll
             for (int n = 0; n < NT8; ++n) {
-                *reinterpret_cast<float2 *>(dst + gid * MP + 8 * n + 2 * tig) = make_float2(acc[n][0], acc[n][1]);
-                *reinterpret_cast<float2 *>(dst + (gid + 8) * MP + 8 * n + 2 * tig) = make_float2(acc[n][2], acc[n][3]);
-                acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+#pragma unroll
+                for (int i = 1; i < SETS; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        acc[0][n][j] += acc[i][n][j];
+                        acc[i][n][j] = 0.0f;
+                    }
+                *reinterpret_cast<float2 *>(dst + gid * MP + 8 * n + 2 * tig) = make_float2(acc[0][n][0], acc[0][n][1]);
+                *reinterpret_cast<float2 *>(dst + (gid + 8) * MP + 8 * n + 2 * tig) = make_float2(acc[0][n][2], acc[0][n][3]);
+                acc[0][n][0] = acc[0][n][1] = acc[0][n][2] = acc[0][n][3] = 0.0f;
             }
         };
         for (int u = u0; u < u1; u += I8S_AHEAD) {
 #pragma unroll
             for (int i = 0; i < I8S_AHEAD; ++i) {
                 if (u + i >= u1) break;
-                const unsigned *x0 = reinterpret_cast<const unsigned *>(&w[i][0]), *x1 = reinterpret_cast<const unsigned *>(&w[i][1]);
-                unsigned a[4][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    widen4(x0[j], a[j][0], a[j][2]);
-                    widen4(x1[j], a[j][1], a[j][3]);
-                }
-                fetch(w[i]);
+                for (int hk = 0; hk < 2; ++hk) {
+                    const unsigned *x0 = reinterpret_cast<const unsigned *>(&w[i][2 * hk]), *x1 = reinterpret_cast<const unsigned *>(&w[i][2 * hk + 1]);
+                    unsigned a[4][4];
 #pragma unroll
-                for (int n = 0; n < NT8; ++n) {
-                    const int m = 8 * n + gid;
-                    uint4 b[2] = {};
-                    if (m < s.M) {
-                        const uint4 *t = tok + ((size_t)(2 * k) * s.M + m) * 4 + tig;
-                        b[0] = t[0];
-                        b[1] = t[4 * s.M];
+                    for (int j = 0; j < 4; ++j) {
+                        widen4(x0[j], a[j][0], a[j][2]);
+                        widen4(x1[j], a[j][1], a[j][3]);
                     }
-                    mma_f16(acc[n], a[0][0], a[0][1], a[0][2], a[0][3], b[0].x, b[0].y);
-                    mma_f16(acc[n], a[1][0], a[1][1], a[1][2], a[1][3], b[0].z, b[0].w);
-                    mma_f16(acc[n], a[2][0], a[2][1], a[2][2], a[2][3], b[1].x, b[1].y);
-                    mma_f16(acc[n], a[3][0], a[3][1], a[3][2], a[3][3], b[1].z, b[1].w);
+                    if (hk == 1) fetch(w[i]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int n = 0; n < NT8; ++n) {
+                            uint4 b = make_uint4(0, 0, 0, 0);
+                            if (8 * n + gid < s.M) b = t[32 * n + 4 * h * s.M];
+                            mma_f16(acc[(2 * h) % SETS][n], a[2 * h][0], a[2 * h][1], a[2 * h][2], a[2 * h][3], b.x, b.y);
+                            mma_f16(acc[(2 * h + 1) % SETS][n], a[2 * h + 1][0], a[2 * h + 1][1], a[2 * h + 1][2], a[2 * h + 1][3], b.z, b.w);
+                        }
+                    t += 8 * s.M;
                 }
                 if (++k == s.KB) {
                     flush();
                     k = 0;
                     ++g;
+                    t -= (size_t)s.KB * 16 * s.M;
                 }
             }
         }
         if (u1 > u0 && k > 0) flush();
         __syncthreads();
-        // every output of the pass: its group's sums, in warp order
+        // every output of the pass: its group's sums
         const T *resid = reinterpret_cast<const T *>(s.resid);
         T *out = reinterpret_cast<T *>(s.out);
         for (int x = tid; x < rows * s.M; x += I8S_THREADS) {
@@ -860,7 +977,7 @@ __global__ void __launch_bounds__(I8S_THREADS, 1) linear_i8_small_kernel(const _
 
 // ------------------------------------------------------------------- host
 // Tokens that fit every CTA's shared memory go with the weights' stream.
-static bool i8_small(int M, int K) { return M <= I8S_MAX_M && (long)M * ((K + 63) / 64 * 64) * 2 <= I8S_TOKEN_BYTES; }
+static bool i8_small(int M, int K) { return M <= I8S_MAX_M && (long)M * ((K + 127) / 128 * 128) * 2 <= I8S_TOKEN_BYTES; }
 
 template <typename T, int NT8>
 static cudaError_t i8_small_launch(const I8Small &s, cudaStream_t st) {
@@ -871,7 +988,7 @@ static cudaError_t i8_small_launch(const I8Small &s, cudaStream_t st) {
         if (e != cudaSuccess) return e;
         done = true;
     }
-    return launch_pdl(linear_i8_small_kernel<T, NT8>, dim3(s.G), dim3(I8S_THREADS), s.M * s.KB * 128 + part, st, s);
+    return launch_pdl(linear_i8_small_kernel<T, NT8>, dim3(s.G), dim3(I8S_THREADS), s.M * s.KB * 256 + part, st, s);
 }
 template <typename T>
 static cudaError_t i8_small_run(const LinearI8Args &a, cudaStream_t st) {
@@ -879,7 +996,7 @@ static cudaError_t i8_small_run(const LinearI8Args &a, cudaStream_t st) {
     s.M = a.M;
     s.N = a.N;
     s.K = a.K;
-    s.KB = (a.K + 63) / 64;
+    s.KB = (a.K + 127) / 128;
     s.G = std::min(device_sms(), (a.N + 7) / 8);
     s.epi = a.epi;
     s.A = a.A;
@@ -940,7 +1057,7 @@ static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUten
     }
     cudaError_t e = launch_pdl(linear_i8_kernel<T>, dim3(2 * p.s.P), dim3(I8_THREADS), p.smem, st, tw, ta, p.s, err);
     if (e != cudaSuccess || !p.cut) return e;
-    return launch_pdl(linear_i8_merge_kernel<T>, dim3(2 * (p.s.m_tiles * p.s.n_pairs - p.s.n_full), (p.s.NT + 7) / 8), dim3(I8_BM), 0, st, p.s);
+    return launch_pdl(linear_i8_merge_kernel<T>, dim3(2 * (p.s.m_tiles * p.s.n_pairs - p.s.n_full), (p.s.NT + I8M_TOKENS - 1) / I8M_TOKENS), dim3(I8M_THREADS), 0, st, p.s);
 }
 
 cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st) {
