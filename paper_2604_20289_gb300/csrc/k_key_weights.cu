@@ -8,15 +8,12 @@
 // the product and a lane of tensor memory, so the sum over the query rows stays
 // in one thread's registers.
 //
-// A unit is (128 keys, the rows that are summed for them), its steps the unit's key
-// heads x row tiles.  All units' steps form one line that the CTAs share evenly, as
-// in the attention: a unit that one CTA runs whole is written at once, the sums
-// of a cut one leave as partials that key_merge_kernel adds in CTA order, so a call
-// gives the same bits every time.  Where every branch has few rows and the
-// branches share keys, a unit of shared keys takes the rows of as many branches
-// as fit a row tile (packed): the keys are read once for all of them, and every
-// column's sum is kept apart until the unit's end.
+// Three kernels.  Branches of few rows (single tokens, short chunks) wait for the keys'
+// bytes: key_weights_few_kernel streams them into registers, and where the branches share
+// keys it reads them once for the rows of as many branches as fit.  Longer ones are products
+// (key_weights_kernel, tcgen05) and exponentials; fp32 caches have a kernel of their own.
 #include <algorithm>
+#include <climits>
 
 #include "xc_branch.cuh"
 #include "xc_ptx.cuh"
@@ -25,25 +22,29 @@ namespace xc {
 
 constexpr int KW_MAX_B = 1024;           // branches of a call
 constexpr int KW_KEYS = 128, KW_COLS = 128, KW_BUFS = 4;
-constexpr int KW_SWAPS = 2 * KW_BUFS;   // pieces of a step each that one half of the threads may be ahead of the other, and more
+constexpr int KW_SWAPS = 2 * KW_BUFS;    // pieces of a step each that one half of the threads may be ahead of the other, and more
 constexpr float KW_LOG2E = 1.4426950408889634f;
 
 struct KeySched {
     int B, n_q, grp, Hk, causal, G;
     int max_seqs, max_pages, ps, n_pages, shared;
-    int P, n_pt;             // keys and key tiles of the packed shared units (0: none)
-    int packed;              // a row tile holds branches' rows side by side; else one branch's
-    int tt, N, n_ct;         // tokens and columns of a row tile; row tiles (of all rows if packed, else of a branch)
-    int nb;                  // branches of a row tile at most
+    int P, n_pt;             // keys and key tiles of the shared units (few rows only; 0: none)
+    int tt, N, n_ct;         // tokens and columns of a row tile; row tiles (of a branch; with shared units of all rows)
+    int nb;                  // branches of a shared unit's row tile at most
+    int wh, wk;              // few rows: warps over the key heads, over the keys
     float decay, sl2;
     const int *seqs, *len, *table;
     const float *lse;        // [B n_q][Hk grp]
     float *w;
     long w_ld;
     int4 *meta;              // [2 G] what a CTA's cut pieces are
-    float *part;             // [2 G][nb][128]
+    float *part;             // [2 G][128]
 
     __device__ __forceinline__ int limit(int l, int i) const { return causal ? l - n_q + i + 1 : l; }
+    __device__ __forceinline__ void put(int seq, int key, float v) const {
+        float *at = w + (size_t)seq * w_ld + key;
+        *at = decay == 0.0f ? v : fmaf(decay, *at, v);
+    }
 };
 enum { KW_CUT = 1, KW_BEGIN = 2, KW_END = 4 };
 
@@ -54,31 +55,24 @@ struct KeyLens {
     int scan[32];
 };
 
-template <int KT>
-__device__ __forceinline__ int key_tiles(const KeySched &s, int l) {
-    return l > s.P ? (l - s.P + KT - 1) / KT : 0;
-}
-// First row tile that sees the own tile kt of a branch of length l.
-template <int KT>
-__device__ __forceinline__ int key_first_ct(const KeySched &s, int l, int kt) {
-    if (s.packed || !s.causal) return 0;
-    const int i0 = kt * KT - (l - s.n_q);
+// Own tiles of kt keys of a branch of length l.
+__device__ __forceinline__ int key_tiles(const KeySched &s, int l, int kt) { return l > s.P ? (l - s.P + kt - 1) / kt : 0; }
+// Long rows: the first row tile that sees key tile t, and the steps of the tile.
+__device__ __forceinline__ int key_first_ct(const KeySched &s, int l, int t) {
+    if (!s.causal) return 0;
+    const int i0 = t * KW_KEYS - (l - s.n_q);
     return i0 > 0 ? i0 / s.tt : 0;
 }
-template <int KT>
-__device__ __forceinline__ int key_steps(const KeySched &s, int l, int kt) {
-    return s.Hk * ((s.packed ? 1 : s.n_ct) - key_first_ct<KT>(s, l, kt));
-}
-template <int KT>
-__device__ int key_full_tiles(const KeySched &s, int l) {      // own tiles that every row tile sees
-    const int n = key_tiles<KT>(s, l);
-    if (s.packed || !s.causal) return n;
-    return l < s.n_q ? 0 : min(n, (l - s.n_q) / KT + 1);
+__device__ __forceinline__ int key_steps(const KeySched &s, int l, int t) { return s.Hk * (s.n_ct - key_first_ct(s, l, t)); }
+__device__ __forceinline__ int key_full_tiles(const KeySched &s, int l) {      // tiles that every row tile sees
+    const int n = key_tiles(s, l, KW_KEYS);
+    return !s.causal ? n : l < s.n_q ? 0 : min(n, (l - s.n_q) / KW_KEYS + 1);
 }
 
-// Every thread calls it.  line: whether the scan of the steps is wanted too.
-template <int KT>
-__device__ void key_lens(const KeySched &s, KeyLens &L, int *err) {
+// Every thread calls it.  Off: own units before each branch, of kt keys, or with STEPS
+// the steps of the long rows' line.
+template <bool STEPS>
+__device__ void key_lens(const KeySched &s, KeyLens &L, int kt, int *err) {
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int b = tid; b < s.B; b += nt) L.seq[b] = s.seqs[b];
     __syncthreads();
@@ -106,9 +100,13 @@ __device__ void key_lens(const KeySched &s, KeyLens &L, int *err) {
     const int per = (s.B + nt - 1) / nt, b0 = min(tid * per, s.B), b1 = min(b0 + per, s.B);
     int mine = 0;
     for (int b = b0; b < b1; ++b) {
-        const int l = L.len[b], n = key_tiles<KT>(s, l), full = key_full_tiles<KT>(s, l);
-        int x = full * s.Hk * (s.packed ? 1 : s.n_ct);
-        for (int kt = full; kt < n; ++kt) x += key_steps<KT>(s, l, kt);
+        const int l = L.len[b];
+        int x = key_tiles(s, l, kt);
+        if constexpr (STEPS) {
+            const int n = x, full = key_full_tiles(s, l);
+            x = full * s.Hk * s.n_ct;
+            for (int t = full; t < n; ++t) x += key_steps(s, l, t);
+        }
         L.off[b + 1] = x;
         mine += x;
     }
@@ -130,31 +128,24 @@ __device__ void key_lens(const KeySched &s, KeyLens &L, int *err) {
     __syncthreads();
 }
 
+// ------------------------------------------------------------------ long rows
+// A unit is (branch, 128 keys), its steps the key heads x row tiles that see them.  All units'
+// steps form one line that the CTAs share evenly, as in the attention: a unit that one CTA
+// runs whole is written at once, the sums of a cut one leave as partials that key_merge_kernel
+// adds in CTA order, so a call gives the same bits every time.
 struct KeyPiece {
-    int own, b;              // own tile of branch b, or shared tile
-    int kt, key0;            // tile and its first key
-    int t0, ct0, nct;        // first token of row tile ct0; row tiles
+    int b, key0;             // branch, first key
+    int t0, nct;             // first token of the first row tile; row tiles
     int s0, s1, n;           // steps of the piece, of the unit
 };
 struct KeyWalk {
-    int own, b, kt, ct, off, left;
-    template <int KT>
+    int b, t, off, left;
     __device__ __forceinline__ void start(const KeySched &s, const KeyLens &L, int c) {
-        const unsigned pp = (unsigned)s.n_pt * s.n_ct * s.Hk, T = pp + L.off[s.B];
-        const unsigned q = T / s.G, r = T - q * s.G;
-        unsigned x = q * c + min((unsigned)c, r);
+        const unsigned T = L.off[s.B], q = T / s.G, r = T - q * s.G;
+        const unsigned x = q * c + min((unsigned)c, r);
         left = q + ((unsigned)c < r ? 1 : 0);
-        own = b = kt = ct = off = 0;
+        b = t = off = 0;
         if (left == 0) return;
-        if (x < pp) {
-            const int u = x / s.Hk;
-            off = x - u * s.Hk;
-            kt = u / s.n_ct;
-            ct = u - kt * s.n_ct;
-            return;
-        }
-        x -= pp;
-        own = 1;
         int lo = 0, hi = s.B;                          // the last b with off[b] <= x
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -163,76 +154,96 @@ struct KeyWalk {
         }
         b = lo;
         int rest = x - L.off[b];
-        const int l = L.len[b], each = s.Hk * (s.packed ? 1 : s.n_ct), full = key_full_tiles<KT>(s, l);
+        const int l = L.len[b], each = s.Hk * s.n_ct, full = key_full_tiles(s, l);
         if (rest < full * each) {
-            kt = rest / each;
-            off = rest - kt * each;
+            t = rest / each;
+            off = rest - t * each;
             return;
         }
         rest -= full * each;
-        for (kt = full;; ++kt) {
-            const int n = key_steps<KT>(s, l, kt);
+        for (t = full;; ++t) {
+            const int n = key_steps(s, l, t);
             if (rest < n) break;
             rest -= n;
         }
         off = rest;
     }
-    template <int KT>
     __device__ __forceinline__ bool next(const KeySched &s, const KeyLens &L, KeyPiece &p) {
-        while (left > 0) {
-            if (!own && kt == s.n_pt) {                // (n_pt = 0 too)
-                own = 1;
-                b = kt = off = 0;
-            }
-            if (!own) {
-                p.n = s.Hk;
-                p.ct0 = ct;
-                p.t0 = ct * s.tt;
-                p.key0 = kt * KT;
-                p.nct = 1;
-            } else {
-                while (kt >= key_tiles<KT>(s, L.len[b])) {
-                    ++b;
-                    kt = 0;
-                }
-                p.n = key_steps<KT>(s, L.len[b], kt);
-                p.ct0 = key_first_ct<KT>(s, L.len[b], kt);
-                p.t0 = b * s.n_q + p.ct0 * s.tt;
-                p.key0 = s.P + kt * KT;
-                p.nct = (s.packed ? 1 : s.n_ct) - p.ct0;
-            }
-            p.own = own;
-            p.b = b;
-            p.kt = kt;
-            p.s0 = off;
-            p.s1 = min(p.n, off + left);
-            left -= p.s1 - p.s0;
-            off = 0;
-            if (own || ++ct == s.n_ct) {
-                ct = 0;
-                ++kt;
-            }
-            return true;
+        if (left <= 0) return false;
+        while (t >= key_tiles(s, L.len[b], KW_KEYS)) {
+            ++b;
+            t = 0;
         }
-        return false;
+        const int ct0 = key_first_ct(s, L.len[b], t);
+        p.n = key_steps(s, L.len[b], t);
+        p.b = b;
+        p.key0 = t * KW_KEYS;
+        p.t0 = b * s.n_q + ct0 * s.tt;
+        p.nct = s.n_ct - ct0;
+        p.s0 = off;
+        p.s1 = min(p.n, off + left);
+        left -= p.s1 - p.s0;
+        off = 0;
+        ++t;
+        return true;
     }
 };
 
-// ------------------------------------------------------- tensor-core kernel
+// 2^x by Cody and Waite's reduction, two at a time on the FMA pipe: n = round(x), 2^(x - n) by the
+// polynomial of degree 4 of least relative error on [-1/2, 1/2] (2.7e-6 in fp32, Remez exchange), times
+// 2^n.  x <= 127; below -126 the result is 2^-126 or less.
+__device__ __forceinline__ float2 exp2_poly2(float2 x) {
+    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x.x) : "f"(x.x));        // -126
+    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x.y) : "f"(x.y));
+    const float magic = 12582912.0f;
+    const float2 t = __fadd2_rn(x, make_float2(magic, magic)), n = __fadd2_rn(t, make_float2(-magic, -magic));
+    const float2 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
+    auto c2 = [](float c) { return make_float2(c, c); };
+    float2 p = __ffma2_rn(f, c2(0.009570101911f), c2(0.05591786032f));
+    p = __ffma2_rn(p, f, c2(0.2402474483f));
+    p = __ffma2_rn(p, f, c2(0.6931218147f));
+    p = __ffma2_rn(p, f, c2(0.9999992614f));
+    const float2 e = make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000),
+                                 __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000));
+    return __fmul2_rn(p, e);
+}
+
 // Warps: 0 loads (key tiles page by page, row tiles), 1 issues the products, 2 reads
 // the rows' lse and limits, 4-11 take the exponentials (thread = key, two per TMEM
-// quadrant, half of the columns each).
-constexpr int KW_THREADS = 384;
+// quadrant, half of the columns each).  The exponentials bound it: 16 a clock an SM on the
+// special-function unit are 1024 clocks for 128 x 128, the products 512 (head size 128) or 256, so
+// KW_POLY of every 8 pairs go to the FMA pipe.
+constexpr int KW_THREADS = 384, KW_POLY = 3;
 struct KeyRing {
     int ks, qs;              // slots of key tiles, of row tiles
 };
-struct alignas(16) KeyCols {           // what a step's columns need
+struct alignas(16) KeyCols { // what a step's columns need
     float nl[KW_COLS];       // -lse log2(e)
     int lim[KW_COLS];        // keys of the tile that the column's row sees
     int masked;
 };
 
-template <int HD, bool PACKED>
+// A step's products, S^T = K Q^T of head size HD, and what their end tells.  One lane is elected for all of it.
+template <int HD>
+__device__ __forceinline__ void key_issue_step(uint32_t acc, uint64_t k, uint64_t q, uint32_t q_region, uint32_t idesc, uint64_t *q_empty,
+                                               uint64_t *k_empty, uint64_t *s_full) {
+    constexpr uint32_t K_REGION = KW_KEYS * 128;
+    uint32_t leader;
+    asm volatile("{\n\t.reg .pred e;\n\t.reg .b32 r;\n\telect.sync r|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(leader));
+    if (leader) {
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) {
+            const uint64_t a = k + (((i >> 2) * K_REGION + (i & 3) * 32) >> 4), b = q + (((i >> 2) * q_region + (i & 3) * 32) >> 4);
+            tc_mma(acc, a, b, idesc, i > 0 ? 1u : 0u);
+        }
+        tc_commit(q_empty);
+        if (k_empty != nullptr) tc_commit(k_empty);
+        tc_commit(s_full);
+    }
+    __syncwarp();
+}
+
+template <int HD>
 __global__ void __launch_bounds__(KW_THREADS, 1)
     key_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                        const __grid_constant__ KeySched s, const KeyRing ring, int *err) {
@@ -241,14 +252,14 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
     __shared__ KeyLens L;
     __shared__ KeyCols cols[KW_BUFS];
     __shared__ float sh_half[KW_SWAPS][KW_KEYS];
-    __shared__ uint64_t bars[32 + 3 * KW_BUFS + KW_SWAPS + 1];
+    __shared__ uint64_t bars[32 + 2 * KW_BUFS + KW_SWAPS + 1];
     __shared__ uint32_t tmem_slot;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int q_region = s.N * 128, q_bytes = NR * q_region;
     uint8_t *sK = smem, *sQ = smem + ring.ks * K_BYTES;
     uint64_t *k_full = bars, *k_empty = bars + 8, *q_full = bars + 16, *q_empty = bars + 24;
-    uint64_t *s_full = bars + 32, *s_empty = s_full + KW_BUFS, *l_full = s_empty + KW_BUFS;
-    uint64_t *swap = l_full + KW_BUFS, *drained = swap + KW_SWAPS;   // swap: one half's sums are in sh_half
+    uint64_t *s_full = bars + 32, *s_empty = s_full + KW_BUFS;          // s_full: the scores and the columns' lse
+    uint64_t *swap = s_empty + KW_BUFS, *drained = swap + KW_SWAPS;     // swap: one half's sums are in sh_half
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 8; ++i) {
@@ -258,9 +269,8 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             mbar_init(&q_empty[i], 1);
         }
         for (int i = 0; i < KW_BUFS; ++i) {
-            mbar_init(&s_full[i], 1);
+            mbar_init(&s_full[i], 33);
             mbar_init(&s_empty[i], 256);
-            mbar_init(&l_full[i], 32);
         }
         for (int i = 0; i < KW_SWAPS; ++i) mbar_init(&swap[i], 128);
         mbar_init(drained, 1);
@@ -271,33 +281,31 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
     for (int x = threadIdx.x; x < ring.qs * q_bytes / 16; x += KW_THREADS) reinterpret_cast<uint4 *>(sQ)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
     pdl_wait();
-    key_lens<KW_KEYS>(s, L, err);
+    key_lens<true>(s, L, KW_KEYS, err);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = 0;                           // all 512 columns are this CTA's
     KeyWalk walk;
-    walk.start<KW_KEYS>(s, L, blockIdx.x);
+    walk.start(s, L, blockIdx.x);
     KeyPiece p;
 
     if (warp == 0) {
         const int box = min(s.ps, KW_KEYS), log_ps = 31 - __clz(s.ps);
         int kc = 0, qc = 0;
         bool ok = true;
-        while (ok && walk.next<KW_KEYS>(s, L, p)) {
-            const int seq = L.seq[p.own ? p.b : 0];
-            const bool there = seq >= 0 && seq < s.max_seqs;
-            const int keys = (p.own ? L.len[p.b] : s.P) - p.key0;
+        while (ok && walk.next(s, L, p)) {
+            const int seq = L.seq[p.b], keys = L.len[p.b] - p.key0;
             int row = -1;                              // first pool row of this lane's page of the tile
             if (lane * box < KW_KEYS && lane * box < keys) {
-                const int key = p.key0 + lane * box, id = there ? s.table[(size_t)seq * s.max_pages + (key >> log_ps)] : -1;
+                const int key = p.key0 + lane * box, id = s.table[(size_t)seq * s.max_pages + (key >> log_ps)];
                 const bool good = id >= 0 && id < s.n_pages;
                 if (!good && err) atomicOr(err, ERR_BAD_SEQ);
                 row = good ? id * s.ps + (key & (s.ps - 1)) : s.n_pages * s.ps;      // out of range: TMA fills zeros
             }
             const uint32_t k_tx = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box * 128 * NR;
+            int h = p.s0 / p.nct, ct = p.s0 - h * p.nct;
             for (int st = p.s0; st < p.s1; ++st, ++qc) {
-                const int h = PACKED ? st : st / p.nct, ct = PACKED ? 0 : st - h * p.nct;
                 if (st == p.s0 || ct == 0) {
                     const int i = kc % ring.ks;
                     ok = mbar_wait(&k_empty[i], ((kc / ring.ks) & 1) ^ 1, err, ERR_WAIT_PRODUCER);
@@ -318,6 +326,10 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
                         tma_load_3d(sQ + i * q_bytes + r * q_region, &tmQ, &q_full[i], 64 * r, h * s.grp, p.t0 + ct * s.tt);
                 }
                 __syncwarp();
+                if (++ct == p.nct) {
+                    ct = 0;
+                    ++h;
+                }
             }
         }
         if (lane == 0) {                               // every copy has landed before the CTA exits
@@ -330,27 +342,36 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
         auto wait = [&](uint64_t *b, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(b, parity & 1, err, ERR_WAIT_MMA)) != 0;
         };
-        int kc = 0, it = 0;
-        bool ok = true;
-        while (ok && walk.next<KW_KEYS>(s, L, p)) {
-            int ct = PACKED ? 0 : p.s0 % p.nct;
-            for (int st = p.s0; st < p.s1; ++st, ++it) {
-                const int ki = kc % ring.ks, qi = it % ring.qs, buf = it % KW_BUFS;
-                if ((st == p.s0 || ct == 0) && !(ok = wait(&k_full[ki], kc / ring.ks))) break;
-                if (!(ok = wait(&q_full[qi], it / ring.qs) && wait(&s_empty[buf], (it / KW_BUFS) ^ 1))) break;
+        int ki = 0, qi = 0, buf = 0;
+        uint32_t k_ph = 0, q_ph = 0, s_ph = 1;
+        bool ok = true, there = false;                 // there: the next step's rows and buffer have been seen to be ready
+        while (ok && walk.next(s, L, p)) {
+            int ct = p.s0 % p.nct;
+            for (int st = p.s0; st < p.s1; ++st) {
+                if ((st == p.s0 || ct == 0) && !(ok = wait(&k_full[ki], k_ph))) break;
+                if (!__all_sync(0xffffffffu, there) && !(ok = wait(&q_full[qi], q_ph) && wait(&s_empty[buf], s_ph))) break;
                 tc_fence_after();
                 const uint64_t da = dK + (uint64_t)((ki * K_BYTES) >> 4), db = dQ + (uint64_t)((qi * q_bytes) >> 4);
-#pragma unroll
-                for (int k = 0; k < HD / 16; ++k)
-                    tc_mma_warp(tmem + buf * KW_COLS, da + (((k >> 2) * K_REGION + (k & 3) * 32) >> 4),
-                                db + (((k >> 2) * q_region + (k & 3) * 32) >> 4), idesc, k > 0 ? 1u : 0u);
-                tc_commit_warp(&q_empty[qi]);
+                const uint32_t acc = tmem + buf * KW_COLS;
+                uint64_t *q_done = &q_empty[qi], *k_done = nullptr, *s_done = &s_full[buf];
                 if (++ct == p.nct) ct = 0;
-                if (PACKED || ct == 0 || st + 1 == p.s1) {
-                    tc_commit_warp(&k_empty[ki]);
-                    ++kc;
+                if (ct == 0 || st + 1 == p.s1) {
+                    k_done = &k_empty[ki];
+                    if (++ki == ring.ks) {
+                        ki = 0;
+                        k_ph ^= 1;
+                    }
                 }
-                tc_commit_warp(&s_full[buf]);
+                if (++qi == ring.qs) {
+                    qi = 0;
+                    q_ph ^= 1;
+                }
+                if (++buf == KW_BUFS) {
+                    buf = 0;
+                    s_ph ^= 1;
+                }
+                there = mbar_test2(&q_full[qi], q_ph, &s_empty[buf], s_ph);
+                key_issue_step<HD>(acc, da, db, q_region, idesc, q_done, k_done, s_done);
             }
         }
         if (!ok) {                                     // a wait ran out: no product is under way when the CTA ends
@@ -358,6 +379,7 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             wait(drained, 0);
         }
     } else if (warp == 2) {
+        // lse and limits of a step's columns, read a step ahead of when they are stored
         int tk[4], gq[4], it = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -365,163 +387,120 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             tk[i] = c / s.grp;
             gq[i] = c - tk[i] * s.grp;
         }
-        bool ok = true;
-        while (ok && walk.next<KW_KEYS>(s, L, p)) {
-            for (int st = p.s0; st < p.s1; ++st, ++it) {
-                const int h = PACKED ? st : st / p.nct, ct = PACKED ? 0 : st - h * p.nct;
-                const int buf = it % KW_BUFS, t0 = p.t0 + ct * s.tt;
-                const int t_end = p.own ? (p.b + 1) * s.n_q : s.B * s.n_q;
-                float nl[4];
-                int lim[4];
-                bool masked = false;
+        float nl[4];
+        int lim[4];
+        bool masked = false;
+        auto read = [&](const KeyPiece &x, int st) {
+            const int h = st / x.nct, t0 = x.t0 + (st - h * x.nct) * s.tt, t_end = (x.b + 1) * s.n_q, l = L.len[x.b];
+            masked = false;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = t0 + tk[i];
-                    nl[i] = -INFINITY;
-                    lim[i] = 0;
-                    if (lane + 32 * i < s.N) {
-                        if (tk[i] < s.tt && t < t_end) {
-                            const int b = p.own ? p.b : t / s.n_q;
-                            nl[i] = -KW_LOG2E * s.lse[(size_t)t * (s.Hk * s.grp) + h * s.grp + gq[i]];
-                            if (nl[i] == INFINITY) nl[i] = -INFINITY;      // a row that saw no key
-                            lim[i] = min(max(s.limit(L.len[b], t - b * s.n_q) - p.key0, 0), KW_KEYS);
-                        }
-                        masked = masked || lim[i] < KW_KEYS;
+            for (int i = 0; i < 4; ++i) {
+                const int t = t0 + tk[i];
+                nl[i] = -INFINITY;
+                lim[i] = 0;
+                if (lane + 32 * i < s.N) {
+                    if (tk[i] < s.tt && t < t_end) {
+                        nl[i] = s.lse[(size_t)t * (s.Hk * s.grp) + h * s.grp + gq[i]];
+                        lim[i] = min(max(s.limit(l, t - x.b * s.n_q) - x.key0, 0), KW_KEYS);
                     }
+                    masked = masked || lim[i] < KW_KEYS;
                 }
-                ok = mbar_wait(&s_empty[buf], ((it / KW_BUFS) & 1) ^ 1, err, ERR_WAIT_SOFTMAX);
-                if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    cols[buf].nl[lane + 32 * i] = nl[i];
-                    cols[buf].lim[lane + 32 * i] = lim[i];
-                }
-                const unsigned any = __ballot_sync(0xffffffffu, masked);
-                if (lane == 0) cols[buf].masked = any != 0;
-                mbar_arrive(&l_full[buf]);
             }
+        };
+        bool ok = true, more = walk.next(s, L, p);
+        int st = p.s0;
+        if (more) read(p, st);
+        while (ok && more) {
+            const int buf = it % KW_BUFS;
+            float v[4];
+            int m[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {              // a row that saw no key adds nothing
+                v[i] = nl[i] == -INFINITY ? -INFINITY : -KW_LOG2E * nl[i];
+                m[i] = lim[i];
+            }
+            const bool any = __any_sync(0xffffffffu, masked) != 0;
+            if (++st >= p.s1) {
+                more = walk.next(s, L, p);
+                st = p.s0;
+            }
+            if (more) read(p, st);
+            ok = mbar_wait(&s_empty[buf], ((it / KW_BUFS) & 1) ^ 1, err, ERR_WAIT_SOFTMAX);
+            if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                cols[buf].nl[lane + 32 * i] = v[i];
+                cols[buf].lim[lane + 32 * i] = m[i];
+            }
+            if (lane == 0) cols[buf].masked = any;
+            mbar_arrive(&s_full[buf]);
+            ++it;
         }
     } else if (warp >= 4) {
         const int q = warp & 3, half = (warp - 4) >> 2, r = 32 * q + lane;
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
         const int nc = s.N / 16, ch0 = half ? (nc + 1) / 2 : 0, ch1 = half ? nc : (nc + 1) / 2;   // this thread's columns, by 16
+        const float2 sl2 = make_float2(s.sl2, s.sl2);
         if (warp == 4 && lane < 2) s.meta[2 * blockIdx.x + lane] = make_int4(0, 0, 0, 0);
         __syncwarp();
         int it = 0, np = 0;
         bool ok = true;
-        while (ok && walk.next<KW_KEYS>(s, L, p)) {
-            float acc[PACKED ? 64 : 1];
-#pragma unroll
-            for (int i = 0; i < (PACKED ? 64 : 1); ++i) acc[i] = 0.0f;
+        while (ok && walk.next(s, L, p)) {
+            float acc = 0.0f;
             for (int st = p.s0; st < p.s1; ++st, ++it) {
                 const int buf = it % KW_BUFS;
-                const uint32_t ph = (it / KW_BUFS) & 1;
-                ok = mbar_wait(&l_full[buf], ph, err, ERR_WAIT_SOFTMAX) && mbar_wait(&s_full[buf], ph, err, ERR_WAIT_SOFTMAX);
+                ok = mbar_wait(&s_full[buf], (it / KW_BUFS) & 1, err, ERR_WAIT_SOFTMAX);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 tc_fence_after();
                 const bool masked = cols[buf].masked;
-                float2 sum = make_float2(0.0f, 0.0f);
+                float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (ch0 + k >= ch1) break;
-                    const int c = 16 * (ch0 + k);
-                    float x[16];
-                    tmem_ld16_sync(lanes + buf * KW_COLS + c, x);
+                for (int k = 0; k < 2; ++k) {          // 32 columns at a time
+                    if (ch0 + 2 * k >= ch1) break;
+                    const int c = 16 * (ch0 + 2 * k);
+                    const bool two = ch0 + 2 * k + 1 < ch1;
+                    float x[32];
+                    if (two) tmem_ld32_sync(lanes + buf * KW_COLS + c, x);
+                    else tmem_ld16_sync(lanes + buf * KW_COLS + c, *reinterpret_cast<float(*)[16]>(x));
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
+                    for (int i = 0; i < 32; i += 4) {
+                        if (i == 16 && !two) break;
                         const float4 nl = *reinterpret_cast<const float4 *>(&cols[buf].nl[c + i]);
-                        const float2 a = __ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(s.sl2, s.sl2), make_float2(nl.x, nl.y));
-                        const float2 b = __ffma2_rn(make_float2(x[i + 2], x[i + 3]), make_float2(s.sl2, s.sl2), make_float2(nl.z, nl.w));
-                        x[i] = exp2_mufu(a.x);
-                        x[i + 1] = exp2_mufu(a.y);
-                        x[i + 2] = exp2_mufu(b.x);
-                        x[i + 3] = exp2_mufu(b.y);
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
+                        float2 a = __ffma2_rn(make_float2(x[i], x[i + 1]), sl2, make_float2(nl.x, nl.y));
+                        float2 b = __ffma2_rn(make_float2(x[i + 2], x[i + 3]), sl2, make_float2(nl.z, nl.w));
+                        // pairs i / 2 and i / 2 + 1 of 16: KW_POLY of 8 by the polynomial
+                        if ((i / 2 % 8) * KW_POLY / 8 != (i / 2 % 8 + 1) * KW_POLY / 8) a = exp2_poly2(a);
+                        else a = make_float2(exp2_mufu(a.x), exp2_mufu(a.y));
+                        if ((i / 2 % 8 + 1) * KW_POLY / 8 != (i / 2 % 8 + 2) * KW_POLY / 8) b = exp2_poly2(b);
+                        else b = make_float2(exp2_mufu(b.x), exp2_mufu(b.y));
+                        if (masked) {
                             const int4 lim = *reinterpret_cast<const int4 *>(&cols[buf].lim[c + i]);
-                            if (r >= lim.x) x[i] = 0.0f;
-                            if (r >= lim.y) x[i + 1] = 0.0f;
-                            if (r >= lim.z) x[i + 2] = 0.0f;
-                            if (r >= lim.w) x[i + 3] = 0.0f;
+                            a = make_float2(r < lim.x ? a.x : 0.0f, r < lim.y ? a.y : 0.0f);
+                            b = make_float2(r < lim.z ? b.x : 0.0f, r < lim.w ? b.y : 0.0f);
                         }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        if constexpr (PACKED) {
-                            acc[16 * k + i] += x[i];
-                            acc[16 * k + i + 1] += x[i + 1];
-                        } else {
-                            sum = __fadd2_rn(sum, make_float2(x[i], x[i + 1]));
-                        }
+                        sum0 = __fadd2_rn(sum0, a);
+                        sum1 = __fadd2_rn(sum1, b);
                     }
                 }
-                if constexpr (!PACKED) acc[0] += sum.x + sum.y;
+                sum0 = __fadd2_rn(sum0, sum1);
+                acc += sum0.x + sum0.y;
                 tc_fence_before();
                 mbar_arrive(&s_empty[buf]);
             }
             if (!ok) break;
             const bool whole = p.s1 - p.s0 == p.n;
-            const int slot = 2 * blockIdx.x + (np == 0 ? 0 : 1), key = p.key0 + r;
+            const int slot = 2 * blockIdx.x + (np == 0 ? 0 : 1), key = p.key0 + r, sw = np % KW_SWAPS;
             if (!whole && warp == 4 && lane == 0)
-                s.meta[slot] = make_int4(KW_CUT | (p.s0 == 0 ? KW_BEGIN : 0) | (p.s1 == p.n ? KW_END : 0), p.own ? p.b : -1 - p.ct0, p.key0, p.own ? 0x7fffffff : s.P);
-            const int bfirst = p.own ? p.b : p.t0 / s.n_q;
-            auto put = [&](int b, float v) {
-                if (!p.own && key >= s.P) return;
-                if (!whole) {
-                    s.part[((size_t)slot * s.nb + b - bfirst) * KW_KEYS + r] = v;
-                } else if (key < L.len[b]) {
-                    float *at = s.w + (size_t)L.seq[b] * s.w_ld + key;
-                    *at = s.decay == 0.0f ? v : fmaf(s.decay, *at, v);
-                }
-            };
-            const int sw = np % KW_SWAPS;
-            float *other = sh_half[sw];
-            auto take = [&]() -> bool {                // the other half's sums
-                return __all_sync(0xffffffffu, mbar_wait(&swap[sw], (np / KW_SWAPS) & 1, err, ERR_WAIT_SOFTMAX)) != 0;
-            };
-            if constexpr (!PACKED) {
-                if (half == 1) {
-                    other[r] = acc[0];
-                    mbar_arrive(&swap[sw]);
-                } else {
-                    if (!(ok = take())) break;
-                    put(p.b, acc[0] + other[r]);
-                }
+                s.meta[slot] = make_int4(KW_CUT | (p.s0 == 0 ? KW_BEGIN : 0) | (p.s1 == p.n ? KW_END : 0), p.b, p.key0, 0);
+            if (half == 1) {
+                sh_half[sw][r] = acc;
+                mbar_arrive(&swap[sw]);
             } else {
-                // this thread's columns, branch by branch; one branch may lie in both halves
-                const int each = s.n_q * s.grp;
-                const int ncol = min(p.own ? each : (s.B * s.n_q - p.t0) * s.grp, s.tt * s.grp);
-                const int mid = 16 * ((nc + 1) / 2);
-                auto run = [&](int c0, int c1) {
-                    int b = bfirst, end = p.own ? each : ((b + 1) * s.n_q - p.t0) * s.grp;   // the column behind branch b
-                    while (end <= c0) {
-                        end += each;
-                        ++b;
-                    }
-                    float v = half == 1 && c0 < ncol && end - each < mid ? other[r] : 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) {
-                        if (c0 + i < c1) {
-                            v += acc[i];
-                            if (c0 + i + 1 == min(end, ncol)) {
-                                put(b, v);
-                                v = 0.0f;
-                                end += each;
-                                ++b;
-                            }
-                        }
-                    }
-                    if (half == 0) other[r] = v;
-                };
-                if (half == 0) {
-                    run(0, min(mid, ncol));
-                    mbar_arrive(&swap[sw]);
-                } else {
-                    if (!(ok = take())) break;
-                    run(mid, ncol);
-                }
+                ok = __all_sync(0xffffffffu, mbar_wait(&swap[sw], (np / KW_SWAPS) & 1, err, ERR_WAIT_SOFTMAX)) != 0;
+                if (!ok) break;
+                acc += sh_half[sw][r];
+                if (!whole) s.part[(size_t)slot * KW_KEYS + r] = acc;
+                else if (key < L.len[p.b]) s.put(L.seq[p.b], key, acc);
             }
             ++np;
         }
@@ -535,32 +514,210 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
     }
 }
 
-// Adds the pieces of a cut unit in CTA order.  grid: (slots, branches of a row tile).
+// Adds the pieces of a cut unit in CTA order.
 __global__ void __launch_bounds__(KW_KEYS) key_merge_kernel(const __grid_constant__ KeySched s) {
     pdl_wait();
     pdl_release();
     const int4 m = s.meta[blockIdx.x];
     if ((m.x & KW_CUT) == 0 || (m.x & KW_BEGIN) == 0) return;
-    int b = m.y;
-    if (m.y < 0) {
-        b = (-1 - m.y) * s.nb + blockIdx.y;
-        if (b >= s.B) return;
-    } else if (blockIdx.y > 0) {
-        return;
-    }
-    const int seq = s.seqs[b], r = threadIdx.x, key = m.z + r;
-    if (seq < 0 || seq >= s.max_seqs) return;
-    for (int j = 0; j < b; ++j)
-        if (s.seqs[j] == seq) return;                  // listed before
-    const int l = s.len[seq];
-    if (key >= l || key >= m.w || l > s.max_pages * s.ps) return;
-    float v = s.part[((size_t)blockIdx.x * s.nb + blockIdx.y) * KW_KEYS + r];
+    const int seq = s.seqs[m.y], r = threadIdx.x, key = m.z + r;
+    if (key >= s.len[seq]) return;
+    float v = s.part[(size_t)blockIdx.x * KW_KEYS + r];
     for (int c = blockIdx.x / 2 + 1; c < s.G; ++c) {   // the unit goes on as the next CTAs' first piece
-        v += s.part[((size_t)(2 * c) * s.nb + blockIdx.y) * KW_KEYS + r];
+        v += s.part[(size_t)(2 * c) * KW_KEYS + r];
         if (s.meta[2 * c].x & KW_END) break;
     }
-    float *at = s.w + (size_t)seq * s.w_ld + key;
-    *at = s.decay == 0.0f ? v : fmaf(s.decay, *at, v);
+    s.put(seq, key, v);
+}
+
+// ------------------------------------------------------------------- few rows
+// A unit is 16 wk keys with the rows of one branch, or (shared keys) of as many branches as fit
+// 64 columns.  A warp takes 16 of the keys and every wh-th key head: it loads the keys
+// straight into the registers of the MMA's A operand (16 consecutive numbers of a lane are its part of two
+// products; the rows, in shared memory, are laid out to match), the next head's or unit's while it
+// computes, and keeps a sum for every column.  The warps' sums meet in shared memory at the
+// unit's end, in warp order, and one thread writes each (branch, key).  The keys' bytes bound it.
+constexpr int KFEW_THREADS = 512, KFEW_WARPS = KFEW_THREADS / 32, KFEW_COLS = 64, KFEW_PITCH = 20;
+constexpr size_t KFEW_SMEM = 208 * 1024;
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Unit u: its branch (own) or row tile (shared), and its first key.
+struct KeyUnit {
+    int own, b, key0, end;   // end: behind the last key
+    __device__ __forceinline__ KeyUnit(const KeySched &s, const KeyLens &L, int u, int kt) {
+        const int shared = s.n_pt * s.n_ct;
+        own = u >= shared;
+        if (!own) {
+            b = u / s.n_pt;
+            key0 = (u - b * s.n_pt) * kt;
+            end = s.P;
+            return;
+        }
+        const int x = u - shared;
+        int lo = 0, hi = s.B;                          // the last b with off[b] <= x
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (L.off[mid] <= x) lo = mid;
+            else hi = mid;
+        }
+        b = lo;
+        key0 = s.P + (x - L.off[b]) * kt;
+        end = L.len[b];
+    }
+};
+
+template <int HD, int NT8>
+__global__ void __launch_bounds__(KFEW_THREADS, 1)
+    key_weights_few_kernel(const bf16 *__restrict__ q, const long q_ld, const bf16 *__restrict__ k, const __grid_constant__ KeySched s, int *err) {
+    constexpr int CH = HD / 32;                        // 16-byte parts of a lane's key row
+    extern __shared__ __align__(16) uint4 sm_few[];
+    __shared__ KeyLens L;
+    __shared__ __align__(8) int sh_lim[KFEW_COLS];
+    __shared__ int sh_least;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
+    const int ncol = s.N, nt = ncol / 8, kt = 16 * s.wk, wh = warp % s.wh, wk = warp / s.wh;
+    uint4 *sQ = sm_few;                                // [Hk][CH][ncol][4]
+    float *sNl = reinterpret_cast<float *>(sQ + (size_t)s.Hk * CH * ncol * 4);     // [Hk][ncol]
+    float *red = sNl + s.Hk * ncol;                    // [warps][ncol][KFEW_PITCH]
+    pdl_wait();
+    key_lens<false>(s, L, kt, err);
+    pdl_release();
+    const int log_ps = 31 - __clz(s.ps);
+    const int U = s.n_pt * s.n_ct + L.off[s.B], u0 = (int)((long long)U * blockIdx.x / gridDim.x), u1 = (int)((long long)U * (blockIdx.x + 1) / gridDim.x);
+    if (u0 == u1) return;
+    // pool row of the first of this warp's 16 keys of unit u; -1: no keys there, -2: a bad page
+    auto page = [&](int u) -> long {
+        if (u >= u1) return -1;
+        const KeyUnit x(s, L, u, kt);
+        const int key = x.key0 + 16 * wk, seq = L.seq[x.own ? x.b : 0];
+        if (key >= x.end) return -1;
+        const int id = seq >= 0 && seq < s.max_seqs ? s.table[(size_t)seq * s.max_pages + (key >> log_ps)] : -1;
+        if (id < 0 || id >= s.n_pages) {
+            if (err) atomicOr(err, ERR_BAD_SEQ);
+            return -2;
+        }
+        return (long)id * s.ps + (key & (s.ps - 1));
+    };
+    auto load = [&](long row, int h, uint4 (&x)[2][CH]) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                x[r][c] = row >= 0 ? *reinterpret_cast<const uint4 *>(k + ((size_t)(row + gid + 8 * r) * s.Hk + h) * HD + 32 * c + 8 * tig)
+                                   : make_uint4(0, 0, 0, 0);
+    };
+    long row = page(u0), row_next = page(u0 + 1);
+    uint4 x[2][CH];
+    if (wh < s.Hk) load(row, wh, x);
+    int have_own = -1, have_b = -1;                    // whose rows are in shared memory
+    for (int u = u0; u < u1; ++u) {
+        const KeyUnit unit(s, L, u, kt);
+        const int t0 = unit.own ? unit.b * s.n_q : unit.b * s.tt;
+        const int tokens = unit.own ? s.n_q : min(s.tt, s.B * s.n_q - t0), cols = tokens * s.grp;
+        if (unit.own != have_own || unit.b != have_b) {
+            have_own = unit.own;
+            have_b = unit.b;
+            __syncthreads();                           // the last unit's rows have been used
+            for (int y = tid; y < s.Hk * ncol * CH * 4; y += KFEW_THREADS) {
+                const int part = y % (CH * 4), rest = y / (CH * 4), c = rest % ncol, h = rest / ncol;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (c < cols)
+                    v = *reinterpret_cast<const uint4 *>(q + (size_t)(t0 + c / s.grp) * q_ld + (h * s.grp + c % s.grp) * HD + 8 * part);
+                sQ[((size_t)(h * CH + part / 4) * ncol + c) * 4 + part % 4] = v;
+            }
+            for (int y = tid; y < s.Hk * ncol; y += KFEW_THREADS) {
+                const int c = y % ncol, h = y / ncol;
+                float v = -INFINITY;
+                if (c < cols) v = s.lse[(size_t)(t0 + c / s.grp) * (s.Hk * s.grp) + h * s.grp + c % s.grp];
+                sNl[y] = v == -INFINITY ? -INFINITY : -KW_LOG2E * v;       // a row that saw no key adds nothing
+            }
+            if (tid == 0) sh_least = INT_MAX;
+            __syncthreads();
+            if (tid < ncol) {
+                int lim = 0;
+                if (tid < cols) {
+                    const int t = t0 + tid / s.grp, b = t / s.n_q;
+                    lim = s.limit(L.len[b], t - b * s.n_q);
+                    atomicMin(&sh_least, lim);
+                }
+                sh_lim[tid] = lim;
+            }
+            __syncthreads();
+        }
+        const long row_after = page(u + 2);            // the table's entry comes while this unit is computed
+        const int key = unit.key0 + 16 * wk;           // this warp's first key
+        const bool masked = key + 16 > sh_least, there = key < unit.end;
+        float acc[NT8][4] = {};
+        for (int h = wh; h < s.Hk; h += s.wh) {
+            uint4 a[2][CH];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int c = 0; c < CH; ++c) a[r][c] = x[r][c];
+            const bool same = h + s.wh < s.Hk;
+            load(same ? row : row_next, same ? h + s.wh : wh, x);
+            if (!there) continue;
+            const uint4 *qh = sQ + (size_t)h * CH * ncol * 4 + 4 * gid + tig;
+            const float *nl = sNl + h * ncol + 2 * tig;
+#pragma unroll
+            for (int n = 0; n < NT8; ++n) {
+                if (n >= nt) break;
+                float sc[2][4] = {};
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const uint4 b = qh[(size_t)(c * ncol + 8 * n) * 4];
+                    mma_bf16(sc[0], a[0][c].x, a[1][c].x, a[0][c].y, a[1][c].y, b.x, b.y);
+                    mma_bf16(sc[1], a[0][c].z, a[1][c].z, a[0][c].w, a[1][c].w, b.z, b.w);
+                }
+                const float2 l = *reinterpret_cast<const float2 *>(nl + 8 * n);
+                float p[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = exp2_mufu(fmaf(sc[0][j] + sc[1][j], s.sl2, j & 1 ? l.y : l.x));
+                if (masked) {
+                    const int2 lim = *reinterpret_cast<const int2 *>(&sh_lim[8 * n + 2 * tig]);
+                    if (key + gid >= lim.x) p[0] = 0.0f;
+                    if (key + gid >= lim.y) p[1] = 0.0f;
+                    if (key + gid + 8 >= lim.x) p[2] = 0.0f;
+                    if (key + gid + 8 >= lim.y) p[3] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[n][j] += p[j];
+            }
+        }
+        float *mine = red + (size_t)warp * ncol * KFEW_PITCH;
+#pragma unroll
+        for (int n = 0; n < NT8; ++n) {
+            if (n >= nt) break;
+            float *at = mine + (8 * n + 2 * tig) * KFEW_PITCH + gid;
+            at[0] = acc[n][0];
+            at[KFEW_PITCH] = acc[n][1];
+            at[8] = acc[n][2];
+            at[KFEW_PITCH + 8] = acc[n][3];
+        }
+        __syncthreads();
+        // one thread a (branch, key): the warps of the key's 16, the branch's columns
+        const int each = s.n_q * s.grp, branches = unit.own ? 1 : tokens / s.n_q;
+        for (int y = tid; y < branches * kt; y += KFEW_THREADS) {
+            const int j = y / kt, r = y - j * kt, ky = unit.key0 + r;
+            const int b = unit.own ? unit.b : unit.b * s.nb + j;
+            if (ky >= unit.end || ky >= L.len[b]) continue;
+            float v = 0.0f;
+            for (int w = 0; w < s.wh; ++w) {
+                const float *at = red + ((size_t)((r >> 4) * s.wh + w) * ncol + j * each) * KFEW_PITCH + (r & 15);
+                for (int c = 0; c < each; ++c) v += at[c * KFEW_PITCH];
+            }
+            s.put(L.seq[b], ky, v);
+        }
+        __syncthreads();
+        row = row_next;
+        row_next = row_after;
+    }
 }
 
 // ------------------------------------------------------------ fp32 kernel
@@ -579,13 +736,13 @@ __global__ void __launch_bounds__(256)
     float *sK = sm, *sQ = sm + 64 * LD;
     pdl_wait();
     pdl_release();
-    key_lens<KF_KEYS>(s, L, err);
+    key_lens<false>(s, L, KF_KEYS, err);
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, log_ps = 31 - __clz(s.ps), rows = s.n_q * s.grp;
     const float scale = s.sl2;
     int b = 0, before = 0;                             // units of the branches before b
     for (int u = blockIdx.x;; u += gridDim.x) {
-        while (b < s.B && u - before >= key_tiles<KF_KEYS>(s, L.len[b])) {
-            before += key_tiles<KF_KEYS>(s, L.len[b]);
+        while (b < s.B && u - before >= key_tiles(s, L.len[b], KF_KEYS)) {
+            before += key_tiles(s, L.len[b], KF_KEYS);
             ++b;
         }
         if (b == s.B) return;
@@ -664,13 +821,13 @@ __global__ void __launch_bounds__(256)
         if (tid < 64 && key0 + tid < l) {
             float v = 0.0f;
             for (int y = 0; y < 16; ++y) v += sm[y * 64 + tid];
-            float *at = s.w + (size_t)seq * s.w_ld + key0 + tid;
-            *at = s.decay == 0.0f ? v : fmaf(s.decay, *at, v);
+            s.put(seq, key0 + tid, v);
         }
     }
 }
 
 // ------------------------------------------------------------------- host
+static size_t few_smem(int Hk, int N, int head_dim) { return (size_t)Hk * N * (head_dim * 2 + 4) + (size_t)KFEW_WARPS * N * KFEW_PITCH * 4; }
 static KeySched key_plan(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     KeySched s{};
     s.B = B;
@@ -689,51 +846,77 @@ static KeySched key_plan(const xc_kv_cache &c, int B, int n_q, int H, int shared
     s.tt = n_q;
     s.n_ct = 1;
     if (c.dtype == XC_F32) return s;
-    // Branches' rows side by side, whole branches, where two or more fit a row tile.
-    const long long tokens = (long long)B * n_q;
-    s.packed = shared > 0 && B > 1 && 2ll * n_q * s.grp <= KW_COLS;
-    s.tt = s.packed ? std::min(B, KW_COLS / (n_q * s.grp)) * n_q : std::min(KW_COLS / s.grp, n_q);
+    const long long each = (long long)n_q * s.grp;
+    auto fits = [&](long long n) { return n * each <= KFEW_COLS && few_smem(s.Hk, (int)(n * each + 7) / 8 * 8, c.head_dim) <= KFEW_SMEM; };
+    if (fits(1)) {                                     // few rows
+        s.wh = 1;
+        while (s.wh < KFEW_WARPS && s.wh < s.Hk) s.wh *= 2;
+        s.wk = KFEW_WARPS / s.wh;
+        if (shared > 0 && B > 1) {
+            while (s.nb < B && fits(s.nb + 1)) ++s.nb;
+            s.P = shared;
+        }
+        s.tt = s.nb * n_q;
+        s.N = (s.tt * s.grp + 7) / 8 * 8;
+        s.n_ct = (B + s.nb - 1) / s.nb;
+        s.n_pt = (s.P + 16 * s.wk - 1) / (16 * s.wk);
+        return s;
+    }
+    s.tt = std::min(KW_COLS / s.grp, n_q);
     s.N = (s.tt * s.grp + 15) / 16 * 16;
-    s.n_ct = (int)(((s.packed ? tokens : n_q) + s.tt - 1) / s.tt);
-    s.P = s.packed ? shared : 0;
-    s.n_pt = (s.P + KW_KEYS - 1) / KW_KEYS;
-    if (s.packed) s.nb = s.tt / n_q;
+    s.n_ct = (n_q + s.tt - 1) / s.tt;
     return s;
 }
 bool key_weights_fit(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     const KeySched s = key_plan(c, B, n_q, H, shared);
-    const long long tiles = ((long long)c.max_pages * c.page_size + KF_KEYS - 1) / KF_KEYS + 1;
-    const long long ct = c.dtype == XC_F32 ? 1 : s.n_ct;
-    return B <= KW_MAX_B && tiles * B * s.Hk * ct < (1ll << 31);
+    const long long tiles = ((long long)c.max_pages * c.page_size + 15) / 16 + 1;
+    return B <= KW_MAX_B && tiles * B * s.Hk * s.n_ct < (1ll << 31);
 }
 size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
-    if (c.dtype == XC_F32) return 16;
     const KeySched s = key_plan(c, B, n_q, H, shared);
-    return (size_t)2 * s.G * (sizeof(int4) + (size_t)s.nb * KW_KEYS * sizeof(float));
+    return c.dtype == XC_F32 || s.wh > 0 ? 16 : (size_t)2 * s.G * (sizeof(int4) + KW_KEYS * sizeof(float));
 }
 
-template <int HD, bool PACKED>
+template <int HD>
 static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
     constexpr int K_BYTES = KW_KEYS * HD * 2, BUDGET = 200 * 1024;
     static bool done = false;
     if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(key_weights_kernel<HD, PACKED>, cudaFuncAttributeMaxDynamicSharedMemorySize, BUDGET + 1024);
+        const cudaError_t e = cudaFuncSetAttribute(key_weights_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BUDGET + 1024);
         if (e != cudaSuccess) return e;
         done = true;
     }
     const int q_bytes = s.N * HD * 2;
     KeyRing ring;
-    ring.ks = s.n_ct > 2 && !PACKED ? 2 : std::min(8, BUDGET / (K_BYTES + q_bytes));
+    ring.ks = s.n_ct > 2 ? 2 : std::min(8, BUDGET / (K_BYTES + q_bytes));
     ring.qs = std::min(8, (BUDGET - ring.ks * K_BYTES) / q_bytes);
     const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
     CUtensorMap tq, tk;
     if (!make_tmap_heads_bf16(&tq, a.q, HD, (uint64_t)s.Hk * s.grp, (uint64_t)s.B * s.n_q, a.q_ld, s.grp, s.tt) ||
         !make_tmap_bf16(&tk, a.k, rows, cols, c.page_size < KW_KEYS ? c.page_size : KW_KEYS))
         return cudaErrorInvalidValue;
-    const cudaError_t e = launch_pdl(key_weights_kernel<HD, PACKED>, dim3(s.G), dim3(KW_THREADS),
+    const cudaError_t e = launch_pdl(key_weights_kernel<HD>, dim3(s.G), dim3(KW_THREADS),
                                      ring.ks * K_BYTES + ring.qs * q_bytes + 1024, st, tq, tk, s, ring, err);
     if (e != cudaSuccess) return e;
-    return launch_pdl(key_merge_kernel, dim3(2 * s.G, s.nb), dim3(KW_KEYS), 0, st, s);
+    return launch_pdl(key_merge_kernel, dim3(2 * s.G), dim3(KW_KEYS), 0, st, s);
+}
+template <int HD, int NT8>
+static cudaError_t key_launch_few_(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
+    static bool done = false;
+    if (!done) {
+        const cudaError_t e = cudaFuncSetAttribute(key_weights_few_kernel<HD, NT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)KFEW_SMEM);
+        if (e != cudaSuccess) return e;
+        done = true;
+    }
+    return launch_pdl(key_weights_few_kernel<HD, NT8>, dim3(s.G), dim3(KFEW_THREADS), few_smem(s.Hk, s.N, HD), st, reinterpret_cast<const bf16 *>(a.q), a.q_ld,
+                      reinterpret_cast<const bf16 *>(a.k), s, err);
+}
+template <int HD>
+static cudaError_t key_launch_few(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
+    if (s.N <= 8) return key_launch_few_<HD, 1>(a, s, err, st);
+    if (s.N <= 16) return key_launch_few_<HD, 2>(a, s, err, st);
+    if (s.N <= 32) return key_launch_few_<HD, 4>(a, s, err, st);
+    return key_launch_few_<HD, 8>(a, s, err, st);
 }
 template <int HD>
 static cudaError_t key_launch_f32(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
@@ -760,8 +943,8 @@ cudaError_t key_weights(const xc_kv_cache &c, const KeyWeightsArgs &a, void *ws,
     s.meta = reinterpret_cast<int4 *>(ws);
     s.part = reinterpret_cast<float *>(s.meta + 2 * s.G);
     if (c.dtype == XC_BF16) {
-        if (c.head_dim == 64) return s.packed ? key_launch_tc<64, true>(c, a, s, err, st) : key_launch_tc<64, false>(c, a, s, err, st);
-        if (c.head_dim == 128) return s.packed ? key_launch_tc<128, true>(c, a, s, err, st) : key_launch_tc<128, false>(c, a, s, err, st);
+        if (c.head_dim == 64) return s.wh > 0 ? key_launch_few<64>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
+        if (c.head_dim == 128) return s.wh > 0 ? key_launch_few<128>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
         return cudaErrorInvalidValue;
     }
     switch (c.head_dim) {

@@ -63,7 +63,7 @@ def check(dtype, H, hk, hd, ps, lens, n_q, shared, causal, seqs=None, scale=0.0,
     empty = np.isneginf(want_lse)
     assert np.array_equal(np.isneginf(got_lse), empty)
     if not empty.all():
-        assert np.abs(got_lse - want_lse)[~empty].max() <= (4e-5 if dtype == "bf16" else 1e-5)
+        assert np.abs(got_lse[~empty] - want_lse[~empty]).max() <= (4e-5 if dtype == "bf16" else 1e-5)
     # the row of weights is wider than the table's, and what is past a sequence's end may hold anything
     width = cache.table.shape[1] * ps + 12
     old = rand((len(lens), width), "f32", seed + 9).abs()
@@ -184,6 +184,15 @@ def test_a_thousand_branches():
     check("bf16", 1, 1, 64, 16, lens, 2, 0, True)
 
 
+@pytest.mark.parametrize("H,hk,hd,lens,n_q,shared", [
+    (128, 128, 128, [200, 150], 1, 64),                # more key heads than rows fit shared memory
+    (40, 40, 128, [300, 260, 290], 1, 256), (3, 3, 64, [300, 260, 290], 7, 256), (5, 5, 128, [130] * 9, 12, 64),
+    (48, 16, 64, [400, 333], 5, 320), (17, 17, 64, [90, 70], 3, 0), (64, 2, 64, [99, 500, 64], 2, 0), (2, 1, 128, [700], 32, 0),
+    (2, 1, 128, [700], 33, 0), (6, 6, 128, [1000] * 3, 64, 512), (6, 6, 128, [1000] * 3, 65, 512)])
+def test_head_layouts_of_few_rows(H, hk, hd, lens, n_q, shared):
+    check("bf16", H, hk, hd, 32, lens, n_q, shared, True)
+
+
 def test_long_rows_and_many_cuts():
     check("bf16", 1, 1, 128, 64, [19968 + 5 * b for b in range(3)], 1, 19968, True)
     check("bf16", 2, 1, 128, 128, [5000], 1, 0, True)
@@ -230,7 +239,7 @@ def test_refusals():
         with pytest.raises(ValueError):
             xb.op_key_weights(cache, 0, a["seqs"], 1, a["q"], a["lse"], a["w"])
     for bad in (dict(decay=-1.0), dict(decay=float("nan")), dict(scale=-1.0), dict(shared_len=8),
-                dict(workspace=torch.empty(16, dtype=torch.uint8, device=DEV))):
+                dict(workspace=torch.empty(8, dtype=torch.uint8, device=DEV))):
         with pytest.raises(xb.XCacheError):
             xb.op_key_weights(cache, 0, i32([0, 1]), 1, q, lse, w, **bad)
     with pytest.raises(ValueError):
