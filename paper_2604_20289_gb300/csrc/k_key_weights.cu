@@ -14,6 +14,7 @@
 // (key_weights_kernel, tcgen05) and exponentials; fp32 caches have a kernel of their own.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "xc_branch.cuh"
 #include "xc_ptx.cuh"
@@ -22,7 +23,7 @@ namespace xc {
 
 constexpr int KW_MAX_B = 1024;           // branches of a call
 constexpr int KW_KEYS = 128, KW_COLS = 128, KW_BUFS = 4;
-constexpr int KW_SWAPS = 2 * KW_BUFS;    // pieces of a step each that one half of the threads may be ahead of the other, and more
+constexpr int KW_SWAPS = 2 * KW_BUFS;    // pieces of a step each that some of the threads may be ahead of others, and more
 constexpr float KW_LOG2E = 1.4426950408889634f;
 
 struct KeySched {
@@ -189,31 +190,13 @@ struct KeyWalk {
     }
 };
 
-// 2^x by Cody and Waite's reduction, two at a time on the FMA pipe: n = round(x), 2^(x - n) by the
-// polynomial of degree 4 of least relative error on [-1/2, 1/2] (2.7e-6 in fp32, Remez exchange), times
-// 2^n.  x <= 127; below -126 the result is 2^-126 or less.
-__device__ __forceinline__ float2 exp2_poly2(float2 x) {
-    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x.x) : "f"(x.x));        // -126
-    asm("max.NaN.f32 %0, %1, 0fC2FC0000;" : "=f"(x.y) : "f"(x.y));
-    const float magic = 12582912.0f;
-    const float2 t = __fadd2_rn(x, make_float2(magic, magic)), n = __fadd2_rn(t, make_float2(-magic, -magic));
-    const float2 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
-    auto c2 = [](float c) { return make_float2(c, c); };
-    float2 p = __ffma2_rn(f, c2(0.009570101911f), c2(0.05591786032f));
-    p = __ffma2_rn(p, f, c2(0.2402474483f));
-    p = __ffma2_rn(p, f, c2(0.6931218147f));
-    p = __ffma2_rn(p, f, c2(0.9999992614f));
-    const float2 e = make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000),
-                                 __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000));
-    return __fmul2_rn(p, e);
-}
-
 // Warps: 0 loads (key tiles page by page, row tiles), 1 issues the products, 2 reads
-// the rows' lse and limits, 4-11 take the exponentials (thread = key, two per TMEM
-// quadrant, half of the columns each).  The exponentials bound it: 16 a clock an SM on the
-// special-function unit are 1024 clocks for 128 x 128, the products 512 (head size 128) or 256, so
-// KW_POLY of every 8 pairs go to the FMA pipe.
-constexpr int KW_THREADS = 384, KW_POLY = 3;
+// the rows' lse and limits, 4-19 take the exponentials (thread = key; two groups that take steps in
+// turn, two warps per TMEM quadrant in each, half of the columns a warp: all sixteen on every
+// step took 1040 us instead of 780 below).  (A share of the exponentials on the FMA pipe, by Cody and
+// Waite's reduction and a polynomial, made it slower: 2 x 4320 queries over 30240 keys 1040 us without, 1177 with a
+// quarter of them.)
+constexpr int KW_SOFT = 512, KW_THREADS = 128 + KW_SOFT;
 struct KeyRing {
     int ks, qs;              // slots of key tiles, of row tiles
 };
@@ -223,24 +206,21 @@ struct alignas(16) KeyCols { // what a step's columns need
     int masked;
 };
 
-// A step's products, S^T = K Q^T of head size HD, and what their end tells.  One lane is elected for all of it.
-template <int HD>
-__device__ __forceinline__ void key_issue_step(uint32_t acc, uint64_t k, uint64_t q, uint32_t q_region, uint32_t idesc, uint64_t *q_empty,
-                                               uint64_t *k_empty, uint64_t *s_full) {
-    constexpr uint32_t K_REGION = KW_KEYS * 128;
-    uint32_t leader;
-    asm volatile("{\n\t.reg .pred e;\n\t.reg .b32 r;\n\telect.sync r|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(leader));
-    if (leader) {
-#pragma unroll
-        for (int i = 0; i < HD / 16; ++i) {
-            const uint64_t a = k + (((i >> 2) * K_REGION + (i & 3) * 32) >> 4), b = q + (((i >> 2) * q_region + (i & 3) * 32) >> 4);
-            tc_mma(acc, a, b, idesc, i > 0 ? 1u : 0u);
-        }
-        tc_commit(q_empty);
-        if (k_empty != nullptr) tc_commit(k_empty);
-        tc_commit(s_full);
-    }
-    __syncwarp();
+// Four products of a step, S^T (+)= K Q^T over 64 numbers of the head, by one elected lane.
+__device__ __forceinline__ void key_issue4(uint32_t acc, uint64_t k, uint64_t q, uint32_t idesc, uint32_t add) {
+    asm volatile(
+        "{\n\t.reg .pred e, p, t;\n\t.reg .b32 r;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+        "elect.sync r|e, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.eq.b32 t, %4, %4;\n\t"
+        "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+        "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, t;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, t;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, t;\n\t}"
+        ::"r"(acc), "l"(k), "l"(q), "r"(idesc), "r"(add)
+        : "memory");
 }
 
 template <int HD>
@@ -251,7 +231,7 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
     extern __shared__ uint8_t smem_raw[];
     __shared__ KeyLens L;
     __shared__ KeyCols cols[KW_BUFS];
-    __shared__ float sh_half[KW_SWAPS][KW_KEYS];
+    __shared__ float sh_sum[KW_SWAPS][3][KW_KEYS];
     __shared__ uint64_t bars[32 + 2 * KW_BUFS + KW_SWAPS + 1];
     __shared__ uint32_t tmem_slot;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -259,7 +239,7 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
     uint8_t *sK = smem, *sQ = smem + ring.ks * K_BYTES;
     uint64_t *k_full = bars, *k_empty = bars + 8, *q_full = bars + 16, *q_empty = bars + 24;
     uint64_t *s_full = bars + 32, *s_empty = s_full + KW_BUFS;          // s_full: the scores and the columns' lse
-    uint64_t *swap = s_empty + KW_BUFS, *drained = swap + KW_SWAPS;     // swap: one half's sums are in sh_half
+    uint64_t *swap = s_empty + KW_BUFS, *drained = swap + KW_SWAPS;     // swap: the other warps' sums are in sh_sum
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 8; ++i) {
@@ -270,9 +250,9 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
         }
         for (int i = 0; i < KW_BUFS; ++i) {
             mbar_init(&s_full[i], 33);
-            mbar_init(&s_empty[i], 256);
+            mbar_init(&s_empty[i], KW_SOFT / 2);
         }
-        for (int i = 0; i < KW_SWAPS; ++i) mbar_init(&swap[i], 128);
+        for (int i = 0; i < KW_SWAPS; ++i) mbar_init(&swap[i], KW_SOFT - 128);
         mbar_init(drained, 1);
         mbar_fence_init();
     }
@@ -371,7 +351,11 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
                     s_ph ^= 1;
                 }
                 there = mbar_test2(&q_full[qi], q_ph, &s_empty[buf], s_ph);
-                key_issue_step<HD>(acc, da, db, q_region, idesc, q_done, k_done, s_done);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) key_issue4(acc, da + (uint64_t)((r * K_REGION) >> 4), db + (uint64_t)((r * q_region) >> 4), idesc, r);
+                tc_commit_warp(q_done);
+                if (k_done != nullptr) tc_commit_warp(k_done);
+                tc_commit_warp(s_done);
             }
         }
         if (!ok) {                                     // a wait ran out: no product is under way when the CTA ends
@@ -437,9 +421,10 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             ++it;
         }
     } else if (warp >= 4) {
-        const int q = warp & 3, half = (warp - 4) >> 2, r = 32 * q + lane;
+        const int q = warp & 3, part = (warp - 4) >> 2, group = part >> 1, r = 32 * q + lane;
         const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
-        const int nc = s.N / 16, ch0 = half ? (nc + 1) / 2 : 0, ch1 = half ? nc : (nc + 1) / 2;   // this thread's columns, by 16
+        // this thread's columns, by 16: four of 8, or fewer
+        const int nc = s.N / 16, ch0 = (part & 1) * ((nc + 1) / 2), n_ch = (part & 1) ? nc / 2 : (nc + 1) / 2, c0 = 16 * ch0;
         const float2 sl2 = make_float2(s.sl2, s.sl2);
         if (warp == 4 && lane < 2) s.meta[2 * blockIdx.x + lane] = make_int4(0, 0, 0, 0);
         __syncwarp();
@@ -448,38 +433,43 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
         while (ok && walk.next(s, L, p)) {
             float acc = 0.0f;
             for (int st = p.s0; st < p.s1; ++st, ++it) {
+                if ((it & 1) != group) continue;
                 const int buf = it % KW_BUFS;
                 ok = mbar_wait(&s_full[buf], (it / KW_BUFS) & 1, err, ERR_WAIT_SOFTMAX);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 tc_fence_after();
-                const bool masked = cols[buf].masked;
+                const KeyCols &kc = cols[buf];
+                const uint32_t at = lanes + buf * KW_COLS + c0;
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
+                // exponentials of n columns from column c
+                auto run = [&](auto n_, auto masked_, int c, const float *x) {
+                    constexpr int n = decltype(n_)::value;
+                    constexpr bool masked = decltype(masked_)::value;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {          // 32 columns at a time
-                    if (ch0 + 2 * k >= ch1) break;
-                    const int c = 16 * (ch0 + 2 * k);
-                    const bool two = ch0 + 2 * k + 1 < ch1;
-                    float x[32];
-                    if (two) tmem_ld32_sync(lanes + buf * KW_COLS + c, x);
-                    else tmem_ld16_sync(lanes + buf * KW_COLS + c, *reinterpret_cast<float(*)[16]>(x));
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        if (i == 16 && !two) break;
-                        const float4 nl = *reinterpret_cast<const float4 *>(&cols[buf].nl[c + i]);
+                    for (int i = 0; i < n; i += 4) {
+                        const float4 nl = *reinterpret_cast<const float4 *>(&kc.nl[c + i]);
                         float2 a = __ffma2_rn(make_float2(x[i], x[i + 1]), sl2, make_float2(nl.x, nl.y));
                         float2 b = __ffma2_rn(make_float2(x[i + 2], x[i + 3]), sl2, make_float2(nl.z, nl.w));
-                        // pairs i / 2 and i / 2 + 1 of 16: KW_POLY of 8 by the polynomial
-                        if ((i / 2 % 8) * KW_POLY / 8 != (i / 2 % 8 + 1) * KW_POLY / 8) a = exp2_poly2(a);
-                        else a = make_float2(exp2_mufu(a.x), exp2_mufu(a.y));
-                        if ((i / 2 % 8 + 1) * KW_POLY / 8 != (i / 2 % 8 + 2) * KW_POLY / 8) b = exp2_poly2(b);
-                        else b = make_float2(exp2_mufu(b.x), exp2_mufu(b.y));
-                        if (masked) {
-                            const int4 lim = *reinterpret_cast<const int4 *>(&cols[buf].lim[c + i]);
+                        a = make_float2(exp2_mufu(a.x), exp2_mufu(a.y));
+                        b = make_float2(exp2_mufu(b.x), exp2_mufu(b.y));
+                        if constexpr (masked) {
+                            const int4 lim = *reinterpret_cast<const int4 *>(&kc.lim[c + i]);
                             a = make_float2(r < lim.x ? a.x : 0.0f, r < lim.y ? a.y : 0.0f);
                             b = make_float2(r < lim.z ? b.x : 0.0f, r < lim.w ? b.y : 0.0f);
                         }
                         sum0 = __fadd2_rn(sum0, a);
                         sum1 = __fadd2_rn(sum1, b);
+                    }
+                };
+                if (n_ch == 4 && !kc.masked) {
+                    float x[64];
+                    tmem_ld64_sync(at, x);
+                    run(std::integral_constant<int, 64>(), std::false_type(), c0, x);
+                } else {
+                    for (int k = 0; k < n_ch; ++k) {
+                        float x[16];
+                        tmem_ld16_sync(at + 16 * k, x);
+                        run(std::integral_constant<int, 16>(), std::true_type(), c0 + 16 * k, x);
                     }
                 }
                 sum0 = __fadd2_rn(sum0, sum1);
@@ -492,13 +482,13 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             const int slot = 2 * blockIdx.x + (np == 0 ? 0 : 1), key = p.key0 + r, sw = np % KW_SWAPS;
             if (!whole && warp == 4 && lane == 0)
                 s.meta[slot] = make_int4(KW_CUT | (p.s0 == 0 ? KW_BEGIN : 0) | (p.s1 == p.n ? KW_END : 0), p.b, p.key0, 0);
-            if (half == 1) {
-                sh_half[sw][r] = acc;
+            if (part > 0) {
+                sh_sum[sw][part - 1][r] = acc;
                 mbar_arrive(&swap[sw]);
             } else {
                 ok = __all_sync(0xffffffffu, mbar_wait(&swap[sw], (np / KW_SWAPS) & 1, err, ERR_WAIT_SOFTMAX)) != 0;
                 if (!ok) break;
-                acc += sh_half[sw][r];
+                acc += sh_sum[sw][0][r] + sh_sum[sw][1][r] + sh_sum[sw][2][r];
                 if (!whole) s.part[(size_t)slot * KW_KEYS + r] = acc;
                 else if (key < L.len[p.b]) s.put(L.seq[p.b], key, acc);
             }
@@ -879,7 +869,7 @@ size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, 
 
 template <int HD>
 static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
-    constexpr int K_BYTES = KW_KEYS * HD * 2, BUDGET = 200 * 1024;
+    constexpr int K_BYTES = KW_KEYS * HD * 2, BUDGET = 192 * 1024;
     static bool done = false;
     if (!done) {
         const cudaError_t e = cudaFuncSetAttribute(key_weights_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BUDGET + 1024);
