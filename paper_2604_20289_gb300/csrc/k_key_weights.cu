@@ -22,8 +22,8 @@
 namespace xc {
 
 constexpr int KW_MAX_B = 1024;           // branches of a call
-constexpr int KW_KEYS = 128, KW_COLS = 128, KW_BUFS = 4;
-constexpr int KW_SWAPS = 2 * KW_BUFS;    // pieces of a step each that some of the threads may be ahead of others, and more
+constexpr int KW_TILE = 128, KW_KEYS = 2 * KW_TILE, KW_COLS = 128, KW_BUFS = 4;
+constexpr int KW_SWAPS = 4;              // pieces of a step each that a column half may be ahead of the other, and more
 constexpr float KW_LOG2E = 1.4426950408889634f;
 
 struct KeySched {
@@ -39,7 +39,7 @@ struct KeySched {
     float *w;
     long w_ld;
     int4 *meta;              // [2 G] what a CTA's cut pieces are
-    float *part;             // [2 G][128]
+    float *part;             // [2 G][256]
 
     __device__ __forceinline__ int limit(int l, int i) const { return causal ? l - n_q + i + 1 : l; }
     __device__ __forceinline__ void put(int seq, int key, float v) const {
@@ -130,7 +130,7 @@ __device__ void key_lens(const KeySched &s, KeyLens &L, int kt, int *err) {
 }
 
 // ------------------------------------------------------------------ long rows
-// A unit is (branch, 128 keys), its steps the key heads x row tiles that see them.  All units'
+// A unit is (branch, 256 keys), its steps the key heads x row tiles that see them.  All units'
 // steps form one line that the CTAs share evenly, as in the attention: a unit that one CTA
 // runs whole is written at once, the sums of a cut one leave as partials that key_merge_kernel
 // adds in CTA order, so a call gives the same bits every time.
@@ -190,19 +190,16 @@ struct KeyWalk {
     }
 };
 
-// Warps: 0 loads (key tiles page by page, row tiles), 1 issues the products, 2 reads
-// the rows' lse and limits, 4-19 take the exponentials (thread = key; two groups that take steps in
-// turn, two warps per TMEM quadrant in each, half of the columns a warp: all sixteen on every
-// step took 1040 us instead of 780 below).  (A share of the exponentials on the FMA pipe, by Cody and
-// Waite's reduction and a polynomial, made it slower: 2 x 4320 queries over 30240 keys 1040 us without, 1177 with a
-// quarter of them.)
+// Warps: 0 loads (two key tiles of 128 page by page, row tiles), 1 issues the products, 2 reads
+// the rows' lse and limits, 4-19 take the exponentials: eight for either key tile, thread = key,
+// two warps per TMEM quadrant, half of the columns each.  Two key tiles, as every row tile is read from
+// L2 for both: with one, the rows came too late for the products (2 x 4320 queries over 30240 keys, 12 heads x 128:
+// 932 us).  All sixteen warps on every tile: 1040 us.  A share of the exponentials on the FMA pipe (Cody and
+// Waite's reduction and a polynomial) was slower still.
 constexpr int KW_SOFT = 512, KW_THREADS = 128 + KW_SOFT;
-struct KeyRing {
-    int ks, qs;              // slots of key tiles, of row tiles
-};
 struct alignas(16) KeyCols { // what a step's columns need
     float nl[KW_COLS];       // -lse log2(e)
-    int lim[KW_COLS];        // keys of the tile that the column's row sees
+    int lim[KW_COLS];        // keys of the unit that the column's row sees
     int masked;
 };
 
@@ -226,25 +223,27 @@ __device__ __forceinline__ void key_issue4(uint32_t acc, uint64_t k, uint64_t q,
 template <int HD>
 __global__ void __launch_bounds__(KW_THREADS, 1)
     key_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                       const __grid_constant__ KeySched s, const KeyRing ring, int *err) {
-    constexpr int NR = HD / 64, K_REGION = KW_KEYS * 128, K_BYTES = NR * K_REGION;
+                       const __grid_constant__ KeySched s, const int q_slots, int *err) {
+    constexpr int NR = HD / 64, K_REGION = KW_TILE * 128, K_BYTES = NR * K_REGION;
     extern __shared__ uint8_t smem_raw[];
     __shared__ KeyLens L;
-    __shared__ KeyCols cols[KW_BUFS];
-    __shared__ float sh_sum[KW_SWAPS][3][KW_KEYS];
-    __shared__ uint64_t bars[32 + 2 * KW_BUFS + KW_SWAPS + 1];
+    __shared__ KeyCols cols[KW_BUFS / 2];
+    __shared__ float sh_sum[KW_SWAPS][KW_KEYS];
+    __shared__ uint64_t bars[4 + 16 + 2 * KW_BUFS + KW_SWAPS + 1];
     __shared__ uint32_t tmem_slot;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int q_region = s.N * 128, q_bytes = NR * q_region;
-    uint8_t *sK = smem, *sQ = smem + ring.ks * K_BYTES;
-    uint64_t *k_full = bars, *k_empty = bars + 8, *q_full = bars + 16, *q_empty = bars + 24;
-    uint64_t *s_full = bars + 32, *s_empty = s_full + KW_BUFS;          // s_full: the scores and the columns' lse
-    uint64_t *swap = s_empty + KW_BUFS, *drained = swap + KW_SWAPS;     // swap: the other warps' sums are in sh_sum
+    uint8_t *sK = smem, *sQ = smem + 2 * K_BYTES;
+    uint64_t *k_full = bars, *k_empty = bars + 2, *q_full = bars + 4, *q_empty = bars + 12;     // [2] key tiles, [8] row tiles
+    uint64_t *s_full = bars + 20, *s_empty = s_full + KW_BUFS;          // s_full: the scores and the columns' lse
+    uint64_t *swap = s_empty + KW_BUFS, *drained = swap + KW_SWAPS;     // swap: the second half's sums are in sh_sum
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 2; ++i) {
             mbar_init(&k_full[i], 1);
             mbar_init(&k_empty[i], 1);
+        }
+        for (int i = 0; i < 8; ++i) {
             mbar_init(&q_full[i], 1);
             mbar_init(&q_empty[i], 1);
         }
@@ -252,13 +251,13 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             mbar_init(&s_full[i], 33);
             mbar_init(&s_empty[i], KW_SOFT / 2);
         }
-        for (int i = 0; i < KW_SWAPS; ++i) mbar_init(&swap[i], KW_SOFT - 128);
+        for (int i = 0; i < KW_SWAPS; ++i) mbar_init(&swap[i], KW_SOFT / 2);
         mbar_init(drained, 1);
         mbar_fence_init();
     }
     if (warp == 1) tmem_alloc(&tmem_slot, 512);
     // columns that no row tile fills stay zero
-    for (int x = threadIdx.x; x < ring.qs * q_bytes / 16; x += KW_THREADS) reinterpret_cast<uint4 *>(sQ)[x] = make_uint4(0, 0, 0, 0);
+    for (int x = threadIdx.x; x < q_slots * q_bytes / 16; x += KW_THREADS) reinterpret_cast<uint4 *>(sQ)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
     pdl_wait();
     key_lens<true>(s, L, KW_KEYS, err);
@@ -271,41 +270,55 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
     KeyPiece p;
 
     if (warp == 0) {
-        const int box = min(s.ps, KW_KEYS), log_ps = 31 - __clz(s.ps);
-        int kc = 0, qc = 0;
+        const int box = min(s.ps, KW_TILE), log_ps = 31 - __clz(s.ps);
+        int qi = 0, kc = 0, qc = 0;
+        uint32_t q_ph = 1, k_ph = 1;
         bool ok = true;
         while (ok && walk.next(s, L, p)) {
-            const int seq = L.seq[p.b], keys = L.len[p.b] - p.key0;
-            int row = -1;                              // first pool row of this lane's page of the tile
-            if (lane * box < KW_KEYS && lane * box < keys) {
-                const int key = p.key0 + lane * box, id = s.table[(size_t)seq * s.max_pages + (key >> log_ps)];
-                const bool good = id >= 0 && id < s.n_pages;
-                if (!good && err) atomicOr(err, ERR_BAD_SEQ);
-                row = good ? id * s.ps + (key & (s.ps - 1)) : s.n_pages * s.ps;      // out of range: TMA fills zeros
+            const int seq = L.seq[p.b];
+            int row[2];                                // first pool row of this lane's page of either tile
+            uint32_t k_tx[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int key = p.key0 + t * KW_TILE + lane * box;
+                row[t] = -1;
+                if (lane * box < KW_TILE && key < L.len[p.b]) {
+                    const int id = s.table[(size_t)seq * s.max_pages + (key >> log_ps)];
+                    const bool good = id >= 0 && id < s.n_pages;
+                    if (!good && err) atomicOr(err, ERR_BAD_SEQ);
+                    row[t] = good ? id * s.ps + (key & (s.ps - 1)) : s.n_pages * s.ps;      // out of range: TMA fills zeros
+                }
+                k_tx[t] = __popc(__ballot_sync(0xffffffffu, row[t] >= 0)) * box * 128 * NR;
             }
-            const uint32_t k_tx = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box * 128 * NR;
             int h = p.s0 / p.nct, ct = p.s0 - h * p.nct;
             for (int st = p.s0; st < p.s1; ++st, ++qc) {
                 if (st == p.s0 || ct == 0) {
-                    const int i = kc % ring.ks;
-                    ok = mbar_wait(&k_empty[i], ((kc / ring.ks) & 1) ^ 1, err, ERR_WAIT_PRODUCER);
-                    if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
-                    if (lane == 0) mbar_expect_tx(&k_full[i], k_tx);
-                    __syncwarp();
-                    if (row >= 0)
-                        for (int r = 0; r < NR; ++r)
-                            tma_load_2d(sK + i * K_BYTES + r * K_REGION + lane * box * 128, &tmK, &k_full[i], h * HD + 64 * r, row);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        ok = ok && mbar_wait(&k_empty[t], k_ph, err, ERR_WAIT_PRODUCER);
+                        if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+                        if (lane == 0) mbar_expect_tx(&k_full[t], k_tx[t]);
+                        __syncwarp();
+                        if (row[t] >= 0)
+                            for (int r = 0; r < NR; ++r)
+                                tma_load_2d(sK + t * K_BYTES + r * K_REGION + lane * box * 128, &tmK, &k_full[t], h * HD + 64 * r, row[t]);
+                    }
+                    if (!ok) break;
+                    k_ph ^= 1;
                     ++kc;
                 }
-                const int i = qc % ring.qs;
-                ok = mbar_wait(&q_empty[i], ((qc / ring.qs) & 1) ^ 1, err, ERR_WAIT_PRODUCER);
+                ok = mbar_wait(&q_empty[qi], q_ph, err, ERR_WAIT_PRODUCER);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 if (lane == 0) {
-                    mbar_expect_tx(&q_full[i], NR * s.tt * s.grp * 128);
+                    mbar_expect_tx(&q_full[qi], NR * s.tt * s.grp * 128);
                     for (int r = 0; r < NR; ++r)
-                        tma_load_3d(sQ + i * q_bytes + r * q_region, &tmQ, &q_full[i], 64 * r, h * s.grp, p.t0 + ct * s.tt);
+                        tma_load_3d(sQ + qi * q_bytes + r * q_region, &tmQ, &q_full[qi], 64 * r, h * s.grp, p.t0 + ct * s.tt);
                 }
                 __syncwarp();
+                if (++qi == q_slots) {
+                    qi = 0;
+                    q_ph ^= 1;
+                }
                 if (++ct == p.nct) {
                     ct = 0;
                     ++h;
@@ -313,49 +326,49 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
             }
         }
         if (lane == 0) {                               // every copy has landed before the CTA exits
-            for (int j = max(kc - ring.ks, 0); j < kc; ++j) mbar_wait(&k_full[j % ring.ks], (j / ring.ks) & 1, err, ERR_WAIT_PRODUCER);
-            for (int j = max(qc - ring.qs, 0); j < qc; ++j) mbar_wait(&q_full[j % ring.qs], (j / ring.qs) & 1, err, ERR_WAIT_PRODUCER);
+            for (int t = 0; t < 2 && kc > 0; ++t) mbar_wait(&k_full[t], (kc - 1) & 1, err, ERR_WAIT_PRODUCER);
+            for (int j = max(qc - q_slots, 0); j < qc; ++j) mbar_wait(&q_full[j % q_slots], (j / q_slots) & 1, err, ERR_WAIT_PRODUCER);
         }
     } else if (warp == 1) {
-        const uint32_t idesc = idesc_bf16(KW_KEYS, 16, false, false) - ((16u >> 3) << 17) + ((uint32_t)(s.N >> 3) << 17);
+        const uint32_t idesc = idesc_bf16(KW_TILE, 16, false, false) - ((16u >> 3) << 17) + ((uint32_t)(s.N >> 3) << 17);
         const uint64_t dK = sdesc_sw128(smem_u32(sK), 16, 1024), dQ = sdesc_sw128(smem_u32(sQ), 16, 1024);
         auto wait = [&](uint64_t *b, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(b, parity & 1, err, ERR_WAIT_MMA)) != 0;
         };
-        int ki = 0, qi = 0, buf = 0;
+        int qi = 0, buf = 0;
         uint32_t k_ph = 0, q_ph = 0, s_ph = 1;
-        bool ok = true, there = false;                 // there: the next step's rows and buffer have been seen to be ready
+        bool ok = true, there[2] = {false, false};     // the next step's rows and buffers have been seen to be ready
         while (ok && walk.next(s, L, p)) {
             int ct = p.s0 % p.nct;
-            for (int st = p.s0; st < p.s1; ++st) {
-                if ((st == p.s0 || ct == 0) && !(ok = wait(&k_full[ki], k_ph))) break;
-                if (!__all_sync(0xffffffffu, there) && !(ok = wait(&q_full[qi], q_ph) && wait(&s_empty[buf], s_ph))) break;
-                tc_fence_after();
-                const uint64_t da = dK + (uint64_t)((ki * K_BYTES) >> 4), db = dQ + (uint64_t)((qi * q_bytes) >> 4);
-                const uint32_t acc = tmem + buf * KW_COLS;
-                uint64_t *q_done = &q_empty[qi], *k_done = nullptr, *s_done = &s_full[buf];
-                if (++ct == p.nct) ct = 0;
-                if (ct == 0 || st + 1 == p.s1) {
-                    k_done = &k_empty[ki];
-                    if (++ki == ring.ks) {
-                        ki = 0;
-                        k_ph ^= 1;
-                    }
-                }
-                if (++qi == ring.qs) {
-                    qi = 0;
-                    q_ph ^= 1;
-                }
-                if (++buf == KW_BUFS) {
-                    buf = 0;
-                    s_ph ^= 1;
-                }
-                there = mbar_test2(&q_full[qi], q_ph, &s_empty[buf], s_ph);
+            for (int st = p.s0; ok && st < p.s1; ++st) {
+                const bool first = st == p.s0 || ct == 0, last = ct + 1 == p.nct || st + 1 == p.s1;      // of the key tiles
+                const uint64_t db = dQ + (uint64_t)((qi * q_bytes) >> 4);
+                uint64_t *q_done = &q_empty[qi];
+                const int buf0 = buf, q_next = qi + 1 == q_slots ? 0 : qi + 1;
+                const uint32_t s_ph0 = s_ph, q_ph0 = q_ph, q_ph_next = q_next == 0 ? q_ph ^ 1 : q_ph;
+                const int qi0 = qi;
+                buf = buf == KW_BUFS - 2 ? 0 : buf + 2;
+                s_ph ^= buf == 0 ? 1 : 0;
+                const bool t0 = there[0], t1 = there[1];
 #pragma unroll
-                for (int r = 0; r < NR; ++r) key_issue4(acc, da + (uint64_t)((r * K_REGION) >> 4), db + (uint64_t)((r * q_region) >> 4), idesc, r);
-                tc_commit_warp(q_done);
-                if (k_done != nullptr) tc_commit_warp(k_done);
-                tc_commit_warp(s_done);
+                for (int t = 0; t < 2; ++t) {
+                    if (first && !(ok = wait(&k_full[t], k_ph))) break;
+                    if (!__all_sync(0xffffffffu, t == 0 ? t0 : t1) &&
+                        !(ok = (t == 1 || wait(&q_full[qi0], q_ph0)) && wait(&s_empty[buf0 + t], s_ph0))) break;
+                    tc_fence_after();
+                    there[t] = mbar_test2(&q_full[q_next], q_ph_next, &s_empty[buf + t], s_ph);
+                    const uint64_t da = dK + (uint64_t)((t * K_BYTES) >> 4);
+#pragma unroll
+                    for (int r = 0; r < NR; ++r)
+                        key_issue4(tmem + (buf0 + t) * KW_COLS, da + (uint64_t)((r * K_REGION) >> 4), db + (uint64_t)((r * q_region) >> 4), idesc, r);
+                    if (last) tc_commit_warp(&k_empty[t]);
+                    if (t == 1) tc_commit_warp(q_done);
+                    tc_commit_warp(&s_full[buf0 + t]);
+                }
+                if (first) k_ph ^= 1;
+                if (++ct == p.nct) ct = 0;
+                qi = q_next;
+                q_ph = q_ph_next;
             }
         }
         if (!ok) {                                     // a wait ran out: no product is under way when the CTA ends
@@ -395,7 +408,8 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
         int st = p.s0;
         if (more) read(p, st);
         while (ok && more) {
-            const int buf = it % KW_BUFS;
+            const int b2 = it & 1;
+            const uint32_t ph = ((it >> 1) & 1) ^ 1;
             float v[4];
             int m[4];
 #pragma unroll
@@ -409,22 +423,23 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
                 st = p.s0;
             }
             if (more) read(p, st);
-            ok = mbar_wait(&s_empty[buf], ((it / KW_BUFS) & 1) ^ 1, err, ERR_WAIT_SOFTMAX);
+            ok = mbar_wait(&s_empty[2 * b2], ph, err, ERR_WAIT_SOFTMAX) && mbar_wait(&s_empty[2 * b2 + 1], ph, err, ERR_WAIT_SOFTMAX);
             if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                cols[buf].nl[lane + 32 * i] = v[i];
-                cols[buf].lim[lane + 32 * i] = m[i];
+                cols[b2].nl[lane + 32 * i] = v[i];
+                cols[b2].lim[lane + 32 * i] = m[i];
             }
-            if (lane == 0) cols[buf].masked = any;
-            mbar_arrive(&s_full[buf]);
+            if (lane == 0) cols[b2].masked = any;
+            mbar_arrive(&s_full[2 * b2]);
+            mbar_arrive(&s_full[2 * b2 + 1]);
             ++it;
         }
     } else if (warp >= 4) {
-        const int q = warp & 3, part = (warp - 4) >> 2, group = part >> 1, r = 32 * q + lane;
-        const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
+        const int q = warp & 3, half = ((warp - 4) >> 2) & 1, tile = (warp - 4) >> 3, r = tile * KW_TILE + 32 * q + lane;   // key of the unit
+        const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16) + tile * KW_COLS;
         // this thread's columns, by 16: four of 8, or fewer
-        const int nc = s.N / 16, ch0 = (part & 1) * ((nc + 1) / 2), n_ch = (part & 1) ? nc / 2 : (nc + 1) / 2, c0 = 16 * ch0;
+        const int nc = s.N / 16, ch0 = half * ((nc + 1) / 2), n_ch = half ? nc / 2 : (nc + 1) / 2, c0 = 16 * ch0;
         const float2 sl2 = make_float2(s.sl2, s.sl2);
         if (warp == 4 && lane < 2) s.meta[2 * blockIdx.x + lane] = make_int4(0, 0, 0, 0);
         __syncwarp();
@@ -433,13 +448,12 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
         while (ok && walk.next(s, L, p)) {
             float acc = 0.0f;
             for (int st = p.s0; st < p.s1; ++st, ++it) {
-                if ((it & 1) != group) continue;
-                const int buf = it % KW_BUFS;
-                ok = mbar_wait(&s_full[buf], (it / KW_BUFS) & 1, err, ERR_WAIT_SOFTMAX);
+                const int b2 = it & 1;
+                ok = mbar_wait(&s_full[2 * b2 + tile], (it >> 1) & 1, err, ERR_WAIT_SOFTMAX);
                 if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
                 tc_fence_after();
-                const KeyCols &kc = cols[buf];
-                const uint32_t at = lanes + buf * KW_COLS + c0;
+                const KeyCols &kc = cols[b2];
+                const uint32_t at = lanes + 2 * b2 * KW_COLS + c0;
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
                 // exponentials of n columns from column c
                 auto run = [&](auto n_, auto masked_, int c, const float *x) {
@@ -461,10 +475,11 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
                         sum1 = __fadd2_rn(sum1, b);
                     }
                 };
-                if (n_ch == 4 && !kc.masked) {
+                if (n_ch == 4) {
                     float x[64];
                     tmem_ld64_sync(at, x);
-                    run(std::integral_constant<int, 64>(), std::false_type(), c0, x);
+                    if (kc.masked) run(std::integral_constant<int, 64>(), std::true_type(), c0, x);
+                    else run(std::integral_constant<int, 64>(), std::false_type(), c0, x);
                 } else {
                     for (int k = 0; k < n_ch; ++k) {
                         float x[16];
@@ -475,20 +490,20 @@ __global__ void __launch_bounds__(KW_THREADS, 1)
                 sum0 = __fadd2_rn(sum0, sum1);
                 acc += sum0.x + sum0.y;
                 tc_fence_before();
-                mbar_arrive(&s_empty[buf]);
+                mbar_arrive(&s_empty[2 * b2 + tile]);
             }
             if (!ok) break;
             const bool whole = p.s1 - p.s0 == p.n;
             const int slot = 2 * blockIdx.x + (np == 0 ? 0 : 1), key = p.key0 + r, sw = np % KW_SWAPS;
             if (!whole && warp == 4 && lane == 0)
                 s.meta[slot] = make_int4(KW_CUT | (p.s0 == 0 ? KW_BEGIN : 0) | (p.s1 == p.n ? KW_END : 0), p.b, p.key0, 0);
-            if (part > 0) {
-                sh_sum[sw][part - 1][r] = acc;
+            if (half == 1) {
+                sh_sum[sw][r] = acc;
                 mbar_arrive(&swap[sw]);
             } else {
                 ok = __all_sync(0xffffffffu, mbar_wait(&swap[sw], (np / KW_SWAPS) & 1, err, ERR_WAIT_SOFTMAX)) != 0;
                 if (!ok) break;
-                acc += sh_sum[sw][0][r] + sh_sum[sw][1][r] + sh_sum[sw][2][r];
+                acc += sh_sum[sw][r];
                 if (!whole) s.part[(size_t)slot * KW_KEYS + r] = acc;
                 else if (key < L.len[p.b]) s.put(L.seq[p.b], key, acc);
             }
@@ -869,7 +884,7 @@ size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, 
 
 template <int HD>
 static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
-    constexpr int K_BYTES = KW_KEYS * HD * 2, BUDGET = 192 * 1024;
+    constexpr int K_BYTES = KW_TILE * HD * 2, BUDGET = 192 * 1024;
     static bool done = false;
     if (!done) {
         const cudaError_t e = cudaFuncSetAttribute(key_weights_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BUDGET + 1024);
@@ -877,16 +892,14 @@ static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, 
         done = true;
     }
     const int q_bytes = s.N * HD * 2;
-    KeyRing ring;
-    ring.ks = s.n_ct > 2 ? 2 : std::min(8, BUDGET / (K_BYTES + q_bytes));
-    ring.qs = std::min(8, (BUDGET - ring.ks * K_BYTES) / q_bytes);
+    const int q_slots = std::min(8, (BUDGET - 2 * K_BYTES) / q_bytes);
     const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
     CUtensorMap tq, tk;
     if (!make_tmap_heads_bf16(&tq, a.q, HD, (uint64_t)s.Hk * s.grp, (uint64_t)s.B * s.n_q, a.q_ld, s.grp, s.tt) ||
-        !make_tmap_bf16(&tk, a.k, rows, cols, c.page_size < KW_KEYS ? c.page_size : KW_KEYS))
+        !make_tmap_bf16(&tk, a.k, rows, cols, c.page_size < KW_TILE ? c.page_size : KW_TILE))
         return cudaErrorInvalidValue;
     const cudaError_t e = launch_pdl(key_weights_kernel<HD>, dim3(s.G), dim3(KW_THREADS),
-                                     ring.ks * K_BYTES + ring.qs * q_bytes + 1024, st, tq, tk, s, ring, err);
+                                     2 * K_BYTES + q_slots * q_bytes + 1024, st, tq, tk, s, q_slots, err);
     if (e != cudaSuccess) return e;
     return launch_pdl(key_merge_kernel, dim3(2 * s.G), dim3(KW_KEYS), 0, st, s);
 }
