@@ -541,7 +541,8 @@ __global__ void __launch_bounds__(KW_KEYS) key_merge_kernel(const __grid_constan
 // straight into the registers of the MMA's A operand (16 consecutive numbers of a lane are its part of two
 // products; the rows, in shared memory, are laid out to match), the next head's or unit's while it
 // computes, and keeps a sum for every column.  The warps' sums meet in shared memory at the
-// unit's end, in warp order, and one thread writes each (branch, key).  The keys' bytes bound it.
+// unit's end (two places in turn, so that one barrier a unit is enough), in a fixed order, and one thread
+// writes each (branch, key), whose old weight it read when the unit began.  The keys' bytes bound it.
 constexpr int KFEW_THREADS = 512, KFEW_WARPS = KFEW_THREADS / 32, KFEW_COLS = 64, KFEW_PITCH = 20;
 constexpr size_t KFEW_SMEM = 208 * 1024;
 
@@ -577,7 +578,7 @@ struct KeyUnit {
     }
 };
 
-template <int HD, int NT8>
+template <int HD, int NT>
 __global__ void __launch_bounds__(KFEW_THREADS, 1)
     key_weights_few_kernel(const bf16 *__restrict__ q, const long q_ld, const bf16 *__restrict__ k, const __grid_constant__ KeySched s, int *err) {
     constexpr int CH = HD / 32;                        // 16-byte parts of a lane's key row
@@ -586,10 +587,11 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
     __shared__ __align__(8) int sh_lim[KFEW_COLS];
     __shared__ int sh_least;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-    const int ncol = s.N, nt = ncol / 8, kt = 16 * s.wk, wh = warp % s.wh, wk = warp / s.wh;
+    constexpr int ncol = 8 * NT;
+    const int kt = 16 * s.wk, wh = warp % s.wh, wk = warp / s.wh;
     uint4 *sQ = sm_few;                                // [Hk][CH][ncol][4]
     float *sNl = reinterpret_cast<float *>(sQ + (size_t)s.Hk * CH * ncol * 4);     // [Hk][ncol]
-    float *red = sNl + s.Hk * ncol;                    // [warps][ncol][KFEW_PITCH]
+    float *red = sNl + s.Hk * ncol;                    // [2][warps][ncol][KFEW_PITCH]
     pdl_wait();
     key_lens<false>(s, L, kt, err);
     pdl_release();
@@ -658,7 +660,21 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
         const long row_after = page(u + 2);            // the table's entry comes while this unit is computed
         const int key = unit.key0 + 16 * wk;           // this warp's first key
         const bool masked = key + 16 > sh_least, there = key < unit.end;
-        float acc[NT8][4] = {};
+        // this thread's outputs, (branch j, key r) of the unit: the first two
+        const int each = s.n_q * s.grp, outs = (unit.own ? 1 : tokens / s.n_q) * kt;
+        float *at_w[2];
+        float old[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int y = tid + i * KFEW_THREADS, j = y / kt, r = y - j * kt, ky = unit.key0 + r;
+            at_w[i] = nullptr;
+            if (y < outs) {
+                const int b = unit.own ? unit.b : unit.b * s.nb + j;
+                if (ky < unit.end && ky < L.len[b]) at_w[i] = s.w + (size_t)L.seq[b] * s.w_ld + ky;
+            }
+            old[i] = at_w[i] != nullptr && s.decay != 0.0f ? *at_w[i] : 0.0f;
+        }
+        float acc[NT][4] = {};
         for (int h = wh; h < s.Hk; h += s.wh) {
             uint4 a[2][CH];
 #pragma unroll
@@ -671,12 +687,11 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
             const uint4 *qh = sQ + (size_t)h * CH * ncol * 4 + 4 * gid + tig;
             const float *nl = sNl + h * ncol + 2 * tig;
 #pragma unroll
-            for (int n = 0; n < NT8; ++n) {
-                if (n >= nt) break;
+            for (int n = 0; n < NT; ++n) {
                 float sc[2][4] = {};
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    const uint4 b = qh[(size_t)(c * ncol + 8 * n) * 4];
+                    const uint4 b = qh[(c * ncol + 8 * n) * 4];
                     mma_bf16(sc[0], a[0][c].x, a[1][c].x, a[0][c].y, a[1][c].y, b.x, b.y);
                     mma_bf16(sc[1], a[0][c].z, a[1][c].z, a[0][c].w, a[1][c].w, b.z, b.w);
                 }
@@ -695,10 +710,9 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
                 for (int j = 0; j < 4; ++j) acc[n][j] += p[j];
             }
         }
-        float *mine = red + (size_t)warp * ncol * KFEW_PITCH;
+        float *place = red + (u & 1) * KFEW_WARPS * ncol * KFEW_PITCH, *mine = place + warp * ncol * KFEW_PITCH;
 #pragma unroll
-        for (int n = 0; n < NT8; ++n) {
-            if (n >= nt) break;
+        for (int n = 0; n < NT; ++n) {
             float *at = mine + (8 * n + 2 * tig) * KFEW_PITCH + gid;
             at[0] = acc[n][0];
             at[KFEW_PITCH] = acc[n][1];
@@ -706,20 +720,34 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
             at[KFEW_PITCH + 8] = acc[n][3];
         }
         __syncthreads();
-        // one thread a (branch, key): the warps of the key's 16, the branch's columns
-        const int each = s.n_q * s.grp, branches = unit.own ? 1 : tokens / s.n_q;
-        for (int y = tid; y < branches * kt; y += KFEW_THREADS) {
-            const int j = y / kt, r = y - j * kt, ky = unit.key0 + r;
-            const int b = unit.own ? unit.b : unit.b * s.nb + j;
-            if (ky >= unit.end || ky >= L.len[b]) continue;
-            float v = 0.0f;
-            for (int w = 0; w < s.wh; ++w) {
-                const float *at = red + ((size_t)((r >> 4) * s.wh + w) * ncol + j * each) * KFEW_PITCH + (r & 15);
-                for (int c = 0; c < each; ++c) v += at[c * KFEW_PITCH];
+        // the warps of the key's 16, the branch's columns; a warp writes the next unit's sums elsewhere, and those
+        // after them behind a barrier that this comes before
+        auto total = [&](int y) {
+            const int j = y / kt, r = y - j * kt;
+            const float *at = place + ((r >> 4) * s.wh * ncol + j * each) * KFEW_PITCH + (r & 15);
+            float v0 = 0.0f, v1 = 0.0f, v2 = 0.0f, v3 = 0.0f;
+            for (int c = 0; c < each; ++c, at += KFEW_PITCH) {
+                int w = 0;
+                for (; w + 3 < s.wh; w += 4) {
+                    v0 += at[w * ncol * KFEW_PITCH];
+                    v1 += at[(w + 1) * ncol * KFEW_PITCH];
+                    v2 += at[(w + 2) * ncol * KFEW_PITCH];
+                    v3 += at[(w + 3) * ncol * KFEW_PITCH];
+                }
+                for (; w < s.wh; ++w) v0 += at[w * ncol * KFEW_PITCH];
             }
-            s.put(L.seq[b], ky, v);
+            return (v0 + v1) + (v2 + v3);
+        };
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (at_w[i] != nullptr) {
+                const float sum = total(tid + i * KFEW_THREADS);
+                *at_w[i] = s.decay == 0.0f ? sum : fmaf(s.decay, old[i], sum);
+            }
+        for (int y = tid + 2 * KFEW_THREADS; y < outs; y += KFEW_THREADS) {      // many branches of one key head
+            const int j = y / kt, ky = unit.key0 + y - j * kt, b = unit.own ? unit.b : unit.b * s.nb + j;
+            if (ky < unit.end && ky < L.len[b]) s.put(L.seq[b], ky, total(y));
         }
-        __syncthreads();
         row = row_next;
         row_next = row_after;
     }
@@ -832,7 +860,7 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------------- host
-static size_t few_smem(int Hk, int N, int head_dim) { return (size_t)Hk * N * (head_dim * 2 + 4) + (size_t)KFEW_WARPS * N * KFEW_PITCH * 4; }
+static size_t few_smem(int Hk, int N, int head_dim) { return (size_t)Hk * N * (head_dim * 2 + 4) + 2 * (size_t)KFEW_WARPS * N * KFEW_PITCH * 4; }
 static KeySched key_plan(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     KeySched s{};
     s.B = B;
@@ -903,23 +931,18 @@ static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, 
     if (e != cudaSuccess) return e;
     return launch_pdl(key_merge_kernel, dim3(2 * s.G), dim3(KW_KEYS), 0, st, s);
 }
-template <int HD, int NT8>
-static cudaError_t key_launch_few_(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
+template <int HD, int NT>
+static cudaError_t key_launch_few(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
+    if constexpr (NT > 1)
+        if (s.N < 8 * NT) return key_launch_few<HD, NT - 1>(a, s, err, st);
     static bool done = false;
     if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(key_weights_few_kernel<HD, NT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)KFEW_SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(key_weights_few_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)KFEW_SMEM);
         if (e != cudaSuccess) return e;
         done = true;
     }
-    return launch_pdl(key_weights_few_kernel<HD, NT8>, dim3(s.G), dim3(KFEW_THREADS), few_smem(s.Hk, s.N, HD), st, reinterpret_cast<const bf16 *>(a.q), a.q_ld,
-                      reinterpret_cast<const bf16 *>(a.k), s, err);
-}
-template <int HD>
-static cudaError_t key_launch_few(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
-    if (s.N <= 8) return key_launch_few_<HD, 1>(a, s, err, st);
-    if (s.N <= 16) return key_launch_few_<HD, 2>(a, s, err, st);
-    if (s.N <= 32) return key_launch_few_<HD, 4>(a, s, err, st);
-    return key_launch_few_<HD, 8>(a, s, err, st);
+    return launch_pdl(key_weights_few_kernel<HD, NT>, dim3(s.G), dim3(KFEW_THREADS), few_smem(s.Hk, s.N, HD), st,
+                      reinterpret_cast<const bf16 *>(a.q), a.q_ld, reinterpret_cast<const bf16 *>(a.k), s, err);
 }
 template <int HD>
 static cudaError_t key_launch_f32(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
@@ -946,8 +969,8 @@ cudaError_t key_weights(const xc_kv_cache &c, const KeyWeightsArgs &a, void *ws,
     s.meta = reinterpret_cast<int4 *>(ws);
     s.part = reinterpret_cast<float *>(s.meta + 2 * s.G);
     if (c.dtype == XC_BF16) {
-        if (c.head_dim == 64) return s.wh > 0 ? key_launch_few<64>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
-        if (c.head_dim == 128) return s.wh > 0 ? key_launch_few<128>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
+        if (c.head_dim == 64) return s.wh > 0 ? key_launch_few<64, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
+        if (c.head_dim == 128) return s.wh > 0 ? key_launch_few<128, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
         return cudaErrorInvalidValue;
     }
     switch (c.head_dim) {

@@ -187,7 +187,8 @@ def test_a_thousand_branches():
 @pytest.mark.parametrize("H,hk,hd,lens,n_q,shared", [
     (128, 128, 128, [200, 150], 1, 64),                # more key heads than rows fit shared memory
     (40, 40, 128, [300, 260, 290], 1, 256), (3, 3, 64, [300, 260, 290], 7, 256), (5, 5, 128, [130] * 9, 12, 64),
-    (48, 16, 64, [400, 333], 5, 320), (17, 17, 64, [90, 70], 3, 0), (64, 2, 64, [99, 500, 64], 2, 0), (2, 1, 128, [700], 32, 0),
+    (48, 16, 64, [400, 333], 5, 320), (1, 1, 64, [300 + 3 * b for b in range(70)], 1, 288),
+    (2, 2, 128, [300 + b for b in range(66)], 1, 288), (17, 17, 64, [90, 70], 3, 0), (64, 2, 64, [99, 500, 64], 2, 0), (2, 1, 128, [700], 32, 0),
     (2, 1, 128, [700], 33, 0), (6, 6, 128, [1000] * 3, 64, 512), (6, 6, 128, [1000] * 3, 65, 512)])
 def test_head_layouts_of_few_rows(H, hk, hd, lens, n_q, shared):
     check("bf16", H, hk, hd, 32, lens, n_q, shared, True)
