@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
     __shared__ int sh_least;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
     constexpr int ncol = 8 * NT;
-    const int kt = 16 * s.wk, wh = warp % s.wh, wk = warp / s.wh;
+    const int log_kt = 4 + 31 - __clz(s.wk), kt = 1 << log_kt, wh = warp % s.wh, wk = warp / s.wh;
     uint4 *sQ = sm_few;                                // [Hk][CH][ncol][4]
     float *sNl = reinterpret_cast<float *>(sQ + (size_t)s.Hk * CH * ncol * 4);     // [Hk][ncol]
     float *red = sNl + s.Hk * ncol;                    // [2][warps][ncol][KFEW_PITCH]
@@ -598,18 +598,25 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
     const int log_ps = 31 - __clz(s.ps);
     const int U = s.n_pt * s.n_ct + L.off[s.B], u0 = (int)((long long)U * blockIdx.x / gridDim.x), u1 = (int)((long long)U * (blockIdx.x + 1) / gridDim.x);
     if (u0 == u1) return;
-    // pool row of the first of this warp's 16 keys of unit u; -1: no keys there, -2: a bad page
-    auto page = [&](int u) -> long {
-        if (u >= u1) return -1;
+    // Table entry of this warp's 16 keys of unit u (loaded, not looked at), and the first one's place in the page;
+    // the pool row that it makes, -1: no keys, -2: a bad page.
+    auto entry = [&](int u, int &id, int &at) {
+        id = 0;
+        at = -1;
+        if (u >= u1) return;
         const KeyUnit x(s, L, u, kt);
         const int key = x.key0 + 16 * wk, seq = L.seq[x.own ? x.b : 0];
-        if (key >= x.end) return -1;
-        const int id = seq >= 0 && seq < s.max_seqs ? s.table[(size_t)seq * s.max_pages + (key >> log_ps)] : -1;
+        if (key >= x.end) return;
+        at = key & (s.ps - 1);
+        id = seq >= 0 && seq < s.max_seqs ? s.table[(size_t)seq * s.max_pages + (key >> log_ps)] : -1;
+    };
+    auto pool_row = [&](int id, int at) -> long {
+        if (at < 0) return -1;
         if (id < 0 || id >= s.n_pages) {
             if (err) atomicOr(err, ERR_BAD_SEQ);
             return -2;
         }
-        return (long)id * s.ps + (key & (s.ps - 1));
+        return (long)id * s.ps + at;
     };
     auto load = [&](long row, int h, uint4 (&x)[2][CH]) {
 #pragma unroll
@@ -619,7 +626,10 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
                 x[r][c] = row >= 0 ? *reinterpret_cast<const uint4 *>(k + ((size_t)(row + gid + 8 * r) * s.Hk + h) * HD + 32 * c + 8 * tig)
                                    : make_uint4(0, 0, 0, 0);
     };
-    long row = page(u0), row_next = page(u0 + 1);
+    int id0, at0, id1, at1;
+    entry(u0, id0, at0);
+    entry(u0 + 1, id1, at1);
+    long row = pool_row(id0, at0), row_next = pool_row(id1, at1);
     uint4 x[2][CH];
     if (wh < s.Hk) load(row, wh, x);
     int have_own = -1, have_b = -1;                    // whose rows are in shared memory
@@ -631,12 +641,22 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
             have_own = unit.own;
             have_b = unit.b;
             __syncthreads();                           // the last unit's rows have been used
-            for (int y = tid; y < s.Hk * ncol * CH * 4; y += KFEW_THREADS) {
-                const int part = y % (CH * 4), rest = y / (CH * 4), c = rest % ncol, h = rest / ncol;
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (c < cols)
-                    v = *reinterpret_cast<const uint4 *>(q + (size_t)(t0 + c / s.grp) * q_ld + (h * s.grp + c % s.grp) * HD + 8 * part);
-                sQ[((size_t)(h * CH + part / 4) * ncol + c) * 4 + part % 4] = v;
+            const int parts = s.Hk * ncol * CH * 4;
+            constexpr int BATCH = 6;                   // loads in flight
+            for (int y0 = tid; y0 < parts; y0 += BATCH * KFEW_THREADS) {
+                uint4 v[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int y = y0 + i * KFEW_THREADS, part = y % (CH * 4), rest = y / (CH * 4), c = rest % ncol, h = rest / ncol;
+                    v[i] = make_uint4(0, 0, 0, 0);
+                    if (y < parts && c < cols)
+                        v[i] = *reinterpret_cast<const uint4 *>(q + (size_t)(t0 + c / s.grp) * q_ld + (h * s.grp + c % s.grp) * HD + 8 * part);
+                }
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int y = y0 + i * KFEW_THREADS, part = y % (CH * 4), rest = y / (CH * 4), c = rest % ncol, h = rest / ncol;
+                    if (y < parts) sQ[((h * CH + part / 4) * ncol + c) * 4 + part % 4] = v[i];
+                }
             }
             for (int y = tid; y < s.Hk * ncol; y += KFEW_THREADS) {
                 const int c = y % ncol, h = y / ncol;
@@ -657,7 +677,7 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
             }
             __syncthreads();
         }
-        const long row_after = page(u + 2);            // the table's entry comes while this unit is computed
+        entry(u + 2, id1, at1);                        // the table's entry comes while this unit is computed
         const int key = unit.key0 + 16 * wk;           // this warp's first key
         const bool masked = key + 16 > sh_least, there = key < unit.end;
         // this thread's outputs, (branch j, key r) of the unit: the first two
@@ -666,7 +686,7 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
         float old[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int y = tid + i * KFEW_THREADS, j = y / kt, r = y - j * kt, ky = unit.key0 + r;
+            const int y = tid + i * KFEW_THREADS, j = y >> log_kt, r = y & (kt - 1), ky = unit.key0 + r;
             at_w[i] = nullptr;
             if (y < outs) {
                 const int b = unit.own ? unit.b : unit.b * s.nb + j;
@@ -723,18 +743,22 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
         // the warps of the key's 16, the branch's columns; a warp writes the next unit's sums elsewhere, and those
         // after them behind a barrier that this comes before
         auto total = [&](int y) {
-            const int j = y / kt, r = y - j * kt;
+            const int j = y >> log_kt, r = y & (kt - 1);
             const float *at = place + ((r >> 4) * s.wh * ncol + j * each) * KFEW_PITCH + (r & 15);
             float v0 = 0.0f, v1 = 0.0f, v2 = 0.0f, v3 = 0.0f;
-            for (int c = 0; c < each; ++c, at += KFEW_PITCH) {
-                int w = 0;
-                for (; w + 3 < s.wh; w += 4) {
-                    v0 += at[w * ncol * KFEW_PITCH];
-                    v1 += at[(w + 1) * ncol * KFEW_PITCH];
-                    v2 += at[(w + 2) * ncol * KFEW_PITCH];
-                    v3 += at[(w + 3) * ncol * KFEW_PITCH];
+            for (int w = 0; w < s.wh; ++w, at += ncol * KFEW_PITCH) {
+                const float *p = at;
+                int c = each;
+#pragma unroll 2
+                for (; c >= 4; c -= 4, p += 4 * KFEW_PITCH) {
+                    v0 += p[0];
+                    v1 += p[KFEW_PITCH];
+                    v2 += p[2 * KFEW_PITCH];
+                    v3 += p[3 * KFEW_PITCH];
                 }
-                for (; w < s.wh; ++w) v0 += at[w * ncol * KFEW_PITCH];
+                if (c > 0) v0 += p[0];
+                if (c > 1) v1 += p[KFEW_PITCH];
+                if (c > 2) v2 += p[2 * KFEW_PITCH];
             }
             return (v0 + v1) + (v2 + v3);
         };
@@ -745,11 +769,11 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
                 *at_w[i] = s.decay == 0.0f ? sum : fmaf(s.decay, old[i], sum);
             }
         for (int y = tid + 2 * KFEW_THREADS; y < outs; y += KFEW_THREADS) {      // many branches of one key head
-            const int j = y / kt, ky = unit.key0 + y - j * kt, b = unit.own ? unit.b : unit.b * s.nb + j;
+            const int j = y >> log_kt, ky = unit.key0 + (y & (kt - 1)), b = unit.own ? unit.b : unit.b * s.nb + j;
             if (ky < unit.end && ky < L.len[b]) s.put(L.seq[b], ky, total(y));
         }
         row = row_next;
-        row_next = row_after;
+        row_next = pool_row(id1, at1);
     }
 }
 
