@@ -57,7 +57,8 @@ xc_status xc_op_quantize_rows(int dtype, int M, int K, const void *x, signed cha
  * XC_EPI_RESID_GATE as in xc_op_linear; out may be resid.  Any M from 0 below 2^24 and any N from 1;
  * K a multiple of 16 up to 131072.
  *   workspace  device, 256-byte aligned, at least
- *              xc_op_linear_i8_workspace_bytes(); contents on entry are
+ *              xc_op_linear_i8_workspace_bytes() (0 where a call of few tokens needs
+ *              none: then it may be NULL); contents on entry are
  *              ignored; not shared by overlapping calls */
 size_t xc_op_linear_i8_workspace_bytes(int M, int N, int K);
 xc_status xc_op_linear_i8(int dtype, int epilogue, int M, int N, int K, const void *A, const float *a_scale,

@@ -1045,7 +1045,7 @@ static I8Plan i8_plan(int M, int N, int K) {
     p.bytes = p.off_part + (p.cut ? (size_t)4 * s.P * s.NT * I8_BM * sizeof(float) : 0);
     return p;
 }
-size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_small(M, K) ? 256 : i8_plan(M, N, K).bytes; }
+size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_small(M, K) ? 0 : i8_plan(M, N, K).bytes; }
 
 template <typename T>
 static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUtensorMap &ta, int *err, cudaStream_t st) {

@@ -1609,7 +1609,7 @@ xc_status xc_op_linear_i8(int dtype, int epilogue, int M, int N, int K, const vo
         OP_FAIL(XC_EINVAL, "xc_op_linear_i8: gated residual needs gate and resid");
     if (!i8_aligned(A) || !i8_aligned(Wt)) OP_FAIL(XC_EINVAL, "xc_op_linear_i8: A and Wt must be 16-byte aligned");
     const size_t need = linear_i8_workspace_bytes(M, N, K);
-    if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need)
+    if (need > 0 && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need))
         OP_FAIL(XC_EINVAL, "xc_op_linear_i8: workspace of %zu bytes needed (256-byte aligned)", need);
     int *err = op_err_word();
     if (err == nullptr) OP_FAIL(XC_ECUDA, "xc_op_linear_i8: error word");

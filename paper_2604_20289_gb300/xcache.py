@@ -335,10 +335,16 @@ def op_linear(dtype, epilogue, A, Wt, bias, out, gate=None, resid=None, xin=None
                            _stream(stream)))
 
 
+_types = None
+
+
 def _torch_types(dtype):
-    """(the activations' torch type, torch)"""
-    import torch
-    return (torch.float32 if dtype_code(dtype) == XC_F32 else torch.bfloat16), torch
+    """(the activations' torch type, float32, int8)"""
+    global _types
+    if _types is None:
+        import torch
+        _types = {XC_F32: (torch.float32, torch.float32, torch.int8), XC_BF16: (torch.bfloat16, torch.float32, torch.int8)}
+    return _types[dtype_code(dtype)]
 
 
 def _on_device(*tensors):
@@ -352,17 +358,21 @@ def _on_device(*tensors):
 
 def op_quantize_rows(dtype, x, q, scale, stream=None):
     """8-bit integers q [M, K] (int8) and scale [M] (float32) of the rows of x [M, K]; all contiguous."""
-    dt, torch = _torch_types(dtype)
+    dt, f32, i8 = _torch_types(dtype)
     _on_device(x, q, scale)
-    if x.dim() != 2 or x.dtype is not dt or q.shape != x.shape or q.dtype is not torch.int8 or \
-            scale.shape != x.shape[:1] or scale.dtype is not torch.float32 or \
+    if x.dim() != 2 or x.dtype is not dt or q.shape != x.shape or q.dtype is not i8 or \
+            scale.shape != x.shape[:1] or scale.dtype is not f32 or \
             not (x.is_contiguous() and q.is_contiguous() and scale.is_contiguous()):
         raise ValueError("x [M, K] of dtype, q [M, K] int8, scale [M] float32, all contiguous")
     M, K = x.shape
     check(LIB.xc_op_quantize_rows(dtype_code(dtype), M, K, x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(stream)))
 
 
+_I8_BYTES = {}                                    # workspace sizes by shape
+
+
 def op_linear_i8_workspace_bytes(M, N, K) -> int:
+    """0 where a call of few tokens needs none."""
     return LIB.xc_op_linear_i8_workspace_bytes(M, N, K)
 
 
@@ -372,8 +382,7 @@ def op_linear_i8(dtype, epilogue, A, Wq, w_scale, bias, out, gate=None, resid=No
     quantised by the call, or with a_scale [M] (float32) int8.  gate [N] float32 and resid [M, N] of dtype for
     XC_EPI_RESID_GATE.  All contiguous.  workspace: a device tensor of op_linear_i8_workspace_bytes, or None: allocated
     for the call (in a capture: from the graph's memory)."""
-    dt, torch = _torch_types(dtype)
-    f32, i8 = torch.float32, torch.int8
+    dt, f32, i8 = _torch_types(dtype)
     _on_device(A, Wq, w_scale, bias, out, gate, resid, a_scale)
     (M, K), N = A.shape, Wq.shape[0]
     if A.dtype is not (dt if a_scale is None else i8) or Wq.dtype is not i8 or Wq.shape != (N, K) or \
@@ -388,7 +397,12 @@ def op_linear_i8(dtype, epilogue, A, Wq, w_scale, bias, out, gate=None, resid=No
         raise ValueError("gate [N] and a_scale [M] float32, resid [M, N] of dtype, all contiguous")
     cuda = _stream(stream)
     if workspace is None:
-        buf, ws, nbytes = _scratch(LIB.xc_op_linear_i8_workspace_bytes(M, N, K), stream, cuda, A.device)
+        need = _I8_BYTES.get((M, N, K))
+        if need is None:
+            if len(_I8_BYTES) >= 4096:
+                _I8_BYTES.clear()
+            need = _I8_BYTES[M, N, K] = LIB.xc_op_linear_i8_workspace_bytes(M, N, K)
+        buf, ws, nbytes = _scratch(need, stream, cuda, A.device) if need else (None, None, 0)
     else:
         buf, ws, nbytes = _given(workspace)
     st = LIB.xc_op_linear_i8(dtype_code(dtype), epilogue, M, N, K, A.data_ptr(), _ptr(a_scale), Wq.data_ptr(),

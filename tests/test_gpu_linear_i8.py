@@ -285,8 +285,8 @@ def test_streams_and_graphs():
 
 
 def test_refusals():
-    o = operands("bf16", 8, 64, 64)
-    out = torch.empty(8, 64, dtype=torch.bfloat16, device=DEV)
+    o = operands("bf16", 40, 64, 64)
+    out = torch.empty(40, 64, dtype=torch.bfloat16, device=DEV)
     args = dict(A=o["x"], Wq=o["wq"], w_scale=o["ws"], bias=o["bias"], out=out)
 
     def call(epi="bias", **kw):
@@ -299,7 +299,7 @@ def test_refusals():
     for bad in (dict(A=o["x"].float()), dict(A=o["x"].t()), dict(Wq=o["wq"].float()), dict(Wq=o["wq"][:, :48]),
                 dict(w_scale=o["ws"].double()), dict(bias=o["bias"][:63]), dict(out=out.float()), dict(out=out.t()),
                 dict(A=o["x"].cpu()), dict(out=out.cpu()), dict(resid=o["resid"].float()), dict(gate=o["gate"].double()),
-                dict(a_scale=o["ws"][:8])):
+                dict(a_scale=o["ws"][:40])):
         with pytest.raises(ValueError):
             call(**bad)
     for bad in (dict(epi="resid"), dict(workspace=torch.empty(16, dtype=torch.uint8, device=DEV))):
@@ -307,6 +307,6 @@ def test_refusals():
             call(**bad)
         assert e.value.status == xb.XC_EINVAL
     with pytest.raises(xb.XCacheError):
-        call(A=torch.zeros(8, 40, dtype=torch.bfloat16, device=DEV), Wq=torch.zeros(64, 40, dtype=torch.int8, device=DEV))
+        call(A=torch.zeros(40, 40, dtype=torch.bfloat16, device=DEV), Wq=torch.zeros(64, 40, dtype=torch.int8, device=DEV))
     with pytest.raises(ValueError):
-        xb.op_quantize_rows("f32", o["x"], torch.empty_like(o["x"], dtype=torch.int8), torch.empty(8, device=DEV))
+        xb.op_quantize_rows("f32", o["x"], torch.empty_like(o["x"], dtype=torch.int8), torch.empty(40, device=DEV))

@@ -39,7 +39,7 @@ def test_quantise_refusals(xb, kw, msg):
     (dict(epi=2, gate=P), "residual"), (dict(A=P + 8), "aligned"), (dict(W=P + 8), "aligned"), (dict(work=0), "workspace"),
     (dict(work=P + 16), "workspace"), (dict(bytes=100), "workspace")])
 def test_product_refusals(xb, kw, msg):
-    a = dict(dtype=xb.XC_BF16, epi=0, M=4, N=100, K=64, A=P, W=P, ws=P, bias=P, gate=0, resid=0, out=P, work=P, bytes=1 << 40)
+    a = dict(dtype=xb.XC_BF16, epi=0, M=40, N=100, K=64, A=P, W=P, ws=P, bias=P, gate=0, resid=0, out=P, work=P, bytes=1 << 40)
     a.update(kw)
     st = xb.LIB.xc_op_linear_i8(a["dtype"], a["epi"], a["M"], a["N"], a["K"], a["A"], None, a["W"], a["ws"], a["bias"],
                                 a["gate"], a["resid"], a["out"], a["work"], a["bytes"], None)
@@ -51,6 +51,7 @@ def test_nothing_to_do(xb):
     assert xb.LIB.xc_op_quantize_rows(xb.XC_BF16, 0, 64, None, None, None, None) == xb.XC_OK
     assert xb.LIB.xc_op_linear_i8(xb.XC_F32, 0, 0, 8, 64, *[None] * 8, None, 0, None) == xb.XC_OK
     assert xb.op_linear_i8_workspace_bytes(0, 8, 64) == 0
+    assert xb.op_linear_i8_workspace_bytes(4, 8, 64) == 0 and xb.op_linear_i8_workspace_bytes(40, 8, 64) > 0
     assert xb.op_linear_i8_workspace_bytes(4, 8, 40) == 0 and "K a multiple" in xb.last_error(None)
 
 
