@@ -27,6 +27,7 @@ template <typename T> struct Vec8;
 template <> struct Vec8<bf16> {
     uint4 u;
     __device__ __forceinline__ void load(const bf16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void store(bf16 *p) const { *reinterpret_cast<uint4 *>(p) = u; }
     // largest magnitude of the eight and m, as bits (NaN above infinity above the rest)
     __device__ __forceinline__ unsigned top(unsigned m) const {
         unsigned x = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
@@ -47,6 +48,10 @@ template <> struct Vec8<float> {
     __device__ __forceinline__ void load(const float *p) {
         a = reinterpret_cast<const float4 *>(p)[0];
         b = reinterpret_cast<const float4 *>(p)[1];
+    }
+    __device__ __forceinline__ void store(float *p) const {
+        reinterpret_cast<float4 *>(p)[0] = a;
+        reinterpret_cast<float4 *>(p)[1] = b;
     }
     __device__ __forceinline__ unsigned top(unsigned m) const {
         const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -204,6 +209,52 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR == 512 ? 1 : TPR ==
     }
 }
 
+// Few rows: a CTA a row, which waits in shared memory for its largest magnitude.  Latency bound, and the code
+// is short: a loop over a row in registers is unrolled, and its instructions have to be fetched too.
+constexpr int QFEW_BYTES = 48 * 1024;
+template <typename T, typename Q, int THREADS>
+__global__ void __launch_bounds__(THREADS) quantize_few_kernel(const T *__restrict__ x, Q *__restrict__ q, float *__restrict__ scale, const int K) {
+    extern __shared__ __align__(16) uint8_t quant_row[];
+    __shared__ unsigned sh[THREADS / 32];
+    pdl_wait();
+    pdl_release();
+    const int t = threadIdx.x, nv = K / 8, row = blockIdx.x;
+    const T *src = x + (size_t)row * K;
+    T *stage = reinterpret_cast<T *>(quant_row);
+    unsigned top = 0;
+    for (int v0 = t; v0 < nv; v0 += 4 * THREADS) {
+        Vec8<T> z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (v0 + i * THREADS < nv) z[i].load(src + 8 * (v0 + i * THREADS));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (v0 + i * THREADS < nv) {
+                z[i].store(stage + 8 * (v0 + i * THREADS));
+                top = z[i].top(top);
+            }
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((t & 31) == 0) sh[t >> 5] = top;
+    __syncthreads();
+    top = __reduce_max_sync(0xffffffffu, sh[t & (THREADS / 32 - 1)]);
+    if (t == 0) scale[row] = quant_scale(top);
+    const QuantRow qr(top);
+    Q *dst = q + (size_t)row * K;
+#pragma unroll 1
+    for (int v = t; v < nv; v += THREADS) {
+        Vec8<T> z;
+        float e[8];
+        z.load(stage + 8 * v);
+        quant8<T>(z, qr, e);
+        if constexpr (sizeof(Q) == 1) {
+            *reinterpret_cast<uint2 *>(dst + 8 * v) = pack8(e);
+        } else {
+            *reinterpret_cast<uint4 *>(dst + 8 * v) = half8(e);
+        }
+    }
+}
+
 template <typename T, typename Q>
 static cudaError_t quantize_launch(const T *x, Q *q, float *scale, int M, int K, cudaStream_t st) {
     const int nv = K / 8, sms = device_sms();
@@ -212,11 +263,14 @@ static cudaError_t quantize_launch(const T *x, Q *q, float *scale, int M, int K,
         const int cta = tpr < 128 ? 128 : tpr, ctas = (M + cta / tpr - 1) / (cta / tpr);
         return launch_pdl(kernel, dim3(std::min(ctas, per_sm * sms)), dim3(cta), 0, st, x, q, scale, M, K);
     };
-    // Few rows: the most threads a row with which all of them run at one time.  Many: the
-    // fewest that hold a row in registers, so that an SM has many rows' loads under way.
-    if (nv > 128 && M <= sms) return launch(quantize_rows_kernel<T, Q, 512, KEEP>, 512, 1);
-    if (nv > 64 && M <= 3 * sms) return launch(quantize_rows_kernel<T, Q, 256, KEEP>, 256, 3);
-    if (nv > 32 && M <= 5 * sms) return launch(quantize_rows_kernel<T, Q, 128, KEEP>, 128, 5);
+    auto few = [&](auto kernel, int threads) {
+        return launch_pdl(kernel, dim3(M), dim3(threads), (size_t)K * sizeof(T), st, x, q, scale, K);
+    };
+    // Few rows at one time, with the more threads the fewer and the longer they are (8 x 5120 bf16: 6.2 us with
+    // 512 threads, 6.5 with 256; 331 x 13824: 20.9 and 22.7; 560 x 1536: 7.8 and 6.7; in registers 6.5, 23.2 and 7.7).
+    if (nv > 32 && M <= 4 * sms && (size_t)K * sizeof(T) <= QFEW_BYTES)
+        return nv > 1024 || (nv > 256 && M <= 2 * sms) ? few(quantize_few_kernel<T, Q, 512>, 512) : few(quantize_few_kernel<T, Q, 256>, 256);
+    // Many: the fewest threads that hold a row in registers, so that an SM has many rows' loads under way.
     if (nv <= 32 * KEEP) return launch(quantize_rows_kernel<T, Q, 32, KEEP>, 32, 5);
     if (nv <= 128 * KEEP) return launch(quantize_rows_kernel<T, Q, 128, KEEP>, 128, 5);
     if (nv <= 256 * KEEP) return launch(quantize_rows_kernel<T, Q, 256, KEEP>, 256, 3);
