@@ -33,6 +33,7 @@ struct KeySched {
     int tt, N, n_ct;         // tokens and columns of a row tile; row tiles (of a branch; with shared units of all rows)
     int nb;                  // branches of a shared unit's row tile at most
     int wh, wk;              // few rows: warps over the key heads, over the keys
+    int kg;                  // few rows in a stream: keys that its share is counted in
     float decay, sl2;
     const int *seqs, *len, *table;
     const float *lse;        // [B n_q][Hk grp]
@@ -777,6 +778,354 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
     }
 }
 
+// ---------------------------------------------------------- few rows, many keys
+// The line of all keys, kg at a time, is shared evenly by the CTAs; a CTA takes its share in
+// tiles of up to 128 keys of one branch, or (shared keys) of the rows of as many branches as fit 64
+// columns.  A step is a tile and a key head: its keys and rows come by TMA, several steps ahead, so that the
+// keys' bytes bound it.  Warps: 0 loads, 1 issues the products, 2 reads the rows' lse and limits, two groups
+// of four take the exponentials of every other step; thread = key, which adds up each branch's columns in shared
+// memory of its own over the key heads, and the groups in turn write a tile's weights.  Up to eight columns a
+// branch are added up by code for just that many: with a test at each column a step of 48 took 1.75 us.
+constexpr int KST_SOFT = 256, KST_THREADS = 128 + KST_SOFT, KST_COLS = 64, KST_BUFS = 8, KST_SLOTS = 8, KST_NB = 16, KST_BUDGET = 196 * 1024;
+constexpr long long KST_BYTES = 16 << 20;
+
+struct KeyRun {
+    int own, b, key0, end, n;            // n: times kg keys
+    int t0, tokens;                      // its rows
+};
+struct KeyRuns {
+    int u, u1;
+    __device__ __forceinline__ KeyRuns(const KeySched &s, const KeyLens &L) {
+        const long long U = s.n_pt * s.n_ct + L.off[s.B];
+        u = (int)(U * blockIdx.x / gridDim.x);
+        u1 = (int)(U * (blockIdx.x + 1) / gridDim.x);
+    }
+    __device__ __forceinline__ bool next(const KeySched &s, const KeyLens &L, KeyRun &r) {
+        if (u >= u1) return false;
+        const KeyUnit x(s, L, u, s.kg);
+        const int stop = x.own ? s.n_pt * s.n_ct + L.off[x.b + 1] : (x.b + 1) * s.n_pt;
+        r.own = x.own;
+        r.b = x.b;
+        r.key0 = x.key0;
+        r.n = min(KW_TILE / s.kg, min(stop, u1) - u);
+        r.end = min(x.end, x.key0 + r.n * s.kg);
+        r.t0 = x.own ? x.b * s.n_q : x.b * s.tt;
+        r.tokens = x.own ? s.n_q : min(s.tt, s.B * s.n_q - r.t0);
+        u += r.n;
+        return true;
+    }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(KST_THREADS, 1)
+    key_weights_stream_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                              const __grid_constant__ KeySched s, const int slots, int *err) {
+    constexpr int NR = HD / 64, K_REGION = KW_TILE * 128, K_BYTES = NR * K_REGION;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ KeyLens L;
+    __shared__ KeyCols cols[KST_BUFS];
+    __shared__ uint64_t bars[2 * KST_SLOTS + 2 * KST_BUFS + 5];
+    __shared__ uint32_t tmem_slot;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const int q_region = s.N * 128, slot_bytes = K_BYTES + NR * q_region;
+    float *sums = reinterpret_cast<float *>(smem + slots * slot_bytes);            // [2 tiles in turn][2 groups][nb][128]
+    uint64_t *full = bars, *empty = bars + KST_SLOTS, *s_full = empty + KST_SLOTS, *s_empty = s_full + KST_BUFS;
+    uint64_t *added = s_empty + KST_BUFS, *taken = added + 2, *drained = taken + 2;         // a tile's sums are complete; have been read
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < KST_BUFS; ++i) {
+            mbar_init(&s_full[i], 33);
+            mbar_init(&s_empty[i], KST_SOFT / 2);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&added[i], KST_SOFT);
+            mbar_init(&taken[i], KST_SOFT / 2);
+        }
+        mbar_init(drained, 1);
+        mbar_fence_init();
+    }
+    if (warp == 1) tmem_alloc(&tmem_slot, 512);
+    for (int i = 0; i < slots; ++i)                    // columns that no rows fill stay zero
+        for (int x = threadIdx.x; x < NR * q_region / 16; x += KST_THREADS)
+            reinterpret_cast<uint4 *>(smem + i * slot_bytes + K_BYTES)[x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+    pdl_wait();
+    key_lens<false>(s, L, s.kg, err);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = 0;                           // all 512 columns are this CTA's
+    KeyRuns runs(s, L);
+    KeyRun r;
+
+    if (warp == 0) {
+        const int log_ps = 31 - __clz(s.ps);
+        auto entry = [&](const KeyRun &x) {            // table entry of this lane's keys
+            const int seq = L.seq[x.own ? x.b : 0];
+            if (lane >= x.n || seq < 0 || seq >= s.max_seqs) return -1;
+            return s.table[(size_t)seq * s.max_pages + ((x.key0 + lane * s.kg) >> log_ps)];
+        };
+        int i = 0, it = 0;
+        uint32_t ph = 1;
+        bool ok = true, more = runs.next(s, L, r);
+        int id = more ? entry(r) : -1;
+        while (ok && more) {
+            int row = s.n_pages * s.ps;                // out of range: TMA fills zeros
+            if (lane < r.n) {
+                if (id >= 0 && id < s.n_pages) row = id * s.ps + ((r.key0 + lane * s.kg) & (s.ps - 1));
+                else if (err) atomicOr(err, ERR_BAD_SEQ);
+            }
+            const int n = r.n, t0 = r.t0, tx = NR * 128 * (n * s.kg + s.tt * s.grp);
+            more = runs.next(s, L, r);
+            id = more ? entry(r) : -1;                 // on its way while this tile is loaded
+            for (int h = 0; h < s.Hk; ++h, ++it) {
+                ok = mbar_wait(&empty[i], ph, err, ERR_WAIT_PRODUCER);
+                if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+                uint8_t *slot = smem + i * slot_bytes;
+                if (lane == 0) {
+                    mbar_expect_tx(&full[i], tx);
+                    for (int k = 0; k < NR; ++k)
+                        tma_load_3d(slot + K_BYTES + k * q_region, &tmQ, &full[i], 64 * k, h * s.grp, t0);
+                }
+                __syncwarp();
+                if (lane < n)
+                    for (int k = 0; k < NR; ++k)
+                        tma_load_2d(slot + k * K_REGION + lane * s.kg * 128, &tmK, &full[i], h * HD + 64 * k, row);
+                if (++i == slots) {
+                    i = 0;
+                    ph ^= 1;
+                }
+            }
+        }
+        if (lane == 0)                                 // every copy has landed before the CTA exits
+            for (int j = max(it - slots, 0); j < it; ++j) mbar_wait(&full[j % slots], (j / slots) & 1, err, ERR_WAIT_PRODUCER);
+    } else if (warp == 1) {
+        const uint64_t d0 = sdesc_sw128(smem_u32(smem), 16, 1024);
+        auto wait = [&](uint64_t *b, uint32_t parity) {
+            return __all_sync(0xffffffffu, mbar_wait(b, parity, err, ERR_WAIT_MMA)) != 0;
+        };
+        int i = 0, buf = 0;
+        uint32_t ph = 0, s_ph = 1;
+        bool ok = true;
+        while (ok && runs.next(s, L, r)) {
+            const int N = (r.tokens * s.grp + 15) / 16 * 16;
+            const uint32_t idesc = idesc_bf16(KW_TILE, 16, false, false) - ((16u >> 3) << 17) + ((uint32_t)(N >> 3) << 17);
+            for (int h = 0; h < s.Hk; ++h) {
+                if (!(ok = wait(&full[i], ph) && wait(&s_empty[buf], s_ph))) break;
+                tc_fence_after();
+                const uint64_t da = d0 + (uint64_t)((i * slot_bytes) >> 4), db = da + (uint64_t)(K_BYTES >> 4);
+#pragma unroll
+                for (int k = 0; k < NR; ++k)
+                    key_issue4(tmem + buf * KST_COLS, da + (uint64_t)((k * K_REGION) >> 4), db + (uint64_t)((k * q_region) >> 4), idesc, k);
+                tc_commit_warp(&empty[i]);
+                tc_commit_warp(&s_full[buf]);
+                if (++i == slots) {
+                    i = 0;
+                    ph ^= 1;
+                }
+                if (++buf == KST_BUFS) {
+                    buf = 0;
+                    s_ph ^= 1;
+                }
+            }
+        }
+        if (!ok) {                                     // a wait ran out: no product is under way when the CTA ends
+            tc_commit_warp(drained);
+            wait(drained, 0);
+        }
+    } else if (warp == 2) {
+        // lse and limits of a step's columns, two a lane, read a step ahead of when they are stored
+        int tk[2], gq[2], buf = 0, lim[2], lim_now[2];
+        float nl[2];
+        uint32_t ph = 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = lane + 32 * i;
+            tk[i] = c / s.grp;
+            gq[i] = c - tk[i] * s.grp;
+        }
+        auto read = [&](const KeyRun &x, int h) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                nl[i] = -INFINITY;
+                lim[i] = 0;
+                if (tk[i] < x.tokens) {
+                    const int t = x.t0 + tk[i], b = t / s.n_q;
+                    nl[i] = s.lse[(size_t)t * (s.Hk * s.grp) + h * s.grp + gq[i]];
+                    lim[i] = min(max(s.limit(L.len[b], t - b * s.n_q) - x.key0, 0), KW_TILE);
+                }
+            }
+        };
+        int h = 0;
+        bool ok = true, more = runs.next(s, L, r);
+        if (more) read(r, h);
+        while (ok && more) {
+            float v[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {              // a row that saw no key adds nothing
+                v[i] = nl[i] == -INFINITY ? -INFINITY : -KW_LOG2E * nl[i];
+                lim_now[i] = lim[i];
+            }
+            if (++h == s.Hk) {
+                h = 0;
+                more = runs.next(s, L, r);
+            }
+            if (more) read(r, h);
+            ok = mbar_wait(&s_empty[buf], ph, err, ERR_WAIT_SOFTMAX);
+            if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                cols[buf].nl[lane + 32 * i] = v[i];
+                cols[buf].lim[lane + 32 * i] = lim_now[i];
+            }
+            mbar_arrive(&s_full[buf]);
+            if (++buf == KST_BUFS) {
+                buf = 0;
+                ph ^= 1;
+            }
+        }
+    } else if (warp >= 4) {
+        const int q = warp & 3, g = (warp - 4) >> 2, at = 32 * q + lane;         // key of the tile
+        const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
+        const float2 sl2 = make_float2(s.sl2, s.sl2);
+        const int each = s.n_q * s.grp, place = s.nb * KW_TILE;
+        int it = 0, tile = 0;
+        bool ok = true;
+        for (; ok && runs.next(s, L, r); ++tile) {
+            const int n_br = r.own ? 1 : r.tokens / s.n_q, n_col = r.tokens * s.grp, p = tile & 1, key = r.key0 + at, it0 = it;
+            float *mine = sums + (2 * p + g) * place + at;
+            ok = __all_sync(0xffffffffu, mbar_wait(&taken[p], ((tile >> 1) & 1) ^ 1, err, ERR_WAIT_SOFTMAX)) != 0;
+            if (!ok) break;
+            // this group writes the tile: the old weights of eight branches are read ahead, those of more later
+            float *w[8], old[8];
+            auto read = [&](int j0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int b = r.own ? r.b : r.b * s.nb + j0 + j;
+                    w[j] = j0 + j < n_br && key < r.end && key < L.len[b] ? s.w + (size_t)L.seq[b] * s.w_ld + key : nullptr;
+                    old[j] = w[j] != nullptr && s.decay != 0.0f ? *w[j] : 0.0f;
+                }
+            };
+            if ((tile & 1) == g) read(0);
+            bool first = true;
+            for (int h = 0; h < s.Hk; ++h, ++it) {
+                if ((it & 1) != g) continue;
+                const int buf = it & (KST_BUFS - 1);
+                ok = mbar_wait(&s_full[buf], (it / KST_BUFS) & 1, err, ERR_WAIT_SOFTMAX);
+                if (!(ok = __all_sync(0xffffffffu, ok) != 0)) break;
+                tc_fence_after();
+                const KeyCols &kc = cols[buf];
+                const uint32_t from = lanes + buf * KST_COLS;
+                auto put = [&](int j, float v) { mine[j * KW_TILE] = first ? v : mine[j * KW_TILE] + v; };
+                auto exps = [&](int c, float *x) {     // of four columns from column c
+                    const float4 nl = *reinterpret_cast<const float4 *>(&kc.nl[c]);
+                    const int4 lim = *reinterpret_cast<const int4 *>(&kc.lim[c]);
+                    const float2 a = __ffma2_rn(make_float2(x[0], x[1]), sl2, make_float2(nl.x, nl.y));
+                    const float2 b = __ffma2_rn(make_float2(x[2], x[3]), sl2, make_float2(nl.z, nl.w));
+                    x[0] = at < lim.x ? exp2_mufu(a.x) : 0.0f;
+                    x[1] = at < lim.y ? exp2_mufu(a.y) : 0.0f;
+                    x[2] = at < lim.z ? exp2_mufu(b.x) : 0.0f;
+                    x[3] = at < lim.w ? exp2_mufu(b.y) : 0.0f;
+                };
+                auto run = [&](auto each_, auto n_) {  // branches of each_ columns, n_ in all
+                    constexpr int E = decltype(each_)::value, n = decltype(n_)::value;
+                    float x[n];
+                    if constexpr (n == 64) tmem_ld64_sync(from, x);
+                    else if constexpr (n == 48) {
+                        tmem_ld32_sync(from, *reinterpret_cast<float (*)[32]>(x));
+                        tmem_ld16_sync(from + 32, *reinterpret_cast<float (*)[16]>(x + 32));
+                    } else if constexpr (n == 32) tmem_ld32_sync(from, x);
+                    else tmem_ld16_sync(from, x);
+#pragma unroll
+                    for (int i = 0; i < n; i += 4) exps(i, x + i);
+#pragma unroll
+                    for (int j = 0; j < n / E; ++j) {
+                        float sum = x[j * E];
+#pragma unroll
+                        for (int i = 1; i < E; ++i) sum += x[j * E + i];
+                        if (j < n_br) put(j, sum);
+                    }
+                };
+                auto pick = [&](auto each_) {
+                    if (n_col <= 16) run(each_, std::integral_constant<int, 16>());
+                    else if (n_col <= 32) run(each_, std::integral_constant<int, 32>());
+                    else if (n_col <= 48) run(each_, std::integral_constant<int, 48>());
+                    else run(each_, std::integral_constant<int, 64>());
+                };
+                switch (each) {
+                    case 1: pick(std::integral_constant<int, 1>()); break;
+                    case 2: pick(std::integral_constant<int, 2>()); break;
+                    case 3: pick(std::integral_constant<int, 3>()); break;
+                    case 4: pick(std::integral_constant<int, 4>()); break;
+                    case 5: pick(std::integral_constant<int, 5>()); break;
+                    case 6: pick(std::integral_constant<int, 6>()); break;
+                    case 7: pick(std::integral_constant<int, 7>()); break;
+                    case 8: pick(std::integral_constant<int, 8>()); break;
+                    default: {
+                        float sum = 0.0f;
+                        int left = each, j = 0;        // columns of branch j still to come
+                        for (int c = 0; c < n_col; c += 16) {
+                            float x[16];
+                            tmem_ld16_sync(from + c, x);
+#pragma unroll
+                            for (int i = 0; i < 16; i += 4) exps(c + i, x + i);
+                            if (left > 16) {
+                                float2 t = make_float2(x[0], x[1]);
+#pragma unroll
+                                for (int i = 2; i < 16; i += 2) t = __fadd2_rn(t, make_float2(x[i], x[i + 1]));
+                                sum += t.x + t.y;
+                                left -= 16;
+                                continue;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                sum += x[i];
+                                if (--left == 0) {
+                                    if (j < n_br) put(j, sum);
+                                    sum = 0.0f;
+                                    left = each;
+                                    ++j;
+                                }
+                            }
+                        }
+                    }
+                }
+                first = false;
+                tc_fence_before();
+                mbar_arrive(&s_empty[buf]);
+            }
+            if (!ok) break;
+            mbar_arrive(&added[p]);
+            if ((tile & 1) != g) continue;
+            const float *sum0 = sums + 2 * p * place + at, *sum1 = sum0 + place;
+            const bool in0 = s.Hk > 1 || (it0 & 1) == 0, in1 = s.Hk > 1 || (it0 & 1) == 1;        // groups that had a step
+            for (int j0 = 0; j0 < n_br; j0 += 8) {
+                if (j0 > 0) read(j0);
+                if (j0 == 0 && !(ok = __all_sync(0xffffffffu, mbar_wait(&added[p], (tile >> 1) & 1, err, ERR_WAIT_SOFTMAX)) != 0)) break;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (w[j] != nullptr) {
+                        const int from = (j0 + j) * KW_TILE;
+                        const float v = (in0 ? sum0[from] : 0.0f) + (in1 ? sum1[from] : 0.0f);
+                        *w[j] = s.decay == 0.0f ? v : fmaf(s.decay, old[j], v);
+                    }
+            }
+            mbar_arrive(&taken[p]);
+        }
+    }
+    pdl_release();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
 // ------------------------------------------------------------ fp32 kernel
 // 64 keys x 64 rows at a time, 256 threads as 16 x 16: thread (ty, tx) has rows 4 ty..
 // and keys tx + 16 j.  A unit is 64 keys with all their rows, taken in turn.
@@ -905,6 +1254,19 @@ static KeySched key_plan(const xc_kv_cache &c, int B, int n_q, int H, int shared
     if (c.dtype == XC_F32) return s;
     const long long each = (long long)n_q * s.grp;
     auto fits = [&](long long n) { return n * each <= KFEW_COLS && few_smem(s.Hk, (int)(n * each + 7) / 8 * 8, c.head_dim) <= KFEW_SMEM; };
+    const long long keys = (long long)c.max_pages * c.page_size, most = shared > 0 && B > 1 ? shared + B * (keys - shared) : B * keys;
+    if (each <= KST_COLS && (!fits(1) || most * s.Hk * c.head_dim * 2 > KST_BYTES)) {      // few rows in a stream
+        if (shared > 0 && B > 1) {
+            while (s.nb < std::min(B, KST_NB) && (s.nb + 1) * each <= KST_COLS) ++s.nb;
+            s.P = shared;
+        }
+        s.kg = std::min(s.ps, 32);
+        s.tt = s.nb * n_q;
+        s.N = (s.tt * s.grp + 15) / 16 * 16;
+        s.n_ct = (B + s.nb - 1) / s.nb;
+        s.n_pt = s.P / s.kg;
+        return s;
+    }
     if (fits(1)) {                                     // few rows
         s.wh = 1;
         while (s.wh < KFEW_WARPS && s.wh < s.Hk) s.wh *= 2;
@@ -931,7 +1293,7 @@ bool key_weights_fit(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
 }
 size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     const KeySched s = key_plan(c, B, n_q, H, shared);
-    return c.dtype == XC_F32 || s.wh > 0 ? 16 : (size_t)2 * s.G * (sizeof(int4) + KW_KEYS * sizeof(float));
+    return c.dtype == XC_F32 || s.wh > 0 || s.kg > 0 ? 16 : (size_t)2 * s.G * (sizeof(int4) + KW_KEYS * sizeof(float));
 }
 
 template <int HD>
@@ -954,6 +1316,22 @@ static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, 
                                      2 * K_BYTES + q_slots * q_bytes + 1024, st, tq, tk, s, q_slots, err);
     if (e != cudaSuccess) return e;
     return launch_pdl(key_merge_kernel, dim3(2 * s.G), dim3(KW_KEYS), 0, st, s);
+}
+template <int HD>
+static cudaError_t key_launch_stream(const xc_kv_cache &c, const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
+    static bool done = false;
+    if (!done) {
+        const cudaError_t e = cudaFuncSetAttribute(key_weights_stream_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KST_BUDGET + 1024);
+        if (e != cudaSuccess) return e;
+        done = true;
+    }
+    const int slot = (KW_TILE + s.N) * HD * 2, sums = 4 * s.nb * KW_TILE * 4, slots = std::min(KST_SLOTS, (KST_BUDGET - sums) / slot);
+    const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
+    CUtensorMap tq, tk;
+    if (!make_tmap_heads_bf16(&tq, a.q, HD, (uint64_t)s.Hk * s.grp, (uint64_t)s.B * s.n_q, a.q_ld, s.grp, s.tt) ||
+        !make_tmap_bf16(&tk, a.k, rows, cols, s.kg))
+        return cudaErrorInvalidValue;
+    return launch_pdl(key_weights_stream_kernel<HD>, dim3(s.G), dim3(KST_THREADS), slots * slot + sums + 1024, st, tq, tk, s, slots, err);
 }
 template <int HD, int NT>
 static cudaError_t key_launch_few(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
@@ -993,8 +1371,8 @@ cudaError_t key_weights(const xc_kv_cache &c, const KeyWeightsArgs &a, void *ws,
     s.meta = reinterpret_cast<int4 *>(ws);
     s.part = reinterpret_cast<float *>(s.meta + 2 * s.G);
     if (c.dtype == XC_BF16) {
-        if (c.head_dim == 64) return s.wh > 0 ? key_launch_few<64, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
-        if (c.head_dim == 128) return s.wh > 0 ? key_launch_few<128, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
+        if (c.head_dim == 64) return s.kg > 0 ? key_launch_stream<64>(c, a, s, err, st) : s.wh > 0 ? key_launch_few<64, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
+        if (c.head_dim == 128) return s.kg > 0 ? key_launch_stream<128>(c, a, s, err, st) : s.wh > 0 ? key_launch_few<128, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
         return cudaErrorInvalidValue;
     }
     switch (c.head_dim) {
