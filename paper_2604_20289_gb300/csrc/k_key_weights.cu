@@ -8,10 +8,11 @@
 // the product and a lane of tensor memory, so the sum over the query rows stays
 // in one thread's registers.
 //
-// Three kernels.  Branches of few rows (single tokens, short chunks) wait for the keys'
-// bytes: key_weights_few_kernel streams them into registers, and where the branches share
-// keys it reads them once for the rows of as many branches as fit.  Longer ones are products
-// (key_weights_kernel, tcgen05) and exponentials; fp32 caches have a kernel of their own.
+// Four kernels.  Branches of few rows (single tokens, short chunks) wait for the keys'
+// bytes, and where the branches share keys those are read once for the rows of as many branches as
+// fit: key_weights_few_kernel takes few keys straight into registers (it begins sooner),
+// key_weights_stream_kernel many through shared memory and tcgen05 products (it keeps more bytes under way).  Longer rows are
+// products (key_weights_kernel, tcgen05) and exponentials; fp32 caches have a kernel of their own.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -33,7 +34,7 @@ struct KeySched {
     int tt, N, n_ct;         // tokens and columns of a row tile; row tiles (of a branch; with shared units of all rows)
     int nb;                  // branches of a shared unit's row tile at most
     int wh, wk;              // few rows: warps over the key heads, over the keys
-    int kg;                  // few rows in a stream: keys that its share is counted in
+    int stream;              // few rows, many keys
     float decay, sl2;
     const int *seqs, *len, *table;
     const float *lse;        // [B n_q][Hk grp]
@@ -779,18 +780,22 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
 }
 
 // ---------------------------------------------------------- few rows, many keys
-// The line of all keys, kg at a time, is shared evenly by the CTAs; a CTA takes its share in
-// tiles of up to 128 keys of one branch, or (shared keys) of the rows of as many branches as fit 64
-// columns.  A step is a tile and a key head: its keys and rows come by TMA, several steps ahead, so that the
+// A tile is 128 keys with the rows of one branch, or (shared keys) of as many branches as fit 64
+// columns; the CTAs share the line of all tiles evenly (shares in finer steps have more tiles, which
+// cost more than their keys: 4 single tokens over 16384 keys of 12 heads x 128 took 20 us instead of 15).  A step is
+// a tile and a key head: its keys and rows come by TMA, several steps ahead, so that the
 // keys' bytes bound it.  Warps: 0 loads, 1 issues the products, 2 reads the rows' lse and limits, two groups
 // of four take the exponentials of every other step; thread = key, which adds up each branch's columns in shared
 // memory of its own over the key heads, and the groups in turn write a tile's weights.  Up to eight columns a
 // branch are added up by code for just that many: with a test at each column a step of 48 took 1.75 us.
-constexpr int KST_SOFT = 256, KST_THREADS = 128 + KST_SOFT, KST_COLS = 64, KST_BUFS = 8, KST_SLOTS = 8, KST_NB = 16, KST_BUDGET = 196 * 1024;
-constexpr long long KST_BYTES = 16 << 20;
+constexpr int KST_SOFT = 256, KST_THREADS = 128 + KST_SOFT, KST_COLS = 64, KST_BUFS = 8, KST_SLOTS = 8, KST_NB = 16, KST_BUDGET = 204 * 1024;
+// Key bytes, with every table row full, from which few rows go as a stream: below, its barriers and first copies take
+// longer than the keys (4 single tokens, 8 heads x 64: 4096 keys 9.6 us against 6.7, 16384 keys 10.9 against
+// 13.7; 12 heads x 128: 4096 keys 12.2 against 10.9, 8192 keys 12.8 against 15.9).
+constexpr long long KST_BYTES = 12 << 20;
 
 struct KeyRun {
-    int own, b, key0, end, n;            // n: times kg keys
+    int own, b, key0, end;               // end: behind the last key
     int t0, tokens;                      // its rows
 };
 struct KeyRuns {
@@ -802,16 +807,13 @@ struct KeyRuns {
     }
     __device__ __forceinline__ bool next(const KeySched &s, const KeyLens &L, KeyRun &r) {
         if (u >= u1) return false;
-        const KeyUnit x(s, L, u, s.kg);
-        const int stop = x.own ? s.n_pt * s.n_ct + L.off[x.b + 1] : (x.b + 1) * s.n_pt;
+        const KeyUnit x(s, L, u++, KW_TILE);
         r.own = x.own;
         r.b = x.b;
         r.key0 = x.key0;
-        r.n = min(KW_TILE / s.kg, min(stop, u1) - u);
-        r.end = min(x.end, x.key0 + r.n * s.kg);
+        r.end = min(x.end, x.key0 + KW_TILE);
         r.t0 = x.own ? x.b * s.n_q : x.b * s.tt;
         r.tokens = x.own ? s.n_q : min(s.tt, s.B * s.n_q - r.t0);
-        u += r.n;
         return true;
     }
 };
@@ -854,7 +856,7 @@ __global__ void __launch_bounds__(KST_THREADS, 1)
             reinterpret_cast<uint4 *>(smem + i * slot_bytes + K_BYTES)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
     pdl_wait();
-    key_lens<false>(s, L, s.kg, err);
+    key_lens<false>(s, L, KW_TILE, err);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -863,11 +865,12 @@ __global__ void __launch_bounds__(KST_THREADS, 1)
     KeyRun r;
 
     if (warp == 0) {
-        const int log_ps = 31 - __clz(s.ps);
+        const int log_ps = 31 - __clz(s.ps), box = min(s.ps, KW_TILE);
+        auto boxes = [&](const KeyRun &x) { return (x.end - x.key0 + box - 1) / box; };
         auto entry = [&](const KeyRun &x) {            // table entry of this lane's keys
             const int seq = L.seq[x.own ? x.b : 0];
-            if (lane >= x.n || seq < 0 || seq >= s.max_seqs) return -1;
-            return s.table[(size_t)seq * s.max_pages + ((x.key0 + lane * s.kg) >> log_ps)];
+            if (lane >= boxes(x) || seq < 0 || seq >= s.max_seqs) return -1;
+            return s.table[(size_t)seq * s.max_pages + ((x.key0 + lane * box) >> log_ps)];
         };
         int i = 0, it = 0;
         uint32_t ph = 1;
@@ -875,11 +878,11 @@ __global__ void __launch_bounds__(KST_THREADS, 1)
         int id = more ? entry(r) : -1;
         while (ok && more) {
             int row = s.n_pages * s.ps;                // out of range: TMA fills zeros
-            if (lane < r.n) {
-                if (id >= 0 && id < s.n_pages) row = id * s.ps + ((r.key0 + lane * s.kg) & (s.ps - 1));
+            const int n = boxes(r), t0 = r.t0, tx = NR * 128 * (n * box + s.tt * s.grp);
+            if (lane < n) {
+                if (id >= 0 && id < s.n_pages) row = id * s.ps + ((r.key0 + lane * box) & (s.ps - 1));
                 else if (err) atomicOr(err, ERR_BAD_SEQ);
             }
-            const int n = r.n, t0 = r.t0, tx = NR * 128 * (n * s.kg + s.tt * s.grp);
             more = runs.next(s, L, r);
             id = more ? entry(r) : -1;                 // on its way while this tile is loaded
             for (int h = 0; h < s.Hk; ++h, ++it) {
@@ -894,7 +897,7 @@ __global__ void __launch_bounds__(KST_THREADS, 1)
                 __syncwarp();
                 if (lane < n)
                     for (int k = 0; k < NR; ++k)
-                        tma_load_2d(slot + k * K_REGION + lane * s.kg * 128, &tmK, &full[i], h * HD + 64 * k, row);
+                        tma_load_2d(slot + k * K_REGION + lane * box * 128, &tmK, &full[i], h * HD + 64 * k, row);
                 if (++i == slots) {
                     i = 0;
                     ph ^= 1;
@@ -1255,16 +1258,16 @@ static KeySched key_plan(const xc_kv_cache &c, int B, int n_q, int H, int shared
     const long long each = (long long)n_q * s.grp;
     auto fits = [&](long long n) { return n * each <= KFEW_COLS && few_smem(s.Hk, (int)(n * each + 7) / 8 * 8, c.head_dim) <= KFEW_SMEM; };
     const long long keys = (long long)c.max_pages * c.page_size, most = shared > 0 && B > 1 ? shared + B * (keys - shared) : B * keys;
-    if (each <= KST_COLS && (!fits(1) || most * s.Hk * c.head_dim * 2 > KST_BYTES)) {      // few rows in a stream
+    if (each <= KST_COLS && (!fits(1) || most * s.Hk * c.head_dim * 2 > KST_BYTES)) {      // few rows, many keys
         if (shared > 0 && B > 1) {
             while (s.nb < std::min(B, KST_NB) && (s.nb + 1) * each <= KST_COLS) ++s.nb;
             s.P = shared;
         }
-        s.kg = std::min(s.ps, 32);
+        s.stream = 1;
         s.tt = s.nb * n_q;
         s.N = (s.tt * s.grp + 15) / 16 * 16;
         s.n_ct = (B + s.nb - 1) / s.nb;
-        s.n_pt = s.P / s.kg;
+        s.n_pt = (s.P + KW_TILE - 1) / KW_TILE;
         return s;
     }
     if (fits(1)) {                                     // few rows
@@ -1293,7 +1296,7 @@ bool key_weights_fit(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
 }
 size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, int shared) {
     const KeySched s = key_plan(c, B, n_q, H, shared);
-    return c.dtype == XC_F32 || s.wh > 0 || s.kg > 0 ? 16 : (size_t)2 * s.G * (sizeof(int4) + KW_KEYS * sizeof(float));
+    return c.dtype == XC_F32 || s.wh > 0 || s.stream ? 16 : (size_t)2 * s.G * (sizeof(int4) + KW_KEYS * sizeof(float));
 }
 
 template <int HD>
@@ -1329,7 +1332,7 @@ static cudaError_t key_launch_stream(const xc_kv_cache &c, const KeyWeightsArgs 
     const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
     CUtensorMap tq, tk;
     if (!make_tmap_heads_bf16(&tq, a.q, HD, (uint64_t)s.Hk * s.grp, (uint64_t)s.B * s.n_q, a.q_ld, s.grp, s.tt) ||
-        !make_tmap_bf16(&tk, a.k, rows, cols, s.kg))
+        !make_tmap_bf16(&tk, a.k, rows, cols, std::min(s.ps, KW_TILE)))
         return cudaErrorInvalidValue;
     return launch_pdl(key_weights_stream_kernel<HD>, dim3(s.G), dim3(KST_THREADS), slots * slot + sums + 1024, st, tq, tk, s, slots, err);
 }
@@ -1371,8 +1374,8 @@ cudaError_t key_weights(const xc_kv_cache &c, const KeyWeightsArgs &a, void *ws,
     s.meta = reinterpret_cast<int4 *>(ws);
     s.part = reinterpret_cast<float *>(s.meta + 2 * s.G);
     if (c.dtype == XC_BF16) {
-        if (c.head_dim == 64) return s.kg > 0 ? key_launch_stream<64>(c, a, s, err, st) : s.wh > 0 ? key_launch_few<64, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
-        if (c.head_dim == 128) return s.kg > 0 ? key_launch_stream<128>(c, a, s, err, st) : s.wh > 0 ? key_launch_few<128, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
+        if (c.head_dim == 64) return s.stream ? key_launch_stream<64>(c, a, s, err, st) : s.wh > 0 ? key_launch_few<64, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<64>(c, a, s, err, st);
+        if (c.head_dim == 128) return s.stream ? key_launch_stream<128>(c, a, s, err, st) : s.wh > 0 ? key_launch_few<128, KFEW_COLS / 8>(a, s, err, st) : key_launch_tc<128>(c, a, s, err, st);
         return cudaErrorInvalidValue;
     }
     switch (c.head_dim) {

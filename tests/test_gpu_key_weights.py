@@ -48,8 +48,9 @@ def reference(cache, seqs, n_q, q, causal, scale=None):
     return lse.reshape(B * n_q, H), out
 
 
-def check(dtype, H, hk, hd, ps, lens, n_q, shared, causal, seqs=None, scale=0.0, decay=1.0, seed=3, std=1.5, strided=False):
-    cache = make_cache(dtype, hk, hd, ps, lens, shared, seed=seed)
+def check(dtype, H, hk, hd, ps, lens, n_q, shared, causal, seqs=None, scale=0.0, decay=1.0, seed=3, std=1.5, strided=False,
+          max_pages=None):
+    cache = make_cache(dtype, hk, hd, ps, lens, shared, seed=seed, max_pages=max_pages)
     seqs = list(range(len(lens))) if seqs is None else seqs
     q = rand((len(seqs) * n_q, H * hd + (64 if strided else 0)), dtype, seed + 7, std)[:, :H * hd]
     o = torch.empty(len(seqs) * n_q, H * hd, dtype=q.dtype, device=DEV)
@@ -194,16 +195,63 @@ def test_head_layouts_of_few_rows(H, hk, hd, lens, n_q, shared):
     check("bf16", H, hk, hd, 32, lens, n_q, shared, True)
 
 
+def wide(hk, hd, ps, shared=0):
+    """Pages of a table row that allow for more keys than few rows take into registers (12 MB)."""
+    return (13 * 2 ** 20 // (hk * hd * 2) + shared) // ps + 1
+
+
+@pytest.mark.parametrize("H,hk,hd,ps,lens,n_q,shared", [
+    (1, 1, 64, 16, [1], 1, 0), (4, 4, 64, 16, [33, 16, 17, 20], 1, 16), (8, 8, 64, 16, [2017, 2030, 2056, 2016], 1, 2016),
+    (8, 1, 128, 32, [130, 129, 128, 700, 64], 1, 64), (5, 1, 128, 64, [64, 1000, 65], 1, 64),
+    (21, 3, 128, 128, [300, 511, 129, 128, 2000, 131, 140], 1, 128), (40, 8, 128, 32, [4000 + 37 * b for b in range(32)], 1, 3968),
+    (32, 4, 64, 256, [256 + b for b in range(9)], 1, 256), (12, 12, 128, 16, [0, 5, 0, 129], 1, 0), (64, 1, 64, 16, [700, 900], 1, 640),
+    (2, 2, 64, 1024, [3000, 2050], 1, 2048), (2, 2, 64, 16, [64 + (37 * b) % 90 for b in range(130)], 1, 64),
+    (1, 1, 128, 64, [19968 + 5 * b for b in range(3)], 1, 19968), (3, 3, 64, 16, [10, 40, 0], 25, 0), (12, 12, 128, 32, [352, 340, 400, 321], 20, 320),
+    (2, 2, 128, 16, [100 + (13 * b) % 61 for b in range(70)], 3, 0), (1, 1, 64, 32, [160 + b % 30 for b in range(40)], 20, 128),
+    (3, 1, 64, 16, [300, 260, 290, 250], 1, 240), (6, 1, 64, 16, [300, 260, 290, 250], 1, 240), (7, 1, 64, 16, [300, 260, 290, 250] * 2, 1, 240),
+    (2, 1, 64, 64, [400 + b for b in range(30)], 2, 384), (9, 3, 128, 32, [200, 333, 64], 2, 64), (11, 1, 64, 16, [150, 140], 1, 128),
+    (16, 1, 64, 32, [290, 300, 310, 320], 1, 288), (17, 1, 64, 32, [290, 300, 310, 320], 1, 288), (128, 128, 64, 16, [129, 257], 1, 0)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_rows_over_many_keys(H, hk, hd, ps, lens, n_q, shared, causal):
+    check("bf16", H, hk, hd, ps, lens, n_q, shared, causal, max_pages=wide(hk, hd, ps, shared), decay=0.5)
+
+
+@pytest.mark.parametrize("decay", [0.0, 1.0])
+def test_many_keys_decay_scale_strides_and_order(decay):
+    check("bf16", 4, 2, 64, 16, [100, 122, 70], 2, 64, True, seqs=[2, 0], scale=0.3, decay=decay, strided=True, max_pages=wide(2, 64, 16))
+    check("bf16", 4, 2, 64, 16, [100, 122, 70], 2, 0, True, seqs=[1, 2], decay=decay, strided=True, max_pages=wide(2, 64, 16))
+
+
+def test_many_keys_flags():
+    cache, q, lse, w = check("bf16", 2, 2, 64, 16, [100, 122, 300], 1, 64, True, max_pages=wide(2, 64, 16))
+    want, got = torch.zeros_like(w), torch.zeros_like(w)
+    xb.op_key_weights(cache, 0, i32([0, 1, 2]), 1, q, lse, want, shared_len=64, causal=True)
+    assert xb.op_device_error() == 0
+    for last in (1, -1, 3, 1 << 30):                       # listed twice, out of range
+        got.zero_()
+        xb.op_key_weights(cache, 0, i32([0, 1, 2, last]), 1, torch.cat([q, q[:1]]), torch.cat([lse, lse[:1]]), got, shared_len=64, causal=True)
+        assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
+        assert (got - want).abs().max().item() <= 1e-5 * want.max().item()
+    cache.table[2, 5] = 1 << 20                            # a bad page counts as zeros
+    got.zero_()
+    xb.op_key_weights(cache, 0, i32([0, 1, 2]), 1, q, lse, got, shared_len=64, causal=True)
+    assert xb.op_device_error() == xb.XC_DEV_BAD_SEQUENCE
+    zero = torch.exp(-lse[2]).sum().item()
+    assert (got[2, 80:96] - zero).abs().max().item() <= 1e-5 * zero
+    assert torch.equal(got[:2], want[:2]) and torch.equal(got[2, :80], want[2, :80]) and torch.equal(got[2, 96:], want[2, 96:])
+
+
 def test_long_rows_and_many_cuts():
     check("bf16", 1, 1, 128, 64, [19968 + 5 * b for b in range(3)], 1, 19968, True)
     check("bf16", 2, 1, 128, 128, [5000], 1, 0, True)
 
 
-def test_a_captured_step_follows_the_lengths():
+@pytest.mark.parametrize("many", [False, True])
+def test_a_captured_step_follows_the_lengths(many):
     """Attention and weights in one graph: replays see the cache as it is then."""
     H, hk, hd, ps = 4, 2, 64, 16
     lens, longer = [40, 90], [47, 200]
-    cache = make_cache("bf16", hk, hd, ps, longer, 0, dead=0.0)
+    cache = make_cache("bf16", hk, hd, ps, longer, 0, dead=0.0, max_pages=wide(hk, hd, ps) if many else None)
     q = rand((2, H * hd), "bf16", 5, 1.5)
     o, lse = torch.empty_like(q), torch.empty(2, H, device=DEV)
     w = torch.zeros(2, cache.table.shape[1] * ps, device=DEV)
