@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR == 512 ? 1 : TPR ==
 
 // Few rows: a CTA a row, which waits in shared memory for its largest magnitude.  Latency bound, and the code
 // is short: a loop over a row in registers is unrolled, and its instructions have to be fetched too.
-constexpr int QFEW_BYTES = 48 * 1024;
+constexpr int QFEW_BYTES = 48 * 1024 - 256;     // with the warps' maxima, what a CTA has without asking
 template <typename T, typename Q, int THREADS>
 __global__ void __launch_bounds__(THREADS) quantize_few_kernel(const T *__restrict__ x, Q *__restrict__ q, float *__restrict__ scale, const int K) {
     extern __shared__ __align__(16) uint8_t quant_row[];

@@ -64,6 +64,17 @@ def test_rows_are_quantised(dtype, M, K):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K", [(5, 12288), (5, 24576), (5, 12016), (5, 24032), (305, 2064), (305, 8208), (609, 2064), (700, 272), (1300, 12288)])
+def test_rows_at_the_ends_of_shared_memory_and_of_few(dtype, M, K):
+    """Rows that fill the shared memory of a CTA, or just do not, and row counts on either side of the rules."""
+    x = (rand((M, K), M + K) * torch.exp(2 * rand((M, 1), K))).to(tdt(dtype))
+    q, s = quantize(x, dtype)
+    rq, rs = plain_quantize(x)
+    assert torch.equal(q.to(F64), rq)
+    assert torch.equal(s, rs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_halves_go_to_even_numbers(dtype):
     """Every x = a (k + 1/2) / 127 that the type holds, and its neighbours: a = 127 2^e, where the halves are exact, and
     x = a / 2 for every a of 8 bits, which is 63.5 steps."""

@@ -267,7 +267,7 @@ def test_refusals_change_nothing():
         with pytest.raises(ValueError):
             m.evict(*args)
         assert state() == before and xb.op_device_error() == 0
-    assert m.evict([], 8) == [] and m.evict([root], 64) == [list(range(64))] and state() == before
+    assert m.fork(root, 0) == [] and m.evict([], 8) == [] and m.evict([root], 64) == [list(range(64))] and state() == before
     m.evict([root], 33)
     with pytest.raises(ValueError):
         m.step([root], torch.randn(1, 7, d, device=DEV))  # there is room for the tokens, not for their positions
