@@ -196,7 +196,9 @@ struct KeyWalk {
 // the rows' lse and limits, 4-19 take the exponentials: eight for either key tile, thread = key,
 // two warps per TMEM quadrant, half of the columns each.  Two key tiles, as every row tile is read from
 // L2 for both: with one, the rows came too late for the products (2 x 4320 queries over 30240 keys, 12 heads x 128:
-// 932 us).  All sixteen warps on every tile: 1040 us.  A share of the exponentials on the FMA pipe (Cody and
+// 932 us, with two 735).  Products and exponentials take 1024 cycles each of a step's 2200; the tensor pipe, the
+// special-function unit and the issue slots are at 48 % each: the softmax warps' wait, load and exponentials
+// follow one another.  All sixteen warps on every tile: 1040 us.  A share of the exponentials on the FMA pipe (Cody and
 // Waite's reduction and a polynomial) was slower still.
 constexpr int KW_SOFT = 512, KW_THREADS = 128 + KW_SOFT;
 struct alignas(16) KeyCols { // what a step's columns need
@@ -544,7 +546,8 @@ __global__ void __launch_bounds__(KW_KEYS) key_merge_kernel(const __grid_constan
 // products; the rows, in shared memory, are laid out to match), the next head's or unit's while it
 // computes, and keeps a sum for every column.  The warps' sums meet in shared memory at the
 // unit's end (two places in turn, so that one barrier a unit is enough), in a fixed order, and one thread
-// writes each (branch, key), whose old weight it read when the unit began.  The keys' bytes bound it.
+// writes each (branch, key), whose old weight it read when the unit began.  Latency bounds it: 4 single tokens,
+// 8 heads x 64, 2016 keys 6.7 us.
 constexpr int KFEW_THREADS = 512, KFEW_WARPS = KFEW_THREADS / 32, KFEW_COLS = 64, KFEW_PITCH = 20;
 constexpr size_t KFEW_SMEM = 208 * 1024;
 
@@ -788,6 +791,8 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
 // of four take the exponentials of every other step; thread = key, which adds up each branch's columns in shared
 // memory of its own over the key heads, and the groups in turn write a tile's weights.  Up to eight columns a
 // branch are added up by code for just that many: with a test at each column a step of 48 took 1.75 us.
+// 8 single tokens, 40 / 8 heads x 128, 38880 shared + 1..1500 own keys: 25.8 us (in registers 49.4), 7 until the first
+// tile is there, then 6.3 TB/s.
 constexpr int KST_SOFT = 256, KST_THREADS = 128 + KST_SOFT, KST_COLS = 64, KST_BUFS = 8, KST_SLOTS = 8, KST_NB = 16, KST_BUDGET = 204 * 1024;
 // Key bytes, with every table row full, from which few rows go as a stream: below, its barriers and first copies take
 // longer than the keys (4 single tokens, 8 heads x 64: 4096 keys 9.6 us against 6.7, 16384 keys 10.9 against

@@ -512,7 +512,7 @@ class KVCache:
         self.ptr = ctypes.addressof(self.desc)
         self._ws = {}                             # stream -> (tensor, pointer, bytes)
         self._attn_bytes, self._axes = {}, {}     # workspace sizes by shape, axis arrays by value
-        self._weigh_bytes = {}
+        self._weigh_bytes, self._evict_bytes = {}, {}
         self._page_bytes = LIB.xc_op_kv_workspace_bytes(self.ptr)
 
     @classmethod
@@ -757,7 +757,9 @@ def op_kv_evict(cache: KVCache, seqs, keep: int, weights=None, n_first=0, n_last
     w, sw = _weights(cache, weights) if weights is not None else (None, 0)
     cuda = _stream(stream)
     if workspace is None:
-        need = op_kv_evict_workspace_bytes(cache, n, keep)
+        need = cache._evict_bytes.get((n, keep))
+        if need is None:
+            need = cache.note(cache._evict_bytes, (n, keep), op_kv_evict_workspace_bytes(cache, n, keep))
         buf, ws, nbytes = cache.workspace(need, cuda)
     else:
         buf, ws, nbytes = _given(workspace)
