@@ -292,3 +292,40 @@ def test_steps_and_evictions_on_streams_in_turn():
         with torch.cuda.stream(streams[(i + 1) % 2]):
             b.step([sb], 23)
             b.evict([sb], 31, 0, 31)
+
+
+@pytest.mark.parametrize("dtype,n_q,max_pages", [("bf16", 1, 4), ("bf16", 1, 400), ("bf16", 70, 4), ("f32", 3, 4)])
+def test_offsets_past_32_bits(dtype, n_q, max_pages):
+    """Pages whose element offsets pass 2^31: read for their keys' weights, and moved by an eviction."""
+    ps, hk, hd, n_pages = 64, 8, 128, 40000                     # 2.6e9 elements
+    if torch.cuda.mem_get_info()[0] < 32 << 30:
+        pytest.skip("needs 32 GB")
+    cache = xb.KVCache.empty(dtype, 1, n_pages, ps, hk, hd, 3, max_pages)
+    pages, L = [n_pages - 1, n_pages - 3], 101                  # few keys, many, long rows by the table's width and n_q
+    g = torch.Generator(device=DEV).manual_seed(1)
+
+    def r(*shape):
+        return torch.randn(*shape, generator=g, device=DEV).to(tdt(dtype))
+
+    for p in pages:
+        cache.k[0, p], cache.v[0, p] = r(ps, hk * hd), r(ps, hk * hd)
+        cache.ref[p] = 1
+    cache.table[1, :2] = torch.tensor(pages, dtype=torch.int32, device=DEV)
+    cache.len[1] = L
+    seqs = torch.tensor([1], dtype=torch.int32, device=DEV)
+    q, w = r(n_q, 2 * hk * hd), torch.zeros(3, max_pages * ps, device=DEV)
+    o, lse = torch.empty_like(q), torch.empty(n_q, 2 * hk, device=DEV)
+    xb.op_branch_attention(cache, 0, seqs, n_q, q, o, causal=True, lse=lse)
+    xb.op_key_weights(cache, 0, seqs, n_q, q, lse, w, causal=True)
+    assert xb.op_device_error() == 0
+    k = torch.cat([cache.k[0, p] for p in pages])[:L].double().view(L, hk, hd).repeat_interleave(2, 1)
+    s = torch.einsum("ihd,jhd->hij", q.double().view(n_q, 2 * hk, hd), k) / math.sqrt(hd)
+    s.masked_fill_(torch.arange(L, device=DEV)[None] > L - n_q + torch.arange(n_q, device=DEV)[:, None], -math.inf)
+    want = torch.softmax(s, -1).sum((0, 1)).cpu().numpy()
+    assert rel_l2(host(w[1, :L]), want) <= 1e-5 and not w[1, L:].any() and not w[0].any() and not w[2].any()
+    before, rows = host(w[1, :L]), [torch.cat([t[0, p] for p in pages]) for t in (cache.k, cache.v)]
+    kept = torch.empty(1, 70, dtype=torch.int32, device=DEV)
+    xb.op_kv_evict(cache, seqs, 70, w, n_first=3, n_last=20, kept=kept)
+    assert xb.op_device_error() == 0 and kept[0].tolist() == chosen(before, L, 70, 3, 20)
+    for t, old in zip((cache.k, cache.v), rows):
+        assert torch.equal(torch.cat([t[0, p] for p in pages])[:70], old[kept[0].long()])
