@@ -329,3 +329,65 @@ def test_offsets_past_32_bits(dtype, n_q, max_pages):
     assert xb.op_device_error() == 0 and kept[0].tolist() == chosen(before, L, 70, 3, 20)
     for t, old in zip((cache.k, cache.v), rows):
         assert torch.equal(torch.cat([t[0, p] for p in pages])[:70], old[kept[0].long()])
+
+
+def test_a_step_with_its_eviction_in_one_graph():
+    """Projection, norm and rotation into the cache, attention, weights, output projection and eviction, captured once:
+    replays do what the same calls do, bit by bit, while another stream makes calls of its own."""
+    H, hk, hd, d, ps, n, B, keep = 8, 4, 64, 256, 16, 5, 3, 40
+    dt, rows = torch.bfloat16, (8 + 2 * 4) * 64
+    g = torch.Generator(device=DEV).manual_seed(2)
+
+    def r(*shape, std=1.0):
+        return std * torch.randn(*shape, generator=g, device=DEV)
+
+    wq, ws, wo, wos = (torch.empty(s, dtype=t, device=DEV) for s, t in
+                       (((rows, d), torch.int8), ((rows,), torch.float32), ((d, H * hd), torch.int8), ((d,), torch.float32)))
+    xb.op_quantize_rows("bf16", r(rows, d, std=d ** -0.5).to(dt), wq, ws)
+    xb.op_quantize_rows("bf16", r(d, H * hd, std=(H * hd) ** -0.5).to(dt), wo, wos)
+    bias, bo, gate, gamma = r(rows, std=0.05), r(d, std=0.05), torch.ones(d, device=DEV), torch.ones(hd, device=DEV)
+    rotation = torch.empty(2 * (hd // 2) * 64, device=DEV)
+    xb.op_rope_table([hd // 2], [64], 1e4, rotation)
+    xs = [r(B * n, d).to(dt) for _ in range(12)]
+
+    def state():
+        c = xb.KVCache.empty("bf16", 1, 20, ps, hk, hd, 4, 4)
+        return dict(c=c, w=torch.zeros(4, 64, device=DEV), x=torch.zeros(B * n, d, dtype=dt, device=DEV), ids=torch.tensor([2, 0, 3], dtype=torch.int32, device=DEV),
+                    pos=torch.zeros(B * n, 1, dtype=torch.int32, device=DEV), slots=torch.empty(B, n, dtype=torch.int32, device=DEV),
+                    qkv=torch.empty(B * n, rows, dtype=dt, device=DEV), q=torch.empty(B * n, H * hd, dtype=dt, device=DEV),
+                    o=torch.empty(B * n, H * hd, dtype=dt, device=DEV), lse=torch.empty(B * n, H, device=DEV),
+                    y=torch.empty(B * n, d, dtype=dt, device=DEV), kept=torch.empty(B, keep, dtype=torch.int32, device=DEV))
+
+    def step(s):
+        c, q, dq, dk = s["c"], s["qkv"], H * hd, hk * hd
+        xb.op_kv_extend(c, s["ids"], n, s["slots"])
+        xb.op_linear_i8("bf16", xb.XC_EPI_BIAS, s["x"], wq, ws, bias, q)
+        xb.op_qk_norm_rope(c, 0, q[:, :dq], q[:, dq:dq + dk], q[:, dq + dk:], gamma, gamma, s["pos"], [hd // 2], [64], rotation,
+                           s["slots"].view(-1), s["q"])
+        xb.op_branch_attention(c, 0, s["ids"], n, s["q"], s["o"], causal=True, lse=s["lse"])
+        xb.op_key_weights(c, 0, s["ids"], n, s["q"], s["lse"], s["w"], causal=True, decay=0.9)
+        xb.op_linear_i8("bf16", xb.XC_EPI_RESID_GATE, s["o"], wo, wos, bo, s["y"], gate=gate, resid=s["x"])
+        xb.op_kv_evict(c, s["ids"], keep, s["w"], n_first=2, n_last=8, kept=s["kept"])
+
+    eager, replayed, other = state(), state(), state()
+    warm = state()
+    step(warm)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(replayed)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for i, x in enumerate(xs):
+        for s in (eager, replayed):
+            s["x"].copy_(x)
+            s["pos"].fill_(i)
+        step(eager)
+        graph.replay()
+        with torch.cuda.stream(side):
+            step(other)
+        for name in ("y", "w", "kept", "lse"):
+            assert torch.equal(eager[name].view(torch.uint8), replayed[name].view(torch.uint8)), (i, name)
+        assert all(torch.equal(getattr(eager["c"], t), getattr(replayed["c"], t)) for t in ("ref", "table", "len"))
+    torch.cuda.synchronize()
+    assert eager["c"].len.tolist() == [keep, 0, keep, keep] and xb.op_device_error() == 0
+    assert eager["kept"][:, 0].tolist() == [0] * B and int((eager["c"].ref > 0).sum()) == B * 3
