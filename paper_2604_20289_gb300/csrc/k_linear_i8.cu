@@ -472,9 +472,10 @@ __device__ __forceinline__ void i8_turn(float (&x)[16], int lane) {
 // Warps: 0 loads weights, 1 issues the products, 2 loads tokens, 4-11 widen the weights (thread = channel =
 // TMEM lane, a half of each tile's depth to either four warps), 12-19 write the outputs (two
 // per TMEM quadrant, half of the tokens each).
-// 12960 tokens x 13824 x 5120: 1031 us, 1.78 PFLOP/s (the tensor pipe 76 % busy, the rest the clock under the
-// power cap and the tiles' ends); 331 tokens x 5120 x 13824: 27 us from the first product to the last, 890 cycles a
-// depth of 128 where the products take 704.
+// 12960 tokens x 13824 x 5120: 1031 us, 1.78 PFLOP/s, the tensor pipe 76 % busy; 331 tokens x 5120 x 13824: 27 us from
+// the first product to the last.  A depth of 128 takes 970 and 870 cycles where the products of 192 and 176 tokens
+// take 768 and 704, with hardly a wait for operands (clock counters): probably shared memory's bandwidth, of which
+// the products read 64 bytes a clock, the copies write 85 and the widening reads 22, 171 of 128.
 template <typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     linear_i8_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
