@@ -86,6 +86,8 @@ class BranchedLayers:
                 t = w[name]
                 if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
                     raise ValueError(f"layer {layer}: {name}: contiguous CUDA tensor {list(shape)} of {dtype} expected")
+                if dtype is torch.int8 and t.data_ptr() % 16 != 0:
+                    raise ValueError(f"layer {layer}: {name}: 16-byte aligned memory expected")
 
     def _linear(self, epilogue, x, w, name, out, workspace=None, resid=None, stream=None):
         gate = None if resid is None else self.ones
@@ -105,11 +107,13 @@ class BranchedLayers:
         x, o = (torch.zeros(1, n, dtype=dt, device="cuda") for n in (self.d, self.H * self.hd))
         y, qkv = torch.empty_like(x), torch.empty(1, w["qkv_w"].shape[0], dtype=dt, device="cuda")
         xb.op_ln_mod(self.dtype, x, self.zeros, self.zeros, y, eps=self.eps)
-        self._linear(xb.XC_EPI_BIAS, y, w, "qkv", qkv)
+        for each in {v["qkv_w"].dtype: v for v in self.weights}.values():  # a layer of either kind
+            self._linear(xb.XC_EPI_BIAS, y, each, "qkv", qkv)
         dq, dk, none = o.shape[1], self.Hk * self.hd, self._ids([-1])      # slot -1: no keys are kept
         xb.op_qk_norm_rope(c, 0, qkv[:, :dq], qkv[:, dq:dq + dk], qkv[:, dq + dk:], w["gamma_q"], w["gamma_k"],
                            self._ids([0]), self.pairs, self.n_pos, self.rotation, none, o, eps=self.eps)
-        self._linear(xb.XC_EPI_RESID_GATE, o, w, "o", y, resid=x)
+        for each in {v["o_w"].dtype: v for v in self.weights}.values():
+            self._linear(xb.XC_EPI_RESID_GATE, o, each, "o", y, resid=x)
 
     def _on_current_stream(self):
         """Orders the current stream after the object's earlier calls.  Every method that

@@ -281,6 +281,24 @@ def test_refusals_change_nothing():
     assert xb.op_device_error() == 0
 
 
+def test_layers_of_either_kind():
+    """Sizes that only the 8-bit product takes (384 channels) are refused at once where any layer is of the other kind."""
+    from paper_2604_20289_gb300 import branches
+    H, hk, hd, d = 4, 1, 64, 256
+    w = branches.random_layers(2, d, H, hk, hd, "bf16")
+    q = branches.quantize_layers(w)
+    size = dict(n_pages=8, page_size=16, max_seqs=2, max_len=64)
+    for layers in (w, [q[0], w[1]], [w[0], q[1]]):
+        with pytest.raises(xb.XCacheError):
+            branches.BranchedLayers(layers, H, hk, hd, **size)
+    odd = torch.empty(q[0]["o_w"].numel() + 16, dtype=torch.int8, device=DEV)[8:-8].view(q[0]["o_w"].shape)
+    with pytest.raises(ValueError):
+        branches.BranchedLayers([q[0], dict(q[1], o_w=odd)], H, hk, hd, **size)
+    m = branches.BranchedLayers([q[0], dict(q[1], o_w=w[1]["o_w"])], H, hk, hd, **size)      # mixed, where both take it
+    y = m.step([m.new()], torch.randn(1, 20, d, device=DEV))
+    assert y.isfinite().all() and xb.op_device_error() == 0
+
+
 def test_steps_and_evictions_on_streams_in_turn():
     a, b = (Rollout("f32", True, 4, 2, 32, 5e-3, 1e-2) for _ in range(2))
     streams = [torch.cuda.Stream() for _ in range(2)]
