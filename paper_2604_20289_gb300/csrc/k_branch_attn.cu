@@ -1210,7 +1210,8 @@ __global__ void __launch_bounds__(THREADS, PREFIX ? (KB == 8 ? 3 : 4) * COMBINE_
             acc[i] = make_float4(acc[i].x * a, acc[i].y * a, acc[i].z * a, acc[i].w * a);
 #pragma unroll
             for (int k = 0; k < KB; ++k) {
-                if (ml[i][k].x == -INFINITY) continue;     // no key of this piece for the row
+                // no key of this piece for the row; a row of NaN has no maximum either, but a sum that is NaN
+                if (ml[i][k].x == -INFINITY && ml[i][k].y == 0.0f) continue;
                 const float w = exp2f(ml[i][k].x - use);
                 den[i] = fmaf(w, ml[i][k].y, den[i]);
                 acc[i].x = fmaf(w, x[i][k].x, acc[i].x);
