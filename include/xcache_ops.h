@@ -330,7 +330,9 @@ xc_status xc_op_branch_attention(const xc_kv_cache *cache, int layer, int n_bran
 
 /* The same call, and lse [n_branches * n_q][n_heads] (float, or NULL): the log of
  * each row's sum of exp(scale * (q . k_j)) over the keys it sees, -infinity
- * where it sees none. */
+ * where it sees none (or scores of -infinity alone).  A NaN score makes it NaN, a
+ * score of +infinity, or past fp32's range, +infinity (with a NaN beside it:
+ * either), and the row of o NaN. */
 xc_status xc_op_branch_attention_lse(const xc_kv_cache *cache, int layer, int n_branches, const int *seqs, int n_q,
                                      int n_heads, const void *q, long q_stride, int shared_len, int causal,
                                      float scale, void *o, long o_stride, float *lse, void *workspace,
@@ -343,7 +345,8 @@ xc_status xc_op_branch_attention_lse(const xc_kv_cache *cache, int layer, int n_
  * over the tokens t and heads h of branch b, s = seqs[b], j < len[s].  Every row
  * adds 1 in all.  One array serves every layer of a step: decay of the step in the first
  * layer's call, 1 in the others'.  decay = 0 does not read the old weights.  A row
- * whose lse is -infinity adds nothing.
+ * whose lse is -infinity adds nothing, one whose lse is NaN makes every key it sees NaN, and one
+ * whose lse is +infinity the keys of infinite or NaN score (it gives the others nothing).
  *   weights     device float [max_seqs][w_stride], w_stride >= max_pages * page_size;
  *               entries past len[s] are neither read nor written, so those of new tokens must be 0
  *               (or decay 0)

@@ -60,8 +60,11 @@ struct BranchSched {
     // length on the line of a unit of n key tiles
     __host__ __device__ __forceinline__ int line_len(int n) const { return n > 0 ? n + lead : 0; }
     // log sum_j exp(scale q . k_j) of a row, from its max m (log2 units) and sum l: -inf without keys
+    // (no term: l = 0).  l is NaN where a score is NaN (m passes over those) and where the
+    // largest is +inf, whose weight is 2^(inf - inf): m is +inf then, and so is the log.
     __device__ __forceinline__ void put_lse(int t, int head, float m, float l) const {
-        lse[(size_t)t * (Hk * grp) + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        const float y = l == 0.0f ? -INFINITY : m == INFINITY ? INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        lse[(size_t)t * (Hk * grp) + head] = y;
     }
     // keys that query i of a branch of length l sees
     __host__ __device__ __forceinline__ int limit(int l, int i) const {
