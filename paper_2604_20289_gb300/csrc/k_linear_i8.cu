@@ -403,13 +403,6 @@ __device__ __forceinline__ float i8_epilogue(int epi, float acc, float sa, float
     return y;
 }
 
-// Half of a tile of tokens into both CTAs of the pair: the bytes count on the barrier at the same place in either.
-__device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *tm, uint64_t *bar, int x, int y) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3}], [%4], %5;"
-        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(smem_u32(bar)), "h"((unsigned short)3)
-        : "memory");
-}
 // The products of one slot of depth 64 (A in tensor memory) and what their end tells: one
 // lane is elected for all of it (an election for each instruction took the issuing warp as long
 // as the products take).
@@ -427,12 +420,9 @@ __device__ __forceinline__ void i8_issue_slot(uint32_t acc, uint32_t a, uint64_t
         "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, t;\n\t"
         "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, t;\n\t"
         "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t"
-        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%6], %7;\n\t}"
-        ::"r"(acc), "r"(a), "l"(b), "r"(idesc), "r"(first), "r"(smem_u32(a_empty)), "r"(smem_u32(b_empty)), "h"((unsigned short)3)
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}"
+        ::"r"(acc), "r"(a), "l"(b), "r"(idesc), "r"(first), "r"(smem_u32(a_empty)), "r"(smem_u32(b_empty))
         : "memory");
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
 }
 
 // Exchanges between lanes that turn a lane's 16 tokens of one channel into 8 consecutive
@@ -466,18 +456,19 @@ __device__ __forceinline__ void i8_turn(float (&x)[16], int lane) {
     for (int i = 0; i < 16; ++i) x[i] = y[i];
 }
 
-// Two CTAs run neighbouring tiles of channels with the same tokens: each loads half of the
-// tokens for both, which halves what they ask of L2 (a tile of 192 tokens and depth 64 is 32 KB
-// in 384 cycles of products, more than L2 hands an SM).
+// Two CTAs run neighbouring tiles of channels with the same tokens at the same time, so that
+// one of them finds the tokens in L2; each loads its own, and neither touches the other's shared
+// memory.  (One copy into both, by multicast, took 3 % off a chunk.  But the tokens are in the caller's workspace,
+// which nothing here shows to be this GPU's memory, and replicas on several GPUs run this kernel too.)
 // Warps: 0 loads weights, 1 issues the products, 2 loads tokens, 4-11 widen the weights (thread = channel =
 // TMEM lane, a half of each tile's depth to either four warps), 12-19 write the outputs (two
 // per TMEM quadrant, half of the tokens each).
-// 12960 tokens x 13824 x 5120: 1031 us, 1.78 PFLOP/s, the tensor pipe 76 % busy; 331 tokens x 5120 x 13824: 27 us from
-// the first product to the last.  A depth of 128 takes 970 and 870 cycles where the products of 192 and 176 tokens
-// take 768 and 704, with hardly a wait for operands (clock counters): probably shared memory's bandwidth, of which
+// 12960 tokens x 13824 x 5120: 1066 us, 1.72 PFLOP/s; 331 tokens x 5120 x 13824: 28 us from
+// the first product to the last.  A depth of 128 takes 1045 and 900 cycles where the products of 192 and 176 tokens
+// take 768 and 704, with 3 % of the time spent waiting for operands (clock counters): probably shared memory's bandwidth, of which
 // the products read 64 bytes a clock, the copies write 85 and the widening reads 22, 171 of 128.
 template <typename T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
+__global__ void __launch_bounds__(I8_THREADS, 1)
     linear_i8_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                      const __grid_constant__ I8Sched s, int *err) {
     extern __shared__ uint8_t smem_raw[];
@@ -490,7 +481,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     uint64_t *w_full = bars, *w_empty = w_full + I8_MAX_W, *b_full = w_empty + I8_MAX_W, *b_empty = b_full + I8_MAX_B;
     uint64_t *a_full = b_empty + I8_MAX_B, *a_empty = a_full + I8_MAX_A;
     uint64_t *acc_full = a_empty + I8_MAX_A, *acc_empty = acc_full + 2, *drained = acc_empty + 2;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < s.wst; ++i) {
             mbar_init(&w_full[i], 1);
@@ -498,7 +489,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
         }
         for (int i = 0; i < s.bst; ++i) {
             mbar_init(&b_full[i], 1);
-            mbar_init(&b_empty[i], 2);                 // both CTAs have read their copy of the tokens
+            mbar_init(&b_empty[i], 1);
         }
         for (int i = 0; i < s.as; ++i) {
             mbar_init(&a_full[i], 128);
@@ -514,7 +505,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     if (warp == 1) tmem_alloc(&tmem_slot, 512);
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                                // the other CTA's barriers are set up too
     tc_fence_after();
     const uint32_t tmem = 0;                           // all 512 columns are this CTA's (a constant stays in uniform registers)
     const int a_col = 2 * s.acs;
@@ -544,7 +534,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     } else if (warp == 2) {
         if (lane == 0) {
             pdl_wait();
-            const int half = s.NT / 2 * rank;          // rows of the tile that this CTA loads for both
             int i = 0, it = 0;
             uint32_t ph = 1;
             bool ok = true;
@@ -552,7 +541,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
                 for (int kt = 2 * w.k0; kt < 2 * w.k1; ++kt, ++it) {
                     if (!(ok = mbar_wait(&b_empty[i], ph, err, ERR_WAIT_PRODUCER))) break;
                     mbar_expect_tx(&b_full[i], b_bytes);
-                    tma_load_2d_pair(sB + i * b_bytes + half * 128, &tmA, &b_full[i], 64 * kt, w.mb * s.NT + half);
+                    tma_load_2d(sB + i * b_bytes, &tmA, &b_full[i], 64 * kt, w.mb * s.NT);
                     if (++i == s.bst) {
                         i = 0;
                         ph ^= 1;
@@ -597,6 +586,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
                 there = mbar_test2(&b_full[i], ph, &a_full[a], a_ph);
                 i8_issue_slot(acc, ta, db, idesc, first, a_done, b_done);
             }
+            // (the outputs wait for this one, which comes after the slots' commits: the CTA outlives them all)
             if (ok) tc_commit_warp(&acc_full[buf]);
         }
         if (!ok) {                                     // a wait ran out: no product is under way when the CTA ends
@@ -733,7 +723,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8_THREADS, 1)
     pdl_release();
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                                // the other CTA writes here no more
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -1137,7 +1126,7 @@ cudaError_t linear_i8(const LinearI8Args &a, void *ws, int *err, cudaStream_t st
     s.vec = a.N % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(a.resid)) & 15) == 0;
     CUtensorMap tw, ta;
     if (!make_tmap_2d(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.W, a.N, a.K, I8_BM, 128) ||
-        !make_tmap_2d(&ta, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, tokens, a.M, a.K, s.NT / 2, 64))
+        !make_tmap_2d(&ta, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, tokens, a.M, a.K, s.NT, 64))
         return cudaErrorInvalidValue;
     cudaError_t e;
     if (a.a_scale != nullptr) {
