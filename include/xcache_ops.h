@@ -4,7 +4,8 @@
  * These run ONE kernel of the chunk step on caller-owned device buffers, so
  * that each step of the path can be checked against the CPU oracle at full
  * size.  xc_chunk_step runs exactly these kernels.  All pointers are DEVICE
- * pointers; `stream` is a cudaStream_t (NULL = legacy default stream);
+ * pointers, to memory of the current device (workspaces too); `stream` is a
+ * cudaStream_t of it (NULL = legacy default stream);
  * every call is asynchronous.  Activations use `dtype` (XC_F32: float32,
  * XC_BF16: bfloat16); vectors such as bias / gate / shift / scale are float32.
  * Weights are K-major: Wt [N][K] holds W^T of y = x W.

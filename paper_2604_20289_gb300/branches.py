@@ -37,7 +37,8 @@ class BranchedLayers:
     max_len tokens at a time, at positions below max_pos (max_len).  track: None, or the factor (0 to 1) by
     which a sequence's ``key_weights`` shrink with each of its steps, before that step's
     weights, of all layers, heads and new tokens, are added.  A call runs on the stream that is
-    current when it is made, after the object's earlier calls on whatever stream.
+    current when it is made, after the object's earlier calls on whatever stream; the device that was
+    current when the object was made is current in every call.
     ``cache`` is for reading: its sequences change through this object alone."""
 
     def __init__(self, weights, n_heads, n_kv_heads, head_dim, n_pages, page_size=64, max_seqs=64, max_len=4096,
@@ -84,8 +85,9 @@ class BranchedLayers:
                     here[name + "_s"] = ((n,), torch.float32)
             for name, (shape, dtype) in here.items():
                 t = w[name]
-                if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-                    raise ValueError(f"layer {layer}: {name}: contiguous CUDA tensor {list(shape)} of {dtype} expected")
+                if t.shape != shape or t.dtype != dtype or t.get_device() != self.cache.device or not t.is_contiguous():
+                    raise ValueError(f"layer {layer}: {name}: contiguous CUDA tensor {list(shape)} of {dtype} on the "
+                                     "current device expected")
                 if dtype is torch.int8 and t.data_ptr() % 16 != 0:
                     raise ValueError(f"layer {layer}: {name}: 16-byte aligned memory expected")
 
@@ -118,6 +120,8 @@ class BranchedLayers:
     def _on_current_stream(self):
         """Orders the current stream after the object's earlier calls.  Every method that
         launches work begins with it: its temporaries and its launches are then of one stream."""
+        if torch.cuda.current_device() != self.cache.device:
+            raise ValueError(f"CUDA device {self.cache.device}, which holds the cache, is not the current one")
         st = torch.cuda.current_stream()
         if st != self._last:
             st.wait_stream(self._last)
@@ -169,8 +173,8 @@ class BranchedLayers:
         seq, = self._in_use([seq])
         part = self.length[seq] % self.cache.page_size != 0
         self._room(n if part else 0)
-        ids = self._take(n)
         self._on_current_stream()
+        ids = self._take(n)
         try:
             to = self._ids(ids)
             rows = to.long()
@@ -293,8 +297,8 @@ class BranchedLayers:
         """Appends x [len(seqs), n, d] to the sequences and returns the layers' output
         of the new tokens (same shape).  Every new token sees its sequence up to itself."""
         seqs = self._in_use(seqs)
-        if x.dim() != 3 or x.shape[0] != len(seqs) or x.shape[2] != self.d or not x.is_cuda:
-            raise ValueError(f"x: CUDA tensor [{len(seqs)}, n, {self.d}] expected")
+        if x.dim() != 3 or x.shape[0] != len(seqs) or x.shape[2] != self.d or x.get_device() != self.cache.device:
+            raise ValueError(f"x: CUDA tensor [{len(seqs)}, n, {self.d}] on the cache's device expected")
         B, n, d = x.shape
         if n == 0 or B == 0:
             return x

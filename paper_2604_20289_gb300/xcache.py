@@ -480,8 +480,9 @@ class KVCache:
     """Handle on a paged key / value cache (xc_kv_cache) over the caller's torch
     CUDA tensors: k, v [n_layers, n_pages, page_size, n_kv_heads * head_dim]
     (float32 or bfloat16), ref [n_pages], table [max_seqs, max_pages] and len
-    [max_seqs] int32, all contiguous.  Keeps the tensors, and one workspace per
-    stream that grows to the largest call.  ``empty`` allocates them.
+    [max_seqs] int32, all contiguous and on one device, which is the current one in
+    every call.  Keeps the tensors, and one workspace per stream that grows to the
+    largest call.  ``empty`` allocates them.
 
     A call that torch captures into a graph (``torch.cuda.graph``) takes a
     workspace of its own from the graph's memory instead: it lives as long as the
@@ -499,9 +500,11 @@ class KVCache:
         for t in (ref, table, length):
             if t.dtype != torch.int32:
                 raise ValueError("ref, table and len are int32")
+        self.device = k.get_device()
         for t in (k, v, ref, table, length):
-            if not t.is_contiguous() or not t.is_cuda:
-                raise ValueError("cache tensors are contiguous CUDA tensors")
+            if not t.is_contiguous() or not t.is_cuda or t.get_device() != self.device:
+                raise ValueError("cache tensors are contiguous CUDA tensors of one device")
+        self._current_device = torch._C._cuda_getDevice
         self.k, self.v, self.ref, self.table, self.len = k, v, ref, table, length
         self.dtype, self.n_kv_heads, self.head_dim = dtype, n_kv_heads, head_dim
         self.page_size = k.shape[2]
@@ -548,10 +551,16 @@ class KVCache:
         return ws
 
     def int32(self, t, n: int) -> int:
-        """Device pointer of a contiguous int32 CUDA tensor of n elements."""
-        if t.dtype is not self._int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError(f"expected a contiguous int32 CUDA tensor of {n} elements")
+        """Device pointer of a contiguous int32 tensor of n elements on the cache's device."""
+        if t.dtype is not self._int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != self.device:
+            raise ValueError(f"expected a contiguous int32 CUDA tensor of {n} elements on the cache's device")
         return t.data_ptr()
+
+    def stream(self, stream) -> int:
+        """cudaStream_t of a call, which runs on the cache's device."""
+        if self._current_device() != self.device:
+            raise ValueError(f"the cache is on CUDA device {self.device}, which is not the current one")
+        return _stream(stream)
 
 
 def _scratch(nbytes, stream, cuda, device):
@@ -567,8 +576,9 @@ def _scratch(nbytes, stream, cuda, device):
 
 def _given(workspace):
     """(tensor, pointer, bytes) of the caller's own workspace."""
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace: expected a contiguous CUDA tensor")
+    import torch
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("workspace: expected a contiguous CUDA tensor on the current device")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -580,7 +590,7 @@ def op_kv_workspace_bytes(cache: KVCache) -> int:
 
 def op_kv_fork(cache: KVCache, src, dst, stream=None, workspace=None):
     """Sequence dst[i] becomes a copy of src[i] (int32 CUDA tensors)."""
-    st = _stream(stream)
+    st = cache.stream(stream)
     n = src.numel()
     buf, ws, nbytes = cache.workspace(cache._page_bytes, st) if workspace is None else _given(workspace)
     check(LIB.xc_op_kv_fork(cache.ptr, n, cache.int32(src, n), cache.int32(dst, n), ws, nbytes, st))
@@ -588,7 +598,7 @@ def op_kv_fork(cache: KVCache, src, dst, stream=None, workspace=None):
 
 def op_kv_extend(cache: KVCache, seqs, n_new: int, slots, stream=None, workspace=None):
     """Appends n_new tokens to every listed sequence; slots [n, n_new] int32 receives their cache slots."""
-    st = _stream(stream)
+    st = cache.stream(stream)
     n = seqs.numel()
     buf, ws, nbytes = cache.workspace(cache._page_bytes, st) if workspace is None else _given(workspace)
     check(LIB.xc_op_kv_extend(cache.ptr, n, cache.int32(seqs, n), n_new, cache.int32(slots, n * n_new), ws, nbytes,
@@ -597,12 +607,12 @@ def op_kv_extend(cache: KVCache, seqs, n_new: int, slots, stream=None, workspace
 
 def op_kv_free(cache: KVCache, seqs, stream=None):
     n = seqs.numel()
-    check(LIB.xc_op_kv_free(cache.ptr, n, cache.int32(seqs, n), _stream(stream)))
+    check(LIB.xc_op_kv_free(cache.ptr, n, cache.int32(seqs, n), cache.stream(stream)))
 
 
 def op_kv_compact(cache: KVCache, n_live, stream=None, workspace=None):
     """n_live: int32 CUDA tensor of one element, receives the pages in use."""
-    st = _stream(stream)
+    st = cache.stream(stream)
     buf, ws, nbytes = cache.workspace(cache._page_bytes, st) if workspace is None else _given(workspace)
     check(LIB.xc_op_kv_compact(cache.ptr, cache.int32(n_live, 1), ws, nbytes, st))
 
@@ -644,15 +654,16 @@ def op_qk_norm_rope(cache: KVCache, layer, q, k, v, gamma_q, gamma_k, pos, axis_
     (sq, u0), (sk, u1), (sv, u2), (so, u3) = q.stride(), k.stride(), v.stride(), q_out.stride()
     if u0 != 1 or u1 != 1 or u2 != 1 or u3 != 1:
         raise ValueError("rows must have unit column stride")
-    if not (q.is_cuda and k.is_cuda and v.is_cuda and q_out.is_cuda and gamma_q.is_cuda and gamma_k.is_cuda and
-            table.is_cuda):
-        raise ValueError("expected CUDA tensors")
+    dev = cache.device
+    if not (q.get_device() == k.get_device() == v.get_device() == q_out.get_device() == gamma_q.get_device() ==
+            gamma_k.get_device() == table.get_device() == dev):
+        raise ValueError("expected CUDA tensors on the cache's device")
     if T == 1:
         sq, sk, sv, so = dq, dk, dk, dq
     st = LIB.xc_op_qk_norm_rope(cache.ptr, layer, T, dq // hd, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv,
                                 gamma_q.data_ptr(), gamma_k.data_ptr(), eps, n, c_pairs, c_pos,
                                 cache.int32(pos, T * n), table.data_ptr(), half_split, cache.int32(slots, T),
-                                q_out.data_ptr(), so, _stream(stream))
+                                q_out.data_ptr(), so, cache.stream(stream))
     if st:
         check(st)
 
@@ -662,8 +673,9 @@ def op_branch_attention_workspace_bytes(cache: KVCache, n_branches, n_q, n_heads
 
 
 def _lse(cache: KVCache, lse, rows, heads) -> int:
-    if lse.shape != (rows, heads) or lse.dtype is not cache._float32 or not lse.is_contiguous() or not lse.is_cuda:
-        raise ValueError("lse: contiguous float32 CUDA tensor [len(seqs) * n_q, n_heads]")
+    if lse.shape != (rows, heads) or lse.dtype is not cache._float32 or not lse.is_contiguous() or \
+            lse.get_device() != cache.device:
+        raise ValueError("lse: contiguous float32 tensor [len(seqs) * n_q, n_heads] on the cache's device")
     return lse.data_ptr()
 
 
@@ -679,13 +691,13 @@ def op_branch_attention(cache: KVCache, layer, seqs, n_q, q, o, shared_len=0, ca
     (sq, u0), (so, u1) = q.stride(), o.stride()
     if u0 != 1 or u1 != 1:
         raise ValueError("rows must have unit column stride")
-    if not (q.is_cuda and o.is_cuda):
-        raise ValueError("expected CUDA tensors")
+    if not (q.get_device() == o.get_device() == cache.device):
+        raise ValueError("expected CUDA tensors on the cache's device")
     if T == 1:
         sq = so = dq
     if lse is not None:
         lse = _lse(cache, lse, T, dq // hd)
-    cuda = _stream(stream)
+    cuda = cache.stream(stream)
     if workspace is None:
         key = (B, n_q, dq, shared_len)
         need = cache._attn_bytes.get(key)
@@ -709,8 +721,10 @@ def _weights(cache: KVCache, weights) -> tuple:
     """(pointer, row stride) of the keys' weights."""
     if weights.dim() != 2 or weights.shape[0] != cache.table.shape[0] or \
             weights.shape[1] < cache.table.shape[1] * cache.page_size or weights.dtype is not cache._float32 or \
-            not weights.is_cuda or weights.stride(1) != 1 or (weights.shape[0] > 1 and weights.stride(0) < weights.shape[1]):
-        raise ValueError("weights: float32 CUDA tensor [max_seqs, max_pages * page_size] with unit column stride")
+            weights.get_device() != cache.device or weights.stride(1) != 1 or \
+            (weights.shape[0] > 1 and weights.stride(0) < weights.shape[1]):
+        raise ValueError("weights: float32 tensor [max_seqs, max_pages * page_size] with unit column stride on the "
+                         "cache's device")
     return weights.data_ptr(), max(weights.stride(0), weights.shape[1])
 
 
@@ -721,15 +735,15 @@ def op_key_weights(cache: KVCache, layer, seqs, n_q, q, lse, weights, shared_len
     of op_key_weights_workspace_bytes, or None for the cache's own."""
     B, hd = seqs.numel(), cache.head_dim
     T, dq = q.shape
-    if T != B * n_q or dq % hd or q.dtype is not cache.torch_dtype or not q.is_cuda:
-        raise ValueError("q: CUDA tensor [len(seqs) * n_q, n_heads * head_dim] of the cache's dtype")
+    if T != B * n_q or dq % hd or q.dtype is not cache.torch_dtype or q.get_device() != cache.device:
+        raise ValueError("q: [len(seqs) * n_q, n_heads * head_dim] of the cache's dtype, on its device")
     sq, u0 = q.stride()
     if u0 != 1:
         raise ValueError("rows must have unit column stride")
     if T == 1:
         sq = dq
     w, sw = _weights(cache, weights)
-    cuda = _stream(stream)
+    cuda = cache.stream(stream)
     if workspace is None:
         key = (B, n_q, dq, shared_len)
         need = cache._weigh_bytes.get(key)
@@ -755,7 +769,7 @@ def op_kv_evict(cache: KVCache, seqs, keep: int, weights=None, n_first=0, n_last
     op_kv_evict_workspace_bytes, or None for the cache's own."""
     n = seqs.numel()
     w, sw = _weights(cache, weights) if weights is not None else (None, 0)
-    cuda = _stream(stream)
+    cuda = cache.stream(stream)
     if workspace is None:
         need = cache._evict_bytes.get((n, keep))
         if need is None:
