@@ -669,18 +669,14 @@ static cudaError_t launch_attn_(const CUtensorMap &tq, const CUtensorMap &tk, co
                                 int Lq, int n_keys, int d, const AttnSplit &sp, bool split, int n_combine, void *ws,
                                 const uint8_t *skip, int *err, int *n_launched, cudaStream_t st) {
     using A = AttnTile<HD>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<HD, WAVE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             A::SMEM_BYTES);
-        if (e != cudaSuccess) return e;
-        attr_set = true;
-    }
+    static DeviceSet asked{0};
+    cudaError_t e = allow_smem(attn_tc_kernel<HD, WAVE>, A::SMEM_BYTES, asked);
+    if (e != cudaSuccess) return e;
     const int n_sm = sm_count();
     float *ws_o = split ? reinterpret_cast<float *>(ws) : nullptr;
     float2 *ws_ml = split ? reinterpret_cast<float2 *>(ws_o + 2 * ((size_t)n_sm + 1) * 256 * HD) : nullptr;
-    cudaError_t e = launch_pdl(attn_tc_kernel<HD, WAVE>, dim3(sp.G), dim3(A::THREADS), A::SMEM_BYTES, st, tq, tk,
-                               tv, o, Lq, n_keys, d, sp, ws_o, ws_ml, skip, err);
+    e = launch_pdl(attn_tc_kernel<HD, WAVE>, dim3(sp.G), dim3(A::THREADS), A::SMEM_BYTES, st, tq, tk,
+                   tv, o, Lq, n_keys, d, sp, ws_o, ws_ml, skip, err);
     if (e != cudaSuccess) return e;
     if (n_launched) *n_launched = 1;
     if (split && n_combine > 0) {

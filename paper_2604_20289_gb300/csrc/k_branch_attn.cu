@@ -1348,19 +1348,12 @@ size_t branch_attn_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, 
     return branch_plan(c, B, n_q, H, shared).bytes;
 }
 
-template <typename K> static cudaError_t allow_smem(K kernel, int bytes, bool &done) {
-    if (done) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    done = e == cudaSuccess;
-    return e;
-}
-
 template <int HD, int QT>
 static cudaError_t launch_tc(const xc_kv_cache &c, const BranchAttnArgs &a, const BranchPlan &p, float sl2, int *err,
                              cudaStream_t st) {
     using A = BranchTile<HD, QT>;
-    static bool done = false;
-    cudaError_t e = allow_smem(branch_attn_kernel<HD, QT>, A::SMEM_BYTES, done);
+    static DeviceSet asked{0};
+    cudaError_t e = allow_smem(branch_attn_kernel<HD, QT>, A::SMEM_BYTES, asked);
     if (e != cudaSuccess) return e;
     const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
     const uint32_t box = c.page_size < 128 ? c.page_size : 128;
@@ -1374,8 +1367,8 @@ static cudaError_t launch_tc(const xc_kv_cache &c, const BranchAttnArgs &a, cons
 template <int HD>
 static cudaError_t launch_f32(const BranchAttnArgs &a, const BranchPlan &p, float sl2, int *err, cudaStream_t st) {
     using A = BranchTileF32<HD>;
-    static bool done = false;
-    cudaError_t e = allow_smem(branch_attn_f32_kernel<HD>, A::SMEM_BYTES, done);
+    static DeviceSet asked{0};
+    cudaError_t e = allow_smem(branch_attn_f32_kernel<HD>, A::SMEM_BYTES, asked);
     if (e != cudaSuccess) return e;
     return launch_pdl(branch_attn_f32_kernel<HD>, dim3(p.s.G), dim3(256), A::SMEM_BYTES, st,
                       reinterpret_cast<const float *>(a.q), a.q_ld, reinterpret_cast<const float *>(a.k),

@@ -570,12 +570,9 @@ static cudaError_t launch_tc(const CUtensorMap &ta, const CUtensorMap &tb, const
     auto kern = gemm_tc_kernel<BN, EPI>;
     EpiMaps em;
     if (!build_epi_maps<EPI>(em, ep)) return cudaErrorInvalidValue;
-    static bool attr_set = false;
-    if (!attr_set) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES);
-        if (e != cudaSuccess) return e;
-        attr_set = true;
-    }
+    static DeviceSet asked{0};
+    const cudaError_t e = allow_smem(kern, G::SMEM_BYTES, asked);
+    if (e != cudaSuccess) return e;
     const int n_sm = gemm_sm_count();
     const int n_tiles = (ep.N / BN) * ((ep.M + GEMM_BM - 1) / GEMM_BM);
     const int grid = n_tiles < n_sm ? n_tiles : n_sm;

@@ -1325,12 +1325,9 @@ size_t key_weights_workspace_bytes(const xc_kv_cache &c, int B, int n_q, int H, 
 template <int HD>
 static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
     constexpr int K_BYTES = KW_TILE * HD * 2, BUDGET = 192 * 1024;
-    static bool done = false;
-    if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(key_weights_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BUDGET + 1024);
-        if (e != cudaSuccess) return e;
-        done = true;
-    }
+    static DeviceSet asked{0};
+    cudaError_t e = allow_smem(key_weights_kernel<HD>, BUDGET + 1024, asked);
+    if (e != cudaSuccess) return e;
     const int q_bytes = s.N * HD * 2;
     const int q_slots = std::min(8, (BUDGET - 2 * K_BYTES) / q_bytes);
     const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
@@ -1338,19 +1335,16 @@ static cudaError_t key_launch_tc(const xc_kv_cache &c, const KeyWeightsArgs &a, 
     if (!make_tmap_heads_bf16(&tq, a.q, HD, (uint64_t)s.Hk * s.grp, (uint64_t)s.B * s.n_q, a.q_ld, s.grp, s.tt) ||
         !make_tmap_bf16(&tk, a.k, rows, cols, c.page_size < KW_TILE ? c.page_size : KW_TILE))
         return cudaErrorInvalidValue;
-    const cudaError_t e = launch_pdl(key_weights_kernel<HD>, dim3(s.G), dim3(KW_THREADS),
-                                     2 * K_BYTES + q_slots * q_bytes + 1024, st, tq, tk, s, q_slots, err);
+    e = launch_pdl(key_weights_kernel<HD>, dim3(s.G), dim3(KW_THREADS),
+                   2 * K_BYTES + q_slots * q_bytes + 1024, st, tq, tk, s, q_slots, err);
     if (e != cudaSuccess) return e;
     return launch_pdl(key_merge_kernel, dim3(2 * s.G), dim3(KW_KEYS), 0, st, s);
 }
 template <int HD>
 static cudaError_t key_launch_stream(const xc_kv_cache &c, const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
-    static bool done = false;
-    if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(key_weights_stream_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KST_BUDGET + 1024);
-        if (e != cudaSuccess) return e;
-        done = true;
-    }
+    static DeviceSet asked{0};
+    const cudaError_t e = allow_smem(key_weights_stream_kernel<HD>, KST_BUDGET + 1024, asked);
+    if (e != cudaSuccess) return e;
     const int slot = (KW_TILE + s.N) * HD * 2, sums = 4 * s.nb * KW_TILE * 4, slots = std::min(KST_SLOTS, (KST_BUDGET - sums) / slot);
     const uint64_t rows = (uint64_t)c.n_pages * c.page_size, cols = (uint64_t)c.n_kv_heads * HD;
     CUtensorMap tq, tk;
@@ -1363,12 +1357,9 @@ template <int HD, int NT>
 static cudaError_t key_launch_few(const KeyWeightsArgs &a, const KeySched &s, int *err, cudaStream_t st) {
     if constexpr (NT > 1)
         if (s.N < 8 * NT) return key_launch_few<HD, NT - 1>(a, s, err, st);
-    static bool done = false;
-    if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(key_weights_few_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)KFEW_SMEM);
-        if (e != cudaSuccess) return e;
-        done = true;
-    }
+    static DeviceSet asked{0};
+    const cudaError_t e = allow_smem(key_weights_few_kernel<HD, NT>, (int)KFEW_SMEM, asked);
+    if (e != cudaSuccess) return e;
     return launch_pdl(key_weights_few_kernel<HD, NT>, dim3(s.G), dim3(KFEW_THREADS), few_smem(s.Hk, s.N, HD), st,
                       reinterpret_cast<const bf16 *>(a.q), a.q_ld, reinterpret_cast<const bf16 *>(a.k), s, err);
 }
@@ -1377,12 +1368,11 @@ static cudaError_t key_launch_f32(const KeyWeightsArgs &a, const KeySched &s, in
     if constexpr (C > 1)
         if (s.Hk < C) return key_launch_f32<HD, C / 2>(a, s, err, st);
     constexpr int SMEM = 2 * 64 * (HD + 4) * 4;
-    static bool done = false;
-    if (!done && SMEM > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(key_weights_f32_kernel<HD, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    static DeviceSet asked{0};
+    if (SMEM > 48 * 1024) {
+        const cudaError_t e = allow_smem(key_weights_f32_kernel<HD, C>, SMEM, asked);
         if (e != cudaSuccess) return e;
     }
-    done = true;
     return launch_pdl(key_weights_f32_kernel<HD, C>, dim3(4 * s.G / C * C), dim3(256), SMEM, st, reinterpret_cast<const float *>(a.q), a.q_ld,
                       reinterpret_cast<const float *>(a.k), s, err);
 }

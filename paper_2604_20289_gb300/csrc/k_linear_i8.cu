@@ -1029,13 +1029,10 @@ static bool i8_small(int M, int K) { return M <= I8S_MAX_M && (long)M * ((K + 12
 
 template <typename T, int NT8>
 static cudaError_t i8_small_launch(const I8Small &s, cudaStream_t st) {
-    static bool done = false;
+    static DeviceSet asked{0};
     const int part = (I8S_GROUPS + I8S_WARPS) * 16 * 8 * NT8 * 4;
-    if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(linear_i8_small_kernel<T, NT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, I8S_TOKEN_BYTES + part);
-        if (e != cudaSuccess) return e;
-        done = true;
-    }
+    const cudaError_t e = allow_smem(linear_i8_small_kernel<T, NT8>, I8S_TOKEN_BYTES + part, asked);
+    if (e != cudaSuccess) return e;
     return launch_pdl(linear_i8_small_kernel<T, NT8>, dim3(s.G), dim3(I8S_THREADS), s.M * s.KB * 256 + part, st, s);
 }
 template <typename T>
@@ -1097,13 +1094,10 @@ size_t linear_i8_workspace_bytes(int M, int N, int K) { return i8_small(M, K) ? 
 
 template <typename T>
 static cudaError_t i8_launch(const I8Plan &p, const CUtensorMap &tw, const CUtensorMap &ta, int *err, cudaStream_t st) {
-    static bool done = false;
-    if (!done) {
-        const cudaError_t e = cudaFuncSetAttribute(linear_i8_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, I8_SMEM + 1024);
-        if (e != cudaSuccess) return e;
-        done = true;
-    }
-    cudaError_t e = launch_pdl(linear_i8_kernel<T>, dim3(2 * p.s.P), dim3(I8_THREADS), p.smem, st, tw, ta, p.s, err);
+    static DeviceSet asked{0};
+    cudaError_t e = allow_smem(linear_i8_kernel<T>, I8_SMEM + 1024, asked);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(linear_i8_kernel<T>, dim3(2 * p.s.P), dim3(I8_THREADS), p.smem, st, tw, ta, p.s, err);
     if (e != cudaSuccess || !p.cut) return e;
     return launch_pdl(linear_i8_merge_kernel<T>, dim3(2 * (p.s.m_tiles * p.s.n_pairs - p.s.n_full), (p.s.NT + I8M_TOKENS - 1) / I8M_TOKENS), dim3(I8M_THREADS), 0, st, p.s);
 }

@@ -6,6 +6,7 @@
 
 #include "../../include/xcache.h"
 #include "../../include/xcache_ops.h"
+#include "xc_device.h"
 
 namespace xc {
 

@@ -1,0 +1,75 @@
+"""What the library keeps for a device is kept for each device.  No GPU is needed: the host
+code is compiled against stand-ins of the CUDA runtime's calls."""
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2604_20289_gb300", "csrc")
+FAKES = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+static int g_dev = 0, g_fail = 0;
+struct Ask { int dev, bytes; };
+static std::vector<Ask> g_asked;
+extern "C" cudaError_t cudaGetDevice(int *d) { *d = g_dev; return g_dev < 0 ? cudaErrorNoDevice : cudaSuccess; }
+extern "C" cudaError_t cudaFuncSetAttribute(const void *, cudaFuncAttribute, int v) {
+    if (g_fail) return cudaErrorInvalidValue;
+    g_asked.push_back({g_dev, v});
+    return cudaSuccess;
+}
+#define EXPECT(x) do { if (!(x)) { std::printf("line %d: %s\n", __LINE__, #x); std::exit(1); } } while (0)
+"""
+
+
+def run(tmp_path, body):
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no host compiler")
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text('#include "xc_device.h"\n' + FAKES + "int main() {\n" + body + "\n    return 0;\n}\n")
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.run([cxx, "-std=c++17", "-I", CSRC, "-I", os.path.join(cuda, "include"), str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
+
+
+def test_shared_memory_is_asked_for_on_each_device(tmp_path):
+    run(tmp_path, r"""
+    xc::DeviceSet a{0}, b{0};
+    void (*kernel)(int) = nullptr;
+    for (int round = 0; round < 2; ++round)
+        for (int dev : {0, 3, 63}) {
+            g_dev = dev;
+            EXPECT(xc::allow_smem(kernel, 100000, a) == cudaSuccess);
+        }
+    EXPECT(g_asked.size() == 3 && g_asked[0].dev == 0 && g_asked[1].dev == 3 && g_asked[2].dev == 63 && g_asked[1].bytes == 100000);
+    EXPECT(xc::allow_smem(kernel, 90000, b) == cudaSuccess && g_asked.size() == 4);   // another kernel
+    g_dev = 5;
+    g_fail = 1;
+    EXPECT(xc::allow_smem(kernel, 100000, a) == cudaErrorInvalidValue);               // not remembered as done
+    g_fail = 0;
+    EXPECT(xc::allow_smem(kernel, 100000, a) == cudaSuccess && g_asked.back().dev == 5);
+    for (int dev : {-1, 64, 1000}) {
+        g_dev = dev;
+        EXPECT(xc::allow_smem(kernel, 100000, a) != cudaSuccess);
+    }
+    EXPECT(g_asked.size() == 5);
+""")
+
+
+def sources():
+    for name in sorted(os.listdir(CSRC)):
+        with open(os.path.join(CSRC, name)) as f:
+            yield name, f.read()
+
+
+def test_no_source_asks_once_for_the_process():
+    for name, text in sources():
+        if name != "xc_device.h":
+            assert "cudaFuncSetAttribute" not in text, name
+        assert not re.search(r"static bool \w+ = false", text), name
