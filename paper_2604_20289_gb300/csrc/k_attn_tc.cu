@@ -649,18 +649,8 @@ __global__ void __launch_bounds__(COMBINE_ROWS)
 
 bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 
-static int sm_count() {
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0;
-        cudaGetDevice(&dev);
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 1;
-    }
-    return n;
-}
-
 size_t attn_workspace_bytes(int head_dim) {
-    const size_t slots = 2 * ((size_t)sm_count() + 1);
+    const size_t slots = 2 * ((size_t)device_sms() + 1);
     return slots * 256 * ((size_t)head_dim * sizeof(float) + sizeof(float2));
 }
 
@@ -672,7 +662,7 @@ static cudaError_t launch_attn_(const CUtensorMap &tq, const CUtensorMap &tk, co
     static DeviceSet asked{0};
     cudaError_t e = allow_smem(attn_tc_kernel<HD, WAVE>, A::SMEM_BYTES, asked);
     if (e != cudaSuccess) return e;
-    const int n_sm = sm_count();
+    const int n_sm = device_sms();
     float *ws_o = split ? reinterpret_cast<float *>(ws) : nullptr;
     float2 *ws_ml = split ? reinterpret_cast<float2 *>(ws_o + 2 * ((size_t)n_sm + 1) * 256 * HD) : nullptr;
     e = launch_pdl(attn_tc_kernel<HD, WAVE>, dim3(sp.G), dim3(A::THREADS), A::SMEM_BYTES, st, tq, tk,
@@ -705,7 +695,7 @@ static cudaError_t launch_attn(const CUtensorMap &tq, const CUtensorMap &tk, con
     sp.n_qblk = (Lq + A::QT * A::BQ - 1) / (A::QT * A::BQ);
     const int n_units = sp.n_qblk * n_heads;
     sp.T = (long long)n_units * sp.n_kt;
-    const int n_sm = sm_count();
+    const int n_sm = device_sms();
     const bool split = n_units > n_sm && ws != nullptr && ws_bytes >= attn_workspace_bytes(HD);
     sp.G = split ? n_sm : n_units;
     sp.W = n_units / sp.G;

@@ -539,16 +539,6 @@ static bool build_epi_maps(EpiMaps &em, const EpiParams &ep) {
     }
 }
 
-static int gemm_sm_count() {
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0;
-        cudaGetDevice(&dev);
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 1;
-    }
-    return n;
-}
-
 // Output tile width for an M x N GEMM.  128 when 128 x 256 tiles would leave
 // SMs idle.  Otherwise the persistent grid runs ceil(tiles / SMs) rounds of
 // tiles; a 128 x 256 tile costs about 1.75 times a 128 x 128 one (it reuses
@@ -556,7 +546,7 @@ static int gemm_sm_count() {
 // more than the 128-wide tiles' rounds.
 int gemm_tc_bn(int M, int N) {
     if (N % 256 != 0) return 128;
-    const long m_tiles = (M + GEMM_BM - 1) / GEMM_BM, n_sm = gemm_sm_count();
+    const long m_tiles = (M + GEMM_BM - 1) / GEMM_BM, n_sm = device_sms();
     if (m_tiles * (N / 256) < n_sm) return 128;
     const long r256 = (m_tiles * (N / 256) + n_sm - 1) / n_sm;
     const long r128 = (m_tiles * (N / 128) + n_sm - 1) / n_sm;
@@ -573,7 +563,7 @@ static cudaError_t launch_tc(const CUtensorMap &ta, const CUtensorMap &tb, const
     static DeviceSet asked{0};
     const cudaError_t e = allow_smem(kern, G::SMEM_BYTES, asked);
     if (e != cudaSuccess) return e;
-    const int n_sm = gemm_sm_count();
+    const int n_sm = device_sms();
     const int n_tiles = (ep.N / BN) * ((ep.M + GEMM_BM - 1) / GEMM_BM);
     const int grid = n_tiles < n_sm ? n_tiles : n_sm;
     return launch_pdl(kern, dim3(grid), dim3(320), G::SMEM_BYTES, st, ta, tb, em, ep, K, skip, err);

@@ -88,5 +88,4 @@ bool make_tmap_2d(CUtensorMap *m, CUtensorMapDataType type, int elem, const void
                   uint32_t box_rows, uint32_t box_cols);
 // Device error word of the operator entry points (NULL if it cannot be made).
 int *op_error_word();
-int device_sms();
 }  // namespace xc

@@ -11,17 +11,6 @@
 
 using namespace xc;
 
-int xc::device_sms() {
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0, x = 0;
-        cudaGetDevice(&dev);
-        if (cudaDeviceGetAttribute(&x, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || x < 1) return 1;
-        n = x;
-    }
-    return n;
-}
-
 namespace {
 
 xc_status fail(xc_status st, const char *fmt, ...) {

@@ -14,6 +14,19 @@ inline int current_device() {
     return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < MAX_DEVICES ? dev : -1;
 }
 
+// Multiprocessors of the current device (1 where the device does not say).
+inline int device_sms() {
+    static std::atomic<int> sms[MAX_DEVICES];
+    const int dev = current_device();
+    if (dev < 0) return 1;
+    int n = sms[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 1;
+        sms[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 // A kernel's leave to take more dynamic shared memory than a CTA has without asking holds on the
 // device it was asked for.  `asked`: the devices where it was, one set for each kernel.
 using DeviceSet = std::atomic<unsigned long long>;

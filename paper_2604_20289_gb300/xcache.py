@@ -368,7 +368,7 @@ def op_quantize_rows(dtype, x, q, scale, stream=None):
     check(LIB.xc_op_quantize_rows(dtype_code(dtype), M, K, x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(stream)))
 
 
-_I8_BYTES = {}                                    # workspace sizes by shape
+_I8_BYTES = {}                                    # workspace sizes by device and shape
 
 
 def op_linear_i8_workspace_bytes(M, N, K) -> int:
@@ -397,11 +397,12 @@ def op_linear_i8(dtype, epilogue, A, Wq, w_scale, bias, out, gate=None, resid=No
         raise ValueError("gate [N] and a_scale [M] float32, resid [M, N] of dtype, all contiguous")
     cuda = _stream(stream)
     if workspace is None:
-        need = _I8_BYTES.get((M, N, K))
+        key = A.get_device(), M, N, K
+        need = _I8_BYTES.get(key)
         if need is None:
             if len(_I8_BYTES) >= 4096:
                 _I8_BYTES.clear()
-            need = _I8_BYTES[M, N, K] = LIB.xc_op_linear_i8_workspace_bytes(M, N, K)
+            need = _I8_BYTES[key] = LIB.xc_op_linear_i8_workspace_bytes(M, N, K)
         buf, ws, nbytes = _scratch(need, stream, cuda, A.device) if need else (None, None, 0)
     else:
         buf, ws, nbytes = _given(workspace)

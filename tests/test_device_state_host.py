@@ -17,6 +17,12 @@ static int g_dev = 0, g_fail = 0;
 struct Ask { int dev, bytes; };
 static std::vector<Ask> g_asked;
 extern "C" cudaError_t cudaGetDevice(int *d) { *d = g_dev; return g_dev < 0 ? cudaErrorNoDevice : cudaSuccess; }
+static int g_looked = 0, g_sms[64] = {152, 148, 0, 16};
+extern "C" cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr, int d) {
+    ++g_looked;
+    *v = g_sms[d];
+    return g_fail ? cudaErrorInvalidValue : cudaSuccess;
+}
 extern "C" cudaError_t cudaFuncSetAttribute(const void *, cudaFuncAttribute, int v) {
     if (g_fail) return cudaErrorInvalidValue;
     g_asked.push_back({g_dev, v});
@@ -62,6 +68,54 @@ def test_shared_memory_is_asked_for_on_each_device(tmp_path):
 """)
 
 
+def test_multiprocessors_are_each_device_s(tmp_path):
+    run(tmp_path, r"""
+    for (int round = 0; round < 2; ++round) {
+        const int devs[] = {0, 1, 3}, want[] = {152, 148, 16};
+        for (int i = 0; i < 3; ++i) {
+            g_dev = devs[i];
+            EXPECT(xc::device_sms() == want[i]);
+        }
+    }
+    EXPECT(g_looked == 3);
+    g_dev = 5;
+    g_sms[5] = 100;
+    g_fail = 1;
+    EXPECT(xc::device_sms() == 1);                 // a failure is not remembered
+    g_fail = 0;
+    EXPECT(xc::device_sms() == 100);
+    for (int dev : {-1, 64}) {
+        g_dev = dev;
+        EXPECT(xc::device_sms() == 1);
+    }
+""")
+
+
+def test_a_product_s_workspace_is_each_device_s(monkeypatch):
+    """Its size follows the multiprocessors."""
+    torch = pytest.importorskip("torch")
+    from test_devices_host import BF16, F32, I8, Tensor
+    if not os.path.exists(os.path.join(ROOT, "paper_2604_20289_gb300", "libxcache.so")):
+        from paper_2604_20289_gb300 import build
+        build.build()
+    from paper_2604_20289_gb300 import xcache as xb
+    here, got = [0], []
+
+    class Lib:
+        xc_op_linear_i8_workspace_bytes = staticmethod(lambda *a: 1000 + here[0])
+        xc_op_linear_i8 = staticmethod(lambda *a: 0)
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: here[0], raising=False)
+    monkeypatch.setattr(xb, "LIB", Lib)
+    monkeypatch.setattr(xb, "_I8_BYTES", {})
+    monkeypatch.setattr(xb, "_scratch", lambda n, *a: (got.append(n), 1 << 20, n))
+    for dev in (0, 1, 0, 1):
+        here[0] = dev
+        xb.op_linear_i8("bf16", 0, Tensor((40, 64), BF16, dev), Tensor((32, 64), I8, dev), Tensor((32,), F32, dev),
+                        Tensor((32,), F32, dev), Tensor((40, 32), BF16, dev), stream=7)
+    assert got == [1000, 1001, 1000, 1001]
+
+
 def sources():
     for name in sorted(os.listdir(CSRC)):
         with open(os.path.join(CSRC, name)) as f:
@@ -72,4 +126,5 @@ def test_no_source_asks_once_for_the_process():
     for name, text in sources():
         if name != "xc_device.h":
             assert "cudaFuncSetAttribute" not in text, name
+            assert "cudaDevAttrMultiProcessorCount" not in text or name in ("k_gate.cu", "xc_api.cu"), name     # (not kept there)
         assert not re.search(r"static bool \w+ = false", text), name
