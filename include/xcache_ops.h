@@ -200,8 +200,8 @@ xc_status xc_op_gate_static(int dtype, int n_cams, int tokens_per_cam, int d, co
  * value sets a bit of the word xc_op_device_error() returns --
  * XC_DEV_CACHE_FULL or XC_DEV_BAD_SEQUENCE for the page calls, of which fork,
  * extend and evict then change nothing; XC_DEV_BAD_POSITION for a position or slot out of range,
- * whose token is then skipped.  The first operator call of a process sets up
- * that word; it should come before any stream capture. */
+ * whose token is then skipped.  The first operator call on a device sets up
+ * that device's word; it should come before any stream capture. */
 typedef struct {
     int dtype, n_layers, n_pages, page_size, n_kv_heads, head_dim, max_seqs, max_pages;
     void *k, *v;
@@ -366,7 +366,7 @@ xc_status xc_op_key_weights(const xc_kv_cache *cache, int layer, int n_branches,
  * as the graph, and must not be shared with calls that overlap a replay. */
 int xc_op_stream_capturing(void *stream);
 
-/* Reads and clears the process-wide device error word of operator calls
+/* Reads and clears the current device's error word of operator calls
  * (synchronising).  0 = no error. */
 int xc_op_device_error(void);
 

@@ -1195,10 +1195,8 @@ int xc_chunk_index(const xc_ctx *ctx) { return ctx == nullptr ? -1 : ctx->n; }
 
 void xc_debug_fail_alloc(int n) { g_fail_alloc.store(n > 0 ? n : 0); }
 
-static int *op_err_word();
-
 xc_status xc_debug_expire_wait(xc_ctx *ctx) {
-    int *err = ctx != nullptr ? ctx->d_err : op_err_word();
+    int *err = ctx != nullptr ? ctx->d_err : xc::device_error_word();
     if (err == nullptr) {
         set_err(nullptr, "xc_debug_expire_wait: no device error word");
         return XC_ECUDA;
@@ -1502,17 +1500,8 @@ xc_status xc_chunk_step(xc_ctx *ctx, const float *latent, const float *action, f
 }
 
 // ---------------------------------------------------------------- op entries
-static int *op_err_word() {
-    static int *p = nullptr;
-    if (p == nullptr) {
-        if (cudaMalloc(&p, sizeof(int)) != cudaSuccess) return nullptr;
-        cudaMemset(p, 0, sizeof(int));
-    }
-    return p;
-}
-
 int xc_op_device_error(void) {
-    int *p = op_err_word();
+    int *p = xc::device_error_word();
     if (p == nullptr) return -1;
     cudaDeviceSynchronize();
     int e = 0;
@@ -1559,7 +1548,7 @@ xc_status xc_op_linear(int dtype, int epilogue, int M, int N, int K, const void 
         const int bn = gemm_tc_bn(M, N);
         if (!make_tmap_bf16(&ta, A, M, K, 128) || !make_tmap_bf16(&tb, Wt, N, K, bn))
             OP_FAIL(XC_EINVAL, "xc_op_linear: tensor map (alignment?)");
-        OP_CK(gemm_tc(epilogue, bn, ta, tb, ep, K, nullptr, op_err_word(), st));
+        OP_CK(gemm_tc(epilogue, bn, ta, tb, ep, K, nullptr, xc::device_error_word(), st));
     } else if (dtype == XC_F32) {
         if (N % 16 != 0) OP_FAIL(XC_EINVAL, "xc_op_linear: f32 needs N %% 16 == 0");
         OP_CK(gemm_simt(epilogue, ep, reinterpret_cast<const float *>(A), reinterpret_cast<const float *>(Wt), K,
@@ -1611,7 +1600,7 @@ xc_status xc_op_linear_i8(int dtype, int epilogue, int M, int N, int K, const vo
     const size_t need = linear_i8_workspace_bytes(M, N, K);
     if (need > 0 && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need))
         OP_FAIL(XC_EINVAL, "xc_op_linear_i8: workspace of %zu bytes needed (256-byte aligned)", need);
-    int *err = op_err_word();
+    int *err = xc::device_error_word();
     if (err == nullptr) OP_FAIL(XC_ECUDA, "xc_op_linear_i8: error word");
     const LinearI8Args a{dtype, epilogue, M, N, K, A, a_scale, Wt, w_scale, bias, gate, resid, out};
     OP_CK(linear_i8(a, workspace, err, reinterpret_cast<cudaStream_t>(stream)));
@@ -1671,7 +1660,7 @@ xc_status xc_op_qkv_rope(int dtype, int n_cams, int frames, int gh, int gw, int 
         const int bn = gemm_tc_bn(M, 3 * d);
         if (!make_tmap_bf16(&ta, A, M, d, 128) || !make_tmap_bf16(&tb, Wt, 3 * (uint64_t)d, d, bn))
             OP_FAIL(XC_EINVAL, "xc_op_qkv_rope: tensor map");
-        OP_CK(gemm_tc(EPI_QKV_ROPE, bn, ta, tb, ep, d, nullptr, op_err_word(), st));
+        OP_CK(gemm_tc(EPI_QKV_ROPE, bn, ta, tb, ep, d, nullptr, xc::device_error_word(), st));
     } else if (dtype == XC_F32) {
         OP_CK(gemm_simt(EPI_QKV_ROPE, ep, reinterpret_cast<const float *>(A), reinterpret_cast<const float *>(Wt), d,
                         nullptr, st));
@@ -1699,7 +1688,7 @@ xc_status xc_op_attention(int dtype, int Lq, int n_keys, int n_heads, int head_d
             !make_tmap_bf16(&tv, v, n_keys, d, 128))
             OP_FAIL(XC_EINVAL, "xc_op_attention: tensor map");
         OP_CK(attn_tc(head_dim, tq, tk, tv, reinterpret_cast<bf16 *>(o), Lq, n_keys, n_heads, d, workspace,
-                      workspace_bytes, nullptr, op_err_word(), nullptr, st));
+                      workspace_bytes, nullptr, xc::device_error_word(), nullptr, st));
     } else if (dtype == XC_F32) {
         OP_CK(attn_simt(head_dim, reinterpret_cast<const float *>(q), reinterpret_cast<const float *>(k),
                         reinterpret_cast<const float *>(v), reinterpret_cast<float *>(o), Lq, n_keys, n_heads,
@@ -1746,5 +1735,3 @@ xc_status xc_op_residual_reuse(int dtype, long n, const void *x, const void *rha
 }
 
 }  // extern "C"
-
-int *xc::op_error_word() { return op_err_word(); }

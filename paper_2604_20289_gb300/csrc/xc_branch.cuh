@@ -86,6 +86,4 @@ bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t co
 // 2-D map of a row-major [rows][cols] matrix of `elem`-byte elements, box of 128 bytes x box_rows, 128-byte swizzle.
 bool make_tmap_2d(CUtensorMap *m, CUtensorMapDataType type, int elem, const void *base, uint64_t rows, uint64_t cols,
                   uint32_t box_rows, uint32_t box_cols);
-// Device error word of the operator entry points (NULL if it cannot be made).
-int *op_error_word();
 }  // namespace xc

@@ -77,7 +77,7 @@ xc_status check_axes(const char *who, int n_axes, const int *pairs, const int *n
         if (s_ != XC_OK) return s_;          \
     } while (0)
 #define ERR_WORD(err, who)                                     \
-    int *err = op_error_word();                                \
+    int *err = device_error_word();                            \
     if (err == nullptr) return fail(XC_ECUDA, who ": error word")
 cudaStream_t as_stream(void *s) { return reinterpret_cast<cudaStream_t>(s); }
 

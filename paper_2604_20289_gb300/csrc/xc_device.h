@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <mutex>
 
 namespace xc {
 
@@ -25,6 +26,29 @@ inline int device_sms() {
         sms[dev].store(n, std::memory_order_relaxed);
     }
     return n;
+}
+
+// The word in the current device's memory in which the operators' kernels set error bits; NULL if
+// it cannot be made.  Made by the first call on a device, which must not be in a capture.
+inline int *device_error_word() {
+    static std::atomic<int *> words[MAX_DEVICES];
+    static std::mutex making;
+    const int dev = current_device();
+    if (dev < 0) return nullptr;
+    int *word = words[dev].load(std::memory_order_acquire);
+    if (word != nullptr) return word;
+    std::lock_guard<std::mutex> one(making);
+    word = words[dev].load(std::memory_order_acquire);
+    if (word != nullptr) return word;
+    void *p = nullptr;
+    if (cudaMalloc(&p, sizeof(int)) != cudaSuccess) return nullptr;
+    if (cudaMemset(p, 0, sizeof(int)) != cudaSuccess) {
+        cudaFree(p);
+        return nullptr;
+    }
+    word = static_cast<int *>(p);
+    words[dev].store(word, std::memory_order_release);
+    return word;
 }
 
 // A kernel's leave to take more dynamic shared memory than a CTA has without asking holds on the

@@ -23,6 +23,19 @@ extern "C" cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr, int d) {
     *v = g_sms[d];
     return g_fail ? cudaErrorInvalidValue : cudaSuccess;
 }
+static int g_made = 0, g_freed = 0, g_word[8], g_where[8];
+extern "C" cudaError_t cudaMalloc(void **p, size_t n) {
+    if (g_fail & 1) return cudaErrorMemoryAllocation;
+    g_where[g_made] = g_dev;
+    *p = &g_word[g_made++];
+    return n == 4 ? cudaSuccess : cudaErrorInvalidValue;
+}
+extern "C" cudaError_t cudaMemset(void *p, int v, size_t n) {
+    if (g_fail & 2) return cudaErrorInvalidValue;
+    for (size_t i = 0; i < n; ++i) static_cast<char *>(p)[i] = (char)v;
+    return cudaSuccess;
+}
+extern "C" cudaError_t cudaFree(void *) { return ++g_freed, cudaSuccess; }
 extern "C" cudaError_t cudaFuncSetAttribute(const void *, cudaFuncAttribute, int v) {
     if (g_fail) return cudaErrorInvalidValue;
     g_asked.push_back({g_dev, v});
@@ -91,6 +104,28 @@ def test_multiprocessors_are_each_device_s(tmp_path):
 """)
 
 
+def test_the_error_word_is_in_the_device_s_own_memory(tmp_path):
+    run(tmp_path, r"""
+    for (int &w : g_word) w = 7;
+    g_dev = 2;
+    int *two = xc::device_error_word();
+    g_dev = 0;
+    int *zero = xc::device_error_word();
+    EXPECT(two != nullptr && zero != nullptr && two != zero && *two == 0 && *zero == 0 && g_where[0] == 2 && g_where[1] == 0);
+    g_dev = 2;
+    EXPECT(xc::device_error_word() == two && g_made == 2);
+    g_dev = 3;
+    for (g_fail = 1; g_fail <= 2; ++g_fail) EXPECT(xc::device_error_word() == nullptr);
+    EXPECT(g_freed == 1 && g_made == 3);
+    g_fail = 0;
+    EXPECT(xc::device_error_word() != nullptr && g_made == 4);
+    for (int dev : {-1, 64}) {
+        g_dev = dev;
+        EXPECT(xc::device_error_word() == nullptr);
+    }
+""")
+
+
 def test_a_product_s_workspace_is_each_device_s(monkeypatch):
     """Its size follows the multiprocessors."""
     torch = pytest.importorskip("torch")
@@ -124,6 +159,7 @@ def sources():
 
 def test_no_source_asks_once_for_the_process():
     for name, text in sources():
+        assert not re.search(r"static int \*\w+ = nullptr;\s+if", text), name
         if name != "xc_device.h":
             assert "cudaFuncSetAttribute" not in text, name
             assert "cudaDevAttrMultiProcessorCount" not in text or name in ("k_gate.cu", "xc_api.cu"), name     # (not kept there)
