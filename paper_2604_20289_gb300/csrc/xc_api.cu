@@ -1614,28 +1614,36 @@ xc_status xc_op_qkv_rope(int dtype, int n_cams, int frames, int gh, int gw, int 
         d % head_dim != 0 || A == nullptr || Wt == nullptr || bias == nullptr || q == nullptr || k == nullptr ||
         v == nullptr)
         OP_FAIL(XC_EINVAL, "xc_op_qkv_rope: bad argument");
-    // per-call RoPE layout and table (operator path; the chunk step keeps its own)
-    static int *axis = nullptr, *off = nullptr;
-    static float2 *cs = nullptr;
-    static size_t cap_pairs = 0, cap_entries = 0;
+    // per-call RoPE layout and table (operator path; the chunk step keeps its own), on each device
+    struct Tables {
+        int *axis, *off;
+        float2 *cs;
+        size_t pairs, entries;
+    };
+    static Tables tables[MAX_DEVICES];
+    const int dev = current_device();
+    if (dev < 0) OP_FAIL(XC_ECUDA, "xc_op_qkv_rope: no current device");
+    Tables &t = tables[dev];
     std::vector<int> ax, of;
     const int npos[4] = {n_cams, frames, gh, gw};
     const int n_entries = rope_layout(head_dim, npos, ax, of);
     cudaStream_t st0 = reinterpret_cast<cudaStream_t>(stream);
-    if (ax.size() > cap_pairs || (size_t)n_entries > cap_entries) {
+    if (ax.size() > t.pairs || (size_t)n_entries > t.entries) {
         OP_CK(cudaDeviceSynchronize());
-        if (axis) cudaFree(axis);
-        if (off) cudaFree(off);
-        if (cs) cudaFree(cs);
-        cap_pairs = ax.size();
-        cap_entries = (size_t)n_entries;
-        OP_CK(cudaMalloc(&axis, cap_pairs * sizeof(int)));
-        OP_CK(cudaMalloc(&off, cap_pairs * sizeof(int)));
-        OP_CK(cudaMalloc(&cs, cap_entries * sizeof(float2)));
+        cudaFree(t.axis);
+        cudaFree(t.off);
+        cudaFree(t.cs);
+        const size_t pairs = std::max(ax.size(), t.pairs), entries = std::max((size_t)n_entries, t.entries);
+        t = Tables{};                                  // (a failure below leaves no pointer to freed memory)
+        OP_CK(cudaMalloc(&t.axis, pairs * sizeof(int)));
+        OP_CK(cudaMalloc(&t.off, pairs * sizeof(int)));
+        OP_CK(cudaMalloc(&t.cs, entries * sizeof(float2)));
+        t.pairs = pairs;
+        t.entries = entries;
     }
-    OP_CK(cudaMemcpyAsync(axis, ax.data(), ax.size() * sizeof(int), cudaMemcpyHostToDevice, st0));
-    OP_CK(cudaMemcpyAsync(off, of.data(), of.size() * sizeof(int), cudaMemcpyHostToDevice, st0));
-    OP_CK(rope_table(head_dim, (double)rope_theta, chunk * frames, make_int4(n_cams, frames, gh, gw), cs, n_entries,
+    OP_CK(cudaMemcpyAsync(t.axis, ax.data(), ax.size() * sizeof(int), cudaMemcpyHostToDevice, st0));
+    OP_CK(cudaMemcpyAsync(t.off, of.data(), of.size() * sizeof(int), cudaMemcpyHostToDevice, st0));
+    OP_CK(rope_table(head_dim, (double)rope_theta, chunk * frames, make_int4(n_cams, frames, gh, gw), t.cs, n_entries,
                      st0));
     const int npc = frames * gh * gw, M = n_cams * npc;
     EpiParams ep;
@@ -1650,9 +1658,9 @@ xc_status xc_op_qkv_rope(int dtype, int n_cams, int frames, int gh, int gw, int 
     ep.head_dim = head_dim;
     epi_single_grid(ep, frames, gh, gw);
     ep.frame0 = chunk * frames;
-    ep.rope_axis = axis;
-    ep.rope_off = off;
-    ep.rope_cs = cs;
+    ep.rope_axis = t.axis;
+    ep.rope_off = t.off;
+    ep.rope_cs = t.cs;
     cudaStream_t st = st0;
     if (dtype == XC_BF16) {
         if ((3 * d) % 256 != 0 || d % 64 != 0) OP_FAIL(XC_EINVAL, "xc_op_qkv_rope: bf16 needs 3d %% 256, d %% 64");

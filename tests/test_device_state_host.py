@@ -160,6 +160,7 @@ def sources():
 def test_no_source_asks_once_for_the_process():
     for name, text in sources():
         assert not re.search(r"static int \*\w+ = nullptr;\s+if", text), name
+        assert not re.search(r"static \w+ \*\w+ = nullptr[;,]", text), name     # a pointer to one device's memory
         if name != "xc_device.h":
             assert "cudaFuncSetAttribute" not in text, name
             assert "cudaDevAttrMultiProcessorCount" not in text or name in ("k_gate.cu", "xc_api.cu"), name     # (not kept there)
