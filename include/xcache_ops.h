@@ -53,7 +53,7 @@ xc_status xc_op_quantize_rows(int dtype, int M, int K, const void *x, signed cha
  * projection in 8-bit integers.  The activations A [M][K] of `dtype` are
  * quantised by the call as by xc_op_quantize_rows; with a_scale [M] not NULL, A
  * is 8-bit already (Wt, A: [-128, 127]) and dtype is that of resid and out.  The sums are those of
- * the integers while they stay below 2^24 in magnitude, rounded to fp32 above.
+ * the integers while they stay below 2^24 in magnitude (always up to K = 1024), fp32's above.
  * out, resid [M][N] contiguous; epilogue XC_EPI_BIAS, XC_EPI_GELU or
  * XC_EPI_RESID_GATE as in xc_op_linear; out may be resid.  Any M from 0 below 2^24 and any N from 1;
  * K a multiple of 16 up to 131072.

@@ -4,8 +4,11 @@
 //   s_a[m] = max_k |x[m][k]| / 127,   qa[m][k] = round(127 x[m][k] / max_k |x[m][k]|)
 //
 // The tensor core of this part has no fast 8-bit integer kind.  Whole numbers
-// up to 127 are exact in fp16, their products and, below 2^24, their sums in
-// fp32, so the product runs at the fp16 rate with the integer's result; the
+// up to 128 are exact in fp16, their products and, below 2^24, their sums in
+// fp32, so the product runs at the fp16 rate, with the integer's result as long as
+// the sums stay below 2^24 in magnitude: whatever the numbers to a depth of 1024 (1040 for
+// numbers to 127), for most rows much further (random ones grow with the root of the depth).  Past
+// it a sum is fp32's, each step of 16 off by 2^-23 of it at most.  The
 // weights stay 8 bits wide in memory, which is what a step of few tokens
 // waits for.  The tokens are quantised by a kernel of their own (as fp16 whole
 // numbers, ready for TMA); the weights are widened on their way into tensor

@@ -215,6 +215,18 @@ def test_sums_past_24_bits():
     assert ((out.to(F64) - ref).abs() / ref.abs()).max().item() <= 2.0 ** -23 * K / 16
 
 
+@pytest.mark.parametrize("M,N,K", [(4, 300, 13824), (12, 256, 5120), (32, 100, 2064)])
+def test_sums_past_24_bits_of_few_tokens(M, N, K):
+    """The kernel of few tokens: the same bound, K / 16 additions that may drop 2^-23 of the sum each."""
+    o = operands("f32", M, N, K)
+    o["x"] = torch.full((M, K), 3.0, device=DEV)
+    o["x"][::2] *= -1
+    o["wq"] = torch.full((N, K), 127, dtype=torch.int8, device=DEV)
+    assert xb.op_linear_i8_workspace_bytes(M, N, K) == 0
+    out, (ref, _) = run_linear("f32", o, "bias"), plain_linear(o, "bias")
+    assert ((out.to(F64) - ref).abs() / ref.abs()).max().item() <= 2.0 ** -23 * K / 16
+
+
 def test_a_row_that_is_not_finite_spoils_only_its_own_outputs():
     o = operands("bf16", 40, 256, 512)
     o["x"][7, 100], o["x"][20, 3] = float("nan"), float("-inf")
