@@ -792,11 +792,15 @@ __global__ void __launch_bounds__(KFEW_THREADS, 1)
 // memory of its own over the key heads, and the groups in turn write a tile's weights.  Up to eight columns a
 // branch are added up by code for just that many: with a test at each column a step of 48 took 1.75 us.
 // 8 single tokens, 40 / 8 heads x 128, 38880 shared + 1..1500 own keys: 25.8 us (in registers 49.4), 7 until the first
-// tile is there, then 6.3 TB/s.
+// tile is there, then 6.3 TB/s.  At most KST_NB branches a tile: with 8, 16 and 32, 32 branches over 8192 shared keys of
+// 12 heads x 128 took 21.4, 24.3 and 21.3 us, over 32768 keys 64.6, 46.1 and 40.3, 64 over 16384 of 8 x 64
+// 43.4, 38.5 and 41.3: fewer tiles read the keys less often, more have smaller sums and more slots.
 constexpr int KST_SOFT = 256, KST_THREADS = 128 + KST_SOFT, KST_COLS = 64, KST_BUFS = 8, KST_SLOTS = 8, KST_NB = 16, KST_BUDGET = 204 * 1024;
 // Key bytes, with every table row full, from which few rows go as a stream: below, its barriers and first copies take
 // longer than the keys (4 single tokens, 8 heads x 64: 4096 keys 9.6 us against 6.7, 16384 keys 10.9 against
-// 13.7; 12 heads x 128: 4096 keys 12.2 against 10.9, 8192 keys 12.8 against 15.9).
+// 13.7; 12 heads x 128: 4096 keys 12.2 against 10.9, 8192 keys 12.8 against 15.9).  The host has the tables' width
+// and not the lengths, so short sequences in wide tables pay that: 2016 keys a branch of 8 x 64 in rows of
+// 2048 8.5 us, of 4096 9.2 (two caches in turn).
 constexpr long long KST_BYTES = 12 << 20;
 
 struct KeyRun {

@@ -1027,7 +1027,11 @@ __global__ void __launch_bounds__(I8S_THREADS, 1) linear_i8_small_kernel(const _
 }
 
 // ------------------------------------------------------------------- host
-// Tokens that fit every CTA's shared memory go with the weights' stream.
+// Tokens that fit every CTA's shared memory go with the weights' stream.  Against the three kernels, us, weights from DRAM
+// (K 5120, N 15360) or L2 (1536, 4608): 4 tokens 19.2 and 26.4, 5.9 and 8.8; 8 tokens 21.3 and 26.8, 6.4 and 9.3; 16 tokens
+// of 1536 8.5 and 10.3.  The rule is the memory's, and takes the slower side where a warp's sums are
+// many beside its products or the tokens fill the memory: 12 tokens of 5120 32.5 and 27.2, 24 and 32 of 1536
+// 16.7 and 10.6, 17.4 and 11.0, 5 of 13824 (N 5120) 29.1 and 24.9.
 static bool i8_small(int M, int K) { return M <= I8S_MAX_M && (long)M * ((K + 127) / 128 * 128) * 2 <= I8S_TOKEN_BYTES; }
 
 template <typename T, int NT8>
